@@ -86,6 +86,8 @@ typedef struct asynclm_plan_options {
 
 #define ASYNCLM_PLAN_REJECT_ALIASED_WRITES 1  /* error if two sequences append into one page */
 #define ASYNCLM_PLAN_NO_TENSOR_PATH        2  /* keep every row on the warp body              */
+#define ASYNCLM_PLAN_KV8                   4  /* balance for asynclm_kv8_attn_mixed; either kind of plan serves
+                                                 either kind of cache                         */
 
 /* Host-side description of one step's batch (all arrays on the host, int32). */
 typedef struct asynclm_batch {
@@ -378,6 +380,120 @@ int asynclm_latency_model(const double* gen, const double* exec, int32_t n, asyn
                           int32_t* lpt_order);
 int asynclm_async_latency_of_order(const double* gen, const double* exec, const int32_t* order, int32_t n,
                                    double* latency, double* completion);
+
+/*
+ * Rotary positions (the models of the paper's evaluation, Section 6, turn queries and keys by their positions; asynclm_kv_append_rope
+ * above is the plain form, fused into the bf16 append).  Pair j < rotary_dim / 2 of a head turns by the angle position * f_j:
+ *     (x, y) -> m (x cos a - y sin a, y cos a + x sin a),      f_j = theta^(-2j / rotary_dim), m = 1,
+ * values from rotary_dim on pass through.  For contexts beyond the one a model was trained for, f_j and m are scaled:
+ *     LINEAR  f_j / factor
+ *     BANDS   with w = context * f_j / 2 pi turns over the context: f_j where w >= high_freq_factor, f_j / factor where
+ *             w <= low_freq_factor, in between the mixture (1 - t) f_j / factor + t f_j, t = (w - low) / (high - low)
+ *     YARN    (published as arXiv 2309.00071) with j(b) = rotary_dim ln(context / 2 pi b) / (2 ln theta), the pair that turns b times over the
+ *             context, from = max(floor j(beta_fast), 0), to = min(ceil j(beta_slow), rotary_dim - 1) and
+ *             t = (j - from) / (to - from) held to [0, 1]: t f_j / factor + (1 - t) f_j; m = attention_factor, or 0.1 ln(factor) + 1 if it is 0
+ * asynclm_rope_table_init works the frequencies out on the host, once for a model; the calls below take the table (host memory, read
+ * at the call).  Angles, sines and cosines are fp64, a rotated value is within 2^-22 of itself before it is rounded, once, to what
+ * is written.
+ * Errors: INVALID_ARG (NULL; head_dim not a multiple of 8 in 8 .. 256; rotary_dim odd or above head_dim; theta <= 1; factor < 1;
+ * parameters of the chosen scaling that are missing or out of order).
+ */
+#define ASYNCLM_ROPE_HALF        0   /* pairs (j, j + rotary_dim / 2) */
+#define ASYNCLM_ROPE_INTERLEAVED 1   /* pairs (2j, 2j + 1)            */
+#define ASYNCLM_ROPE_UNSCALED 0
+#define ASYNCLM_ROPE_LINEAR   1
+#define ASYNCLM_ROPE_BANDS    2
+#define ASYNCLM_ROPE_YARN     3
+typedef struct asynclm_rope {
+    double  theta;                              /* base, > 1 */
+    double  factor;                             /* of the scaling, >= 1; not read if UNSCALED */
+    double  low_freq_factor, high_freq_factor;  /* BANDS */
+    double  beta_fast, beta_slow;               /* YARN  */
+    double  attention_factor;                   /* YARN; 0 = 0.1 ln(factor) + 1 */
+    int32_t rotary_dim;                         /* 0 = head_dim */
+    int32_t layout;                             /* ASYNCLM_ROPE_HALF / INTERLEAVED */
+    int32_t scaling;
+    int32_t context;                            /* BANDS, YARN: positions the model was trained for */
+} asynclm_rope;
+typedef struct asynclm_rope_table {             /* filled by asynclm_rope_table_init */
+    int32_t magic, head_dim, rotary_dim, layout;
+    double  factor;                             /* m */
+    double  turns[128];                         /* f_j / 2 pi */
+} asynclm_rope_table;
+int asynclm_rope_table_init(const asynclm_rope* rope, int32_t head_dim, asynclm_rope_table* out);
+
+/*
+ * Turns the rows of one or two tensors (queries and keys) by their tokens' positions: row t, head h of each tensor by positions[t].
+ * For caches in bf16: asynclm_rope_apply, then asynclm_kv_append or asynclm_step.
+ *
+ *   positions   device, int32 [tokens] (any value)
+ *   rows        host, n_rows of them; rows of one tensor are in_stride / out_stride values apart (multiples of 8, at least
+ *               heads * head_dim; 0 = dense), so slices of a fused projection's output need no copy.  in == out rotates in place
+ *               (equal strides); tensors that overlap in any other way are not allowed
+ * One kernel on `stream`.  Errors: INVALID_ARG (also: the table was made for another head_dim), CUDA.
+ */
+typedef struct asynclm_rope_rows {
+    const void* in;       /* device, bf16 [tokens][heads][head_dim], 16-byte aligned */
+    void*       out;
+    int64_t     in_stride, out_stride;
+    int32_t     heads;
+    int32_t     reserved;
+} asynclm_rope_rows;
+int asynclm_rope_apply(const asynclm_rope_table* table, const int32_t* positions, int32_t tokens, int32_t head_dim,
+                       const asynclm_rope_rows* rows, int32_t n_rows, void* stream);
+
+/*
+ * Quantised cache.  While function calls run, their sequences keep their KV caches in GPU memory (the trap handler's "keep", Section 5.4),
+ * and every decoding step reads all of the active ones: the cache's bytes are what limits both.  This form takes 8 bits a value
+ * and one byte a row.  A row is the head_dim values of one (token, kv head, K or V); it is held as
+ *     codes   e4m3, x_j * 2^-e rounded to nearest even          standing for code * 2^e
+ *     scale   one byte e + 127 (e8m0), e the least integer >= -100 with max|x_j| <= 448 * 2^e
+ * (values below 2^-110 become zeros).  A row with a value that is not finite gets the byte 255, which stands for NaN, and codes of zero; a
+ * token that sees such a row has NaN in its outputs and its log-sum-exp, tokens that do not see it are untouched.
+ *     kv8_pool    device, 1 byte a value: [num_pages][2 (0 = K, 1 = V)][num_kv_heads][page_size][head_dim]
+ *     kv8_scales  device, 1 byte a row:   [num_pages][num_kv_heads][2 (0 = K, 1 = V)][page_size]
+ * both 16-byte aligned.  Shapes, plans, page tables and the rules on streams are those of the bf16 cache.  A pool that something else has
+ * filled must not hold the codes 0x7f and 0xff (NaN), in rows that are read.
+ *
+ * asynclm_kv8_append is asynclm_kv_append for this cache: the new K and V rows go, quantised, to their sequences' next slots.
+ * With `rope`, the keys are turned by their positions before they are quantised (one rounding, from fp32 to the code), and q, if given,
+ * is turned into q_out.  No other byte of pool or scales is written.
+ *
+ *   rows     host.  k, v: device, bf16 [T][num_kv_heads][head_dim]; q: device, bf16 [T][num_q_heads][head_dim] or NULL; rows of a tensor
+ *            are k_stride, v_stride, q_stride values apart (multiples of 8; 0 = dense); q_out: device, dense, may be q itself if that is dense
+ *   rope     the table of asynclm_rope_table_init for the plan's head_dim, or NULL (then q and q_out must be NULL)
+ * One kernel.  Errors: INVALID_ARG, CUDA.
+ */
+typedef struct asynclm_kv8_rows {
+    const void *k, *v, *q;
+    void*       q_out;
+    int64_t     k_stride, v_stride, q_stride;
+} asynclm_kv8_rows;
+int asynclm_kv8_append(const asynclm_plan_t* plan, const asynclm_kv8_rows* rows, void* kv8_pool, void* kv8_scales,
+                       const asynclm_rope_table* rope, void* stream);
+
+/*
+ * asynclm_attn_mixed over the quantised cache: same plan, queries, masks, results and formulas, with K_j and V_j the values that codes and
+ * scales stand for.  bf16 queries, fp32 accumulation and statistics, bf16 output.
+ * Errors: INVALID_ARG, CUDA.
+ */
+int asynclm_kv8_attn_mixed(const asynclm_plan_t* plan, const void* q, const void* kv8_pool, const void* kv8_scales, void* out, float* lse,
+                           void* stream);
+
+/*
+ * Reads ranges of sequences back as dense bf16 rows (exact: a code times its scale is a bf16 value), for a hand-over to a bf16 pool or to
+ * another server: output row out_indptr[b] + i holds position first[b] + i of sequence b of the plan, i < out_indptr[b + 1] - out_indptr[b].
+ *
+ *   out_indptr    device, int64 [batch + 1], from 0, not falling; total_rows = its last entry (host)
+ *   first         device, int32 [batch]
+ *   k_out, v_out  device, bf16 [total_rows][num_kv_heads][head_dim]
+ * Positions may be any that the sequence has pages for up to ctx_b + q_len_b.  Rows outside that, or whose page id lies outside the pool (the
+ * planner does not look at the pages of a sequence without new tokens), are left unwritten, and asynclm_last_device_status reports
+ * code 45.
+ * One kernel.  Errors: INVALID_ARG, CUDA.
+ */
+int asynclm_kv8_gather(const asynclm_plan_t* plan, const int64_t* out_indptr, const int32_t* first, int64_t total_rows, const void* kv8_pool,
+                       const void* kv8_scales, void* k_out, void* v_out, void* stream);
 
 /*
  * Measurement aid (no counterpart in the paper, none of the method's arithmetic): reads n_blocks

@@ -24,13 +24,18 @@ EXPORTS = [
     "asynclm_static_scratch_bytes", "asynclm_step", "asynclm_read_ceiling", "asynclm_kv_swap_staging_bytes",
     "asynclm_kv_swap_out", "asynclm_kv_swap_in", "asynclm_trap_decide", "asynclm_latency_model",
     "asynclm_async_latency_of_order", "asynclm_token_monitor_step", "asynclm_token_monitor_workspace_bytes",
-    "asynclm_kv_append_rope",
+    "asynclm_kv_append_rope", "asynclm_rope_table_init", "asynclm_rope_apply", "asynclm_kv8_append", "asynclm_kv8_attn_mixed",
+    "asynclm_kv8_gather",
 ]
 
 TRAP_KEEP, TRAP_SWAP, TRAP_RECOMPUTE = 0, 1, 2
 
 PLAN_REJECT_ALIASED_WRITES = 1
 PLAN_NO_TENSOR_PATH = 2
+PLAN_KV8 = 4
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {None: 0, "none": 0, "linear": 1, "bands": 2, "yarn": 3}
 
 
 class AsynclmError(RuntimeError):
@@ -88,6 +93,27 @@ class CPlanInfo(ctypes.Structure):
 ITEM_DTYPE = np.dtype([(n, np.int32) for n in
                        ("seq", "kv_head", "tok0", "ntok", "kv0", "kv1", "path", "cta")])
 
+class CRope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("factor", ctypes.c_double), ("low_freq_factor", ctypes.c_double), ("high_freq_factor", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("attention_factor", ctypes.c_double),
+                ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("context", ctypes.c_int32)]
+
+
+class CRopeTable(ctypes.Structure):
+    _fields_ = [("magic", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("turns", ctypes.c_double * 128)]
+
+
+class CRopeRows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("in_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class CKv8Rows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -131,6 +157,11 @@ def load(rebuild_if_stale: bool = True):
     lib.asynclm_trap_decide.argtypes = [ctypes.POINTER(CTrapModel), i32, ctypes.c_double,
                                         ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(ctypes.c_double)]
+    lib.asynclm_rope_table_init.argtypes = [ctypes.POINTER(CRope), i32, ctypes.POINTER(CRopeTable)]
+    lib.asynclm_rope_apply.argtypes = [ctypes.POINTER(CRopeTable), vp, i32, i32, ctypes.POINTER(CRopeRows), i32, vp]
+    lib.asynclm_kv8_append.argtypes = [vp, ctypes.POINTER(CKv8Rows), vp, vp, ctypes.POINTER(CRopeTable), vp]
+    lib.asynclm_kv8_attn_mixed.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    lib.asynclm_kv8_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp]
     lib.asynclm_static_scratch_bytes.argtypes = []
     lib.asynclm_last_device_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     for name in EXPORTS:
@@ -188,8 +219,8 @@ def _cshape(shape, num_pages: int, sm_scale: float = 0.0) -> CShape:
                   int(num_pages), float(sm_scale), 0)
 
 
-def _copts(num_sms=0, kv_chunk_tokens=0, tensor_min_rows=0, flags=0) -> CPlanOptions:
-    return CPlanOptions(int(num_sms), int(kv_chunk_tokens), int(tensor_min_rows), int(flags))
+def _copts(num_sms=0, kv_chunk_tokens=0, tensor_min_rows=0, flags=0, kv8=False) -> CPlanOptions:
+    return CPlanOptions(int(num_sms), int(kv_chunk_tokens), int(tensor_min_rows), int(flags) | (PLAN_KV8 if kv8 else 0))
 
 
 def _i32(a):
@@ -421,6 +452,109 @@ def asynclm_async_latency_of_order(gen, exe, order):
                                                  ctypes.byref(lat), done.ctypes.data),
            "asynclm_async_latency_of_order")
     return float(lat.value), done[:len(g)]
+
+
+def _rows_of(t, name: str, dtype=None, dense=False):
+    """(address, row stride in values) of a tensor [tokens][heads][head_dim] whose heads lie next to each other.  What the C call cannot see
+    (types, inner strides, devices) is checked here."""
+    import torch
+    if t.dim() != 3 or t.dtype != (dtype or torch.bfloat16) or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor [tokens][heads][head_dim] of {dtype or torch.bfloat16} is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    n, h, d = t.shape
+    if n == 0:
+        return t.data_ptr(), 0
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (dense and n > 1 and t.stride(0) != h * d):
+        raise ValueError(f"{name}: {'rows' if dense else 'the heads of a row'} have to lie next to each other in memory (strides {t.stride()})")
+    return t.data_ptr(), t.stride(0) if n > 1 else 0
+
+
+def _flat(t, name: str, what: str, dtypes=None):
+    if not t.is_cuda or not t.is_contiguous() or (dtypes is not None and t.dtype not in dtypes):
+        raise ValueError(f"{name}: {what} is wanted, not {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
+
+
+_kv8_dtypes = None
+
+
+def _cache8(pool, scales):
+    """Addresses of a quantised cache's two tensors: one byte each (float8_e4m3fn and float8_e8m0fnu, or uint8)."""
+    global _kv8_dtypes
+    if _kv8_dtypes is None:
+        import torch
+        _kv8_dtypes = ((torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8))
+    return (_flat(pool, "kv8_pool", "a contiguous CUDA tensor of float8_e4m3fn or uint8", _kv8_dtypes[0]),
+            _flat(scales, "kv8_scales", "a contiguous CUDA tensor of float8_e8m0fnu or uint8", _kv8_dtypes[1]))
+
+
+def asynclm_rope_table(head_dim: int, theta: float = 500000.0, rotary_dim: int = 0, layout: str = "half", scaling=None, factor: float = 1.0,
+                       context: int = 0, low_freq_factor: float = 1.0, high_freq_factor: float = 4.0, beta_fast: float = 32.0,
+                       beta_slow: float = 1.0, attention_factor: float = 0.0) -> CRopeTable:
+    """The table of rotary frequencies that asynclm_rope_apply and asynclm_kv8_append take (made once for a model).  layout: "half" or
+    "interleaved"; scaling: None, "linear", "bands" or "yarn", with `factor` and, for the last two, `context` (see include/asynclm.h)."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise ValueError(f"layout {layout!r} is one of {list(ROPE_LAYOUTS)}, scaling {scaling!r} of {list(ROPE_SCALINGS)}")
+    rope = CRope(float(theta), float(factor), float(low_freq_factor), float(high_freq_factor), float(beta_fast), float(beta_slow), float(attention_factor),
+                 int(rotary_dim), ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], int(context))
+    table = CRopeTable()
+    _check(load().asynclm_rope_table_init(ctypes.byref(rope), int(head_dim), ctypes.byref(table)), "asynclm_rope_table_init")
+    return table
+
+
+def asynclm_rope_apply(table: CRopeTable, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
+    """Rows [tokens][heads][head_dim] of q (and k) turned by positions[token] (int32, device) into q_out (and k_out); out may be in."""
+    import torch
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together")
+    tokens, _, d = q.shape
+    rows = (CRopeRows * 2)()
+    for n, (x, y, name) in enumerate(((q, q_out, "q"), (k, k_out, "k"))):
+        if x is None:
+            continue
+        (a, sa), (b, sb) = _rows_of(x, name), _rows_of(y, name + "_out")
+        if x.shape != y.shape or x.shape[0] != tokens or x.shape[2] != d:
+            raise ValueError(f"{name}, {name}_out: {tuple(x.shape)} and {tuple(y.shape)} beside q of {tuple(q.shape)}")
+        rows[n] = CRopeRows(a, b, sa, sb, x.shape[1], 0)
+    if positions.numel() != tokens:
+        raise ValueError(f"positions: {positions.numel()} for {tokens} tokens")
+    _check(load().asynclm_rope_apply(ctypes.byref(table), _flat(positions, "positions", "a contiguous CUDA tensor of int32", (torch.int32,)), tokens, d, rows,
+                                     1 if k is None else 2, _stream_ptr(stream)), "asynclm_rope_apply")
+
+
+def asynclm_kv8_append(plan: Plan, k_new, v_new, kv8_pool, kv8_scales, rope: Optional[CRopeTable] = None, q=None, q_out=None, stream=None) -> None:
+    """The step's new K/V rows into the quantised cache; with `rope`, the keys turned by their positions first and q into q_out.  k_new, v_new and q may
+    be slices of a fused projection's output (any row stride)."""
+    (ka, ks), (va, vs) = _rows_of(k_new, "k_new"), _rows_of(v_new, "v_new")
+    (qa, qs), qo = (None, 0), None
+    if q is not None:
+        qa, qs = _rows_of(q, "q")
+        if q_out is None or q_out.shape != q.shape:
+            raise ValueError("q_out: a tensor of q's shape is wanted")
+        qo = _rows_of(q_out, "q_out", dense=True)[0]
+    rows = CKv8Rows(ka, va, qa, qo, ks, vs, qs)
+    pool, scales = _cache8(kv8_pool, kv8_scales)
+    _check(load().asynclm_kv8_append(plan.handle, ctypes.byref(rows), pool, scales, None if rope is None else ctypes.byref(rope),
+                                     _stream_ptr(stream)), "asynclm_kv8_append")
+
+
+def asynclm_kv8_attn_mixed(plan: Plan, q, kv8_pool, kv8_scales, out, lse=None, stream=None) -> None:
+    """asynclm_attn_mixed over the quantised cache."""
+    pool, scales = _cache8(kv8_pool, kv8_scales)
+    _check(load().asynclm_kv8_attn_mixed(plan.handle, q.data_ptr(), pool, scales, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                         _stream_ptr(stream)), "asynclm_kv8_attn_mixed")
+
+
+def asynclm_kv8_gather(plan: Plan, out_indptr, first, kv8_pool, kv8_scales, k_out, v_out, stream=None) -> None:
+    """Positions first[b] + i of every sequence b, i < out_indptr[b + 1] - out_indptr[b], read back into rows out_indptr[b] + i of k_out and v_out
+    (bf16 [rows][kv heads][head_dim]); out_indptr int64 [batch + 1] and first int32 [batch] on the device."""
+    import torch
+    k, v = _rows_of(k_out, "k_out", dense=True)[0], _rows_of(v_out, "v_out", dense=True)[0]
+    if k_out.shape != v_out.shape:
+        raise ValueError(f"k_out, v_out: {tuple(k_out.shape)} and {tuple(v_out.shape)}")
+    pool, scales = _cache8(kv8_pool, kv8_scales)
+    _check(load().asynclm_kv8_gather(plan.handle, _flat(out_indptr, "out_indptr", "a contiguous CUDA tensor of int64", (torch.int64,)),
+                                     _flat(first, "first", "a contiguous CUDA tensor of int32", (torch.int32,)), k_out.shape[0], pool, scales, k, v,
+                                     _stream_ptr(stream)), "asynclm_kv8_gather")
 
 
 def asynclm_read_ceiling(kv_pool, k_block_offsets, v_delta_bytes: int, block_bytes: int, sink, stream=None) -> None:

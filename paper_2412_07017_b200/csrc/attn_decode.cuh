@@ -37,6 +37,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "kv8.cuh"
 
 namespace asynclm {
 
@@ -139,6 +140,14 @@ __device__ __forceinline__ void tma_page_kv(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(0), "r"(kv_head), "r"(2 * page), "r"(bar) : "memory");
 }
 
+// The same for the 8-bit cache: a 4-D tensor of bytes (d values, 16 slots, Hkv heads, 2 * pages) and a box of (d, 16, 1, 2), rows swizzled over 128 bytes at
+// head_dim 128 and over 64 at head_dim 64 (piece c of slot s at c ^ (s & 7), or c ^ (s / 2 & 3)).
+__device__ __forceinline__ void tma_page_kv8(uint32_t dst, const CUtensorMap* map, int kv_head, int page, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(kv_head), "r"(2 * page), "r"(bar) : "memory");
+}
+
 // Four 8x8 b16 matrices; lane l gives the address of row l % 8 of matrix l / 8; thread (g, t) =
 // (lane / 4, lane % 4) receives elements [g][2t], [g][2t+1] of each (transposed: [2t][g], [2t+1][g]).
 __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -165,41 +174,59 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D>
+// The same with f16 operands.
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two floats -> packed f16x2 (lo in the low half).
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// KV8: the cache is the 8-bit one.
+template <int D, bool KV8>
 struct Geometry {
-    static constexpr int HALVES = D / 64;                       // 128-byte pieces of a K or V row
-    static constexpr int BLOCK_BYTES = kPage * D * 2;           // one (page, K|V, head) block
+    static constexpr int HALVES = D / 64;                       // 128-byte pieces of a K or V row (bf16)
+    static constexpr int BLOCK_BYTES = kPage * D * (KV8 ? 1 : 2);      // one (page, K|V, head) block
     static constexpr int PAGE_BYTES = 2 * BLOCK_BYTES;          // K block + V block: one TMA copy
-    static constexpr int WARP_PAGES = 128 / D;                  // pages of a stage that a consumer warp takes, kWarps apart
+    static constexpr int WARP_PAGES = KV8 ? 2 : 128 / D;        // pages of a stage that a consumer warp takes, kWarps apart
     static constexpr int STAGE_PAGES = kWarps * WARP_PAGES;
     static constexpr int STAGE_TOK = STAGE_PAGES * kPage;       // keys per ring stage: 128 or 256
-    static constexpr int STAGE_BYTES = STAGE_PAGES * PAGE_BYTES;      // 64 KiB
+    static constexpr int STAGE_BYTES = STAGE_PAGES * PAGE_BYTES;      // 64 KiB; 8 bits at head_dim 64: 32 KiB
+    static constexpr int SCALE_BYTES = KV8 ? STAGE_PAGES * kKv8ScaleBytes : 0;      // of a stage, behind all stages' pages
+    // Where page i of a stage lies in it.  8 bits: the two pages of a warp side by side, so that its merge state fits into their place.
+    static __device__ __forceinline__ int page_slot(int i) { return KV8 ? i % kWarps * 2 + i / kWarps : i; }
+    static constexpr int WARP_BYTES = KV8 ? WARP_PAGES * PAGE_BYTES : PAGE_BYTES;      // from one warp's merge state to the next one's
     static constexpr int Q_BYTES = kCols * D * 2;               // the unit's query rows, [column][d]
     static constexpr int KSTEPS = D / 16;
     // merge area of a warp inside its page slot: O^T as [column][d + 4] fp32 (the pad keeps the
     // fragment stores conflict-free), then the columns' reference maxima and sums
     static constexpr int O_STRIDE = D + 4;
     static constexpr int STATE_FLOATS = kCols * O_STRIDE + 2 * kCols;
-    static_assert(STATE_FLOATS * 4 <= PAGE_BYTES, "a warp's merge state must fit its page slot");
+    static_assert(STATE_FLOATS * 4 <= WARP_BYTES, "a warp's merge state must fit its page slot");
 };
 
-template <int D>
+template <int D, bool KV8 = false>
 constexpr size_t smem_bytes(int stages) {
-    using Geo = Geometry<D>;
-    return (size_t)stages * (Geo::STAGE_BYTES + Geo::Q_BYTES + sizeof(TileDesc) + 16) +
+    using Geo = Geometry<D, KV8>;
+    return (size_t)stages * (Geo::STAGE_BYTES + Geo::Q_BYTES + Geo::SCALE_BYTES + sizeof(TileDesc) + 16) +
            (size_t)(kHandoffs + kMergeReqs) * (sizeof(TileDesc) + 8) + kMergeReqs * 8 + sizeof(NextItem) + 24 +
            16 + 1024;
 }
 
 // The epilogue warp's loop (see the file comment): combine the consumers' states of a finished item,
 // write the result, give the stage back, and pass a completed split unit on to the merge warp.
-template <int D, int G>
+template <int D, int G, bool KV8>
 __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* __restrict__ out,
                                               float* __restrict__ lse, uint8_t* stage_base,
                                               const TileDesc* handoff, TileDesc* merge_req, uint32_t empty0,
                                               uint32_t done0, uint32_t req0, uint32_t reqfree0,
                                               volatile int* abort_flag) {
-    using Geo = Geometry<D>;
+    using Geo = Geometry<D, KV8>;
     const int lane = threadIdx.x & 31;
     const int Hq = p.num_q_heads;
     int n_req = 0;
@@ -229,7 +256,7 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
         // item's last page and its result for 1.95 us at 4 columns of 128, 1.15 now (us a layer from a graph: 4 decoding sequences
         // 12.66 -> 11.83, 64 over 1-3 K keys 82.6 -> 80.9, 32 with 8 spans 58.6 -> 57.0).  Unrolled passes are slower (12.02): a CTA
         // of a short step fetches this code once.
-        auto state = [&](int w) { return reinterpret_cast<const float*>(stage + (size_t)w * Geo::PAGE_BYTES); };
+        auto state = [&](int w) { return reinterpret_cast<const float*>(stage + (size_t)w * Geo::WARP_BYTES); };
         float wgt[2] = {0.f, 0.f}, inv[2] = {0.f, 0.f}, lse2[2] = {0.f, 0.f};
 #pragma unroll
         for (int q4 = 0; q4 < 2; ++q4) {
@@ -240,11 +267,17 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
 #pragma unroll
             for (int off = 1; off < kWarps; off <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
             wgt[q4] = m == -INFINITY ? 0.f : fast_exp2(m - M);
+            if constexpr (KV8) {      // (a warp all of whose visible keys are NaN has no maximum)
+                if (!(l >= 0.f)) wgt[q4] = l;
+            }
             float L = wgt[q4] != 0.f ? l * wgt[q4] : 0.f;
 #pragma unroll
             for (int off = 1; off < kWarps; off <<= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
             inv[q4] = L > 0.f ? 1.f / L : 0.f;
             lse2[q4] = L > 0.f ? M + log2f(L) : -INFINITY;
+            if constexpr (KV8) {      // a sum that is not a number stays one
+                if (!(L >= 0.f)) inv[q4] = lse2[q4] = L;
+            }
         }
         // four consecutive values of one column per lane and pass; the eight warps' copies are read
         // with independent loads
@@ -411,20 +444,160 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
     if (lane == 0 && part == 0) trace_mark(3);
 }
 
+// One consumer warp's pages of a stage of the 8-bit cache, two of them as two independent chains.
+//   A code is at most 448 and exact in f16, and so are the products of an f16 MMA, so both contractions take the codes as they are:
+//       s = (sum_i cK_i q'_i) * (query scale) * 2^eK           in fp32, a factor for a key and one for a column
+//       O += P' cV,  P' = p * 2^eV = exp2(s + eV - w)          the V row's scale goes into its weight's exponent
+// P' is rounded to f16 (11 bits), with a reference maximum w of its own, that of s + eV: weights and scales may
+// then lie anywhere, and none is lost that matters beside the largest.  The sum of the softmax is that of exp2(s - m), in fp32.
+//   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes of a row, values 4 t .. 4 t + 3 of a
+// 16-value piece: the first two are one k step's low half, the others its high half, and Q is laid out alike.  V (transposed): two neighbouring
+// values of two neighbouring keys; a byte permutation pairs the keys, and value 2 g becomes row g of the piece's MMA, 2 g + 1 row g + 8.
+//   For 32 keys x 128 values that is 32 ldmatrix'd registers of K, as many of V, 64 + 64 cvt, 32 byte permutations and 32 MMAs.
+template <int D, int G>
+__device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, const uint8_t* stage_scales, int warp, int lane, const uint32_t (&qb)[D / 16][2],
+                                          float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1, float& w0, float& w1) {
+    using Geo = Geometry<D, true>;
+    constexpr int WP = Geo::WARP_PAGES, PIECES = D / 16;
+    const int g = lane >> 2, t4 = lane & 3;
+    // lane -> row of an 8x8 matrix: (keys 0-7, piece p), (keys 8-15, p), (keys 0-7, p + 1), (keys 8-15, p + 1)
+    const int key = (lane & 7) + ((lane >> 3) & 1) * 8, half = lane >> 4;
+    const uint32_t row = (uint32_t)key * D, swz = D == 128 ? (uint32_t)(key & 7) : (uint32_t)(key >> 1 & 3);
+    auto page_smem = [&](int pp) { return smem_u32(stage) + (uint32_t)Geo::page_slot(pp * kWarps + warp) * Geo::PAGE_BYTES; };
+    bool on[WP];
+    float sc[WP][4], wv[WP][4], ek[WP][2], ev[WP][2];
+#pragma unroll
+    for (int pp = 0; pp < WP; ++pp) {
+        const int key0 = (pp * kWarps + warp) * kPage, valid = d.rows - key0;
+        on[pp] = pp == 0 || valid > 0;
+        if (!on[pp]) continue;
+        const uint8_t* sb = stage_scales + (pp * kWarps + warp) * kKv8ScaleBytes;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const uint32_t bk = sb[g + 8 * hh], bv = sb[kPage + g + 8 * hh];
+            ek[pp][hh] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
+            ev[pp][hh] = (float)((int)bv - 127);
+        }
+        if (valid < kPage) {
+            // Slots past the sequence's end hold whatever was in the page before, NaN codes included: their scores are masked, but 0 * NaN
+            // would still poison P V, so their V rows are cleared.
+            for (int i = valid * (D / 16) + lane; i < kPage * (D / 16); i += 32)
+                *reinterpret_cast<uint4*>(stage + (size_t)Geo::page_slot(pp * kWarps + warp) * Geo::PAGE_BYTES + Geo::BLOCK_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
+            __syncwarp();
+        }
+    }
+    // ---- S^T = K Q^T
+    float sa[WP][4], sb[WP][4];
+#pragma unroll
+    for (int pp = 0; pp < WP; ++pp)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sa[pp][e] = sb[pp][e] = 0.f;
+#pragma unroll
+    for (int pc = 0; pc < PIECES; pc += 2) {
+#pragma unroll
+        for (int pp = 0; pp < WP; ++pp) {
+            if (!on[pp]) continue;
+            uint32_t r[4];
+            ldsm_x4(page_smem(pp) + row + (((uint32_t)(pc + half) ^ swz) << 4), r);
+            const uint32_t a0[4] = {kv8_decode2(r[0]), kv8_decode2(r[1]), kv8_decode2_hi(r[0]), kv8_decode2_hi(r[1])};
+            const uint32_t a1[4] = {kv8_decode2(r[2]), kv8_decode2(r[3]), kv8_decode2_hi(r[2]), kv8_decode2_hi(r[3])};
+            mma_f16(sa[pp], a0, qb[pc][0], qb[pc][1]);
+            mma_f16(sb[pp], a1, qb[pc + 1][0], qb[pc + 1][1]);
+        }
+    }
+#pragma unroll
+    for (int pp = 0; pp < WP; ++pp) {
+        const int key0 = (pp * kWarps + warp) * kPage;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sc[pp][e] = on[pp] ? (sa[pp][e] + sb[pp][e]) * ((e & 1 ? qs1 : qs0) * ek[pp][e >> 1]) : -INFINITY;      // log2 domain
+            wv[pp][e] = on[pp] ? sc[pp][e] + ev[pp][e >> 1] : -INFINITY;
+        }
+        // ---- mask: key key0 + g (+8) is visible to column c iff it lies below lim0 + token(c)
+        if (d.lim0 < key0 + kPage) {
+            const int lim_a = d.lim0 + (2 * t4) / G - key0, lim_b = d.lim0 + (2 * t4 + 1) / G - key0;
+            if (g >= lim_a) sc[pp][0] = wv[pp][0] = -INFINITY;
+            if (g >= lim_b) sc[pp][1] = wv[pp][1] = -INFINITY;
+            if (g + 8 >= lim_a) sc[pp][2] = wv[pp][2] = -INFINITY;
+            if (g + 8 >= lim_b) sc[pp][3] = wv[pp][3] = -INFINITY;
+        }
+    }
+    // ---- softmax against the lazily moved reference maxima of this thread's two columns, and of their weights of V
+    float c0 = fmaxf(sc[0][0], sc[0][2]), c1 = fmaxf(sc[0][1], sc[0][3]);
+    float x0 = fmaxf(wv[0][0], wv[0][2]), x1 = fmaxf(wv[0][1], wv[0][3]);
+#pragma unroll
+    for (int pp = 1; pp < WP; ++pp) {
+        c0 = fmaxf(c0, fmaxf(sc[pp][0], sc[pp][2]));
+        c1 = fmaxf(c1, fmaxf(sc[pp][1], sc[pp][3]));
+        x0 = fmaxf(x0, fmaxf(wv[pp][0], wv[pp][2]));
+        x1 = fmaxf(x1, fmaxf(wv[pp][1], wv[pp][3]));
+    }
+    if (__any_sync(0xffffffffu, c0 > m0 + kRescaleThreshold || c1 > m1 + kRescaleThreshold || x0 > w0 + kRescaleThreshold || x1 > w1 + kRescaleThreshold)) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+            c0 = fmaxf(c0, __shfl_xor_sync(0xffffffffu, c0, off));
+            c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, off));
+            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, off));
+            x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, off));
+        }
+        auto moved = [](float& ref, float c) {      // the factor on what has been summed against the old reference
+            const float n = fmaxf(ref, c), f = n == -INFINITY ? 1.f : fast_exp2(ref - n);
+            ref = n;
+            return f;
+        };
+        l0 *= moved(m0, c0);
+        l1 *= moved(m1, c1);
+        const float f0 = moved(w0, x0), f1 = moved(w1, x1);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1;
+        }
+    }
+    const float u0 = m0 == -INFINITY ? 0.f : m0, u1 = m1 == -INFINITY ? 0.f : m1;
+    const float y0 = w0 == -INFINITY ? 0.f : w0, y1 = w1 == -INFINITY ? 0.f : w1;
+    uint32_t b0[WP], b1[WP];
+#pragma unroll
+    for (int pp = 0; pp < WP; ++pp) {
+        l0 += fast_exp2(sc[pp][0] - u0) + fast_exp2(sc[pp][2] - u0);
+        l1 += fast_exp2(sc[pp][1] - u1) + fast_exp2(sc[pp][3] - u1);
+        // P' (keys x columns, f16) -> its transpose as the B operand: two 8x8 transposes in registers
+        b0[pp] = movmatrix_t(pack_f16x2(fast_exp2(wv[pp][0] - y0), fast_exp2(wv[pp][1] - y1)));
+        b1[pp] = movmatrix_t(pack_f16x2(fast_exp2(wv[pp][2] - y0), fast_exp2(wv[pp][3] - y1)));
+    }
+    // ---- O^T += V^T P'^T
+#pragma unroll
+    for (int pp = 0; pp < WP; ++pp) {
+        if (!on[pp]) continue;
+#pragma unroll
+        for (int pc = 0; pc < PIECES; pc += 2) {
+            uint32_t r[4];
+            ldsm_x4_t(page_smem(pp) + (uint32_t)Geo::BLOCK_BYTES + row + (((uint32_t)(pc + half) ^ swz) << 4), r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[k] = __byte_perm(r[k], 0, 0x3120);      // bytes (key, value): 00 01 10 11 -> 00 10, 01 11
+            const uint32_t a0[4] = {kv8_decode2(r[0]), kv8_decode2_hi(r[0]), kv8_decode2(r[1]), kv8_decode2_hi(r[1])};
+            const uint32_t a1[4] = {kv8_decode2(r[2]), kv8_decode2_hi(r[2]), kv8_decode2(r[3]), kv8_decode2_hi(r[3])};
+            mma_f16(o[pc], a0, b0[pp], b1[pp]);
+            mma_f16(o[pc + 1], a1, b0[pp], b1[pp]);
+        }
+    }
+}
+
 // The whole kernel body: warps 0-7 consume, warp 8 produces, warps 9 and 10 are the epilogue and the
 // merge warp, any further warps of the CTA return at once (the fused kernel has twelve).  With PREFETCH the first pages of a
 // CTA's first item are brought into L2 out of `pool` ahead (see the consumer warps).
-template <int D, int GT, bool APPEND, bool PREFETCH>
+template <int D, int GT, bool APPEND, bool PREFETCH, bool KV8 = false>
 __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap* kv_map, const __nv_bfloat16* pool,
                                             const __nv_bfloat16* __restrict__ q,
                                             __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
-                                            int S, uint8_t* smem, const AppendSrc& app) {
-    using Geo = Geometry<D>;
+                                            int S, uint8_t* smem, const AppendSrc& app, const uint8_t* scales = nullptr) {
+    using Geo = Geometry<D, KV8>;
     constexpr int G = GT;
+    static_assert(!(APPEND && KV8), "the append inside the attention is the bf16 cache's");
     static_assert(G <= kCols && kCols % G == 0, "heads per kv head must divide the column count");
     uint8_t* stage_base = smem;                                        // 1024-byte aligned
     uint8_t* q_base = stage_base + (size_t)S * Geo::STAGE_BYTES;
-    TileDesc* desc = (TileDesc*)(q_base + (size_t)S * Geo::Q_BYTES);
+    uint8_t* scale_base = q_base + (size_t)S * Geo::Q_BYTES;
+    TileDesc* desc = (TileDesc*)(scale_base + (size_t)S * Geo::SCALE_BYTES);
     TileDesc* handoff = desc + S;                // what the epilogue warp needs to know about a finished item
     TileDesc* merge_req = handoff + kHandoffs;   // completed split units on their way to the merge warp
     NextItem* next_item = (NextItem*)(merge_req + kMergeReqs);
@@ -440,7 +613,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     if (threadIdx.x == 32) asm volatile("prefetch.tensormap [%0];" ::"l"(kv_map));
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(full0 + 8 * s, 1);
+            mbar_init(full0 + 8 * s, KV8 ? 33 : 1);      // (8 bits: and one of each lane's copy of scales)
             mbar_init(empty0 + 8 * s, kWarps);
         }
         for (int h = 0; h < kHandoffs; ++h) mbar_init(done0 + 8 * h, kWarps);
@@ -557,9 +730,22 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                     // checked build only: a bad id is replaced by page 0 (the copy must happen: the stage counts its bytes)
                     if (lane < npages && !page_ok(page, p.num_pages, p.status, kStatusBadPageWarp)) page = 0;
                     if (lane == 0) { if (n == 0) trace_mark(2); trace_add(6, 1); if (first) trace_add(5, 1); }
-                    if (lane < npages)
+                    if constexpr (KV8) {
+                        // The pages, one TMA copy each, and their 32 scale bytes, by cp.async, 16 bytes a lane: another TMA copy for them
+                        // would cost the copy unit more than their bytes do.
+                        const int scale_page = __shfl_sync(0xffffffffu, page, lane >> 1);
+                        if (lane < npages)
+                            tma_page_kv8(smem_u32(stage_base + (size_t)s * Geo::STAGE_BYTES + (size_t)Geo::page_slot(lane) * Geo::PAGE_BYTES),
+                                         kv_map, cur.kv_head, page, full0 + 8 * s);
+                        if (lane >> 1 < npages)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                         ::"r"(smem_u32(scale_base + (size_t)s * Geo::SCALE_BYTES + lane * 16)),
+                                           "l"(scales + kv8_scale_offset(scale_page, lane & 1, cur.kv_head, 0, p.num_kv_heads)) : "memory");
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full0 + 8 * s) : "memory");
+                    } else if (lane < npages) {
                         tma_page_kv(smem_u32(stage_base + (size_t)s * Geo::STAGE_BYTES + (size_t)lane * Geo::PAGE_BYTES),
                                     kv_map, cur.kv_head, page, full0 + 8 * s);
+                    }
                     // the unit's query rows: G * d contiguous values per token, columns in (token, head) order
                     if (first && lane >= 16 && lane - 16 < cur.ntok) {
                         const int tok = lane - 16;
@@ -583,7 +769,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                 landing = max(0, n - S + 1);      // stage s has been used and is given away again below
                 if (lane == 0) {
                     desc[s].flags = kFlagEnd;
-                    mbar_arrive(full0 + 8 * s);
+                    mbar_arrive_n(full0 + 8 * s, KV8 ? 33 : 1);
                 }
             }
         }
@@ -599,7 +785,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     }
 
     if (warp == kEpilogueWarp) {
-        epilogue_loop<D, G>(p, out, lse, stage_base, handoff, merge_req, empty0, done0, req0, reqfree0, abort_flag);
+        epilogue_loop<D, G, KV8>(p, out, lse, stage_base, handoff, merge_req, empty0, done0, req0, reqfree0, abort_flag);
         return;
     }
     // Where nothing is queued and a CTA has one item at most, the fetch warp has nothing to fetch and is a second merge warp.  (Such a
@@ -682,7 +868,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
         const Work* w = reinterpret_cast<const Work*>(head + kHeadWorkCuda);
         const int pages = head[2] < head[3] ? (w->kv_end - w->kv0 + kPage - 1) / kPage : 0;
-        if (pages >= kPrefetchMinPages) prefetch_first_pages<D>(p, pool, head + kHeadPagesCuda, pages, w->kv_head, warp, kWarps, lane);
+        if (pages >= kPrefetchMinPages) prefetch_first_pages<D, KV8>(p, pool, head + kHeadPagesCuda, pages, w->kv_head, warp, kWarps, lane);
     }
     pdl_wait();
     const int g = lane >> 2, t4 = lane & 3;      // fragment coordinates
@@ -698,6 +884,8 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     uint32_t qb[Geo::KSTEPS][2];      // B fragments of Q^T: column g, values 16 ks + 2 t4 (+1) and + 8
     float o[Geo::KSTEPS][4];          // O^T: rows d = 16 i + g (+8), columns 2 t4, 2 t4 + 1
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;      // of columns 2 t4 and 2 t4 + 1
+    // 8 bits: the columns' query scales, and the reference maxima of score + log2(scale of the V row), see below
+    float qs0 = 0.f, qs1 = 0.f, w0 = -INFINITY, w1 = -INFINITY;
     int item_count = 0;
 
     for (int n = 0;; ++n) {
@@ -716,13 +904,40 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         if (d.flags & kFlagFirst) {
             const uint8_t* qs = q_base + (size_t)s * Geo::Q_BYTES;
             const bool col_valid = g < d.ntok * G;
+            if constexpr (KV8) {
+                // The codes go to the tensor core as f16, which holds them exactly; so does the query row, by an f16 copy divided by the
+                // power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value).
+                // Thread (g, t4) holds values 16 ks + 4 t4 .. + 3: the order in which ldmatrix deals out a row's bytes.
+                uint2 w[Geo::KSTEPS];
+                uint32_t most = 0;
 #pragma unroll
-            for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
-                const uint32_t* src = reinterpret_cast<const uint32_t*>(qs + ((size_t)g * D + ks * 16 + t4 * 2) * 2);
-                qb[ks][0] = col_valid ? src[0] : 0u;
-                qb[ks][1] = col_valid ? src[4] : 0u;
+                for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
+                    w[ks] = col_valid ? *reinterpret_cast<const uint2*>(qs + ((size_t)g * D + ks * 16 + t4 * 4) * 2) : make_uint2(0, 0);
+                    most = max(max(most, max(w[ks].x & 0x7fffu, w[ks].x >> 16 & 0x7fffu)), max(w[ks].y & 0x7fffu, w[ks].y >> 16 & 0x7fffu));
+                }
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                const uint32_t e = min(max(most >> 7, 1u), 253u);
+                const float down = __uint_as_float((254u - e) << 23), up = __uint_as_float(e << 23) * qscale;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[ks][e] = 0.f;
+                for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
+                    qb[ks][0] = pack_f16x2(bf16_lo(w[ks].x) * down, bf16_hi(w[ks].x) * down);
+                    qb[ks][1] = pack_f16x2(bf16_lo(w[ks].y) * down, bf16_hi(w[ks].y) * down);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[ks][e] = 0.f;
+                }
+                qs0 = __shfl_sync(0xffffffffu, up, 8 * t4);          // of columns 2 t4 and 2 t4 + 1
+                qs1 = __shfl_sync(0xffffffffu, up, 8 * t4 + 4);
+                w0 = w1 = -INFINITY;
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
+                    const uint32_t* src = reinterpret_cast<const uint32_t*>(qs + ((size_t)g * D + ks * 16 + t4 * 2) * 2);
+                    qb[ks][0] = col_valid ? src[0] : 0u;
+                    qb[ks][1] = col_valid ? src[4] : 0u;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[ks][e] = 0.f;
+                }
             }
             m0 = m1 = -INFINITY;
             l0 = l1 = 0.f;
@@ -733,7 +948,10 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         // 577, 148, which memory bounds, 768 | 644; us of attention a layer: 64 decoding sequences of 32/8 heads over 1-3 K keys
         // 47.8 -> 44.6, 256 of 8/2 heads 29.9 -> 27.8, 32 with 8 spans 49.1 -> 46.3, 100 of 8/2 heads with 20 spans 49.2 -> 42.0.)
         constexpr int WP = Geo::WARP_PAGES;
-        if (warp * kPage < d.rows) {
+        if constexpr (KV8) {
+            if (warp * kPage < d.rows)
+                pages_kv8<D, G>(d, stage, scale_base + (size_t)s * Geo::SCALE_BYTES, warp, lane, qb, o, qs0, qs1, m0, m1, l0, l1, w0, w1);
+        } else if (warp * kPage < d.rows) {
             bool on[WP];
             float sc[WP][4];
 #pragma unroll
@@ -842,20 +1060,31 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         // ---- end of item: leave this warp's state in its own page slot of the stage (only this warp
         // read that slot) for the epilogue warp, and go on
         {
-            float* st = reinterpret_cast<float*>(stage + (size_t)warp * Geo::PAGE_BYTES);
+            float* st = reinterpret_cast<float*>(stage + (size_t)warp * Geo::WARP_BYTES);
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) {
                 l0 += __shfl_xor_sync(0xffffffffu, l0, off);
                 l1 += __shfl_xor_sync(0xffffffffu, l1, off);
             }
             __syncwarp();      // every lane is done reading the page before it is overwritten
+            if constexpr (KV8) {
+                // to the columns' own reference maxima, in fp32; and rows g, g + 8 of a fragment are values 2 g, 2 g + 1
+                const float f0 = m0 == -INFINITY ? 0.f : fast_exp2(w0 - m0), f1 = m1 == -INFINITY ? 0.f : fast_exp2(w1 - m1);
 #pragma unroll
-            for (int i = 0; i < Geo::KSTEPS; ++i) {
-                float* c = st + (size_t)(2 * t4) * Geo::O_STRIDE + 16 * i + g;
-                c[0] = o[i][0];
-                c[Geo::O_STRIDE] = o[i][1];
-                c[8] = o[i][2];
-                c[Geo::O_STRIDE + 8] = o[i][3];
+                for (int i = 0; i < Geo::KSTEPS; ++i) {
+                    float* c = st + (size_t)(2 * t4) * Geo::O_STRIDE + 16 * i + 2 * g;
+                    *reinterpret_cast<float2*>(c) = make_float2(o[i][0] * f0, o[i][2] * f0);
+                    *reinterpret_cast<float2*>(c + Geo::O_STRIDE) = make_float2(o[i][1] * f1, o[i][3] * f1);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < Geo::KSTEPS; ++i) {
+                    float* c = st + (size_t)(2 * t4) * Geo::O_STRIDE + 16 * i + g;
+                    c[0] = o[i][0];
+                    c[Geo::O_STRIDE] = o[i][1];
+                    c[8] = o[i][2];
+                    c[Geo::O_STRIDE + 8] = o[i][3];
+                }
             }
             if (g == 0) {
                 float* ms = st + kCols * Geo::O_STRIDE;

@@ -131,16 +131,16 @@ __device__ __forceinline__ size_t pool_row_offset(int64_t page, int which, int k
 // `kv_head`.  A hint: nothing is read, so it may come before the kernels in front have completed.  Done with ordinary
 // prefetch instructions of warps that have nothing to do yet, because the copy unit would take its 40-60 ns for each
 // page and the first copies stand behind that (a step of 4 sequences over 100-300 keys 8.4 -> 10.4 us).
-template <int D>
+template <int D, bool KV8>
 __device__ __forceinline__ void prefetch_first_pages(const DevPlan& p, const __nv_bfloat16* pool, const int32_t* pages, int num_pages, int kv_head,
                                                      int first, int step, int lane) {
-    constexpr int kLines = kPage * D * 2 / 128;      // of a block: 32 or 16
+    constexpr int kLines = kPage * D * (KV8 ? 1 : 2) / 128;      // of a block: 32 or 16, of 8 bits a value 16 or 8
     for (int k = first; k < min(num_pages, 32); k += step) {
         const int page = __ldg(pages + k);
         if (page < 0 || page >= p.num_pages) continue;      // (the checked build reports it where it is copied)
 #pragma unroll
         for (int l = lane; l < 2 * kLines; l += 32) {
-            const __nv_bfloat16* line = pool + pool_row_offset(page, l / kLines, kv_head, 0, p.num_kv_heads, D) + (l % kLines) * 64;
+            const uint8_t* line = reinterpret_cast<const uint8_t*>(pool) + pool_row_offset(page, l / kLines, kv_head, 0, p.num_kv_heads, D) * (KV8 ? 1 : 2) + (l % kLines) * 128;
             asm volatile("prefetch.global.L2 [%0];" ::"l"(line));
         }
     }

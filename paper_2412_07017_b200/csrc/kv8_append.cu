@@ -1,0 +1,127 @@
+// The append of the 8-bit cache: the step's new K and V rows, quantised as they are written into their page slots, the keys (and, if
+// asked, the queries) turned by their positions on the way.
+//
+// The interrupt block goes to the end of the context (paper Section 3.2): new token i of sequence b sits at position ctx_b + i, in the slot
+// that the planner resolved.  A row is read once, turned in fp32 (rope_rows.cuh), its largest magnitude found by shuffles over the
+// head_dim / 8 lanes that hold it, and its codes and scale written (kv8.cuh): there is one rounding between the projection's bf16 and the code.
+// Bound by memory: 3 d bytes a K or V row and 4 d a query row, in whole 128-byte lines at head_dim 128; for few tokens by launch and latency.
+#include <algorithm>
+
+#include "kernels.h"
+#include "plan_internal.h"
+#include "rope_rows.cuh"
+
+namespace asynclm {
+
+namespace {
+
+struct AppendSets { RowSet set[3]; };      // K, V, Q
+
+__global__ void __launch_bounds__(kRopeRowThreads)
+kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __grid_constant__ AppendSets sets, uint8_t* pool, uint8_t* scales, int tokens) {
+    extern __shared__ uint4 smem[];
+    float4 (*table)[kRopeEntries] = reinterpret_cast<float4 (*)[kRopeEntries]>(smem + kRopeRowThreads);
+    pdl_trigger();   // the attention kernel may start its prologue; it waits for this grid before reading the pool
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int d = p.head_dim, hkv = p.num_kv_heads;
+    const int per_row = d / 8, rows = 32 / per_row;      // lanes of a row (16 or 8), rows of a warp
+    const int v = lane % per_row, sub = lane / per_row;
+    const int r0 = blockIdx.x * tokens, n = min(tokens, p.total_q - r0);
+    const int block = rows * kRopeUnroll;
+    const int blocks_kv = (hkv + block - 1) / block, blocks = 2 * blocks_kv + (sets.set[2].heads + block - 1) / block;
+    // the angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the kernels in front
+    // until those have completed
+    rope_fill(turns, table, n, [&](int i) {
+        const int r = r0 + i, b = __ldg(p.row_seq + r);
+        return __ldg(p.kv_len_before + b) + r - __ldg(p.q_indptr + b);
+    });
+    pdl_wait();
+    __syncthreads();
+    for (int item = warp; item < n * blocks; item += warps) {
+        const int i = item / blocks, b = item % blocks;
+        const int which = b < blocks_kv ? 0 : b < 2 * blocks_kv ? 1 : 2;      // K, V, Q
+        const RowSet& set = sets.set[which];
+        const int h0 = (b - which * blocks_kv) * block + sub;
+        const int64_t slot = which < 2 ? __ldg(p.row_slot + r0 + i) : 0;
+        const __nv_bfloat16* in = set.in + (int64_t)(r0 + i) * set.in_stride + 8 * v;
+        uint4 x[kRopeUnroll];
+        bool on[kRopeUnroll];
+#pragma unroll
+        for (int u = 0; u < kRopeUnroll; ++u) {
+            const int h = h0 + u * rows;
+            on[u] = h < set.heads;
+            x[u] = on[u] ? ldg_nc_v4(in + (int64_t)h * d) : make_uint4(0, 0, 0, 0);
+        }
+        RopeLane cs;
+        const bool turned = set.turned != 0 && turns.rotary_dim > 0;
+        if (turned) cs = rope_lane(turns, table[i], v);
+        const bool page_fine = which == 2 || page_ok(slot / kPage, p.num_pages, p.status, kStatusBadPageAppend);
+#pragma unroll
+        for (int u = 0; u < kRopeUnroll; ++u) {
+            const int h = h0 + u * rows;
+            float y[8];
+            if (turned) {
+                rope_turn(turns, cs, v, lane, smem + warp * 32, x[u], y);
+            } else {
+                const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { y[2 * k] = bf16_lo(w[k]); y[2 * k + 1] = bf16_hi(w[k]); }
+            }
+            if (which == 2) {
+                if (on[u]) {
+                    uint4 o = x[u];
+                    if (8 * v < turns.rotary_dim) o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    *reinterpret_cast<uint4*>(set.out + (int64_t)(r0 + i) * set.out_stride + (int64_t)h * d + 8 * v) = o;
+                }
+                continue;
+            }
+            uint32_t most = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(y[k]) & 0x7fffffffu);
+            for (int off = 1; off < per_row; off <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
+            const uint32_t byte = kv8_scale_byte(most);
+            const float inv = byte == kKv8NanByte ? 0.f : __uint_as_float((254u - byte) << 23);      // 2^-e
+            uint2 codes = make_uint2(kv8_encode2(y[0] * inv, y[1] * inv) | kv8_encode2(y[2] * inv, y[3] * inv) << 16,
+                                     kv8_encode2(y[4] * inv, y[5] * inv) | kv8_encode2(y[6] * inv, y[7] * inv) << 16);
+            if (byte == kKv8NanByte) codes = make_uint2(0, 0);
+            if (on[u] && page_fine) {
+                *reinterpret_cast<uint2*>(pool + kv8_row_offset(slot / kPage, which, h, (int)(slot % kPage), hkv, d) + 8 * v) = codes;
+                if (v == 0) scales[kv8_scale_offset(slot / kPage, which, h, (int)(slot % kPage), hkv)] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+}  // namespace asynclm
+
+extern "C" int asynclm_kv8_append(const asynclm_plan_t* plan, const asynclm_kv8_rows* rows, void* kv8_pool, void* kv8_scales,
+                                  const asynclm_rope_table* rope, void* stream) {
+    using namespace asynclm;
+    if (!plan || plan->magic != kPlanMagic || plan->host_only || !rows) return ASYNCLM_ERR_INVALID_ARG;
+    const DevPlan& d = plan->dev;
+    RopeTurns turns{};
+    if (rope && !rope_turns(rope, d.head_dim, &turns)) return ASYNCLM_ERR_INVALID_ARG;
+    if ((rows->q != nullptr) != (rows->q_out != nullptr) || (rows->q && !rope)) return ASYNCLM_ERR_INVALID_ARG;
+    const int64_t kv = (int64_t)d.num_kv_heads * d.head_dim, qd = (int64_t)d.num_q_heads * d.head_dim;
+    const int64_t ks = rows->k_stride ? rows->k_stride : kv, vs = rows->v_stride ? rows->v_stride : kv, qs = rows->q_stride ? rows->q_stride : qd;
+    if (ks < kv || vs < kv || qs < qd || ((ks | vs | qs) & 7) != 0) return ASYNCLM_ERR_INVALID_ARG;
+    if (rows->q && rows->q == rows->q_out && qs != qd) return ASYNCLM_ERR_INVALID_ARG;      // (q_out is dense)
+    if (d.total_q == 0) return ASYNCLM_OK;
+    if (!rows->k || !rows->v || !kv8_pool || !kv8_scales ||
+        (((uintptr_t)rows->k | (uintptr_t)rows->v | (uintptr_t)rows->q | (uintptr_t)rows->q_out | (uintptr_t)kv8_pool | (uintptr_t)kv8_scales) & 15) != 0)
+        return ASYNCLM_ERR_INVALID_ARG;
+    if (int rc = check_plan_device(plan->device)) return rc;
+    AppendSets sets{};
+    sets.set[0] = RowSet{(const __nv_bfloat16*)rows->k, nullptr, ks, 0, d.num_kv_heads, 1};
+    sets.set[1] = RowSet{(const __nv_bfloat16*)rows->v, nullptr, vs, 0, d.num_kv_heads, 0};
+    if (rows->q) sets.set[2] = RowSet{(const __nv_bfloat16*)rows->q, (__nv_bfloat16*)rows->q_out, qs, qd, d.num_q_heads, 1};
+    PlanUse use(plan, (cudaStream_t)stream);
+    const int tokens = rope_row_tokens(d.total_q), block = 32 / (d.head_dim / 8) * kRopeUnroll;
+    const int blocks = 2 * ((d.num_kv_heads + block - 1) / block) + (sets.set[2].heads + block - 1) / block;
+    const int threads = 32 * std::min(kRopeRowThreads / 32, tokens * blocks);
+    return cuda_status(use.launched(launch_when(!use.dev.full_launch, kv8_append_kernel, dim3((d.total_q + tokens - 1) / tokens), dim3(threads),
+                                                rope_row_smem(tokens), (cudaStream_t)stream, use.dev, turns, sets, (uint8_t*)kv8_pool,
+                                                (uint8_t*)kv8_scales, tokens)));
+}

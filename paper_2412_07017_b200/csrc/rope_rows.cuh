@@ -1,0 +1,161 @@
+// Rows of heads, turned by their tokens' positions and written as bf16 (rope.cu) or as rows of the 8-bit cache (kv8_append.cu).
+//
+// Rotary positions: pair j of a head's first rotary_dim values turns by the angle position * f_j,
+//     (x, y) -> m (x cos a - y sin a, y cos a + x sin a),
+// the pairs being (j, j + rotary_dim / 2) or (2j, 2j + 1), the others passing through.  The frequencies come as turns (f_j / 2 pi) in
+// fp64, where position * turns is reduced to [-1/2, 1/2] and its sine and cosine are taken: an fp32 angle is off by thousandths of a radian at
+// positions of 10^5.  Both are kept as two fp32 numbers, high and low part, and a product difference x c - y s is evaluated with its
+// rounding errors (rope_diff): a value that is left over from two that cancel is as exact, relatively, as any other, and is rounded
+// once, to what is written.  That takes six fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
+//
+// What bounds it: memory (8 bytes of traffic for each pair's eight flops) or, for few tokens, the latency of one chain: positions, angles, rows, stores.
+// A thread holds 8 values of a row, 16 bytes; head_dim / 8 lanes hold a row, so a pair's other half comes by shuffle, and so does a row's
+// maximum.  A warp takes kRopeUnroll times as many rows of ONE token as it has room for and requests them together: the sines and cosines of a
+// lane's values are the same for all heads and are read from shared memory once.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "asynclm.h"
+#include "common.cuh"
+#include "kv8.cuh"
+
+namespace asynclm {
+
+constexpr int kRopeRowThreads = 256;
+constexpr int kRopeUnroll = 4;
+constexpr int kRopeMaxPairs = 128;
+constexpr int kRopeEntries = kRopeMaxPairs + 8;      // of a token's table, see rope_entry
+constexpr int kRopeMaxTokens = 8;                    // of a CTA
+
+// Heads [T][heads][head_dim] of one tensor, rows `stride` values apart.
+struct RowSet {
+    const __nv_bfloat16* in;
+    __nv_bfloat16* out;           // bf16 output, or null: a K or V set of the cache
+    int64_t in_stride, out_stride;
+    int32_t heads;
+    int32_t turned;               // whether the rows are rotated
+};
+
+struct RopeTurns {
+    double turns[kRopeMaxPairs];
+    double factor;
+    int32_t rotary_dim;           // 0: nothing turns
+    int32_t layout;
+};
+
+// Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8 (halves of whole vectors), 4 (interleaved) or each by itself, and lanes
+// next to each other then read entries next to each other.
+__device__ __forceinline__ int rope_group(int rotary_dim, int layout) {
+    return layout == ASYNCLM_ROPE_INTERLEAVED ? 4 : rotary_dim % 16 == 0 ? 8 : 1;
+}
+__device__ __forceinline__ int rope_entry(int j, int m, int per) { return m == 1 ? j : (j % m) * per + j / m; }
+
+// x c - y s with c = c.x + c.y, s = s.x + s.y, x and y of few bits: the first product's rounding error and the low parts are added last (the difference
+// of products by fused multiply-adds is W. Kahan's).
+__device__ __forceinline__ float rope_diff(float x, float2 c, float y, float2 s) {
+    const float p = __fmul_rn(y, s.x);
+    const float err = __fmaf_rn(y, s.x, -p);                       // y s.x = p + err, exactly
+    const float low = __fmaf_rn(x, c.y, -__fmaf_rn(y, s.y, err));
+    return __fadd_rn(__fmaf_rn(x, c.x, -p), low);
+}
+
+// Fills table[i][...] with m cos and m sin (high parts, then low parts) of tokens 0 .. n - 1 of the CTA.  A thread keeps one pair, whose frequency it reads from the kernel's
+// parameters once (lanes that read different entries there take turns).
+template <typename Position>
+__device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kRopeEntries], int n, Position position) {
+    const int pairs = r.rotary_dim / 2;
+    if (pairs == 0) return;
+    const int m = rope_group(r.rotary_dim, r.layout), per = (pairs + m - 1) / m;
+    const int at_once = max(1, (int)blockDim.x / pairs);
+    for (int a = threadIdx.x; a < at_once * pairs; a += blockDim.x) {      // (blocks of fewer threads than pairs: several pairs a thread)
+        const int j = a % pairs;
+        const double f = r.turns[j];
+        const int e = rope_entry(j, m, per);
+        for (int i = a / pairs; i < n; i += at_once) {
+            const double t = (double)position(i) * f;
+            double s, c;
+            sincospi(2.0 * (t - rint(t)), &s, &c);
+            c *= r.factor;
+            s *= r.factor;
+            const float ch = (float)c, sh = (float)s;
+            table[i][e] = make_float4(ch, sh, (float)(c - (double)ch), (float)(s - (double)sh));
+        }
+    }
+}
+
+// This lane's sines and cosines: of its 8 values (halves), or of its 4 pairs (interleaved; c[k], s[k] for k < 4).
+struct RopeLane { float2 c[8], s[8]; };
+
+__device__ __forceinline__ RopeLane rope_lane(const RopeTurns& r, const float4* table, int v) {
+    RopeLane x;
+    const int rd = r.rotary_dim, pairs = rd / 2, m = rope_group(rd, r.layout), per = (pairs + m - 1) / m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float4 cs = make_float4(1.f, 0.f, 0.f, 0.f);
+        const int dim = 8 * v + k;
+        if (r.layout == ASYNCLM_ROPE_INTERLEAVED) {
+            if (k < 4 && 4 * v + k < pairs) cs = table[k * per + v];
+        } else if (dim < rd) {
+            const bool second = dim >= pairs;
+            const int j = second ? dim - pairs : dim;
+            cs = table[rope_entry(j, m, per)];
+            if (second) cs.y = -cs.y, cs.w = -cs.w;      // x c - y s for the first value of a pair, y c + x s for the second
+        }
+        x.c[k] = make_float2(cs.x, cs.z);
+        x.s[k] = make_float2(cs.y, cs.w);
+    }
+    return x;
+}
+
+// y = the lane's 8 values of a row, turned.  All lanes of the warp take part.  `stage`: 512 bytes of the warp's own.
+__device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane& cs, int v, int lane, uint4* stage, const uint4& x, float (&y)[8]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float own[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { own[2 * k] = bf16_lo(w[k]); own[2 * k + 1] = bf16_hi(w[k]); }
+    const int rd = r.rotary_dim, pairs = rd / 2;
+    if (r.layout == ASYNCLM_ROPE_INTERLEAVED) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float a = own[2 * k], b = own[2 * k + 1];
+            const bool on = 4 * v + k < pairs;      // (0 * infinity is not to reach a value that passes through)
+            y[2 * k] = on ? rope_diff(a, cs.c[k], b, cs.s[k]) : a;
+            y[2 * k + 1] = on ? rope_diff(b, cs.c[k], a, make_float2(-cs.s[k].x, -cs.s[k].y)) : b;
+        }
+    } else if (rd % 16 == 0) {
+        // whole vectors: the pairs' other values are those of one other lane
+        const int off = pairs / 8, other = v < off ? lane + off : v < 2 * off ? lane - off : lane;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t p = __shfl_sync(0xffffffffu, w[k], other);
+            y[2 * k] = rope_diff(own[2 * k], cs.c[2 * k], bf16_lo(p), cs.s[2 * k]);
+            y[2 * k + 1] = rope_diff(own[2 * k + 1], cs.c[2 * k + 1], bf16_hi(p), cs.s[2 * k + 1]);
+        }
+    } else {
+        // halves that do not begin on a vector: through shared memory, value by value
+        __syncwarp();
+        stage[lane] = x;
+        __syncwarp();
+        const unsigned short* row = reinterpret_cast<const unsigned short*>(stage + (lane - v));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int dim = 8 * v + k;
+            const float p = dim < rd ? __uint_as_float((uint32_t)row[dim < pairs ? dim + pairs : dim - pairs] << 16) : 0.f;
+            y[k] = rope_diff(own[k], cs.c[k], p, cs.s[k]);
+        }
+    }
+}
+
+// Tokens of a CTA: one while that leaves SMs without a CTA, up to eight, whose angles are then worked out beside each other.
+inline int rope_row_tokens(int total) {
+    int t = (total + 148 * 4 - 1) / (148 * 4);
+    return t < 1 ? 1 : t > kRopeMaxTokens ? kRopeMaxTokens : t;
+}
+// A warp's stage (512 bytes each) and the tables.
+inline size_t rope_row_smem(int tokens) { return (size_t)kRopeRowThreads * sizeof(uint4) + (size_t)tokens * kRopeEntries * sizeof(float4); }
+
+// The table's numbers as kernels take them; false if it is not one that asynclm_rope_table_init made for this head_dim.
+bool rope_turns(const asynclm_rope_table* table, int head_dim, RopeTurns* out);
+
+}  // namespace asynclm
