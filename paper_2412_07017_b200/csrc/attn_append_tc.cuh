@@ -50,6 +50,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "kv8.cuh"
 #include "span_ring.h"
 
 namespace asynclm {
@@ -63,9 +64,12 @@ constexpr int kTile = 64;                        // keys per KV tile: a K or V r
 constexpr float kRescaleThreshold = 8.f;
 constexpr long long kWaitCycles = 2000000000ll;
 constexpr long long kGroupSkewCycles = 600;
+// 8 bits: V rows whose exponents lie further apart than this take the softmax sum of their tile by exponentials of its own.  (The weight of a
+// key is exp2(s + eV - reference), and the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
+constexpr int kFarExponents = 95;
 
 // Per head_dim: shared memory map (offsets from a 1024-byte aligned base) and barriers.
-template <int D>
+template <int D, bool KV8 = false>
 struct Geometry {
     static constexpr int HALVES = D / 64;                                  // 128-byte pieces of a row
     static constexpr uint32_t QHALF_BYTES = kRows * 128;                   // one 64-value half of a Q tile
@@ -76,14 +80,18 @@ struct Geometry {
     static constexpr uint32_t GROUP_BYTES = HALVES * ATOM_BYTES;
     static constexpr uint32_t PAGE_BYTES = 2 * GROUP_BYTES;
     static constexpr uint32_t SLOT_BYTES = kTile / kPage * PAGE_BYTES;
-    static constexpr int RING = ring_slots(D);                             // slots of the K ring and of the V ring
+    static constexpr int RING = KV8 ? ring_slots_kv8(D) : ring_slots(D);   // slots of the K ring and of the V ring
     static constexpr uint32_t OFF_Q = 0;                                   // Q[0], Q[1]
     static constexpr uint32_t OFF_RING = OFF_Q + 2 * QTILE_BYTES;
+    // 8 bits: a tile's scales as the softmax takes them, fp32: 2^eK, eV, 2^-eV of its 64 keys, and whether the exponents are far apart
+    static constexpr uint32_t OFF_SCALE = OFF_RING + 2 * RING * SLOT_BYTES;
+    static constexpr int SCALE_SLOTS = KV8 ? scale_slots(RING) : 0;
+    static constexpr uint32_t SCALE_BYTES = 3 * kTile * 4 + 16;
     // The barriers lie behind everything the warp body uses when the CTA goes on to it: arrivals that nobody
     // waits for (an item's last on kOFree and on the ring's empty barriers) may still be queued in the shared
     // memory pipe then, and would change whatever has been copied there since.
     static constexpr uint32_t OFF_BAR = 224 * 1024;
-    static_assert(OFF_RING + 2 * RING * SLOT_BYTES <= OFF_BAR, "barriers behind the tiles");
+    static_assert(OFF_SCALE + SCALE_SLOTS * SCALE_BYTES <= OFF_BAR, "barriers behind the tiles");
     // S, P and last-P-V hand-offs exist per group b and buffer s: index 2 * b + s
     // (kToken0 + b: it is the turn of group b's MMA warp)
     enum Bar { kQFull = 0, kStats, kOFree, kToken0, kPFull0 = kToken0 + 2, kPvDone0 = kPFull0 + 4, kSFull0 = kPvDone0 + 4,
@@ -186,10 +194,11 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes,
     return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo_bytes >> 4) << 16) |
            ((uint64_t)(sbo_bytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-// Instruction descriptor: bf16 x bf16 -> fp32, M = 128, N = n; b_mn = 1 when B is stored with N
+// Instruction descriptor: bf16 x bf16 (or f16 x f16) -> fp32, M = 128, N = n; b_mn = 1 when B is stored with N
 // contiguous (the V tile), 0 when K is contiguous.
+template <bool F16 = false>
 __host__ __device__ constexpr uint32_t instr_desc(uint32_t n, uint32_t b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+    return (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 // `el`: 1 in the lane that issues, 0 in the others (the warp stays converged, so that operands are uniform).
 __device__ __forceinline__ void mma_f16(uint32_t el, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
@@ -303,6 +312,151 @@ __device__ __forceinline__ TItem load_titem(const Work* rec, bool valid) {
     return r;
 }
 
+// Producer of K (which = 0) or V tiles out of the 8-bit cache, one warp: the MMAs read the codes as f16, which holds them exactly, in the layout
+// that the TMA copies of the bf16 cache leave; their scales go to the softmax (K's producer brings both kinds).  A lane holds D / 8 pieces of
+// 16 codes of a tile and the scale bytes of two rows.  As soon as a piece has been turned and stored, the same piece of the next tile is requested into its
+// registers, so that a tile's loads are in flight while the one before is being turned and waited for.
+template <int D>
+__device__ __forceinline__ void kv8_producer(const DevPlan& p, const uint8_t* __restrict__ pool8, const uint8_t* __restrict__ scales, int which, int lane, int i0, int i1,
+                                             const int32_t* head, uint32_t bar0, uint32_t sbase, uint8_t* smem, volatile int* abort_flag) {
+    using Geo = Geometry<D, true>;
+    constexpr int kPagesPerTile = kTile / kPage;          // 4
+    constexpr int kGroupTiles = 32 / kPagesPerTile;       // tiles whose page ids a warp holds, one to a lane
+    constexpr int kPieces = D / 16;                       // of a row
+    constexpr int kPerPage = kPage * kPieces / 32;        // a lane's pieces of a page: 4 or 2
+    constexpr int kRowsPerOp = 32 / kPieces;              // rows that a warp instruction moves
+    const int Hkv = p.num_kv_heads;
+    const uint32_t ring = sbase + Geo::OFF_RING;
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    auto load_pages = [&](const TItem& it, int first_page) {
+        const int npg = (it.kv_end - it.kv0 + kPage - 1) / kPage;
+        const int idx = first_page + lane;
+        return idx < npg ? __ldg(p.page_indices + it.page0 + idx) : 0;
+    };
+    const int row0 = lane / kPieces, piece = lane % kPieces;      // of the first of a lane's pieces of a page
+    // Where a lane's 32 bytes of a row go inside a page: 16-byte pieces XOR-swizzled by row.  Lanes of the second half of a row store
+    // their two pieces the other way round, so that eight lanes meet all banks.
+    const uint32_t flip = (uint32_t)(piece >> 2) & 1u;
+    auto page_offset = [&](int row, uint32_t k) {
+        return (uint32_t)(row >> 3) * Geo::GROUP_BYTES + (uint32_t)(piece >> 2) * Geo::ATOM_BYTES + (uint32_t)(row & 7) * 128u +
+               (((uint32_t)(2 * (piece & 3)) + k) ^ (uint32_t)(row & 7)) * 16u;
+    };
+    // The tile ahead: its item, place in it, the page ids of its group of tiles and of the group behind (or of the next item's first).
+    TItem cur = load_titem(reinterpret_cast<const Work*>(head + kHeadWorkTensor), i0 < i1), nxt = load_titem(p.works + i0 + 1, i0 + 1 < i1);
+    int pages = head[kHeadPagesTensor + lane], pages_nxt = 0, ii = i0, t = 0;
+    uint4 raw[kPagesPerTile * kPerPage];
+    uint32_t sc = 0;                    // scale bytes of rows 2 * (lane % 8), + 1 of page lane / 8: K, K, V, V
+    pdl_wait();
+    int page_id[kPagesPerTile];         // of the tile ahead
+    int rows = 0;                       // of the tile ahead; 0: none is left
+    auto look = [&]() {                 // takes up the tile at (cur, t)
+        rows = cur.kv_end > 0 ? min(kTile, cur.kv_end - (cur.kv0 + t * kTile)) : 0;
+        const int npages = (rows + kPage - 1) / kPage;
+#pragma unroll
+        for (int k = 0; k < kPagesPerTile; ++k) {
+            page_id[k] = __shfl_sync(0xffffffffu, pages, (t % kGroupTiles) * kPagesPerTile + min(k, max(npages - 1, 0)));
+            if (rows > 0 && !page_ok(page_id[k], p.num_pages, p.status, kStatusBadPageSpan)) page_id[k] = 0;      // (checked build only)
+        }
+        if (which == 0 && rows > 0) {
+            const int k = lane >> 3;
+            const int page = k == 0 ? page_id[0] : k == 1 ? page_id[1] : k == 2 ? page_id[2] : page_id[3];
+            const uint8_t* src = scales + kv8_scale_offset(page, 0, cur.kv_head, 2 * (lane & 7), Hkv);
+            sc = __ldcg(reinterpret_cast<const unsigned short*>(src)) | (uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(src + kPage)) << 16;
+        }
+    };
+    auto load_piece = [&](int k, int i) {
+        raw[k * kPerPage + i] = ldg_nc_v4(pool8 + kv8_row_offset(page_id[k], which, cur.kv_head, i * kRowsPerOp + row0, Hkv, D) + piece * 16);
+    };
+    auto advance = [&]() {              // on to the tile behind
+        if (rows == 0) return;
+        const int ntiles = (cur.kv_end - cur.kv0 + kTile - 1) / kTile;
+        ++t;
+        if (t == ntiles) {
+            cur = nxt;
+            ++ii;
+            nxt = load_titem(p.works + ii + 1, ii + 1 < i1);
+            t = 0;
+        }
+        if (t % kGroupTiles == 0) pages = pages_nxt;
+    };
+    auto ask_pages = [&]() {            // the ids behind this group's, asked for when its first tile is on its way
+        if (rows == 0 || t % kGroupTiles != 0) return;
+        const int ntiles = (cur.kv_end - cur.kv0 + kTile - 1) / kTile;
+        if (t + kGroupTiles < ntiles) pages_nxt = load_pages(cur, (t + kGroupTiles) * kPagesPerTile);
+        else if (nxt.kv_end > 0) pages_nxt = load_pages(nxt, 0);
+    };
+    look();
+#pragma unroll
+    for (int k = 0; k < kPagesPerTile; ++k)
+        if (k * kPage < rows)
+#pragma unroll
+            for (int i = 0; i < kPerPage; ++i) load_piece(k, i);
+    ask_pages();
+    int most = -1000;                   // largest eV of the item so far
+    for (int n = 0; rows > 0; ++n) {
+        const int rows_now = rows;
+        const uint32_t sc_now = sc;
+        const int s = ring_slot(which, n, Geo::RING);
+        if (t == 0) most = -1000;
+        advance();
+        look();
+        if (!mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::RING) & 1u) ^ 1u, abort_flag, p.status, 11 + which)) break;
+        const uint32_t slot = ring + s * Geo::SLOT_BYTES;
+#pragma unroll
+        for (int k = 0; k < kPagesPerTile; ++k) {
+            if (k * kPage < rows_now) {
+#pragma unroll
+                for (int i = 0; i < kPerPage; ++i) {
+                    const int row = i * kRowsPerOp + row0;
+                    uint4 w = raw[k * kPerPage + i];
+                    if (which == 1 && k * kPage + row >= rows_now) w = make_uint4(0, 0, 0, 0);      // slots past the item's end hold anything, and 0 * NaN would poison P V
+                    const uint4 lo = make_uint4(kv8_decode2(w.x), kv8_decode2_hi(w.x), kv8_decode2(w.y), kv8_decode2_hi(w.y));
+                    const uint4 hi = make_uint4(kv8_decode2(w.z), kv8_decode2_hi(w.z), kv8_decode2(w.w), kv8_decode2_hi(w.w));
+                    const uint32_t at = slot + (uint32_t)k * Geo::PAGE_BYTES;
+                    const uint4 a = flip ? hi : lo, b = flip ? lo : hi;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + page_offset(row, flip)), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + page_offset(row, flip ^ 1u)), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+                }
+            }
+            if (k * kPage < rows) {
+#pragma unroll
+                for (int i = 0; i < kPerPage; ++i) load_piece(k, i);
+            }
+        }
+        ask_pages();
+        if (which == 0) {
+            // A row of V that is not finite (its codes are zeros) makes its key's score NaN, so that only those who see it are hit.  Keys behind the end are
+            // masked, whatever stands here.
+            float* v = reinterpret_cast<float*>(smem + Geo::OFF_SCALE + (uint32_t)(n % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
+            const int key = (lane >> 3) * kPage + 2 * (lane & 7);
+            float ks[2], ev[2], iv[2];
+            int hi = -1000, lo = 1000;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t bk = sc_now >> (8 * e) & 0xffu, bv = sc_now >> (16 + 8 * e) & 0xffu;
+                const int x = bv == kKv8NanByte ? kKv8LeastExponent : (int)bv - 127;
+                ks[e] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);
+                ev[e] = (float)x;
+                iv[e] = __uint_as_float((uint32_t)(127 - max(x, -126)) << 23);
+                if (key + e < rows_now) hi = max(hi, x), lo = min(lo, x);
+            }
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            most = max(most, hi);
+            *reinterpret_cast<float2*>(v + key) = make_float2(ks[0], ks[1]);
+            *reinterpret_cast<float2*>(v + kTile + key) = make_float2(ev[0], ev[1]);
+            *reinterpret_cast<float2*>(v + 2 * kTile + key) = make_float2(iv[0], iv[1]);
+            if (lane == 0) v[3 * kTile] = most - lo > kFarExponents ? 1.f : 0.f;
+        }
+        fence_async_smem();      // the MMAs read through the asynchronous proxy
+        __syncwarp();
+#ifdef ASYNCLM_DEBUG
+        if (which == 0 && blockIdx.x == 0 && p.debug_stall_tile == n + 1) continue;      // (see the other producer)
+#endif
+        if (lane == 0) mbar_arrive(bar(Geo::kRingFull0 + s));
+    }
+}
+
 // The whole kernel body, called by all twelve warps with `smem` 1024-byte aligned.
 // ALONE: in the kernel of steps that have span tiles only.  A launch starts on cold instruction caches, and there every line
 // of code that is fetched for the first time stands in the way: the P V of an unfinished last tile is a loop, and the output rows
@@ -311,12 +465,13 @@ __device__ __forceinline__ TItem load_titem(const Work* rec, bool valid) {
 // 14.04 | 13.68 (14.04), one span over 2000 keys 15.6 | 15.1 (15.2), head_dim 64 9.57 | 9.47 (9.18), 24 sequences with spans of 33-96
 // tokens 70.3 | 69.1, 8192 tokens 545 | 528.  Beside the warp body's code it is a loss: 8 sequences of 32-131 K keys with two
 // 256-token spans 917 | 925.
-template <int D, int G, bool ALONE>
+// KV8: the cache is the 8-bit one, at `pool8` and `scales` (span_map and pool are not used): its producers are kv8_producer.
+template <int D, int G, bool ALONE, bool KV8 = false>
 __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* span_map, const __nv_bfloat16* __restrict__ q,
                                         const __nv_bfloat16* pool,
                                         __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
-                                        uint8_t* smem) {
-    using Geo = Geometry<D>;
+                                        uint8_t* smem, const uint8_t* pool8 = nullptr, const uint8_t* scales = nullptr) {
+    using Geo = Geometry<D, KV8>;
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bar0 = sbase + Geo::OFF_BAR;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
@@ -344,15 +499,15 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             mbar_init(bar(Geo::kSFull0 + b), 1);
         }
         for (int s = 0; s < 2 * Geo::RING; ++s) {
-            mbar_init(bar(Geo::kRingFull0 + s), s < Geo::RING ? 1 : 33);      // V tiles: see the producers
-            mbar_init(bar(Geo::kRingEmpty0 + s), 2);
+            mbar_init(bar(Geo::kRingFull0 + s), KV8 || s < Geo::RING ? 1 : 33);      // V tiles: see the producers
+            mbar_init(bar(Geo::kRingEmpty0 + s), KV8 && s < Geo::RING ? 8 : 2);      // (8 bits: every warp reads a K tile's scales and releases it)
         }
         mbar_init(bar(Geo::kMmaDrain), 2);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (threadIdx.x == kProducerWarpK * 32) asm volatile("prefetch.tensormap [%0];" ::"l"(span_map));
+    if (!KV8 && threadIdx.x == kProducerWarpK * 32) asm volatile("prefetch.tensormap [%0];" ::"l"(span_map));
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(sbase + Geo::OFF_TMEM_PTR), "r"(kTmemCols) : "memory");
@@ -364,7 +519,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
     const uint32_t tmem = *tmem_ptr;
 
     if (warp >= 8) {
-      if (warp == kProducerWarpK || warp == kProducerWarpV) {
+      if (KV8 && (warp == kProducerWarpK || warp == kProducerWarpV)) {
+        kv8_producer<D>(p, pool8, scales, warp == kProducerWarpV ? 1 : 0, lane, i0, i1, head, bar0, sbase, smem, abort_flag);
+      } else if (!KV8 && (warp == kProducerWarpK || warp == kProducerWarpV)) {
         // ------------------------------------------------------------------ producer warps
         const int which = warp == kProducerWarpV ? 1 : 0;       // 0: K tiles, 1: V tiles
         const uint32_t ring = sbase + Geo::OFF_RING;
@@ -478,7 +635,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             ++turn_no;
         };
         auto pass_token = [&]() { if (lane == 0) mbar_arrive(bar(Geo::kToken0 + (b ^ 1))); };
-        constexpr uint32_t idesc_pv = instr_desc(D, 1);
+        constexpr uint32_t idesc_pv = instr_desc<KV8>(D, 1);
         const uint32_t ocol = tmem + kColO + (uint32_t)(D * b);
         TItem it_next = load_titem(head_work, i0 < i1);
         const long long t_loop = trace_clock();
@@ -498,7 +655,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             if (ok) tc_fence_after();
             const uint64_t qd = smem_desc(sbase + Geo::OFF_Q + (dual ? (uint32_t)b * Geo::QTILE_BYTES : 0u), 16, 1024);
             const int last_pages = (it.kv_end - (it.kv0 + (ntiles - 1) * kTile) + kPage - 1) / kPage;      // of the item's last tile
-            const uint32_t idesc_last = instr_desc(16u * (uint32_t)last_pages, 0);
+            const uint32_t idesc_last = instr_desc<KV8>(16u * (uint32_t)last_pages, 0);
             // where the group's next K and V tile lie
             RingPlace kp = ring_place(base + (dual ? 0 : b), Geo::RING), vp = kp;
             auto next_place = [&](RingPlace& x) { x = ring_next(x, dual ? 1 : 2, Geo::RING); };
@@ -530,11 +687,11 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 // The tiles were written by TMA copies, but for the rows of an unfinished last V page: those came by cp.async,
                 // through the generic proxy, and the MMAs read through the asynchronous one.  The full barrier orders
                 // the two, the fence makes the bytes visible across.
-                if (pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
+                if (!KV8 && pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
                 const uint32_t buf = tmem + kColS + 128u * (uint32_t)b + 64u * (uint32_t)(c & 1);      // S and P
                 const uint64_t vd = smem_desc(tile_addr(1, vp), Geo::ATOM_BYTES, Geo::GROUP_BYTES);
                 const uint64_t kd = smem_desc(tile_addr(0, kp), 16, Geo::GROUP_BYTES);
-                const uint32_t idesc_qk = jn == ntiles - 1 ? idesc_last : instr_desc(kTile, 0);
+                const uint32_t idesc_qk = jn == ntiles - 1 ? idesc_last : instr_desc<KV8>(kTile, 0);
                 const uint32_t done = bar((qk ? Geo::kSFull0 : Geo::kPvDone0) + 2 * b + (c & 1));
                 if (pv) {
                     const long long tw = trace_clock();
@@ -627,12 +784,41 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
             for (int c = kQV / 2; c < kQV; ++c) w[c] = (valid && dual) ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
         };
-        // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.
+        // 8 bits: the whole row always, because its scale is wanted (see below)
+        auto load_q_row = [&](const TItem& x, uint4 (&w)[kQV]) {
+            const int r = (x.ntok * G > kRows ? 128 * b : 0) + m;
+            const bool valid = x.kv_end > 0 && r / G < x.ntok;
+            const uint4* src = reinterpret_cast<const uint4*>(q + ((size_t)(x.q_row0 + r / G) * Hq + (size_t)x.kv_head * G + r % G) * D);
+#pragma unroll
+            for (int c = 0; c < kQV; ++c) w[c] = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+        };
+        // and as f16, divided by the power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value);
+        // returns the factor on the scores
+        auto f16_row = [&](uint4 (&w)[kQV]) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int c = 0; c < kQV; ++c) {
+                const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = max(most, max(x[e] & 0x7fffu, x[e] >> 16 & 0x7fffu));
+            }
+            const uint32_t e = min(max(most >> 7, 1u), 253u);
+            const float down = __uint_as_float((254u - e) << 23);
+            auto two = [&](uint32_t x) {
+                const __half2 h = __floats2half2_rn(bf16_lo(x) * down, bf16_hi(x) * down);
+                return *reinterpret_cast<const uint32_t*>(&h);
+            };
+#pragma unroll
+            for (int c = 0; c < kQV; ++c) w[c] = make_uint4(two(w[c].x), two(w[c].y), two(w[c].z), two(w[c].w));
+            return __uint_as_float(e << 23) * qscale;
+        };
+        // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.  (8 bits: a K slot
+        // after two of each of four warps, all of which wait for the tile themselves: one that came late would find the slot's next phase over.)
         auto release = [&](int which, int t, bool dual) { mbar_arrive_n(bar(Geo::kRingEmpty0 + ring_slot(which, t, Geo::RING)), dual ? 1u : 2u); };
         TItem it_next = load_titem(head_work, i0 < i1);
         uint4 q_next[kQV];
         pdl_wait();
-        load_q(it_next, q_next);
+        if constexpr (KV8) load_q_row(it_next, q_next); else load_q(it_next, q_next);
         for (int ii = i0; ii < i1 && ok; ++ii, ++item_no) {
             const TItem it = it_next;
             const int ntiles = (it.kv_end - it.kv0 + kTile - 1) / kTile;
@@ -647,6 +833,15 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             if (item_no > 0) {
                 ok = mbar_wait_warp(bar(Geo::kOFree), (uint32_t)(item_no - 1) & 1u, abort_flag, p.status, 36);
                 if (!ok) break;
+            }
+            float2 row_scale2 = make_float2(0.f, 0.f);
+            if constexpr (KV8) {
+                const float x = f16_row(q_next);
+                row_scale2 = make_float2(x, x);
+                if (!dual && b == 1) {
+#pragma unroll
+                    for (int c = 0; c < kQV / 2; ++c) q_next[c] = q_next[c + kQV / 2];
+                }
             }
 #pragma unroll
             for (int c = 0; c < kQV; ++c)
@@ -680,14 +875,36 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 uint32_t rr[64];
                 tmem_ld32(sb, *reinterpret_cast<uint32_t(*)[32]>(&rr[0]));
                 tmem_ld32(sb + 32u, *reinterpret_cast<uint32_t(*)[32]>(&rr[32]));
+                // (8 bits) the tile's scales were written before its K tile was handed over, which this wait sees once more: the slot is this
+                // tile's until the release below
+                const float* tile_scales = nullptr;
+                if constexpr (KV8) {
+                    const RingPlace x = ring_place(kv_base + j, Geo::RING);
+                    ok = __all_sync(0xffffffffu, mbar_wait_spin(bar(Geo::kRingFull0 + x.slot), x.parity, abort_flag, p.status, 33));
+                    if (!ok) break;
+                    tile_scales = reinterpret_cast<const float*>(smem + Geo::OFF_SCALE + (uint32_t)((kv_base + j) % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
+                }
                 // This S complete means every MMA issued for the group before it is complete: the ring slots they
                 // read go back to the producers, the K tile of j now, and the V tile of j - lead (its P V was
                 // issued in front of this Q K^T).
-                if (m == 0) {
-                    release(0, kv_base + j, dual);
-                    if (u >= 2) release(1, kv_base + j - lead, dual);
-                }
+                if (KV8 ? lane == 0 : m == 0) release(0, kv_base + j, dual);
+                if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
                 tmem_wait_ld();
+                if constexpr (KV8) {
+                    // x = score + eV (log2 domain): the exponent of the key's weight of V, whose row is read without its scale
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float4 ks = *reinterpret_cast<const float4*>(tile_scales + 4 * e), ev = *reinterpret_cast<const float4*>(tile_scales + kTile + 4 * e);
+                        const float2 a = __ffma2_rn(__fmul2_rn(make_float2(__uint_as_float(rr[4 * e]), __uint_as_float(rr[4 * e + 1])), row_scale2),
+                                                    make_float2(ks.x, ks.y), make_float2(ev.x, ev.y));
+                        const float2 c = __ffma2_rn(__fmul2_rn(make_float2(__uint_as_float(rr[4 * e + 2]), __uint_as_float(rr[4 * e + 3])), row_scale2),
+                                                    make_float2(ks.z, ks.w), make_float2(ev.z, ev.w));
+                        rr[4 * e] = __float_as_uint(a.x);
+                        rr[4 * e + 1] = __float_as_uint(a.y);
+                        rr[4 * e + 2] = __float_as_uint(c.x);
+                        rr[4 * e + 3] = __float_as_uint(c.y);
+                    }
+                }
                 if (!__all_sync(0xffffffffu, vis == kTile)) {
 #pragma unroll
                     for (int e = 0; e < 64; ++e)
@@ -706,7 +923,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) cm[c] = fmaxf(cm[c], sv(16 * c + 15));
-                const float cmax = fmax3(fmaxf(cm[0], cm[1]), cm[2], cm[3]) * qscale;      // log2 domain
+                const float cmax = fmax3(fmaxf(cm[0], cm[1]), cm[2], cm[3]) * (KV8 ? 1.f : qscale);      // log2 domain
                 if (__any_sync(0xffffffffu, cmax > m_ref + kRescaleThreshold)) {
                     // Move the reference maximum (rare after the first tile; a row without one takes any visible
                     // key's): rescale the running sum and O[b].  O[b] is at rest once the P V of the group's
@@ -747,6 +964,33 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
                 const float2 nm2 = make_float2(-m_use, -m_use);
                 uint32_t pk[32];
+                if constexpr (KV8) {
+                    // P' = exp2(x - m_ref) as f16 (11 bits); the sum takes it without the scale of V, 2^-eV times it
+                    if (tile_scales[3 * kTile] == 0.f) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float4 iv = *reinterpret_cast<const float4*>(tile_scales + 2 * kTile + 2 * e);
+                            const float2 x0 = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), nm2);
+                            const float2 x1 = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e + 2]), __uint_as_float(rr[2 * e + 3])), nm2);
+                            const float2 p0 = make_float2(fast_exp2(x0.x), fast_exp2(x0.y)), p1 = make_float2(fast_exp2(x1.x), fast_exp2(x1.y));
+                            l2 = __ffma2_rn(p0, make_float2(iv.x, iv.y), l2);
+                            l2b = __ffma2_rn(p1, make_float2(iv.z, iv.w), l2b);
+                            const __half2 h0 = __floats2half2_rn(p0.x, p0.y), h1 = __floats2half2_rn(p1.x, p1.y);
+                            pk[e] = *reinterpret_cast<const uint32_t*>(&h0);
+                            pk[e + 1] = *reinterpret_cast<const uint32_t*>(&h1);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float2 ev = *reinterpret_cast<const float2*>(tile_scales + kTile + 2 * e);
+                            const float2 x = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), nm2);
+                            l2.x += fast_exp2(x.x - ev.x);
+                            l2.y += fast_exp2(x.y - ev.y);
+                            const __half2 h = __floats2half2_rn(fast_exp2(x.x), fast_exp2(x.y));
+                            pk[e] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                    }
+                } else
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                     const float2 x = __ffma2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), qscale2, nm2);
@@ -765,7 +1009,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             }
             if (!ok) break;
             const float l_sum = (l2.x + l2.y) + (l2b.x + l2b.y);
-            load_q(it_next, q_next);        // in flight during the epilogue
+            if constexpr (KV8) load_q_row(it_next, q_next);        // in flight during the epilogue
+            else load_q(it_next, q_next);
             if (lane == 0) trace_event(1 + warp, ev, 33);
             // ---- epilogue.  The groups' (max, sum) go through columns 0-1 of their S buffers, which are
             // idle from the group's last P V until the next item's first Q K^T.
@@ -792,10 +1037,10 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             float w0, w1, lse2;          // weights of O[0] and O[1] in this thread's output row
             int c_begin, c_end;          // 32-column chunks of the row this thread writes
             if (dual) {
-                const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
+                const float inv = l_sum > 0.f ? 1.f / l_sum : KV8 ? l_sum : 0.f;      // (8 bits: a sum that is not a number stays one)
                 w0 = b == 0 ? inv : 0.f;
                 w1 = b == 1 ? inv : 0.f;
-                lse2 = l_sum > 0.f ? m_ref + log2f(l_sum) : -INFINITY;
+                lse2 = l_sum > 0.f ? m_ref + log2f(l_sum) : KV8 && l_sum != 0.f ? l_sum : -INFINITY;
                 c_begin = 0; c_end = D / 32;
             } else {
                 // the two groups hold two KV splits of the same rows: merge them; a group writes slices of 64 values,
@@ -807,13 +1052,13 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float m0 = __uint_as_float(x0), l0 = __uint_as_float(y0);
                 const float m1 = __uint_as_float(x1), l1 = __uint_as_float(y1);
                 const float M = fmaxf(m0, m1);
-                const float a0 = l0 > 0.f ? fast_exp2(m0 - M) : 0.f;
-                const float a1 = l1 > 0.f ? fast_exp2(m1 - M) : 0.f;
+                const float a0 = l0 > 0.f ? fast_exp2(m0 - M) : KV8 ? l0 : 0.f;
+                const float a1 = l1 > 0.f ? fast_exp2(m1 - M) : KV8 ? l1 : 0.f;
                 const float L = a0 * l0 + a1 * l1;
-                const float inv = L > 0.f ? 1.f / L : 0.f;
+                const float inv = L > 0.f ? 1.f / L : KV8 ? L : 0.f;
                 w0 = a0 * inv;
                 w1 = a1 * inv;
-                lse2 = L > 0.f ? M + log2f(L) : -INFINITY;
+                lse2 = L > 0.f ? M + log2f(L) : KV8 && L != 0.f ? L : -INFINITY;
                 c_begin = 2 * b; c_end = min(2 * b + 2, D / 32);
             }
             const bool use0 = __any_sync(0xffffffffu, w0 != 0.f), use1 = __any_sync(0xffffffffu, w1 != 0.f);

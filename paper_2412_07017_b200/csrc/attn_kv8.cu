@@ -1,6 +1,8 @@
 // Attention over the 8-bit cache: the entry point, its kernels and launcher.  The bodies are those of the bf16 cache, with the cache's
-// format as a template parameter (attn_decode.cuh: what a consumer warp does with a page).
+// format as a template parameter (attn_decode.cuh: what a consumer warp does with a page; attn_append_tc.cuh: how tiles get into shared
+// memory).  Which kernel runs follows the same rules as there (attn_kernels.cu).
 #include "asynclm.h"
+#include "attn_append_tc.cuh"
 #include "attn_decode.cuh"
 #include "attn_launch.cuh"
 #include "plan_internal.h"
@@ -20,19 +22,73 @@ attn_decode_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, co
 }
 
 template <int D, int G>
+__global__ void __launch_bounds__(tc::kThreads, 1)
+attn_append_tc_kv8_kernel(DevPlan p, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
+                          float* __restrict__ lse) {
+    extern __shared__ uint8_t smem_raw[];
+    pdl_trigger();
+    if (threadIdx.x == 0) {
+        trace_mark(0);
+        for (int s = 8; s < 16; ++s) trace_set(s, 0);
+    }
+    tc::tc_body<D, G, true, true>(p, nullptr, q, nullptr, out, lse, aligned_smem(smem_raw), pool, scales);
+    if (threadIdx.x == 0) trace_mark(1);
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(tc::kThreads, 1)
+attn_fused_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q,
+                      __nv_bfloat16* __restrict__ out, float* __restrict__ lse, int S) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = aligned_smem(smem_raw);
+    pdl_trigger();
+    if (threadIdx.x == 0) { trace_mark(0); trace_set(1, 0); trace_set(5, 0); trace_set(6, 0); trace_set(7, 0); }
+    const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
+    if (threadIdx.x < 3) asm volatile("prefetch.global.L2 [%0];" ::"l"(head + 32 * threadIdx.x));      // (as in attn_fused_kernel)
+    if (threadIdx.x == 32) asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map));
+    if (head[0] == head[1]) {
+        dec::decode_body<D, G, false, false, true>(p, &kv_map, nullptr, q, out, lse, S, smem, AppendSrc{}, scales);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 8; s < 16; ++s) trace_set(s, 0);
+    }
+    tc::tc_body<D, G, false, true>(p, nullptr, q, nullptr, out, lse, smem, pool, scales);
+    if (threadIdx.x == 0) trace_mark(1);
+    if (head[2] == head[3] && p.queue_count == 0) return;      // nothing left for the warp body
+    __syncthreads();      // tensor memory released, shared memory free for the second phase
+    dec::decode_body<D, G, false, false, true>(p, &kv_map, nullptr, q, out, lse, S, smem, AppendSrc{}, scales);
+}
+
+template <int D, int G>
 cudaError_t launch_kv8_impl(const DevPlan& p, const void* q, const void* pool, const void* scales, void* out, float* lse, cudaStream_t stream) {
-    if (p.num_items_tensor > 0) return cudaErrorNotSupported;
-    if (p.num_items_cuda == 0) return cudaSuccess;
+    const bool has_tensor = p.num_items_tensor > 0, has_cuda = p.num_items_cuda > 0;
+    if (!has_tensor && !has_cuda) return cudaSuccess;
     if (p.num_pages > kMaxMapPages) return cudaErrorInvalidValue;
     constexpr int S = decode_stages<D, true>();
-    constexpr size_t smem = dec::smem_bytes<D, true>(S);
-    cudaError_t e = allow_smem<attn_decode_kv8_kernel<D, G>>(smem);
-    if (e != cudaSuccess) return e;
+    constexpr size_t smem_warp = dec::smem_bytes<D, true>(S), smem_span = tc::Geometry<D, true>::SMEM_BYTES, smem_both = std::max(smem_warp, smem_span);
+    static_assert(smem_warp - 1024 <= tc::Geometry<D, true>::OFF_BAR, "the span body's barriers stay clear of the warp body");
+    const auto *pool8 = (const uint8_t*)pool, *scales8 = (const uint8_t*)scales;
+    const auto* q16 = (const __nv_bfloat16*)q;
+    auto* out16 = (__nv_bfloat16*)out;
     CUtensorMap map;
-    e = pool_map(kKv8Map, p, pool, &map);
-    if (e != cudaSuccess) return e;
-    return launch_when(!p.full_launch, attn_decode_kv8_kernel<D, G>, dim3(p.num_ctas_cuda), dim3(dec::kThreads), smem, stream, p, map, (const uint8_t*)pool,
-                       (const uint8_t*)scales, (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, S);
+    if (has_cuda)
+        if (cudaError_t e = pool_map(kKv8Map, p, pool, &map)) return e;
+    if (has_tensor && has_cuda && p.num_ctas_tensor == p.num_ctas_cuda) {
+        if (cudaError_t e = allow_smem<attn_fused_kv8_kernel<D, G>>(smem_both)) return e;
+        return launch_when(!p.full_launch, attn_fused_kv8_kernel<D, G>, dim3(p.num_ctas_cuda), dim3(tc::kThreads), smem_both, stream, p, map, pool8, scales8,
+                           q16, out16, lse, S);
+    }
+    if (has_tensor) {
+        if (cudaError_t e = allow_smem<attn_append_tc_kv8_kernel<D, G>>(smem_span)) return e;
+        if (cudaError_t e = launch_when(!p.full_launch, attn_append_tc_kv8_kernel<D, G>, dim3(p.num_ctas_tensor), dim3(tc::kThreads), smem_span, stream, p,
+                                        pool8, scales8, q16, out16, lse))
+            return e;
+    }
+    if (!has_cuda) return cudaSuccess;
+    if (cudaError_t e = allow_smem<attn_decode_kv8_kernel<D, G>>(smem_warp)) return e;
+    return launch_when(!p.full_launch, attn_decode_kv8_kernel<D, G>, dim3(p.num_ctas_cuda), dim3(dec::kThreads), smem_warp, stream, p, map, pool8, scales8, q16,
+                       out16, lse, S);
 }
 
 template <int D>

@@ -803,7 +803,7 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     }
 
     // ---- units ------------------------------------------------------------------------------
-    const bool tensor_wanted = !(opts && (opts->flags & (ASYNCLM_PLAN_NO_TENSOR_PATH | ASYNCLM_PLAN_KV8)));      // (the span body reads the bf16 cache only)
+    const bool tensor_wanted = !(opts && (opts->flags & ASYNCLM_PLAN_NO_TENSOR_PATH));
     const int tensor_min_rows =
         (opts && opts->tensor_min_rows > 0) ? opts->tensor_min_rows : default_tensor_min_rows(shape->head_dim);
     const int TQ = tensor_tile_tokens(G);

@@ -31,6 +31,13 @@ namespace tc {
 
 // Slots of one ring: 80 KiB of 64-key tiles.
 ASYNCLM_HD constexpr int ring_slots(int head_dim) { return 640 / head_dim; }
+// The same for the 8-bit cache, whose tiles' scales need room beside the rings: at head_dim 128 one slot less (its producers hold another tile in registers).
+ASYNCLM_HD constexpr int ring_slots_kv8(int head_dim) { return head_dim == 128 ? 4 : ring_slots(head_dim); }
+// Slots for those scales, which every warp of a softmax group reads until it hands its weights over.  When the producer fills tile t, every warp of its
+// group has released tile t - slots, at the start of its softmax, so it is through with the group's tile before that, t - slots - 1 (both groups on every
+// tile) or t - slots - 2 (alternate tiles), and the other group's warps, which have released t - slots - 1, are through with t - slots - 3.  So
+// t - slots - 3 may be overwritten; one more makes the number even.
+ASYNCLM_HD constexpr int scale_slots(int slots) { return slots + 4; }
 // Slot (K ring first, then V ring) of the CTA's t-th K (which = 0) or V (which = 1) tile.
 ASYNCLM_HD constexpr int ring_slot(int which, int t, int slots) { return which * slots + t % slots; }
 // How often that slot has been used before.
