@@ -198,6 +198,9 @@ def _calls():
                 ext.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.asynclm_plan, lib.asynclm_kv_append, lib.asynclm_kv_append_rope,
                                                                             lib.asynclm_attn_mixed, lib.asynclm_step)),
                          torch.cuda.current_device, raw)
+                ext.bind_kv8(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.asynclm_kv8_append, lib.asynclm_kv8_attn_mixed, lib.asynclm_kv8_gather,
+                                                                               lib.asynclm_rope_apply)),
+                             torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.uint8, torch.int32, torch.int64)
         except (ImportError, OSError, RuntimeError, AttributeError, TypeError) as e:
             ext = False
             warnings.warn(f"the per-layer calls go through ctypes, because their extension cannot be built or loaded: {e}", RuntimeWarning, stacklevel=3)
@@ -503,6 +506,10 @@ def asynclm_rope_table(head_dim: int, theta: float = 500000.0, rotary_dim: int =
 
 def asynclm_rope_apply(table: CRopeTable, positions, q, q_out, k=None, k_out=None, stream=None) -> None:
     """Rows [tokens][heads][head_dim] of q (and k) turned by positions[token] (int32, device) into q_out (and k_out); out may be in."""
+    if ext := _calls():
+        rc = ext.rope(ctypes.addressof(table), positions, q, q_out, k, k_out, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_rope_apply")
     import torch
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out come together")
@@ -524,6 +531,10 @@ def asynclm_rope_apply(table: CRopeTable, positions, q, q_out, k=None, k_out=Non
 def asynclm_kv8_append(plan: Plan, k_new, v_new, kv8_pool, kv8_scales, rope: Optional[CRopeTable] = None, q=None, q_out=None, stream=None) -> None:
     """The step's new K/V rows into the quantised cache; with `rope`, the keys turned by their positions first and q into q_out.  k_new, v_new and q may
     be slices of a fused projection's output (any row stride)."""
+    if ext := _calls():
+        rc = ext.kv8_append(None if plan is None else plan.handle, k_new, v_new, kv8_pool, kv8_scales, 0 if rope is None else ctypes.addressof(rope), q, q_out, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_kv8_append")
     (ka, ks), (va, vs) = _rows_of(k_new, "k_new"), _rows_of(v_new, "v_new")
     (qa, qs), qo = (None, 0), None
     if q is not None:
@@ -539,6 +550,10 @@ def asynclm_kv8_append(plan: Plan, k_new, v_new, kv8_pool, kv8_scales, rope: Opt
 
 def asynclm_kv8_attn_mixed(plan: Plan, q, kv8_pool, kv8_scales, out, lse=None, stream=None) -> None:
     """asynclm_attn_mixed over the quantised cache."""
+    if ext := _calls():
+        rc = ext.kv8_attn(plan.handle, q, kv8_pool, kv8_scales, out, lse, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_kv8_attn_mixed")
     pool, scales = _cache8(kv8_pool, kv8_scales)
     _check(load().asynclm_kv8_attn_mixed(plan.handle, q.data_ptr(), pool, scales, out.data_ptr(), None if lse is None else lse.data_ptr(),
                                          _stream_ptr(stream)), "asynclm_kv8_attn_mixed")
@@ -547,6 +562,10 @@ def asynclm_kv8_attn_mixed(plan: Plan, q, kv8_pool, kv8_scales, out, lse=None, s
 def asynclm_kv8_gather(plan: Plan, out_indptr, first, kv8_pool, kv8_scales, k_out, v_out, stream=None) -> None:
     """Positions first[b] + i of every sequence b, i < out_indptr[b + 1] - out_indptr[b], read back into rows out_indptr[b] + i of k_out and v_out
     (bf16 [rows][kv heads][head_dim]); out_indptr int64 [batch + 1] and first int32 [batch] on the device."""
+    if ext := _calls():
+        rc = ext.kv8_gather(plan.handle, out_indptr, first, kv8_pool, kv8_scales, k_out, v_out, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_kv8_gather")
     import torch
     k, v = _rows_of(k_out, "k_out", dense=True)[0], _rows_of(v_out, "v_out", dense=True)[0]
     if k_out.shape != v_out.shape:

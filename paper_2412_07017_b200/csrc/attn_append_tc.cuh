@@ -46,6 +46,7 @@
 #pragma once
 #include <cuda.h>
 
+#include <cfloat>
 #include <climits>
 
 #include "common.cuh"
@@ -59,12 +60,26 @@ namespace tc {
 
 constexpr int kThreads = 384;
 constexpr int kProducerWarpK = 8, kMmaWarp = 9, kProducerWarpV = 10;      // 11: the second MMA warp
+// 8-bit cache: warp 8 brings K tiles, warps 10, 12, 13 and 15 turn V tiles, a page each, so that each of the four schedulers has one (14 is idle).  An SM has 128
+// registers for each thread of sixteen warps; the eight softmax (or consumer) warps take 32 more each from the others, at the start, for the whole kernel.
+constexpr int kThreadsKv8 = 512, kLaunchRegs = 128, kLowRegs = 160, kHighRegs = 96;
+static_assert(2 * kLowRegs + 2 * kHighRegs <= 4 * kLaunchRegs, "no more registers than the launch has");
+template <int ROLE>
+__device__ __forceinline__ void split_registers() {      // ROLE 0: warps 0-7, 1: warps 8-15
+    if constexpr (ROLE == 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kLowRegs));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHighRegs));
+}
 constexpr int kRows = 128;                       // query rows per row tile
 constexpr int kTile = 64;                        // keys per KV tile: a K or V ring slot, an S buffer
 constexpr float kRescaleThreshold = 8.f;
 constexpr long long kWaitCycles = 2000000000ll;
 constexpr long long kGroupSkewCycles = 600;
-// 8 bits: V rows whose exponents lie further apart than this take the softmax sum of their tile by exponentials of its own.  (The weight of a
+// 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest e) is an f16 number exactly (the least code
+// is 2^-9, the least f16 number 2^-24), and the softmax has one eV for the tile.  (A row's exponent follows its largest value; in a
+// trained model's cache they differ by a few.)  Otherwise the tile holds the codes alone, and the softmax takes an eV for every key: right for any, but
+// 32 more 16-byte reads of shared memory a warp and tile, at 4 cycles each.
+constexpr int kNearExponents = 15;
+// Of the latter, V rows whose exponents lie further apart than this take the softmax sum of their tile by exponentials of its own.  (The weight of a
 // key is exp2(s + eV - reference), and the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
 constexpr int kFarExponents = 95;
 
@@ -80,12 +95,20 @@ struct Geometry {
     static constexpr uint32_t GROUP_BYTES = HALVES * ATOM_BYTES;
     static constexpr uint32_t PAGE_BYTES = 2 * GROUP_BYTES;
     static constexpr uint32_t SLOT_BYTES = kTile / kPage * PAGE_BYTES;
-    static constexpr int RING = KV8 ? ring_slots_kv8(D) : ring_slots(D);   // slots of the K ring and of the V ring
+    static constexpr int RING_K = KV8 ? ring_slots_kv8(0, D) : ring_slots(D), RING_V = KV8 ? ring_slots_kv8(1, D) : ring_slots(D);      // slots of the rings
+    static constexpr int RINGS = RING_K + RING_V;
+    static __host__ __device__ constexpr int ring(int which) { return which ? RING_V : RING_K; }
+    static __host__ __device__ constexpr int slot(int which, int t) { return (which ? RING_K : 0) + ring_slot(0, t, ring(which)); }      // of tile t, K ring first
     static constexpr uint32_t OFF_Q = 0;                                   // Q[0], Q[1]
     static constexpr uint32_t OFF_RING = OFF_Q + 2 * QTILE_BYTES;
-    // 8 bits: a tile's scales as the softmax takes them, fp32: 2^eK, eV, 2^-eV of its 64 keys, and whether the exponents are far apart
-    static constexpr uint32_t OFF_SCALE = OFF_RING + 2 * RING * SLOT_BYTES;
-    static constexpr int SCALE_SLOTS = KV8 ? scale_slots(RING) : 0;
+    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^-eV of all its keys and 0, or 1 (2: far apart) in the third place; behind them
+    // 2^eK of each of its 64 keys, and eV and 2^-eV of each where they differ
+    static constexpr uint32_t K_SLOT_BYTES = KV8 ? (uint32_t)(kTile * D) : SLOT_BYTES;
+    static __host__ __device__ constexpr uint32_t slot_offset(int which, int s) {      // of the s-th slot of a ring
+        return OFF_RING + (which ? RING_K * K_SLOT_BYTES + (uint32_t)s * SLOT_BYTES : (uint32_t)s * K_SLOT_BYTES);
+    }
+    static constexpr uint32_t OFF_SCALE = OFF_RING + RING_K * K_SLOT_BYTES + RING_V * SLOT_BYTES;
+    static constexpr int SCALE_SLOTS = KV8 ? scale_slots(RING_K) : 0;
     static constexpr uint32_t SCALE_BYTES = 3 * kTile * 4 + 16;
     // The barriers lie behind everything the warp body uses when the CTA goes on to it: arrivals that nobody
     // waits for (an item's last on kOFree and on the ring's empty barriers) may still be queued in the shared
@@ -95,7 +118,7 @@ struct Geometry {
     // S, P and last-P-V hand-offs exist per group b and buffer s: index 2 * b + s
     // (kToken0 + b: it is the turn of group b's MMA warp)
     enum Bar { kQFull = 0, kStats, kOFree, kToken0, kPFull0 = kToken0 + 2, kPvDone0 = kPFull0 + 4, kSFull0 = kPvDone0 + 4,
-               kRingFull0 = kSFull0 + 4, kRingEmpty0 = kRingFull0 + 2 * RING, kMmaDrain = kRingEmpty0 + 2 * RING, kNumBars };
+               kRingFull0 = kSFull0 + 4, kRingEmpty0 = kRingFull0 + RINGS, kMmaDrain = kRingEmpty0 + RINGS, kNumBars };
     static constexpr uint32_t OFF_TMEM_PTR = OFF_BAR + 8 * kNumBars;
     static constexpr uint32_t OFF_ABORT = OFF_TMEM_PTR + 8;
     static constexpr uint32_t SMEM_BYTES = OFF_ABORT + 8 + 1024;
@@ -194,6 +217,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes,
     return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo_bytes >> 4) << 16) |
            ((uint64_t)(sbo_bytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
+// The same for rows of 64 bytes, 64-byte swizzle: groups of 8 rows lie 512 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc64(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (32ull << 32) | (1ull << 46) | (4ull << 61);
+}
 // Instruction descriptor: bf16 x bf16 (or f16 x f16) -> fp32, M = 128, N = n; b_mn = 1 when B is stored with N
 // contiguous (the V tile), 0 when K is contiguous.
 template <bool F16 = false>
@@ -205,6 +232,13 @@ __device__ __forceinline__ void mma_f16(uint32_t el, uint32_t d_tmem, uint64_t a
     asm volatile(
         "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
         "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc), "r"(el) : "memory");
+}
+// The same with e4m3 operands, 32 values a step.
+__device__ __forceinline__ void mma_f8(uint32_t el, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc), "r"(el) : "memory");
 }
 // True in exactly one lane of a converged warp.
@@ -312,149 +346,245 @@ __device__ __forceinline__ TItem load_titem(const Work* rec, bool valid) {
     return r;
 }
 
-// Producer of K (which = 0) or V tiles out of the 8-bit cache, one warp: the MMAs read the codes as f16, which holds them exactly, in the layout
-// that the TMA copies of the bf16 cache leave; their scales go to the softmax (K's producer brings both kinds).  A lane holds D / 8 pieces of
-// 16 codes of a tile and the scale bytes of two rows.  As soon as a piece has been turned and stored, the same piece of the next tile is requested into its
-// registers, so that a tile's loads are in flight while the one before is being turned and waited for.
-template <int D>
-__device__ __forceinline__ void kv8_producer(const DevPlan& p, const uint8_t* __restrict__ pool8, const uint8_t* __restrict__ scales, int which, int lane, int i0, int i1,
-                                             const int32_t* head, uint32_t bar0, uint32_t sbase, uint8_t* smem, volatile int* abort_flag) {
-    using Geo = Geometry<D, true>;
-    constexpr int kPagesPerTile = kTile / kPage;          // 4
-    constexpr int kGroupTiles = 32 / kPagesPerTile;       // tiles whose page ids a warp holds, one to a lane
-    constexpr int kPieces = D / 16;                       // of a row
-    constexpr int kPerPage = kPage * kPieces / 32;        // a lane's pieces of a page: 4 or 2
-    constexpr int kRowsPerOp = 32 / kPieces;              // rows that a warp instruction moves
-    const int Hkv = p.num_kv_heads;
-    const uint32_t ring = sbase + Geo::OFF_RING;
-    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    auto load_pages = [&](const TItem& it, int first_page) {
-        const int npg = (it.kv_end - it.kv0 + kPage - 1) / kPage;
-        const int idx = first_page + lane;
-        return idx < npg ? __ldg(p.page_indices + it.page0 + idx) : 0;
-    };
-    const int row0 = lane / kPieces, piece = lane % kPieces;      // of the first of a lane's pieces of a page
-    // Where a lane's 32 bytes of a row go inside a page: 16-byte pieces XOR-swizzled by row.  Lanes of the second half of a row store
-    // their two pieces the other way round, so that eight lanes meet all banks.
-    const uint32_t flip = (uint32_t)(piece >> 2) & 1u;
-    auto page_offset = [&](int row, uint32_t k) {
-        return (uint32_t)(row >> 3) * Geo::GROUP_BYTES + (uint32_t)(piece >> 2) * Geo::ATOM_BYTES + (uint32_t)(row & 7) * 128u +
-               (((uint32_t)(2 * (piece & 3)) + k) ^ (uint32_t)(row & 7)) * 16u;
-    };
-    // The tile ahead: its item, place in it, the page ids of its group of tiles and of the group behind (or of the next item's first).
-    TItem cur = load_titem(reinterpret_cast<const Work*>(head + kHeadWorkTensor), i0 < i1), nxt = load_titem(p.works + i0 + 1, i0 + 1 < i1);
-    int pages = head[kHeadPagesTensor + lane], pages_nxt = 0, ii = i0, t = 0;
-    uint4 raw[kPagesPerTile * kPerPage];
-    uint32_t sc = 0;                    // scale bytes of rows 2 * (lane % 8), + 1 of page lane / 8: K, K, V, V
-    pdl_wait();
-    int page_id[kPagesPerTile];         // of the tile ahead
-    int rows = 0;                       // of the tile ahead; 0: none is left
-    auto look = [&]() {                 // takes up the tile at (cur, t)
-        rows = cur.kv_end > 0 ? min(kTile, cur.kv_end - (cur.kv0 + t * kTile)) : 0;
-        const int npages = (rows + kPage - 1) / kPage;
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+// The largest exponent of a tile's rows, `bytes` being the scale bytes of this lane's rows key and key + 1; whether the others lie at most kNearExponents
+// below it.  Rows of the least exponent are left out: those of zeros have it, and what else has it is below 2^-91.  False where a row
+// is not finite.
+__device__ __forceinline__ bool tile_exponents(uint32_t bytes, int key, int rows, int& top) {
+    int hi = kKv8LeastExponent, lo = 1000;
 #pragma unroll
-        for (int k = 0; k < kPagesPerTile; ++k) {
-            page_id[k] = __shfl_sync(0xffffffffu, pages, (t % kGroupTiles) * kPagesPerTile + min(k, max(npages - 1, 0)));
-            if (rows > 0 && !page_ok(page_id[k], p.num_pages, p.status, kStatusBadPageSpan)) page_id[k] = 0;      // (checked build only)
+    for (int e = 0; e < 2; ++e) {
+        const int b = (int)(bytes >> (8 * e) & 0xffu) - 127;
+        if (key + e < rows) {
+            hi = max(hi, b);
+            if (b > kKv8LeastExponent) lo = min(lo, b);
         }
-        if (which == 0 && rows > 0) {
-            const int k = lane >> 3;
-            const int page = k == 0 ? page_id[0] : k == 1 ? page_id[1] : k == 2 ? page_id[2] : page_id[3];
-            const uint8_t* src = scales + kv8_scale_offset(page, 0, cur.kv_head, 2 * (lane & 7), Hkv);
-            sc = __ldcg(reinterpret_cast<const unsigned short*>(src)) | (uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(src + kPage)) << 16;
-        }
-    };
-    auto load_piece = [&](int k, int i) {
-        raw[k * kPerPage + i] = ldg_nc_v4(pool8 + kv8_row_offset(page_id[k], which, cur.kv_head, i * kRowsPerOp + row0, Hkv, D) + piece * 16);
-    };
-    auto advance = [&]() {              // on to the tile behind
-        if (rows == 0) return;
+    }
+    top = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    return top <= 127 && top - lo <= kNearExponents;      // (the byte 255 is 128)
+}
+// 2^(byte - 127 - top) as f16, zero where it is below 2^-15.
+__device__ __forceinline__ uint32_t near_factor(uint32_t byte, int top) {
+    const int e = (int)byte - 127 - top + 15;
+    return e > 0 ? (uint32_t)min(e, 15) << 10 : e == 0 ? 0x200u : 0u;
+}
+
+// How a producer of the 8-bit cache goes through a CTA's tiles: the item at hand and the one behind it, the place in it, the page ids of the tile's group (one to a
+// lane) and of the group behind (or of the next item's first).
+struct TileCursor {
+    TItem cur, nxt;
+    int pages, pages_nxt, ii, t;
+
+    static constexpr int kPagesPerTile = kTile / kPage, kGroupTiles = 32 / kPagesPerTile;
+
+    __device__ __forceinline__ int load_pages(const DevPlan& p, const TItem& it, int first_page, int lane) const {
+        const int npg = (it.kv_end - it.kv0 + kPage - 1) / kPage, idx = first_page + lane;
+        return idx < npg ? __ldg(p.page_indices + it.page0 + idx) : 0;
+    }
+    __device__ __forceinline__ void start(const DevPlan& p, const int32_t* head, int i0, int i1, int lane) {
+        cur = load_titem(reinterpret_cast<const Work*>(head + kHeadWorkTensor), i0 < i1);
+        nxt = load_titem(p.works + i0 + 1, i0 + 1 < i1);
+        pages = head[kHeadPagesTensor + lane];
+        pages_nxt = 0;
+        ii = i0;
+        t = 0;
+    }
+    // rows of the tile at hand; 0: none is left
+    __device__ __forceinline__ int rows() const { return cur.kv_end > 0 ? min(kTile, cur.kv_end - (cur.kv0 + t * kTile)) : 0; }
+    // id of its page k (of its last one, for k beyond), for all lanes to ask together
+    __device__ __forceinline__ int page(const DevPlan& p, int k, int rows) const {
+        int id = __shfl_sync(0xffffffffu, pages, t % kGroupTiles * kPagesPerTile + min(k, (rows + kPage - 1) / kPage - 1));
+        if (!page_ok(id, p.num_pages, p.status, kStatusBadPageSpan)) id = 0;      // (checked build only)
+        return id;
+    }
+    // on to the next tile; the ids of the group behind are asked for with a group's first tile
+    __device__ __forceinline__ void next(const DevPlan& p, int i1, int lane) {
         const int ntiles = (cur.kv_end - cur.kv0 + kTile - 1) / kTile;
-        ++t;
-        if (t == ntiles) {
+        if (t % kGroupTiles == 0) {
+            if (t + kGroupTiles < ntiles) pages_nxt = load_pages(p, cur, (t + kGroupTiles) * kPagesPerTile, lane);
+            else if (nxt.kv_end > 0) pages_nxt = load_pages(p, nxt, 0, lane);
+        }
+        if (++t == ntiles) {
             cur = nxt;
             ++ii;
             nxt = load_titem(p.works + ii + 1, ii + 1 < i1);
             t = 0;
         }
         if (t % kGroupTiles == 0) pages = pages_nxt;
+    }
+};
+
+// Producer of K tiles out of the 8-bit cache, one warp.  The MMAs take the codes as they are (kind::f8f6f4; Q is the sum of two rows of e4m3, see f8_row), so a tile is four
+// TMA copies; what the warp has to work out is the tile's scales for the softmax.  Their bytes come one tile ahead, two rows to a lane.
+template <int D>
+__device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorMap* map, const uint8_t* __restrict__ scales, int lane, int i0, int i1, const int32_t* head,
+                                               uint32_t bar0, uint32_t sbase, uint8_t* smem, volatile int* abort_flag) {
+    using Geo = Geometry<D, true>;
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    const int key = (lane >> 3) * kPage + 2 * (lane & 7);      // the lane's rows: key, key + 1
+    TileCursor c;
+    c.start(p, head, i0, i1, lane);
+    int rows = c.rows(), kv_head = c.cur.kv_head, begins = 1, id = 0;
+    unsigned short bytes_k = 0, bytes_v = 0;
+    pdl_wait();
+    auto take = [&]() {      // the tile at the cursor: this lane's page id and scale bytes
+        rows = c.rows();
+        if (rows == 0) return;
+        kv_head = c.cur.kv_head;
+        begins = c.t == 0;
+        id = c.page(p, lane, rows);
+        const uint8_t* at = scales + kv8_scale_offset(c.page(p, lane >> 3, rows), 0, kv_head, 2 * (lane & 7), p.num_kv_heads);
+        bytes_k = __ldcg(reinterpret_cast<const unsigned short*>(at));      // (nothing touches them before their tile's turn: no wait here)
+        bytes_v = __ldcg(reinterpret_cast<const unsigned short*>(at + kPage));
+        c.next(p, i1, lane);
     };
-    auto ask_pages = [&]() {            // the ids behind this group's, asked for when its first tile is on its way
-        if (rows == 0 || t % kGroupTiles != 0) return;
-        const int ntiles = (cur.kv_end - cur.kv0 + kTile - 1) / kTile;
-        if (t + kGroupTiles < ntiles) pages_nxt = load_pages(cur, (t + kGroupTiles) * kPagesPerTile);
-        else if (nxt.kv_end > 0) pages_nxt = load_pages(nxt, 0);
-    };
-    look();
-#pragma unroll
-    for (int k = 0; k < kPagesPerTile; ++k)
-        if (k * kPage < rows)
-#pragma unroll
-            for (int i = 0; i < kPerPage; ++i) load_piece(k, i);
-    ask_pages();
+    take();
     int most = -1000;                   // largest eV of the item so far
-    for (int n = 0; rows > 0; ++n) {
-        const int rows_now = rows;
-        const uint32_t sc_now = sc;
-        const int s = ring_slot(which, n, Geo::RING);
-        if (t == 0) most = -1000;
-        advance();
-        look();
-        if (!mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::RING) & 1u) ^ 1u, abort_flag, p.status, 11 + which)) break;
-        const uint32_t slot = ring + s * Geo::SLOT_BYTES;
+    int n = 0;
+    for (; rows > 0; ++n) {
+        const int s = Geo::slot(0, n), rows_now = rows;
+        if (!mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::RING_K) & 1u) ^ 1u, abort_flag, p.status, 11)) break;
+#ifdef ASYNCLM_DEBUG
+        const bool stall = blockIdx.x == 0 && p.debug_stall_tile == n + 1;      // (see the other producer)
+#else
+        constexpr bool stall = false;
+#endif
+        const int npages = (rows_now + kPage - 1) / kPage;
+        const uint32_t full = bar(Geo::kRingFull0 + s);
+        if (lane == 0 && !stall) mbar_arrive_expect_tx(full, (uint32_t)(npages * kPage * D));
+        __syncwarp();
+        if (lane < npages && !stall)
+            asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                         ::"r"(sbase + Geo::slot_offset(0, s) + (uint32_t)lane * (kPage * D)), "l"(map), "r"(0), "r"(0), "r"(kv_head), "r"(2 * id), "r"(full) : "memory");
+        // What the softmax needs of the tile: every key's 2^eK; the tile's eV and 2^-eV, or every key's.  A row of V that is not finite (its codes are
+        // zeros) makes its key's score NaN, so that only those who see it are hit.  Keys behind the end are masked, whatever stands here.
+        const uint32_t k_now = bytes_k, v_now = bytes_v;
+        if (begins) most = -1000;
+        take();
+        float* v = reinterpret_cast<float*>(smem + Geo::OFF_SCALE + (uint32_t)(n % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
+        float ks[2];
 #pragma unroll
-        for (int k = 0; k < kPagesPerTile; ++k) {
-            if (k * kPage < rows_now) {
-#pragma unroll
-                for (int i = 0; i < kPerPage; ++i) {
-                    const int row = i * kRowsPerOp + row0;
-                    uint4 w = raw[k * kPerPage + i];
-                    if (which == 1 && k * kPage + row >= rows_now) w = make_uint4(0, 0, 0, 0);      // slots past the item's end hold anything, and 0 * NaN would poison P V
-                    const uint4 lo = make_uint4(kv8_decode2(w.x), kv8_decode2_hi(w.x), kv8_decode2(w.y), kv8_decode2_hi(w.y));
-                    const uint4 hi = make_uint4(kv8_decode2(w.z), kv8_decode2_hi(w.z), kv8_decode2(w.w), kv8_decode2_hi(w.w));
-                    const uint32_t at = slot + (uint32_t)k * Geo::PAGE_BYTES;
-                    const uint4 a = flip ? hi : lo, b = flip ? lo : hi;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + page_offset(row, flip)), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + page_offset(row, flip ^ 1u)), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
-                }
-            }
-            if (k * kPage < rows) {
-#pragma unroll
-                for (int i = 0; i < kPerPage; ++i) load_piece(k, i);
-            }
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t bk = k_now >> (8 * e) & 0xffu, bv = v_now >> (8 * e) & 0xffu;
+            ks[e] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);
         }
-        ask_pages();
-        if (which == 0) {
-            // A row of V that is not finite (its codes are zeros) makes its key's score NaN, so that only those who see it are hit.  Keys behind the end are
-            // masked, whatever stands here.
-            float* v = reinterpret_cast<float*>(smem + Geo::OFF_SCALE + (uint32_t)(n % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
-            const int key = (lane >> 3) * kPage + 2 * (lane & 7);
-            float ks[2], ev[2], iv[2];
-            int hi = -1000, lo = 1000;
+        *reinterpret_cast<float2*>(v + 4 + key) = make_float2(ks[0], ks[1]);
+        int top;
+        const bool near = tile_exponents(v_now, key, rows_now, top);
+        if (near) most = max(most, top);
+        if (near && most - top <= kFarExponents) {
+            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4((float)top, two_to(-top), 0.f, 0.f);
+        } else {
+            int lo = 1000;
+            float ev[2], iv[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint32_t bk = sc_now >> (8 * e) & 0xffu, bv = sc_now >> (16 + 8 * e) & 0xffu;
-                const int x = bv == kKv8NanByte ? kKv8LeastExponent : (int)bv - 127;
-                ks[e] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);
+                const uint32_t bv = v_now >> (8 * e) & 0xffu;
+                const int x = near ? top : bv == kKv8NanByte ? kKv8LeastExponent : max((int)bv - 127, -126);
                 ev[e] = (float)x;
-                iv[e] = __uint_as_float((uint32_t)(127 - max(x, -126)) << 23);
-                if (key + e < rows_now) hi = max(hi, x), lo = min(lo, x);
+                iv[e] = two_to(-x);
+                if (key + e < rows_now) lo = min(lo, x), most = max(most, x);
             }
-            hi = __reduce_max_sync(0xffffffffu, hi);
             lo = __reduce_min_sync(0xffffffffu, lo);
-            most = max(most, hi);
-            *reinterpret_cast<float2*>(v + key) = make_float2(ks[0], ks[1]);
-            *reinterpret_cast<float2*>(v + kTile + key) = make_float2(ev[0], ev[1]);
-            *reinterpret_cast<float2*>(v + 2 * kTile + key) = make_float2(iv[0], iv[1]);
-            if (lane == 0) v[3 * kTile] = most - lo > kFarExponents ? 1.f : 0.f;
+            most = __reduce_max_sync(0xffffffffu, most);
+            *reinterpret_cast<float2*>(v + 4 + kTile + key) = make_float2(ev[0], ev[1]);
+            *reinterpret_cast<float2*>(v + 4 + 2 * kTile + key) = make_float2(iv[0], iv[1]);
+            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4(0.f, 0.f, most - lo > kFarExponents ? 2.f : 1.f, 0.f);
+        }
+        __syncwarp();
+        if (lane == 0 && !stall) mbar_arrive(full);
+    }
+    // The copies land before shared memory goes away or on to the warp body, where a role has given up.
+    const long long t0 = clock64();
+    for (int k = max(0, n - Geo::RING_K); k < n; ++k)
+        while (!mbar_try_wait(bar(Geo::kRingFull0 + Geo::slot(0, k)), (uint32_t)ring_use(k, Geo::RING_K) & 1u) && clock64() - t0 < kWaitCycles) {}
+}
+
+// Producer of one page of every V tile out of the 8-bit cache, one warp: the P V MMAs read the codes as f16, which holds them exactly, in the layout
+// that the TMA copies of the bf16 cache leave, with their scales as far as these are near each other (see kNearExponents).  A lane holds D / 32 pieces of
+// 16 codes of its page, for two tiles: the piece of the tile after next is requested when that of the one at hand has been turned and stored.
+template <int D>
+__device__ __forceinline__ void kv8_v_producer(const DevPlan& p, const uint8_t* __restrict__ pool8, const uint8_t* __restrict__ scales, int part, int lane, int i0, int i1,
+                                               const int32_t* head, uint32_t bar0, uint8_t* smem, volatile int* abort_flag) {
+    using Geo = Geometry<D, true>;
+    constexpr int kPieces = D / 16;                       // 16-code pieces of a row
+    constexpr int kMine = kPage * kPieces / 32;           // a lane's pieces of a page: 4 or 2
+    constexpr int kRowsPerOp = 32 / kPieces;              // rows that a warp instruction moves
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    // The row of a lane's first piece, and which piece of the row it is.  Eight lanes take four pieces of two rows next to each other, so that
+    // the 16 bytes that each of them stores at once, at an even piece of an even row or an odd one of an odd row, meet all banks.
+    const int piece = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+    const int row0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    static_assert(kRowsPerOp == 4 || kRowsPerOp == 8, "rows of a warp instruction");
+    // Where the two 16-byte halves of a piece go inside a page (pieces XOR-swizzled by row): those of row0; four rows further on it is the same place with bit 6
+    // turned, 512 bytes on.
+    const uint32_t at_row = (uint32_t)part * Geo::PAGE_BYTES + (uint32_t)(piece >> 2) * Geo::ATOM_BYTES + (uint32_t)row0 * 128u +
+                            ((uint32_t)(2 * (piece & 3)) ^ (uint32_t)row0) * 16u;
+    const uint32_t src_lane = (uint32_t)row0 * D + (uint32_t)piece * 16u;
+    const int key = (lane >> 3) * kPage + 2 * (lane & 7);      // the rows whose scale bytes the lane has: key, key + 1
+    TileCursor c;
+    c.start(p, head, i0, i1, lane);
+    struct Ahead {
+        uint4 raw[kMine];
+        int rows;                 // of the tile; 0: none is left
+        unsigned short bytes;
+    };
+    pdl_wait();
+    auto take = [&](Ahead& h) {
+        h.rows = c.rows();
+        if (h.rows == 0) return;
+        const uint8_t* src = pool8 + kv8_row_offset(c.page(p, part, h.rows), 1, c.cur.kv_head, 0, p.num_kv_heads, D) + src_lane;
+        h.bytes = __ldcg(reinterpret_cast<const unsigned short*>(
+            scales + kv8_scale_offset(c.page(p, lane >> 3, h.rows), 1, c.cur.kv_head, 2 * (lane & 7), p.num_kv_heads)));
+        if (part * kPage < h.rows)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) h.raw[i] = ldg_nc_v4(src + i * kRowsPerOp * D);
+        c.next(p, i1, lane);
+    };
+    int n = 0;
+    auto turn = [&](Ahead& h) {      // the tile in `h`, and the one at the cursor into its place; false at the end
+        if (h.rows == 0) return false;
+        const int rows = h.rows, s = Geo::slot(1, n);
+        int top;
+        const bool near = tile_exponents(h.bytes, key, rows, top);
+        const uint32_t factors = near ? near_factor(h.bytes & 0xffu, top) | near_factor(h.bytes >> 8, top) << 16 : 0x3c003c00u;      // f16, of the lane's two rows
+        uint32_t f[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            f[i] = __byte_perm(__shfl_sync(0xffffffffu, factors, part * 8 + (i * kRowsPerOp + row0) / 2), 0, (row0 & 1) != 0 ? 0x3232 : 0x1010);
+        if (!mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::RING_V) & 1u) ^ 1u, abort_flag, p.status, 12)) return false;
+        if (part * kPage < rows) {
+            const uint32_t slot = Geo::slot_offset(1, s - Geo::RING_K);
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t odd = D == 128 ? i & 1 : 0;
+                const uint32_t to = slot + (uint32_t)(D == 128 ? i >> 1 : i) * Geo::GROUP_BYTES + odd * 512u + (at_row ^ odd * 64u);
+                uint4 w = h.raw[i];
+                // slots past the item's end hold anything, and 0 * NaN would poison P V
+                if (rows < kTile && part * kPage + i * kRowsPerOp + row0 >= rows) w = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(smem + to) = make_uint4(mul_f16x2(kv8_decode2(w.x), f[i]), mul_f16x2(kv8_decode2_hi(w.x), f[i]),
+                                                                  mul_f16x2(kv8_decode2(w.y), f[i]), mul_f16x2(kv8_decode2_hi(w.y), f[i]));
+                *reinterpret_cast<uint4*>(smem + (to ^ 16u)) = make_uint4(mul_f16x2(kv8_decode2(w.z), f[i]), mul_f16x2(kv8_decode2_hi(w.z), f[i]),
+                                                                          mul_f16x2(kv8_decode2(w.w), f[i]), mul_f16x2(kv8_decode2_hi(w.w), f[i]));
+            }
         }
         fence_async_smem();      // the MMAs read through the asynchronous proxy
         __syncwarp();
-#ifdef ASYNCLM_DEBUG
-        if (which == 0 && blockIdx.x == 0 && p.debug_stall_tile == n + 1) continue;      // (see the other producer)
-#endif
         if (lane == 0) mbar_arrive(bar(Geo::kRingFull0 + s));
-    }
+        take(h);
+        ++n;
+        return true;
+    };
+    Ahead a, b;
+    a.bytes = b.bytes = 0;
+    take(a);
+    take(b);
+    while (turn(a) && turn(b)) {}
 }
 
 // The whole kernel body, called by all twelve warps with `smem` 1024-byte aligned.
@@ -465,8 +595,9 @@ __device__ __forceinline__ void kv8_producer(const DevPlan& p, const uint8_t* __
 // 14.04 | 13.68 (14.04), one span over 2000 keys 15.6 | 15.1 (15.2), head_dim 64 9.57 | 9.47 (9.18), 24 sequences with spans of 33-96
 // tokens 70.3 | 69.1, 8192 tokens 545 | 528.  Beside the warp body's code it is a loss: 8 sequences of 32-131 K keys with two
 // 256-token spans 917 | 925.
-// KV8: the cache is the 8-bit one, at `pool8` and `scales` (span_map and pool are not used): its producers are kv8_producer.
-template <int D, int G, bool ALONE, bool KV8 = false>
+// KV8: the cache is the 8-bit one, at `pool8` and `scales`, span_map is that of its K blocks (pool is not used): kv8_k_producer and kv8_v_producer.  ROLE: this call is
+// warps 0-7's (0) or those behind (1), whose registers differ, or everybody's (-1).
+template <int D, int G, bool ALONE, bool KV8 = false, int ROLE = -1>
 __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* span_map, const __nv_bfloat16* __restrict__ q,
                                         const __nv_bfloat16* pool,
                                         __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
@@ -498,16 +629,16 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             mbar_init(bar(Geo::kPvDone0 + b), 1);
             mbar_init(bar(Geo::kSFull0 + b), 1);
         }
-        for (int s = 0; s < 2 * Geo::RING; ++s) {
-            mbar_init(bar(Geo::kRingFull0 + s), KV8 || s < Geo::RING ? 1 : 33);      // V tiles: see the producers
-            mbar_init(bar(Geo::kRingEmpty0 + s), KV8 && s < Geo::RING ? 8 : 2);      // (8 bits: every warp reads a K tile's scales and releases it)
+        for (int s = 0; s < Geo::RINGS; ++s) {
+            mbar_init(bar(Geo::kRingFull0 + s), KV8 ? (s < Geo::RING_K ? 2 : 4) : s < Geo::RING_K ? 1 : 33);      // V tiles: see the producers
+            mbar_init(bar(Geo::kRingEmpty0 + s), KV8 && s < Geo::RING_K ? 8 : 2);      // (8 bits: every warp reads a K tile's scales and releases it)
         }
         mbar_init(bar(Geo::kMmaDrain), 2);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (!KV8 && threadIdx.x == kProducerWarpK * 32) asm volatile("prefetch.tensormap [%0];" ::"l"(span_map));
+    if (threadIdx.x == kProducerWarpK * 32) asm volatile("prefetch.tensormap [%0];" ::"l"(span_map));
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(sbase + Geo::OFF_TMEM_PTR), "r"(kTmemCols) : "memory");
@@ -518,9 +649,11 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr;
 
-    if (warp >= 8) {
-      if (KV8 && (warp == kProducerWarpK || warp == kProducerWarpV)) {
-        kv8_producer<D>(p, pool8, scales, warp == kProducerWarpV ? 1 : 0, lane, i0, i1, head, bar0, sbase, smem, abort_flag);
+    if (ROLE < 0 ? warp >= 8 : ROLE == 1) {
+      if (KV8 && warp == kProducerWarpK) {
+        kv8_k_producer<D>(p, span_map, scales, lane, i0, i1, head, bar0, sbase, smem, abort_flag);
+      } else if (KV8 && (warp == kProducerWarpV || warp == 12 || warp == 13 || warp == 15)) {
+        kv8_v_producer<D>(p, pool8, scales, warp == 15 ? 3 : warp % 10 == 0 ? 0 : warp - 11, lane, i0, i1, head, bar0, smem, abort_flag);
       } else if (!KV8 && (warp == kProducerWarpK || warp == kProducerWarpV)) {
         // ------------------------------------------------------------------ producer warps
         const int which = warp == kProducerWarpV ? 1 : 0;       // 0: K tiles, 1: V tiles
@@ -534,7 +667,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             asm volatile("cp.async.wait_all;" ::: "memory");
             const long long t0 = clock64();
             for (int k = k0; k < k1; ++k)
-                while (!mbar_try_wait(bar(Geo::kRingFull0 + ring_slot(which, k, Geo::RING)), (uint32_t)ring_use(k, Geo::RING) & 1u) &&
+                while (!mbar_try_wait(bar(Geo::kRingFull0 + Geo::slot(which, k)), (uint32_t)ring_use(k, Geo::ring(which)) & 1u) &&
                        clock64() - t0 < kWaitCycles) {}
         };
         constexpr int kPagesPerTile = kTile / kPage;          // 4
@@ -555,9 +688,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 for (int t = t0; t < t1 && ok; ++t, ++n) {
                     const int rows = min(kTile, cur.kv_end - (cur.kv0 + t * kTile));
                     const int npages = (rows + kPage - 1) / kPage;
-                    const int s = ring_slot(which, n, Geo::RING);
+                    const int s = Geo::slot(which, n);
                     if (lane == 0 && which == 0) trace_event(9, ev, 40);
-                    ok = mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::RING) & 1u) ^ 1u, abort_flag, p.status, 11 + which);
+                    ok = mbar_wait_warp(bar(Geo::kRingEmpty0 + s), ((uint32_t)ring_use(n, Geo::ring(which)) & 1u) ^ 1u, abort_flag, p.status, 11 + which);
                     if (!ok) break;
                     if (lane == 0 && which == 0) trace_event(9, ev, 42);
                     const uint32_t full = bar(Geo::kRingFull0 + s), slot_addr = ring + s * Geo::SLOT_BYTES;
@@ -612,8 +745,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
         }
         // The copies land before shared memory goes away or on to the warp body.  The MMA warps have normally waited for
         // each of them, but another role may have given up meanwhile, whether or not this one has seen it.
-        land_copies(max(0, n - Geo::RING), n);
-      } else {
+        land_copies(max(0, n - Geo::ring(which)), n);
+      } else if (!KV8 || warp < kThreads / 32) {
         // ------------------------------------------------------------------ MMA issuers
         // One warp per softmax group, running convergently, issues the group's MMAs through an elected lane.  A
         // turn is one KV tile of the group: its P V and the Q K^T of the group's next tile
@@ -653,18 +786,19 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             if (ok && item_no > 0) ok = mbar_wait_spin(bar(Geo::kOFree), (uint32_t)(item_no - 1) & 1u, abort_flag, p.status, 27);
             tr_item += trace_clock() - t_item;
             if (ok) tc_fence_after();
-            const uint64_t qd = smem_desc(sbase + Geo::OFF_Q + (dual ? (uint32_t)b * Geo::QTILE_BYTES : 0u), 16, 1024);
+            const uint64_t qd = KV8 && D == 64 ? smem_desc64(sbase + Geo::OFF_Q + (dual ? (uint32_t)b * Geo::QTILE_BYTES : 0u))
+                                               : smem_desc(sbase + Geo::OFF_Q + (dual ? (uint32_t)b * Geo::QTILE_BYTES : 0u), 16, 1024);
             const int last_pages = (it.kv_end - (it.kv0 + (ntiles - 1) * kTile) + kPage - 1) / kPage;      // of the item's last tile
-            const uint32_t idesc_last = instr_desc<KV8>(16u * (uint32_t)last_pages, 0);
+            const uint32_t idesc_last = instr_desc<KV8>(16u * (uint32_t)last_pages, 0);      // (8 bits: e4m3, whose number is f16's)
             // where the group's next K and V tile lie
-            RingPlace kp = ring_place(base + (dual ? 0 : b), Geo::RING), vp = kp;
-            auto next_place = [&](RingPlace& x) { x = ring_next(x, dual ? 1 : 2, Geo::RING); };
+            RingPlace kp = ring_place(base + (dual ? 0 : b), Geo::RING_K), vp = ring_place(base + (dual ? 0 : b), Geo::RING_V);
+            auto next_place = [&](int which, RingPlace& x) { x = ring_next(x, dual ? 1 : 2, Geo::ring(which)); };
             auto wait_tile = [&](int which, const RingPlace& x, int code) {
                 const long long tw = trace_clock();
-                ok = ok && mbar_wait_spin(bar(Geo::kRingFull0 + which * Geo::RING + x.slot), x.parity, abort_flag, p.status, code);
+                ok = ok && mbar_wait_spin(bar(Geo::kRingFull0 + (which ? Geo::RING_K : 0) + x.slot), x.parity, abort_flag, p.status, code);
                 tr_kv += trace_clock() - tw;
             };
-            auto tile_addr = [&](int which, const RingPlace& x) { return sbase + Geo::OFF_RING + (uint32_t)(which * Geo::RING + x.slot) * Geo::SLOT_BYTES; };
+            auto tile_addr = [&](int which, const RingPlace& x) { return sbase + Geo::slot_offset(which, x.slot); };
             // u = -2, -1: the Q K^T of the group's first two tiles; u >= 0: the turn of its u-th tile, the P V of
             // tile j and the Q K^T of tile j + lead back to back once everything they read is there.  K/V tiles
             // are waited for first (they are normally there already), P last, so that nothing stands between
@@ -690,7 +824,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 if (!KV8 && pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
                 const uint32_t buf = tmem + kColS + 128u * (uint32_t)b + 64u * (uint32_t)(c & 1);      // S and P
                 const uint64_t vd = smem_desc(tile_addr(1, vp), Geo::ATOM_BYTES, Geo::GROUP_BYTES);
-                const uint64_t kd = smem_desc(tile_addr(0, kp), 16, Geo::GROUP_BYTES);
+                const uint64_t kd = !KV8 ? smem_desc(tile_addr(0, kp), 16, Geo::GROUP_BYTES) : D == 64 ? smem_desc64(tile_addr(0, kp)) : smem_desc(tile_addr(0, kp), 16, 1024);
                 const uint32_t idesc_qk = jn == ntiles - 1 ? idesc_last : instr_desc<KV8>(kTile, 0);
                 const uint32_t done = bar((qk ? Geo::kSFull0 : Geo::kPvDone0) + 2 * b + (c & 1));
                 if (pv) {
@@ -722,6 +856,13 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
                         if (ks == D / 16 - 2) pass_token();      // the other warp's first MMA queues behind the last two
+                        if constexpr (KV8) {
+                            // Q is hi + lo, a tile each of one byte a value; a step is 32 values, and K's are the same for both
+                            constexpr int kSteps = D / 32;
+                            const uint64_t step = (uint64_t)((uint32_t)(ks % kSteps) * 32u >> 4);
+                            mma_f8(el, buf, qd + (uint64_t)((uint32_t)(ks / kSteps) * (uint32_t)(kRows * D) >> 4) + step, kd + step, idesc_qk, ks > 0);
+                            continue;
+                        }
                         // the address field counts 16-byte units and cannot carry out of its 14 bits here
                         const uint64_t qoff = (uint64_t)(((uint32_t)(ks >> 2) * Geo::QHALF_BYTES + (uint32_t)(ks & 3) * 32u) >> 4);
                         const uint64_t koff = (uint64_t)(((uint32_t)(ks >> 2) * Geo::ATOM_BYTES + (uint32_t)(ks & 3) * 32u) >> 4);
@@ -730,8 +871,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 }
                 mma_commit(el, done);
                 if (!qk) pass_token();
-                if (pv) next_place(vp);
-                if (qk) next_place(kp);
+                if (pv) next_place(1, vp);
+                if (qk) next_place(0, kp);
                 if (lane == 0) trace_event(b ? 10 : 0, ev, 26 + b);
             }
             if (!dual && b == 1 && (ntiles & 1) != 0) {      // group 0 has a turn more
@@ -792,9 +933,10 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
             for (int c = 0; c < kQV; ++c) w[c] = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
         };
-        // and as f16, divided by the power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value);
-        // returns the factor on the scores
-        auto f16_row = [&](uint4 (&w)[kQV]) {
+        // and as e4m3, scaled by a power of two to a largest value in 2^7 .. 2^8, in two parts: bf16's eight bits are those of a code and of the code of what
+        // is left, exactly down to 2^-9 of the largest value, and off by 2^-18 of it below.  Puts the thread's share (all of the row, or value half b) into the
+        // Q tile and returns the factor on the scores.
+        auto f8_row = [&](const uint4 (&w)[kQV], bool dual) {
             uint32_t most = 0;
 #pragma unroll
             for (int c = 0; c < kQV; ++c) {
@@ -802,19 +944,39 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
                 for (int e = 0; e < 4; ++e) most = max(most, max(x[e] & 0x7fffu, x[e] >> 16 & 0x7fffu));
             }
-            const uint32_t e = min(max(most >> 7, 1u), 253u);
-            const float down = __uint_as_float((254u - e) << 23);
-            auto two = [&](uint32_t x) {
-                const __half2 h = __floats2half2_rn(bf16_lo(x) * down, bf16_hi(x) * down);
-                return *reinterpret_cast<const uint32_t*>(&h);
+            const uint32_t e = min(max(most >> 7, 8u), 253u);
+            const float up = __uint_as_float((261u - e) << 23);
+            auto split = [&](uint32_t x, uint32_t& hi, uint32_t& lo) {      // two values -> two codes and two of the rest
+                const float a = bf16_lo(x) * up, c = bf16_hi(x) * up;
+                hi = kv8_encode2(a, c);
+                const uint32_t back = kv8_decode2(hi);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
+                lo = kv8_encode2(a - f.x, c - f.y);
             };
+            const uint32_t tile = Geo::OFF_Q + (dual ? (uint32_t)b * Geo::QTILE_BYTES : 0u) + (uint32_t)m * D;
+            const uint32_t swz = D == 128 ? (uint32_t)(m & 7) : (uint32_t)(m >> 1 & 3);
 #pragma unroll
-            for (int c = 0; c < kQV; ++c) w[c] = make_uint4(two(w[c].x), two(w[c].y), two(w[c].z), two(w[c].w));
-            return __uint_as_float(e << 23) * qscale;
+            for (int c = 0; c < kQV; c += 2) {      // 16 values: a 16-byte piece of either tile
+                if (!dual && (c >= kQV / 2) != (b == 1)) continue;
+                const uint32_t x[8] = {w[c].x, w[c].y, w[c].z, w[c].w, w[c + 1].x, w[c + 1].y, w[c + 1].z, w[c + 1].w};
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t h0, l0, h1, l1;
+                    split(x[2 * k], h0, l0);
+                    split(x[2 * k + 1], h1, l1);
+                    hi[k] = h0 | h1 << 16;
+                    lo[k] = l0 | l1 << 16;
+                }
+                const uint32_t at = tile + (((uint32_t)(c / 2) ^ swz) << 4);
+                *reinterpret_cast<uint4*>(smem + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4*>(smem + at + kRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+            return fmaxf(__uint_as_float((e - 7u) << 23) * qscale, FLT_MIN);      // (a masked score is -inf, and stays it)
         };
         // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.  (8 bits: a K slot
         // after two of each of four warps, all of which wait for the tile themselves: one that came late would find the slot's next phase over.)
-        auto release = [&](int which, int t, bool dual) { mbar_arrive_n(bar(Geo::kRingEmpty0 + ring_slot(which, t, Geo::RING)), dual ? 1u : 2u); };
+        auto release = [&](int which, int t, bool dual) { mbar_arrive_n(bar(Geo::kRingEmpty0 + Geo::slot(which, t)), dual ? 1u : 2u); };
         TItem it_next = load_titem(head_work, i0 < i1);
         uint4 q_next[kQV];
         pdl_wait();
@@ -834,22 +996,18 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 ok = mbar_wait_warp(bar(Geo::kOFree), (uint32_t)(item_no - 1) & 1u, abort_flag, p.status, 36);
                 if (!ok) break;
             }
-            float2 row_scale2 = make_float2(0.f, 0.f);
+            float row_scale = 0.f;
             if constexpr (KV8) {
-                const float x = f16_row(q_next);
-                row_scale2 = make_float2(x, x);
-                if (!dual && b == 1) {
+                row_scale = f8_row(q_next, dual);
+            } else {
 #pragma unroll
-                    for (int c = 0; c < kQV / 2; ++c) q_next[c] = q_next[c + kQV / 2];
-                }
+                for (int c = 0; c < kQV; ++c)
+                    if (dual || c < kQV / 2) {
+                        const int cc = dual ? c : c + kQV / 2 * b;      // chunk of the row
+                        *reinterpret_cast<uint4*>(smem + Geo::OFF_Q + (dual ? b * Geo::QTILE_BYTES : 0u) + (cc >> 3) * Geo::QHALF_BYTES + m * 128 +
+                                                  (((cc & 7) ^ (m & 7)) << 4)) = q_next[c];
+                    }
             }
-#pragma unroll
-            for (int c = 0; c < kQV; ++c)
-                if (dual || c < kQV / 2) {
-                    const int cc = dual ? c : c + kQV / 2 * b;      // chunk of the row
-                    *reinterpret_cast<uint4*>(smem + Geo::OFF_Q + (dual ? b * Geo::QTILE_BYTES : 0u) + (cc >> 3) * Geo::QHALF_BYTES + m * 128 +
-                                              (((cc & 7) ^ (m & 7)) << 4)) = q_next[c];
-                }
             fence_async_smem();
             mbar_arrive(bar(Geo::kQFull));
             if (lane == 0) trace_event(1 + warp, ev, 37);
@@ -879,7 +1037,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 // tile's until the release below
                 const float* tile_scales = nullptr;
                 if constexpr (KV8) {
-                    const RingPlace x = ring_place(kv_base + j, Geo::RING);
+                    const RingPlace x = ring_place(kv_base + j, Geo::RING_K);
                     ok = __all_sync(0xffffffffu, mbar_wait_spin(bar(Geo::kRingFull0 + x.slot), x.parity, abort_flag, p.status, 33));
                     if (!ok) break;
                     tile_scales = reinterpret_cast<const float*>(smem + Geo::OFF_SCALE + (uint32_t)((kv_base + j) % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
@@ -890,19 +1048,26 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 if (KV8 ? lane == 0 : m == 0) release(0, kv_base + j, dual);
                 if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
                 tmem_wait_ld();
+                // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V, whose tile leaves eV out: the tile's eV, which
+                // comes in below, or each key's
+                float4 tile = make_float4(0.f, 0.f, 0.f, 0.f);
+                float x_scale = row_scale;
                 if constexpr (KV8) {
-                    // x = score + eV (log2 domain): the exponent of the key's weight of V, whose row is read without its scale
+                    tile = *reinterpret_cast<const float4*>(tile_scales);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float4 ks = *reinterpret_cast<const float4*>(tile_scales + 4 * e), ev = *reinterpret_cast<const float4*>(tile_scales + kTile + 4 * e);
-                        const float2 a = __ffma2_rn(__fmul2_rn(make_float2(__uint_as_float(rr[4 * e]), __uint_as_float(rr[4 * e + 1])), row_scale2),
-                                                    make_float2(ks.x, ks.y), make_float2(ev.x, ev.y));
-                        const float2 c = __ffma2_rn(__fmul2_rn(make_float2(__uint_as_float(rr[4 * e + 2]), __uint_as_float(rr[4 * e + 3])), row_scale2),
-                                                    make_float2(ks.z, ks.w), make_float2(ev.z, ev.w));
+                        const float4 ks = *reinterpret_cast<const float4*>(tile_scales + 4 + 4 * e);
+                        const float2 a = __fmul2_rn(make_float2(__uint_as_float(rr[4 * e]), __uint_as_float(rr[4 * e + 1])), make_float2(ks.x, ks.y));
+                        const float2 c = __fmul2_rn(make_float2(__uint_as_float(rr[4 * e + 2]), __uint_as_float(rr[4 * e + 3])), make_float2(ks.z, ks.w));
                         rr[4 * e] = __float_as_uint(a.x);
                         rr[4 * e + 1] = __float_as_uint(a.y);
                         rr[4 * e + 2] = __float_as_uint(c.x);
                         rr[4 * e + 3] = __float_as_uint(c.y);
+                    }
+                    if (__builtin_expect(tile.z != 0.f, 0)) {
+                        x_scale = 1.f;
+#pragma unroll
+                        for (int e = 0; e < 64; ++e) rr[e] = __float_as_uint(fmaf(__uint_as_float(rr[e]), row_scale, tile_scales[4 + kTile + e]));
                     }
                 }
                 if (!__all_sync(0xffffffffu, vis == kTile)) {
@@ -923,7 +1088,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) cm[c] = fmaxf(cm[c], sv(16 * c + 15));
-                const float cmax = fmax3(fmaxf(cm[0], cm[1]), cm[2], cm[3]) * (KV8 ? 1.f : qscale);      // log2 domain
+                const float cmax = KV8 ? fmaf(fmax3(fmaxf(cm[0], cm[1]), cm[2], cm[3]), x_scale, tile.x)
+                                       : fmax3(fmaxf(cm[0], cm[1]), cm[2], cm[3]) * qscale;      // log2 domain
                 if (__any_sync(0xffffffffu, cmax > m_ref + kRescaleThreshold)) {
                     // Move the reference maximum (rare after the first tile; a row without one takes any visible
                     // key's): rescale the running sum and O[b].  O[b] is at rest once the P V of the group's
@@ -966,27 +1132,34 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 uint32_t pk[32];
                 if constexpr (KV8) {
                     // P' = exp2(x - m_ref) as f16 (11 bits); the sum takes it without the scale of V, 2^-eV times it
-                    if (tile_scales[3 * kTile] == 0.f) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float4 iv = *reinterpret_cast<const float4*>(tile_scales + 2 * kTile + 2 * e);
-                            const float2 x0 = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), nm2);
-                            const float2 x1 = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e + 2]), __uint_as_float(rr[2 * e + 3])), nm2);
-                            const float2 p0 = make_float2(fast_exp2(x0.x), fast_exp2(x0.y)), p1 = make_float2(fast_exp2(x1.x), fast_exp2(x1.y));
-                            l2 = __ffma2_rn(p0, make_float2(iv.x, iv.y), l2);
-                            l2b = __ffma2_rn(p1, make_float2(iv.z, iv.w), l2b);
-                            const __half2 h0 = __floats2half2_rn(p0.x, p0.y), h1 = __floats2half2_rn(p1.x, p1.y);
-                            pk[e] = *reinterpret_cast<const uint32_t*>(&h0);
-                            pk[e + 1] = *reinterpret_cast<const uint32_t*>(&h1);
-                        }
-                    } else {
+                    if (__builtin_expect(tile.z == 0.f, 1)) {
+                        const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(tile.x - m_use, tile.x - m_use);
+                        float2 s2 = make_float2(0.f, 0.f), s2b = s2;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
-                            const float2 ev = *reinterpret_cast<const float2*>(tile_scales + kTile + 2 * e);
+                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), scale2, b2);
+                            const float2 pe = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                            if (e & 1) s2b = __fadd2_rn(s2b, pe); else s2 = __fadd2_rn(s2, pe);
+                            const __half2 h = __floats2half2_rn(pe.x, pe.y);
+                            pk[e] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        const float2 iv2 = make_float2(tile.y, tile.y);
+                        l2 = __ffma2_rn(s2, iv2, l2);
+                        l2b = __ffma2_rn(s2b, iv2, l2b);
+                    } else {
+                        const bool far = tile.z == 2.f;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float2 ev = *reinterpret_cast<const float2*>(tile_scales + 4 + kTile + 2 * e), iv = *reinterpret_cast<const float2*>(tile_scales + 4 + 2 * kTile + 2 * e);
                             const float2 x = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), nm2);
-                            l2.x += fast_exp2(x.x - ev.x);
-                            l2.y += fast_exp2(x.y - ev.y);
-                            const __half2 h = __floats2half2_rn(fast_exp2(x.x), fast_exp2(x.y));
+                            const float2 pe = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                            if (far) {
+                                l2.x += fast_exp2(x.x - ev.x);
+                                l2.y += fast_exp2(x.y - ev.y);
+                            } else {
+                                l2 = __ffma2_rn(pe, iv, l2);
+                            }
+                            const __half2 h = __floats2half2_rn(pe.x, pe.y);
                             pk[e] = *reinterpret_cast<const uint32_t*>(&h);
                         }
                     }

@@ -174,9 +174,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The same with f16 operands.
+// The same with f16 operands (not volatile: the compiler may move it between loads).
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -197,6 +197,7 @@ struct Geometry {
     static constexpr int STAGE_PAGES = kWarps * WARP_PAGES;
     static constexpr int STAGE_TOK = STAGE_PAGES * kPage;       // keys per ring stage: 128 or 256
     static constexpr int STAGE_BYTES = STAGE_PAGES * PAGE_BYTES;      // 64 KiB; 8 bits at head_dim 64: 32 KiB
+    static constexpr int KV8_STAGES = D == 128 ? 3 : 6;         // as many as fit
     static constexpr int SCALE_BYTES = KV8 ? STAGE_PAGES * kKv8ScaleBytes : 0;      // of a stage, behind all stages' pages
     // Where page i of a stage lies in it.  8 bits: the two pages of a warp side by side, so that its merge state fits into their place.
     static __device__ __forceinline__ int page_slot(int i) { return KV8 ? i % kWarps * 2 + i / kWarps : i; }
@@ -444,48 +445,45 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
     if (lane == 0 && part == 0) trace_mark(3);
 }
 
-// One consumer warp's pages of a stage of the 8-bit cache, two of them as two independent chains.
+// One consumer warp's two pages of a stage of the 8-bit cache, as two independent chains.
 //   A code is at most 448 and exact in f16, and so are the products of an f16 MMA, so both contractions take the codes as they are:
-//       s = (sum_i cK_i q'_i) * (query scale) * 2^eK           in fp32, a factor for a key and one for a column
-//       O += P' cV,  P' = p * 2^eV = exp2(s + eV - w)          the V row's scale goes into its weight's exponent
-// P' is rounded to f16 (11 bits), with a reference maximum w of its own, that of s + eV: weights and scales may
-// then lie anywhere, and none is lost that matters beside the largest.  The sum of the softmax is that of exp2(s - m), in fp32.
+//       x = (sum_i cK_i q'_i) * (query scale * 2^eK) + eV      in fp32: the score, and the V row's scale as an exponent
+//       O += P' cV,  P' = p * 2^eV = exp2(x - ref)
+// P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere, and none is lost that matters
+// beside the largest.  The softmax sum is that of P' 2^-eV in fp32, against the same reference; where an eV lies outside a
+// window within which P' cannot have vanished and yet count (kLeastWindow; rows of zeros have the least exponent of all), the pages' sums take
+// exponentials of their own.  Against two references, one for sums and one for weights, this saves half of the exponentials.
 //   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes of a row, values 4 t .. 4 t + 3 of a
 // 16-value piece: the first two are one k step's low half, the others its high half, and Q is laid out alike.  V (transposed): two neighbouring
 // values of two neighbouring keys; a byte permutation pairs the keys, and value 2 g becomes row g of the piece's MMA, 2 g + 1 row g + 8.
-//   For 32 keys x 128 values that is 32 ldmatrix'd registers of K, as many of V, 64 + 64 cvt, 32 byte permutations and 32 MMAs.
+//   Cycles of a warp's two pages at head_dim 128 (64): 2030 (1480), of which the K and V parts with their 64 (32) cvt each 550 (290).  Turning codes into f16 with
+// integer instructions, seven for four codes, takes the K part to 1100 (570).
+constexpr uint32_t kLeastWindow = 87, kWindow = 95;      // scale bytes 87 .. 182: 2^-40 .. 2^55
+
 template <int D, int G>
 __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, const uint8_t* stage_scales, int warp, int lane, const uint32_t (&qb)[D / 16][2],
-                                          float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1, float& w0, float& w1) {
+                                          float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1) {
     using Geo = Geometry<D, true>;
     constexpr int WP = Geo::WARP_PAGES, PIECES = D / 16;
     const int g = lane >> 2, t4 = lane & 3;
     // lane -> row of an 8x8 matrix: (keys 0-7, piece p), (keys 8-15, p), (keys 0-7, p + 1), (keys 8-15, p + 1)
     const int key = (lane & 7) + ((lane >> 3) & 1) * 8, half = lane >> 4;
     const uint32_t row = (uint32_t)key * D, swz = D == 128 ? (uint32_t)(key & 7) : (uint32_t)(key >> 1 & 3);
-    auto page_smem = [&](int pp) { return smem_u32(stage) + (uint32_t)Geo::page_slot(pp * kWarps + warp) * Geo::PAGE_BYTES; };
-    bool on[WP];
-    float sc[WP][4], wv[WP][4], ek[WP][2], ev[WP][2];
+    const uint32_t page0 = smem_u32(stage) + (uint32_t)Geo::page_slot(warp) * Geo::PAGE_BYTES;      // the other page follows
+    if ((WP - 1) * kWarps * kPage + (warp + 1) * kPage > d.rows) {
+        // Slots past the sequence's end hold whatever was there before, NaN codes included: their scores are masked below, but 0 * NaN would still poison
+        // P V, so their V rows are cleared.  That goes for a whole page behind the end, too.
 #pragma unroll
-    for (int pp = 0; pp < WP; ++pp) {
-        const int key0 = (pp * kWarps + warp) * kPage, valid = d.rows - key0;
-        on[pp] = pp == 0 || valid > 0;
-        if (!on[pp]) continue;
-        const uint8_t* sb = stage_scales + (pp * kWarps + warp) * kKv8ScaleBytes;
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const uint32_t bk = sb[g + 8 * hh], bv = sb[kPage + g + 8 * hh];
-            ek[pp][hh] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
-            ev[pp][hh] = (float)((int)bv - 127);
-        }
-        if (valid < kPage) {
-            // Slots past the sequence's end hold whatever was in the page before, NaN codes included: their scores are masked, but 0 * NaN
-            // would still poison P V, so their V rows are cleared.
-            for (int i = valid * (D / 16) + lane; i < kPage * (D / 16); i += 32)
-                *reinterpret_cast<uint4*>(stage + (size_t)Geo::page_slot(pp * kWarps + warp) * Geo::PAGE_BYTES + Geo::BLOCK_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
-            __syncwarp();
-        }
+        for (int pp = 0; pp < WP; ++pp)
+            for (int i = max(d.rows - (pp * kWarps + warp) * kPage, 0) * (D / 16) + lane; i < kPage * (D / 16); i += 32)
+                *reinterpret_cast<uint4*>(stage + (size_t)(Geo::page_slot(warp) + pp) * Geo::PAGE_BYTES + Geo::BLOCK_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
+        __syncwarp();
     }
+    uint32_t kr[WP][PIECES / 2][4];
+#pragma unroll
+    for (int pc = 0; pc < PIECES; pc += 2)
+#pragma unroll
+        for (int pp = 0; pp < WP; ++pp) ldsm_x4(page0 + pp * Geo::PAGE_BYTES + row + (((uint32_t)(pc + half) ^ swz) << 4), kr[pp][pc / 2]);
     // ---- S^T = K Q^T
     float sa[WP][4], sb[WP][4];
 #pragma unroll
@@ -496,82 +494,86 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
     for (int pc = 0; pc < PIECES; pc += 2) {
 #pragma unroll
         for (int pp = 0; pp < WP; ++pp) {
-            if (!on[pp]) continue;
-            uint32_t r[4];
-            ldsm_x4(page_smem(pp) + row + (((uint32_t)(pc + half) ^ swz) << 4), r);
+            const uint32_t(&r)[4] = kr[pp][pc / 2];
             const uint32_t a0[4] = {kv8_decode2(r[0]), kv8_decode2(r[1]), kv8_decode2_hi(r[0]), kv8_decode2_hi(r[1])};
             const uint32_t a1[4] = {kv8_decode2(r[2]), kv8_decode2(r[3]), kv8_decode2_hi(r[2]), kv8_decode2_hi(r[3])};
             mma_f16(sa[pp], a0, qb[pc][0], qb[pc][1]);
             mma_f16(sb[pp], a1, qb[pc + 1][0], qb[pc + 1][1]);
         }
     }
+    float x[WP][4], ev[WP][2], iv[WP][2];
+    bool far = false;
 #pragma unroll
     for (int pp = 0; pp < WP; ++pp) {
         const int key0 = (pp * kWarps + warp) * kPage;
+        const uint8_t* sb8 = stage_scales + key0 / kPage * kKv8ScaleBytes + g;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sc[pp][e] = on[pp] ? (sa[pp][e] + sb[pp][e]) * ((e & 1 ? qs1 : qs0) * ek[pp][e >> 1]) : -INFINITY;      // log2 domain
-            wv[pp][e] = on[pp] ? sc[pp][e] + ev[pp][e >> 1] : -INFINITY;
+        for (int hh = 0; hh < 2; ++hh) {      // keys g and g + 8
+            const uint32_t bk = sb8[8 * hh], bv = sb8[kPage + 8 * hh];
+            const float ek = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
+            ev[pp][hh] = __uint_as_float(0x4b000000u | bv) - (8388608.f + 127.f);                   // bv - 127
+            iv[pp][hh] = __uint_as_float((254u - bv) << 23);                                        // 2^-eV inside the window
+            far = far || bv - kLeastWindow > kWindow;
+            x[pp][2 * hh] = fmaf(sa[pp][2 * hh] + sb[pp][2 * hh], qs0 * ek, ev[pp][hh]);            // log2 domain
+            x[pp][2 * hh + 1] = fmaf(sa[pp][2 * hh + 1] + sb[pp][2 * hh + 1], qs1 * ek, ev[pp][hh]);
         }
-        // ---- mask: key key0 + g (+8) is visible to column c iff it lies below lim0 + token(c)
-        if (d.lim0 < key0 + kPage) {
-            const int lim_a = d.lim0 + (2 * t4) / G - key0, lim_b = d.lim0 + (2 * t4 + 1) / G - key0;
-            if (g >= lim_a) sc[pp][0] = wv[pp][0] = -INFINITY;
-            if (g >= lim_b) sc[pp][1] = wv[pp][1] = -INFINITY;
-            if (g + 8 >= lim_a) sc[pp][2] = wv[pp][2] = -INFINITY;
-            if (g + 8 >= lim_b) sc[pp][3] = wv[pp][3] = -INFINITY;
+        // ---- mask: key key0 + g (+8) is visible to column c iff it lies below lim0 + token(c), and in the stage at all
+        if (min(d.lim0, d.rows) < key0 + kPage) {
+            const int lim_a = min(d.lim0 + (2 * t4) / G, d.rows) - key0, lim_b = min(d.lim0 + (2 * t4 + 1) / G, d.rows) - key0;
+            if (g >= lim_a) x[pp][0] = -INFINITY;
+            if (g >= lim_b) x[pp][1] = -INFINITY;
+            if (g + 8 >= lim_a) x[pp][2] = -INFINITY;
+            if (g + 8 >= lim_b) x[pp][3] = -INFINITY;
         }
     }
-    // ---- softmax against the lazily moved reference maxima of this thread's two columns, and of their weights of V
-    float c0 = fmaxf(sc[0][0], sc[0][2]), c1 = fmaxf(sc[0][1], sc[0][3]);
-    float x0 = fmaxf(wv[0][0], wv[0][2]), x1 = fmaxf(wv[0][1], wv[0][3]);
+    // ---- softmax against the lazily moved reference maxima of this thread's two columns
+    float c0 = fmaxf(x[0][0], x[0][2]), c1 = fmaxf(x[0][1], x[0][3]);
 #pragma unroll
     for (int pp = 1; pp < WP; ++pp) {
-        c0 = fmaxf(c0, fmaxf(sc[pp][0], sc[pp][2]));
-        c1 = fmaxf(c1, fmaxf(sc[pp][1], sc[pp][3]));
-        x0 = fmaxf(x0, fmaxf(wv[pp][0], wv[pp][2]));
-        x1 = fmaxf(x1, fmaxf(wv[pp][1], wv[pp][3]));
+        c0 = fmaxf(c0, fmaxf(x[pp][0], x[pp][2]));
+        c1 = fmaxf(c1, fmaxf(x[pp][1], x[pp][3]));
     }
-    if (__any_sync(0xffffffffu, c0 > m0 + kRescaleThreshold || c1 > m1 + kRescaleThreshold || x0 > w0 + kRescaleThreshold || x1 > w1 + kRescaleThreshold)) {
+    if (__any_sync(0xffffffffu, c0 > m0 + kRescaleThreshold || c1 > m1 + kRescaleThreshold)) {
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
             c0 = fmaxf(c0, __shfl_xor_sync(0xffffffffu, c0, off));
             c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, off));
-            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, off));
-            x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, off));
         }
-        auto moved = [](float& ref, float c) {      // the factor on what has been summed against the old reference
-            const float n = fmaxf(ref, c), f = n == -INFINITY ? 1.f : fast_exp2(ref - n);
-            ref = n;
-            return f;
-        };
-        l0 *= moved(m0, c0);
-        l1 *= moved(m1, c1);
-        const float f0 = moved(w0, x0), f1 = moved(w1, x1);
+        const float n0 = fmaxf(m0, c0), n1 = fmaxf(m1, c1);
+        const float f0 = n0 == -INFINITY ? 1.f : fast_exp2(m0 - n0);
+        const float f1 = n1 == -INFINITY ? 1.f : fast_exp2(m1 - n1);
+        m0 = n0; m1 = n1;
+        l0 *= f0; l1 *= f1;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1;
         }
     }
     const float u0 = m0 == -INFINITY ? 0.f : m0, u1 = m1 == -INFINITY ? 0.f : m1;
-    const float y0 = w0 == -INFINITY ? 0.f : w0, y1 = w1 == -INFINITY ? 0.f : w1;
+    far = __any_sync(0xffffffffu, far);
     uint32_t b0[WP], b1[WP];
 #pragma unroll
     for (int pp = 0; pp < WP; ++pp) {
-        l0 += fast_exp2(sc[pp][0] - u0) + fast_exp2(sc[pp][2] - u0);
-        l1 += fast_exp2(sc[pp][1] - u1) + fast_exp2(sc[pp][3] - u1);
+        const float p0 = fast_exp2(x[pp][0] - u0), p1 = fast_exp2(x[pp][1] - u1);
+        const float p2 = fast_exp2(x[pp][2] - u0), p3 = fast_exp2(x[pp][3] - u1);
+        if (!far) {
+            l0 = fmaf(p2, iv[pp][1], fmaf(p0, iv[pp][0], l0));
+            l1 = fmaf(p3, iv[pp][1], fmaf(p1, iv[pp][0], l1));
+        } else {
+            l0 += fast_exp2(x[pp][0] - u0 - ev[pp][0]) + fast_exp2(x[pp][2] - u0 - ev[pp][1]);
+            l1 += fast_exp2(x[pp][1] - u1 - ev[pp][0]) + fast_exp2(x[pp][3] - u1 - ev[pp][1]);
+        }
         // P' (keys x columns, f16) -> its transpose as the B operand: two 8x8 transposes in registers
-        b0[pp] = movmatrix_t(pack_f16x2(fast_exp2(wv[pp][0] - y0), fast_exp2(wv[pp][1] - y1)));
-        b1[pp] = movmatrix_t(pack_f16x2(fast_exp2(wv[pp][2] - y0), fast_exp2(wv[pp][3] - y1)));
+        b0[pp] = movmatrix_t(pack_f16x2(p0, p1));
+        b1[pp] = movmatrix_t(pack_f16x2(p2, p3));
     }
     // ---- O^T += V^T P'^T
 #pragma unroll
     for (int pp = 0; pp < WP; ++pp) {
-        if (!on[pp]) continue;
 #pragma unroll
         for (int pc = 0; pc < PIECES; pc += 2) {
             uint32_t r[4];
-            ldsm_x4_t(page_smem(pp) + (uint32_t)Geo::BLOCK_BYTES + row + (((uint32_t)(pc + half) ^ swz) << 4), r);
+            ldsm_x4_t(page0 + (uint32_t)(pp * Geo::PAGE_BYTES + Geo::BLOCK_BYTES) + row + (((uint32_t)(pc + half) ^ swz) << 4), r);
 #pragma unroll
             for (int k = 0; k < 4; ++k) r[k] = __byte_perm(r[k], 0, 0x3120);      // bytes (key, value): 00 01 10 11 -> 00 10, 01 11
             const uint32_t a0[4] = {kv8_decode2(r[0]), kv8_decode2_hi(r[0]), kv8_decode2(r[1]), kv8_decode2_hi(r[1])};
@@ -585,12 +587,14 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
 // The whole kernel body: warps 0-7 consume, warp 8 produces, warps 9 and 10 are the epilogue and the
 // merge warp, any further warps of the CTA return at once (the fused kernel has twelve).  With PREFETCH the first pages of a
 // CTA's first item are brought into L2 out of `pool` ahead (see the consumer warps).
-template <int D, int GT, bool APPEND, bool PREFETCH, bool KV8 = false>
+// ROLE: as in the span body.
+template <int D, int GT, bool APPEND, bool PREFETCH, bool KV8 = false, int ROLE = -1>
 __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap* kv_map, const __nv_bfloat16* pool,
                                             const __nv_bfloat16* __restrict__ q,
                                             __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
-                                            int S, uint8_t* smem, const AppendSrc& app, const uint8_t* scales = nullptr) {
+                                            int stages, uint8_t* smem, const AppendSrc& app, const uint8_t* scales = nullptr) {
     using Geo = Geometry<D, KV8>;
+    const int S = KV8 ? Geo::KV8_STAGES : stages;      // (a constant spares every role the division)
     constexpr int G = GT;
     static_assert(!(APPEND && KV8), "the append inside the attention is the bf16 cache's");
     static_assert(G <= kCols && kCols % G == 0, "heads per kv head must divide the column count");
@@ -626,8 +630,8 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
 
     const int Hq = p.num_q_heads;
 
-    if (warp > kFetchWarp) return;      // further warps of the CTA have nothing to do
-    if (warp == kProducerWarp) {
+    if (ROLE != 0 && warp > kFetchWarp) return;      // further warps of the CTA have nothing to do
+    if (ROLE != 0 && warp == kProducerWarp) {
         // ------------------------------------------------------------------ producer warp
         // Its own first item (if the planner gave it one) comes inline in the CTA's header with its
         // first 32 page ids, so that the first copies leave after one round trip to memory; every
@@ -738,7 +742,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                             tma_page_kv8(smem_u32(stage_base + (size_t)s * Geo::STAGE_BYTES + (size_t)Geo::page_slot(lane) * Geo::PAGE_BYTES),
                                          kv_map, cur.kv_head, page, full0 + 8 * s);
                         if (lane >> 1 < npages)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                            asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;"
                                          ::"r"(smem_u32(scale_base + (size_t)s * Geo::SCALE_BYTES + lane * 16)),
                                            "l"(scales + kv8_scale_offset(scale_page, lane & 1, cur.kv_head, 0, p.num_kv_heads)) : "memory");
                         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full0 + 8 * s) : "memory");
@@ -784,7 +788,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         return;
     }
 
-    if (warp == kEpilogueWarp) {
+    if (ROLE != 0 && warp == kEpilogueWarp) {
         epilogue_loop<D, G, KV8>(p, out, lse, stage_base, handoff, merge_req, empty0, done0, req0, reqfree0, abort_flag);
         return;
     }
@@ -794,12 +798,12 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
         return p.queue_count == 0 && head[3] - head[2] <= 1;
     };
-    if (warp == kMergeWarp) {
+    if (ROLE != 0 && warp == kMergeWarp) {
         if (two_mergers()) merge_loop<D, G, 2>(p, out, lse, merge_req, req0, reqfree0, abort_flag, 0);
         else merge_loop<D, G, 1>(p, out, lse, merge_req, req0, reqfree0, abort_flag, 0);
         return;
     }
-    if (warp == kFetchWarp) {
+    if (ROLE != 0 && warp == kFetchWarp) {
         // ------------------------------------------------------------------ fetch warp
         // Runs one item ahead of the producer: the CTA's own items (beyond the first, which the producer
         // reads from the header itself), then the queue, one atomic add per chunk.  A chunk is claimed
@@ -859,6 +863,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         return;
     }
 
+    if constexpr (ROLE == 1) return;
     // ---------------------------------------------------------------------- consumer warps
     // Pages ahead of the ring, only where they pay: in the kernel of steps without span tiles, and for items that are not all latency.
     // (us a layer from a graph, without | with: 4 decoding sequences over 0.5-4 K keys 13.6 | 12.6, 64 over 1-3 K 87.3 | 85.7; with
@@ -884,8 +889,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     uint32_t qb[Geo::KSTEPS][2];      // B fragments of Q^T: column g, values 16 ks + 2 t4 (+1) and + 8
     float o[Geo::KSTEPS][4];          // O^T: rows d = 16 i + g (+8), columns 2 t4, 2 t4 + 1
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;      // of columns 2 t4 and 2 t4 + 1
-    // 8 bits: the columns' query scales, and the reference maxima of score + log2(scale of the V row), see below
-    float qs0 = 0.f, qs1 = 0.f, w0 = -INFINITY, w1 = -INFINITY;
+    float qs0 = 0.f, qs1 = 0.f;      // 8 bits: the columns' query scales
     int item_count = 0;
 
     for (int n = 0;; ++n) {
@@ -928,7 +932,6 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                 }
                 qs0 = __shfl_sync(0xffffffffu, up, 8 * t4);          // of columns 2 t4 and 2 t4 + 1
                 qs1 = __shfl_sync(0xffffffffu, up, 8 * t4 + 4);
-                w0 = w1 = -INFINITY;
             } else {
 #pragma unroll
                 for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
@@ -950,7 +953,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         constexpr int WP = Geo::WARP_PAGES;
         if constexpr (KV8) {
             if (warp * kPage < d.rows)
-                pages_kv8<D, G>(d, stage, scale_base + (size_t)s * Geo::SCALE_BYTES, warp, lane, qb, o, qs0, qs1, m0, m1, l0, l1, w0, w1);
+                pages_kv8<D, G>(d, stage, scale_base + (size_t)s * Geo::SCALE_BYTES, warp, lane, qb, o, qs0, qs1, m0, m1, l0, l1);
         } else if (warp * kPage < d.rows) {
             bool on[WP];
             float sc[WP][4];
@@ -1068,13 +1071,12 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             }
             __syncwarp();      // every lane is done reading the page before it is overwritten
             if constexpr (KV8) {
-                // to the columns' own reference maxima, in fp32; and rows g, g + 8 of a fragment are values 2 g, 2 g + 1
-                const float f0 = m0 == -INFINITY ? 0.f : fast_exp2(w0 - m0), f1 = m1 == -INFINITY ? 0.f : fast_exp2(w1 - m1);
+                // rows g and g + 8 of a fragment are values 2 g and 2 g + 1
 #pragma unroll
                 for (int i = 0; i < Geo::KSTEPS; ++i) {
                     float* c = st + (size_t)(2 * t4) * Geo::O_STRIDE + 16 * i + 2 * g;
-                    *reinterpret_cast<float2*>(c) = make_float2(o[i][0] * f0, o[i][2] * f0);
-                    *reinterpret_cast<float2*>(c + Geo::O_STRIDE) = make_float2(o[i][1] * f1, o[i][3] * f1);
+                    *reinterpret_cast<float2*>(c) = make_float2(o[i][0], o[i][2]);
+                    *reinterpret_cast<float2*>(c + Geo::O_STRIDE) = make_float2(o[i][1], o[i][3]);
                 }
             } else {
 #pragma unroll

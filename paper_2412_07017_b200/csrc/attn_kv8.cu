@@ -21,9 +21,16 @@ attn_decode_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, co
     dec::decode_body<D, G, false, true, true>(p, &kv_map, reinterpret_cast<const __nv_bfloat16*>(pool), q, out, lse, S, aligned_smem(smem_raw), AppendSrc{}, scales);
 }
 
+template <int D, int G, int ROLE>
+__device__ __forceinline__ void span_kv8(const DevPlan& p, const CUtensorMap* k_map, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q,
+                                         __nv_bfloat16* __restrict__ out, float* __restrict__ lse, uint8_t* smem) {
+    tc::split_registers<ROLE>();
+    tc::tc_body<D, G, true, true, ROLE>(p, k_map, q, nullptr, out, lse, smem, pool, scales);
+}
+
 template <int D, int G>
-__global__ void __launch_bounds__(tc::kThreads, 1)
-attn_append_tc_kv8_kernel(DevPlan p, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
+__global__ void __launch_bounds__(tc::kThreadsKv8, 1)
+attn_append_tc_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap k_map, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
                           float* __restrict__ lse) {
     extern __shared__ uint8_t smem_raw[];
     pdl_trigger();
@@ -31,33 +38,40 @@ attn_append_tc_kv8_kernel(DevPlan p, const uint8_t* pool, const uint8_t* scales,
         trace_mark(0);
         for (int s = 8; s < 16; ++s) trace_set(s, 0);
     }
-    tc::tc_body<D, G, true, true>(p, nullptr, q, nullptr, out, lse, aligned_smem(smem_raw), pool, scales);
+    if (threadIdx.x < 256) span_kv8<D, G, 0>(p, &k_map, pool, scales, q, out, lse, aligned_smem(smem_raw));
+    else span_kv8<D, G, 1>(p, &k_map, pool, scales, q, out, lse, aligned_smem(smem_raw));
     if (threadIdx.x == 0) trace_mark(1);
 }
 
+template <int D, int G, int ROLE>
+__device__ __forceinline__ void fused_kv8(const DevPlan& p, const CUtensorMap* kv_map, const CUtensorMap* k_map, const uint8_t* pool, const uint8_t* scales,
+                                          const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, int S, uint8_t* smem) {
+    tc::split_registers<ROLE>();
+    const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
+    if (head[0] != head[1]) {
+        if (threadIdx.x == 0) {
+            for (int s = 8; s < 16; ++s) trace_set(s, 0);
+        }
+        tc::tc_body<D, G, false, true, ROLE>(p, k_map, q, nullptr, out, lse, smem, pool, scales);
+        if (threadIdx.x == 0) trace_mark(1);
+        if (head[2] == head[3] && p.queue_count == 0) return;      // nothing left for the warp body
+        __syncthreads();      // tensor memory released, shared memory free for the second phase
+    }
+    dec::decode_body<D, G, false, false, true, ROLE>(p, kv_map, nullptr, q, out, lse, S, smem, AppendSrc{}, scales);
+}
+
 template <int D, int G>
-__global__ void __launch_bounds__(tc::kThreads, 1)
-attn_fused_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q,
+__global__ void __launch_bounds__(tc::kThreadsKv8, 1)
+attn_fused_kv8_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, const __grid_constant__ CUtensorMap k_map, const uint8_t* pool, const uint8_t* scales, const __nv_bfloat16* __restrict__ q,
                       __nv_bfloat16* __restrict__ out, float* __restrict__ lse, int S) {
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = aligned_smem(smem_raw);
     pdl_trigger();
     if (threadIdx.x == 0) { trace_mark(0); trace_set(1, 0); trace_set(5, 0); trace_set(6, 0); trace_set(7, 0); }
     const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
     if (threadIdx.x < 3) asm volatile("prefetch.global.L2 [%0];" ::"l"(head + 32 * threadIdx.x));      // (as in attn_fused_kernel)
     if (threadIdx.x == 32) asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map));
-    if (head[0] == head[1]) {
-        dec::decode_body<D, G, false, false, true>(p, &kv_map, nullptr, q, out, lse, S, smem, AppendSrc{}, scales);
-        return;
-    }
-    if (threadIdx.x == 0) {
-        for (int s = 8; s < 16; ++s) trace_set(s, 0);
-    }
-    tc::tc_body<D, G, false, true>(p, nullptr, q, nullptr, out, lse, smem, pool, scales);
-    if (threadIdx.x == 0) trace_mark(1);
-    if (head[2] == head[3] && p.queue_count == 0) return;      // nothing left for the warp body
-    __syncthreads();      // tensor memory released, shared memory free for the second phase
-    dec::decode_body<D, G, false, false, true>(p, &kv_map, nullptr, q, out, lse, S, smem, AppendSrc{}, scales);
+    if (threadIdx.x < 256) fused_kv8<D, G, 0>(p, &kv_map, &k_map, pool, scales, q, out, lse, S, aligned_smem(smem_raw));
+    else fused_kv8<D, G, 1>(p, &kv_map, &k_map, pool, scales, q, out, lse, S, aligned_smem(smem_raw));
 }
 
 template <int D, int G>
@@ -67,21 +81,24 @@ cudaError_t launch_kv8_impl(const DevPlan& p, const void* q, const void* pool, c
     if (p.num_pages > kMaxMapPages) return cudaErrorInvalidValue;
     constexpr int S = decode_stages<D, true>();
     constexpr size_t smem_warp = dec::smem_bytes<D, true>(S), smem_span = tc::Geometry<D, true>::SMEM_BYTES, smem_both = std::max(smem_warp, smem_span);
+    static_assert(S == dec::Geometry<D, true>::KV8_STAGES, "as many stages as fit");
     static_assert(smem_warp - 1024 <= tc::Geometry<D, true>::OFF_BAR, "the span body's barriers stay clear of the warp body");
     const auto *pool8 = (const uint8_t*)pool, *scales8 = (const uint8_t*)scales;
     const auto* q16 = (const __nv_bfloat16*)q;
     auto* out16 = (__nv_bfloat16*)out;
-    CUtensorMap map;
+    CUtensorMap map, k_map;
     if (has_cuda)
         if (cudaError_t e = pool_map(kKv8Map, p, pool, &map)) return e;
+    if (has_tensor)
+        if (cudaError_t e = pool_map(kK8Map, p, pool, &k_map)) return e;
     if (has_tensor && has_cuda && p.num_ctas_tensor == p.num_ctas_cuda) {
         if (cudaError_t e = allow_smem<attn_fused_kv8_kernel<D, G>>(smem_both)) return e;
-        return launch_when(!p.full_launch, attn_fused_kv8_kernel<D, G>, dim3(p.num_ctas_cuda), dim3(tc::kThreads), smem_both, stream, p, map, pool8, scales8,
+        return launch_when(!p.full_launch, attn_fused_kv8_kernel<D, G>, dim3(p.num_ctas_cuda), dim3(tc::kThreadsKv8), smem_both, stream, p, map, k_map, pool8, scales8,
                            q16, out16, lse, S);
     }
     if (has_tensor) {
         if (cudaError_t e = allow_smem<attn_append_tc_kv8_kernel<D, G>>(smem_span)) return e;
-        if (cudaError_t e = launch_when(!p.full_launch, attn_append_tc_kv8_kernel<D, G>, dim3(p.num_ctas_tensor), dim3(tc::kThreads), smem_span, stream, p,
+        if (cudaError_t e = launch_when(!p.full_launch, attn_append_tc_kv8_kernel<D, G>, dim3(p.num_ctas_tensor), dim3(tc::kThreadsKv8), smem_span, stream, p, k_map,
                                         pool8, scales8, q16, out16, lse))
             return e;
     }

@@ -29,7 +29,8 @@ typedef CUresult (*ReplaceAddressFn)(CUtensorMap*, void*);
 //         (dec::tma_page_kv)
 //   span  (64 values, 8 slots, d / 64 row halves, 2 groups of 8 slots, pages x K|V x Hkv), a box is one block (tc::tma_page)
 //   kv8   the 8-bit cache: (d bytes, 16 slots, Hkv, pages x K|V), a box as kv's; at head_dim 64 with the 64-byte swizzle (dec::tma_page_kv8)
-enum PoolMap { kKvMap, kSpanMap, kKv8Map };
+//   k8    the same, a box is one block (tc::kv8_k_producer)
+enum PoolMap { kKvMap, kSpanMap, kKv8Map, kK8Map };
 
 constexpr int64_t kMaxMapPages = 0x3fffffff;
 
@@ -50,9 +51,9 @@ cudaError_t make_pool_map(PoolMap kind, const DevPlan& p, const void* pool, CUte
     const cuuint64_t strides_span[4] = {d * 2, 128, 8 * d * 2, kPage * d * 2};
     const cuuint32_t box_kv[5] = {64, kPage, (cuuint32_t)(d / 64), 1, 2}, box_span[5] = {64, 8, (cuuint32_t)(d / 64), 2, 1};
     const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    if (kind == kKv8Map) {
+    if (kind == kKv8Map || kind == kK8Map) {
         const cuuint64_t dims[4] = {d, kPage, hkv, blocks}, strides[3] = {d, kPage * d, hkv * kPage * d};
-        const cuuint32_t box[4] = {(cuuint32_t)d, kPage, 1, 2};
+        const cuuint32_t box[4] = {(cuuint32_t)d, kPage, 1, kind == kKv8Map ? 2u : 1u};
         const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                   d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -86,8 +87,8 @@ cudaError_t allow_smem(size_t bytes) {
 cudaError_t pool_map(PoolMap kind, const DevPlan& p, const void* pool, CUtensorMap* map) {
     struct Entry { int64_t pages; int hkv, d; CUtensorMap map; };
     constexpr int kEntries = 8;
-    thread_local Entry cache[3][kEntries] = {};
-    thread_local int next[3] = {};
+    thread_local Entry cache[4][kEntries] = {};
+    thread_local int next[4] = {};
     static std::atomic<ReplaceAddressFn> replace_fn{nullptr};
     ReplaceAddressFn replace = replace_fn.load(std::memory_order_acquire);
     if (replace == nullptr) {

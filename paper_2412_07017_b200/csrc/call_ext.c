@@ -16,8 +16,15 @@ static int (*fn_append)(const asynclm_plan_t*, const void*, const void*, void*, 
 static int (*fn_append_rope)(const asynclm_plan_t*, const void*, const void*, void*, void*, double, void*);
 static int (*fn_attn)(const asynclm_plan_t*, const void*, const void*, void*, float*, void*);
 static int (*fn_step)(const asynclm_plan_t*, const void*, const void*, const void*, void*, void*, float*, void*);
+static int (*fn_kv8_append)(const asynclm_plan_t*, const asynclm_kv8_rows*, void*, void*, const asynclm_rope_table*, void*);
+static int (*fn_kv8_attn)(const asynclm_plan_t*, const void*, const void*, const void*, void*, float*, void*);
+static int (*fn_kv8_gather)(const asynclm_plan_t*, const int64_t*, const int32_t*, int64_t, const void*, const void*, void*, void*, void*);
+static int (*fn_rope)(const asynclm_rope_table*, const int32_t*, int32_t, int32_t, const asynclm_rope_rows*, int32_t, void*);
 static PyObject *current_device, *raw_stream;      /* callables: () -> device, (device) -> stream handle */
 static PyObject *s_data_ptr, *s_numel, *s_cuda_stream, *s_num_q_heads, *s_num_kv_heads, *s_head_dim, *s_page_size;
+/* what a tensor is asked for, and the dtypes of rows, of a quantised cache's tensors and of indices */
+static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous;
+static PyObject *t_bf16, *t_e4m3, *t_e8m0, *t_u8, *t_i32, *t_i64;
 
 /* (these return -1 with an exception set on failure) */
 static int address(PyObject* tensor, void** out) {
@@ -185,12 +192,184 @@ static PyObject* py_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+static PyObject* py_bind_kv8(PyObject* self, PyObject* args) {
+    Py_ssize_t append, attn, gather, rope;
+    PyObject *bf16, *e4m3, *e8m0, *u8, *i32, *i64;
+    if (!PyArg_ParseTuple(args, "nnnnOOOOOO", &append, &attn, &gather, &rope, &bf16, &e4m3, &e8m0, &u8, &i32, &i64)) return NULL;
+    fn_kv8_append = (void*)append;
+    fn_kv8_attn = (void*)attn;
+    fn_kv8_gather = (void*)gather;
+    fn_rope = (void*)rope;
+    Py_XSETREF(t_bf16, Py_NewRef(bf16));
+    Py_XSETREF(t_e4m3, Py_NewRef(e4m3));
+    Py_XSETREF(t_e8m0, Py_NewRef(e8m0));
+    Py_XSETREF(t_u8, Py_NewRef(u8));
+    Py_XSETREF(t_i32, Py_NewRef(i32));
+    Py_XSETREF(t_i64, Py_NewRef(i64));
+    Py_RETURN_NONE;
+}
+
+/* 1 if the tensor is on a GPU and of one of the two dtypes, 0 if not, -1 with an exception set on failure */
+static int is_cuda_of(PyObject* t, PyObject* type, PyObject* or_type) {
+    PyObject* v = PyObject_GetAttr(t, s_is_cuda);
+    if (!v) return -1;
+    const int on = v == Py_True;
+    Py_DECREF(v);
+    if (!on) return 0;
+    v = PyObject_GetAttr(t, s_dtype);
+    if (!v) return -1;
+    const int right = v == type || v == or_type;
+    Py_DECREF(v);
+    return right;
+}
+
+static int flat(PyObject* t, PyObject* type, PyObject* or_type, void** out) {
+    const int right = is_cuda_of(t, type, or_type);
+    if (right <= 0) return right;
+    PyObject* v = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+    if (!v) return -1;
+    const int whole = v == Py_True;
+    Py_DECREF(v);
+    if (!whole) return 0;
+    return address(t, out) ? -1 : 1;
+}
+
+/* Rows [n][heads][d] of bf16 whose heads lie next to each other: address, shape and row stride.  1, 0 or -1 as above. */
+typedef struct rows_view {
+    void* ptr;
+    Py_ssize_t n, heads, d, stride;
+} rows_view;
+static int rows_of(PyObject* t, rows_view* r) {
+    const int right = is_cuda_of(t, t_bf16, NULL);
+    if (right <= 0) return right;
+    Py_ssize_t dim[3], step[3];
+    for (int which = 0; which < 2; ++which) {
+        PyObject* v = which ? PyObject_CallMethodNoArgs(t, s_stride) : PyObject_GetAttr(t, s_shape);
+        if (!v) return -1;
+        if (!PyTuple_Check(v) || PyTuple_GET_SIZE(v) != 3) {
+            Py_DECREF(v);
+            return 0;
+        }
+        for (int k = 0; k < 3; ++k) (which ? step : dim)[k] = PyLong_AsSsize_t(PyTuple_GET_ITEM(v, k));
+        Py_DECREF(v);
+        if (PyErr_Occurred()) return -1;
+    }
+    if (dim[0] > 0 && ((dim[2] > 1 && step[2] != 1) || (dim[1] > 1 && step[1] != dim[2]))) return 0;
+    r->n = dim[0];
+    r->heads = dim[1];
+    r->d = dim[2];
+    r->stride = dim[0] > 1 ? step[0] : 0;
+    return address(t, &r->ptr) ? -1 : 1;
+}
+static int dense(const rows_view* r) { return r->n <= 1 || r->stride == r->heads * r->d; }
+
+/* The calls of the quantised cache and of rotary rows: status, or None where an argument is not of the kind that needs no conversion
+ * or is wrong in a way that the C call cannot see (binding.py says how). `rope`: the address of a table, or 0. */
+#define TAKE(x) do { const int got_ = (x); if (got_ < 0) return NULL; if (got_ == 0) Py_RETURN_NONE; } while (0)
+
+/* kv8_append(handle, k_new, v_new, kv8_pool, kv8_scales, rope, q, q_out, stream) */
+static PyObject* py_kv8_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected");
+    rows_view k, v, q = {0}, qo = {0};
+    void *plan, *pool, *scales, *rope, *stream;
+    if (handle_of(a[0], &plan) || handle_of(a[5], &rope)) return NULL;
+    TAKE(rows_of(a[1], &k));
+    TAKE(rows_of(a[2], &v));
+    TAKE(flat(a[3], t_e4m3, t_u8, &pool));
+    TAKE(flat(a[4], t_e8m0, t_u8, &scales));
+    if (a[6] != Py_None) {
+        if (a[7] == Py_None) Py_RETURN_NONE;
+        TAKE(rows_of(a[6], &q));
+        TAKE(rows_of(a[7], &qo));
+        if (q.n != qo.n || q.heads != qo.heads || q.d != qo.d || !dense(&qo)) Py_RETURN_NONE;
+    }
+    if (stream_of(a[8], &stream)) return NULL;
+    const asynclm_kv8_rows rows = {k.ptr, v.ptr, q.ptr, qo.ptr, k.stride, v.stride, q.stride};
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_kv8_append(plan, &rows, pool, scales, rope, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* kv8_attn(handle, q, kv8_pool, kv8_scales, out, lse, stream) */
+static PyObject* py_kv8_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected");
+    void *plan, *q, *pool, *scales, *out, *lse, *stream;
+    if (handle_of(a[0], &plan) || address(a[1], &q)) return NULL;
+    TAKE(flat(a[2], t_e4m3, t_u8, &pool));
+    TAKE(flat(a[3], t_e8m0, t_u8, &scales));
+    if (address(a[4], &out) || address_or_null(a[5], &lse) || stream_of(a[6], &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_kv8_attn(plan, q, pool, scales, out, lse, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* kv8_gather(handle, out_indptr, first, kv8_pool, kv8_scales, k_out, v_out, stream) */
+static PyObject* py_kv8_gather(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "8 arguments expected");
+    rows_view k, v;
+    void *plan, *indptr, *first, *pool, *scales, *stream;
+    if (handle_of(a[0], &plan)) return NULL;
+    TAKE(flat(a[1], t_i64, NULL, &indptr));
+    TAKE(flat(a[2], t_i32, NULL, &first));
+    TAKE(flat(a[3], t_e4m3, t_u8, &pool));
+    TAKE(flat(a[4], t_e8m0, t_u8, &scales));
+    TAKE(rows_of(a[5], &k));
+    TAKE(rows_of(a[6], &v));
+    if (k.n != v.n || k.heads != v.heads || k.d != v.d || !dense(&k) || !dense(&v)) Py_RETURN_NONE;
+    if (stream_of(a[7], &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_kv8_gather(plan, indptr, first, k.n, pool, scales, k.ptr, v.ptr, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* rope(table, positions, q, q_out, k, k_out, stream) */
+static PyObject* py_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected");
+    rows_view in[2], out[2];
+    void *table, *positions, *stream;
+    if (handle_of(a[0], &table)) return NULL;
+    if ((a[4] == Py_None) != (a[5] == Py_None)) Py_RETURN_NONE;
+    const int sets = a[4] == Py_None ? 1 : 2;
+    asynclm_rope_rows rows[2];
+    for (int k = 0; k < sets; ++k) {
+        TAKE(rows_of(a[2 + 2 * k], &in[k]));
+        TAKE(rows_of(a[3 + 2 * k], &out[k]));
+        if (in[k].n != out[k].n || in[k].heads != out[k].heads || in[k].d != out[k].d || in[k].n != in[0].n || in[k].d != in[0].d) Py_RETURN_NONE;
+        if (in[k].n > INT32_MAX || in[k].heads > INT32_MAX || in[k].d > INT32_MAX) Py_RETURN_NONE;
+        rows[k] = (asynclm_rope_rows){in[k].ptr, out[k].ptr, in[k].stride, out[k].stride, (int32_t)in[k].heads, 0};
+    }
+    TAKE(flat(a[1], t_i32, NULL, &positions));
+    PyObject* count = PyObject_CallMethodNoArgs(a[1], s_numel);
+    if (!count) return NULL;
+    const Py_ssize_t tokens = PyLong_AsSsize_t(count);
+    Py_DECREF(count);
+    if (PyErr_Occurred()) return NULL;
+    if (tokens != in[0].n) Py_RETURN_NONE;
+    if (stream_of(a[6], &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_rope(table, positions, (int32_t)tokens, (int32_t)in[0].d, rows, sets, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, "bind(plan, append, append_rope, attn, step, current_device, raw_stream)"},
                                 {"plan", (PyCFunction)(void*)py_plan, METH_FASTCALL, NULL},
                                 {"append", (PyCFunction)(void*)py_append, METH_FASTCALL, NULL},
                                 {"append_rope", (PyCFunction)(void*)py_append_rope, METH_FASTCALL, NULL},
                                 {"attn", (PyCFunction)(void*)py_attn, METH_FASTCALL, NULL},
                                 {"step", (PyCFunction)(void*)py_step, METH_FASTCALL, NULL},
+                                {"bind_kv8", py_bind_kv8, METH_VARARGS, "bind_kv8(append, attn, gather, rope, bf16, e4m3, e8m0, uint8, int32, int64)"},
+                                {"kv8_append", (PyCFunction)(void*)py_kv8_append, METH_FASTCALL, NULL},
+                                {"kv8_attn", (PyCFunction)(void*)py_kv8_attn, METH_FASTCALL, NULL},
+                                {"kv8_gather", (PyCFunction)(void*)py_kv8_gather, METH_FASTCALL, NULL},
+                                {"rope", (PyCFunction)(void*)py_rope, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "call_ext", NULL, -1, methods};
 
@@ -202,6 +381,12 @@ PyMODINIT_FUNC PyInit_call_ext(void) {
     s_num_kv_heads = PyUnicode_InternFromString("num_kv_heads");
     s_head_dim = PyUnicode_InternFromString("head_dim");
     s_page_size = PyUnicode_InternFromString("page_size");
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_cuda = PyUnicode_InternFromString("is_cuda");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (!s_shape || !s_stride || !s_dtype || !s_is_cuda || !s_is_contiguous) return NULL;
     if (!s_data_ptr || !s_numel || !s_cuda_stream || !s_num_q_heads || !s_num_kv_heads || !s_head_dim || !s_page_size) return NULL;
     return PyModule_Create(&module);
 }

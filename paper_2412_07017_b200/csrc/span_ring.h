@@ -31,8 +31,8 @@ namespace tc {
 
 // Slots of one ring: 80 KiB of 64-key tiles.
 ASYNCLM_HD constexpr int ring_slots(int head_dim) { return 640 / head_dim; }
-// The same for the 8-bit cache, whose tiles' scales need room beside the rings: at head_dim 128 one slot less (its producers hold another tile in registers).
-ASYNCLM_HD constexpr int ring_slots_kv8(int head_dim) { return head_dim == 128 ? 4 : ring_slots(head_dim); }
+// The same for the 8-bit cache, whose K tiles are the codes themselves (8 KB, 4 KB at head_dim 64) and whose V tiles are f16, with room for the tiles' scales.
+ASYNCLM_HD constexpr int ring_slots_kv8(int which, int head_dim) { return head_dim == 128 ? 6 : which ? 11 : 10; }
 // Slots for those scales, which every warp of a softmax group reads until it hands its weights over.  When the producer fills tile t, every warp of its
 // group has released tile t - slots, at the start of its softmax, so it is through with the group's tile before that, t - slots - 1 (both groups on every
 // tile) or t - slots - 2 (alternate tiles), and the other group's warps, which have released t - slots - 1, are through with t - slots - 3.  So
