@@ -821,7 +821,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 // The tiles were written by TMA copies, but for the rows of an unfinished last V page: those came by cp.async,
                 // through the generic proxy, and the MMAs read through the asynchronous one.  The full barrier orders
                 // the two, the fence makes the bytes visible across.
-                if (!KV8 && pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
+                if (pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
                 const uint32_t buf = tmem + kColS + 128u * (uint32_t)b + 64u * (uint32_t)(c & 1);      // S and P
                 const uint64_t vd = smem_desc(tile_addr(1, vp), Geo::ATOM_BYTES, Geo::GROUP_BYTES);
                 const uint64_t kd = !KV8 ? smem_desc(tile_addr(0, kp), 16, Geo::GROUP_BYTES) : D == 64 ? smem_desc64(tile_addr(0, kp)) : smem_desc(tile_addr(0, kp), 16, 1024);

@@ -17,7 +17,8 @@ namespace {
 
 struct AppendSets { RowSet set[3]; };      // K, V, Q
 
-__global__ void __launch_bounds__(kRopeRowThreads)
+template <int FORM>
+__global__ void __launch_bounds__(kRopeRowThreads, rope_ctas(FORM))
 kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __grid_constant__ AppendSets sets, uint8_t* pool, uint8_t* scales, int tokens) {
     extern __shared__ uint4 smem[];
     float4 (*table)[kRopeEntries] = reinterpret_cast<float4 (*)[kRopeEntries]>(smem + kRopeRowThreads);
@@ -29,47 +30,64 @@ kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __gr
     const int r0 = blockIdx.x * tokens, n = min(tokens, p.total_q - r0);
     const int block = rows * kRopeUnroll;
     const int blocks_kv = (hkv + block - 1) / block, blocks = 2 * blocks_kv + (sets.set[2].heads + block - 1) / block;
-    // the angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the kernels in front
-    // until those have completed
-    rope_fill(turns, table, n, [&](int i) {
+    auto kind = [&](int b) { return b < blocks_kv ? 0 : b < 2 * blocks_kv ? 1 : 2; };      // K, V, Q
+    struct Block { uint4 x[kRopeUnroll]; };
+    auto load = [&](int item) {
+        Block l;
+        const int i = item / blocks, b = item % blocks, which = kind(b);
+        const RowSet& set = sets.set[which];
+        const int h0 = (b - which * blocks_kv) * block + sub;
+        const __nv_bfloat16* in = set.in + (int64_t)(r0 + i) * set.in_stride + 8 * v;
+#pragma unroll
+        for (int u = 0; u < kRopeUnroll; ++u)
+            l.x[u] = item < n * blocks && h0 + u * rows < set.heads ? ldg_nc_v4(in + (int64_t)(h0 + u * rows) * d) : make_uint4(0, 0, 0, 0);
+        return l;
+    };
+    // The angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the kernels in front until those
+    // have completed.  Where all CTAs start at once the angles overlap the tail of the kernel in front; in a longer grid the first rows are
+    // requested in front of them.
+    const bool rows_first = gridDim.x > 148 * 2;
+    Block next;
+    if (rows_first) {
+        pdl_wait();
+        next = load(warp);
+    }
+    rope_fill<FORM>(turns, table, n, [&](int i) {
         const int r = r0 + i, b = __ldg(p.row_seq + r);
         return __ldg(p.kv_len_before + b) + r - __ldg(p.q_indptr + b);
     });
-    pdl_wait();
+    if (!rows_first) {
+        pdl_wait();
+        next = load(warp);
+    }
     __syncthreads();
     for (int item = warp; item < n * blocks; item += warps) {
-        const int i = item / blocks, b = item % blocks;
-        const int which = b < blocks_kv ? 0 : b < 2 * blocks_kv ? 1 : 2;      // K, V, Q
+        const Block now = next;
+        next = load(item + warps);
+        const int i = item / blocks, b = item % blocks, which = kind(b);
         const RowSet& set = sets.set[which];
         const int h0 = (b - which * blocks_kv) * block + sub;
         const int64_t slot = which < 2 ? __ldg(p.row_slot + r0 + i) : 0;
-        const __nv_bfloat16* in = set.in + (int64_t)(r0 + i) * set.in_stride + 8 * v;
-        uint4 x[kRopeUnroll];
-        bool on[kRopeUnroll];
-#pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-            const int h = h0 + u * rows;
-            on[u] = h < set.heads;
-            x[u] = on[u] ? ldg_nc_v4(in + (int64_t)h * d) : make_uint4(0, 0, 0, 0);
-        }
-        RopeLane cs;
+        RopeLane<FORM> cs;
         const bool turned = set.turned != 0 && turns.rotary_dim > 0;
-        if (turned) cs = rope_lane(turns, table[i], v);
+        if (turned) cs = rope_lane<FORM>(turns, table[i], v);
         const bool page_fine = which == 2 || page_ok(slot / kPage, p.num_pages, p.status, kStatusBadPageAppend);
 #pragma unroll
         for (int u = 0; u < kRopeUnroll; ++u) {
             const int h = h0 + u * rows;
+            const bool on = h < set.heads;
+            const uint4 x = now.x[u];
             float y[8];
             if (turned) {
-                rope_turn(turns, cs, v, lane, smem + warp * 32, x[u], y);
+                rope_turn<FORM>(turns, cs, v, lane, smem + warp * 32, x, y);
             } else {
-                const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) { y[2 * k] = bf16_lo(w[k]); y[2 * k + 1] = bf16_hi(w[k]); }
             }
             if (which == 2) {
-                if (on[u]) {
-                    uint4 o = x[u];
+                if (on) {
+                    uint4 o = x;
                     if (8 * v < turns.rotary_dim) o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
                     *reinterpret_cast<uint4*>(set.out + (int64_t)(r0 + i) * set.out_stride + (int64_t)h * d + 8 * v) = o;
                 }
@@ -84,7 +102,7 @@ kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __gr
             uint2 codes = make_uint2(kv8_encode2(y[0] * inv, y[1] * inv) | kv8_encode2(y[2] * inv, y[3] * inv) << 16,
                                      kv8_encode2(y[4] * inv, y[5] * inv) | kv8_encode2(y[6] * inv, y[7] * inv) << 16);
             if (byte == kKv8NanByte) codes = make_uint2(0, 0);
-            if (on[u] && page_fine) {
+            if (on && page_fine) {
                 *reinterpret_cast<uint2*>(pool + kv8_row_offset(slot / kPage, which, h, (int)(slot % kPage), hkv, d) + 8 * v) = codes;
                 if (v == 0) scales[kv8_scale_offset(slot / kPage, which, h, (int)(slot % kPage), hkv)] = (uint8_t)byte;
             }
@@ -118,10 +136,16 @@ extern "C" int asynclm_kv8_append(const asynclm_plan_t* plan, const asynclm_kv8_
     sets.set[1] = RowSet{(const __nv_bfloat16*)rows->v, nullptr, vs, 0, d.num_kv_heads, 0};
     if (rows->q) sets.set[2] = RowSet{(const __nv_bfloat16*)rows->q, (__nv_bfloat16*)rows->q_out, qs, qd, d.num_q_heads, 1};
     PlanUse use(plan, (cudaStream_t)stream);
-    const int tokens = rope_row_tokens(d.total_q), block = 32 / (d.head_dim / 8) * kRopeUnroll;
+    const int tokens = rope_row_tokens(d.total_q, rope_form(turns)), block = 32 / (d.head_dim / 8) * kRopeUnroll;
     const int blocks = 2 * ((d.num_kv_heads + block - 1) / block) + (sets.set[2].heads + block - 1) / block;
     const int threads = 32 * std::min(kRopeRowThreads / 32, tokens * blocks);
-    return cuda_status(use.launched(launch_when(!use.dev.full_launch, kv8_append_kernel, dim3((d.total_q + tokens - 1) / tokens), dim3(threads),
-                                                rope_row_smem(tokens), (cudaStream_t)stream, use.dev, turns, sets, (uint8_t*)kv8_pool,
-                                                (uint8_t*)kv8_scales, tokens)));
+    const auto launch = [&](auto kernel) {
+        return cuda_status(use.launched(launch_when(!use.dev.full_launch, kernel, dim3((d.total_q + tokens - 1) / tokens), dim3(threads), rope_row_smem(tokens),
+                                                    (cudaStream_t)stream, use.dev, turns, sets, (uint8_t*)kv8_pool, (uint8_t*)kv8_scales, tokens)));
+    };
+    switch (rope_form(turns)) {
+        case kRopeHalves: return launch(kv8_append_kernel<kRopeHalves>);
+        case kRopePairs: return launch(kv8_append_kernel<kRopePairs>);
+        default: return launch(kv8_append_kernel<kRopeOddHalves>);
+    }
 }

@@ -1,9 +1,9 @@
 // The 8-bit cache read back: ranges of sequences as dense bf16 rows.
 //
 // Output row out_indptr[b] + i is position first[b] + i of sequence b, found through the plan's page table; its values are code * 2^e, exact in
-// bf16.  Bound by memory: d + 1 bytes read and 2 d written for each K or V row.  A thread turns 16 codes (16 bytes) into 32 bytes; head_dim / 16
-// lanes take a row, a warp 4 or 8 rows that follow each other, which in the pool are next to each other inside a page (and in the output Hkv rows
-// apart, whole 128-byte lines each).  The row's place is looked up once, by bisection over out_indptr, and serves all its heads.
+// bf16.  Bound by memory: d + 1 bytes read and 2 d written for each K or V row.  A thread turns 8 codes into 16 bytes; head_dim / 8
+// lanes take a row, a warp 2 or 4 rows that follow each other, which in the pool are next to each other inside a page (and in the output Hkv rows
+// apart, whole 128-byte lines each).  (With 16 codes to a thread every store instruction leaves half of each 32-byte sector to the next one.)  The row's place is looked up once, by bisection over out_indptr, and serves all its heads.
 #include <algorithm>
 
 #include "kernels.h"
@@ -15,14 +15,14 @@ namespace asynclm {
 namespace {
 
 constexpr int kGatherThreads = 256;
-constexpr int kGatherUnroll = 4;
+constexpr int kGatherUnroll = 8;
 
 __global__ void __launch_bounds__(kGatherThreads)
 kv8_gather_kernel(DevPlan p, const int64_t* out_indptr, const int32_t* first, const uint8_t* __restrict__ pool, const uint8_t* __restrict__ scales,
                   uint4* __restrict__ k_out, uint4* __restrict__ v_out, int64_t total, int heads_per_cta) {
     pdl_trigger();
     pdl_wait();
-    const int d = p.head_dim, hkv = p.num_kv_heads, per_row = d / 16;
+    const int d = p.head_dim, hkv = p.num_kv_heads, per_row = d / 8;
     const int v = threadIdx.x % per_row;
     const int64_t row = (int64_t)blockIdx.x * (kGatherThreads / per_row) + threadIdx.x / per_row;
     if (row >= total) return;
@@ -47,13 +47,13 @@ kv8_gather_kernel(DevPlan p, const int64_t* out_indptr, const int32_t* first, co
     const int slot = (int)(pos % kPage);
     const int c0 = blockIdx.y * heads_per_cta, c1 = min(c0 + heads_per_cta, 2 * hkv);      // (kv head, K|V) pairs, K heads first
     for (int c = c0; c < c1; c += kGatherUnroll) {
-        uint4 codes[kGatherUnroll];
+        uint2 codes[kGatherUnroll];
         uint32_t byte[kGatherUnroll];
 #pragma unroll
         for (int u = 0; u < kGatherUnroll; ++u) {
             const int which = c + u >= hkv, h = c + u - which * hkv;
             if (c + u < c1) {
-                codes[u] = ldg_nc_v4(pool + kv8_row_offset(page, which, h, slot, hkv, d) + 16 * v);
+                codes[u] = __ldcg(reinterpret_cast<const uint2*>(pool + kv8_row_offset(page, which, h, slot, hkv, d) + 8 * v));
                 byte[u] = __ldcg(scales + kv8_scale_offset(page, which, h, slot, hkv));
             }
         }
@@ -62,18 +62,16 @@ kv8_gather_kernel(DevPlan p, const int64_t* out_indptr, const int32_t* first, co
             if (c + u >= c1) break;
             const int which = c + u >= hkv, h = c + u - which * hkv;
             const float s = kv8_scale(byte[u]);
-            const uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
-            uint32_t o[8];
+            const uint32_t w[2] = {codes[u].x, codes[u].y};
+            uint32_t o[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2; ++k) {
                 const uint32_t a = kv8_decode2(w[k]), bb = kv8_decode2_hi(w[k]);
                 const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fb = __half22float2(*reinterpret_cast<const __half2*>(&bb));
                 o[2 * k] = pack_bf16x2(fa.x * s, fa.y * s);
                 o[2 * k + 1] = pack_bf16x2(fb.x * s, fb.y * s);
             }
-            uint4* dst = (which ? v_out : k_out) + ((size_t)row * hkv + h) * (d / 8) + 2 * v;
-            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            (which ? v_out : k_out)[((size_t)row * hkv + h) * (d / 8) + v] = make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
 }
@@ -92,7 +90,7 @@ extern "C" int asynclm_kv8_gather(const asynclm_plan_t* plan, const int64_t* out
         (((uintptr_t)kv8_pool | (uintptr_t)kv8_scales | (uintptr_t)k_out | (uintptr_t)v_out) & 15) != 0)
         return ASYNCLM_ERR_INVALID_ARG;
     if (int rc = check_plan_device(plan->device)) return rc;
-    const int rows = kGatherThreads / (d.head_dim / 16);
+    const int rows = kGatherThreads / (d.head_dim / 8);
     const int64_t ctas = (total_rows + rows - 1) / rows;
     if (ctas > INT32_MAX) return ASYNCLM_ERR_INVALID_ARG;
     // few rows: their heads are spread over more CTAs, until the SMs have a few each

@@ -17,8 +17,9 @@ constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 struct RopeSets { RowSet set[2]; };
 
-// Grid: one CTA for `tokens` tokens; its warps take blocks of rows of one token.
-__global__ void __launch_bounds__(kRopeRowThreads)
+// Grid: one CTA for `tokens` tokens; its warps take blocks of rows of one token, and request the next block's rows before they turn one's.
+template <int FORM>
+__global__ void __launch_bounds__(kRopeRowThreads, rope_ctas(FORM))
 rope_apply_kernel(const __grid_constant__ RopeTurns turns, const __grid_constant__ RopeSets sets, const int32_t* positions, int total, int head_dim, int tokens) {
     extern __shared__ uint4 smem[];
     float4 (*table)[kRopeEntries] = reinterpret_cast<float4 (*)[kRopeEntries]>(smem + kRopeRowThreads);
@@ -29,32 +30,39 @@ rope_apply_kernel(const __grid_constant__ RopeTurns turns, const __grid_constant
     const int r0 = blockIdx.x * tokens, n = min(tokens, total - r0);
     const int block = rows * kRopeUnroll;
     const int blocks0 = (sets.set[0].heads + block - 1) / block, blocks = blocks0 + (sets.set[1].heads + block - 1) / block;
-    pdl_wait();      // rows and positions belong to the kernels in front until those have completed
-    rope_fill(turns, table, n, [&](int i) { return __ldcg(positions + r0 + i); });
-    __syncthreads();
-    for (int item = warp; item < n * blocks; item += warps) {
+    struct Block { uint4 x[kRopeUnroll]; };
+    auto load = [&](int item) {
+        Block l;
         const int i = item / blocks, b = item % blocks;
         const RowSet& set = sets.set[b < blocks0 ? 0 : 1];
         const int h0 = (b < blocks0 ? b : b - blocks0) * block + sub;
         const __nv_bfloat16* in = set.in + (int64_t)(r0 + i) * set.in_stride + 8 * v;
-        __nv_bfloat16* out = set.out + (int64_t)(r0 + i) * set.out_stride + 8 * v;
-        uint4 x[kRopeUnroll];
-        bool on[kRopeUnroll];
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-            const int h = h0 + u * rows;
-            on[u] = sub < rows && h < set.heads;
-            x[u] = on[u] ? __ldcg(reinterpret_cast<const uint4*>(in + (int64_t)h * head_dim)) : make_uint4(0, 0, 0, 0);
-        }
-        const RopeLane cs = rope_lane(turns, table[i], v);
-        const bool passes = 8 * v >= turns.rotary_dim;      // none of the lane's values turns: they are copied as they are
+        for (int u = 0; u < kRopeUnroll; ++u)
+            l.x[u] = item < n * blocks && sub < rows && h0 + u * rows < set.heads ? __ldcg(reinterpret_cast<const uint4*>(in + (int64_t)(h0 + u * rows) * head_dim))
+                                                                                 : make_uint4(0, 0, 0, 0);
+        return l;
+    };
+    pdl_wait();      // rows and positions belong to the kernels in front until those have completed
+    Block next = load(warp);
+    rope_fill<FORM>(turns, table, n, [&](int i) { return __ldcg(positions + r0 + i); });
+    __syncthreads();
+    const bool passes = 8 * v >= turns.rotary_dim;      // none of the lane's values turns: they are copied as they are
+    for (int item = warp; item < n * blocks; item += warps) {
+        const Block now = next;
+        next = load(item + warps);
+        const int i = item / blocks, b = item % blocks;
+        const RowSet& set = sets.set[b < blocks0 ? 0 : 1];
+        const int h0 = (b < blocks0 ? b : b - blocks0) * block + sub;
+        __nv_bfloat16* out = set.out + (int64_t)(r0 + i) * set.out_stride + 8 * v;
+        const RopeLane<FORM> cs = rope_lane<FORM>(turns, table[i], v);
 #pragma unroll
         for (int u = 0; u < kRopeUnroll; ++u) {
             float y[8];
-            rope_turn(turns, cs, v, lane, smem + warp * 32, x[u], y);
-            uint4 o = x[u];
+            rope_turn<FORM>(turns, cs, v, lane, smem + warp * 32, now.x[u], y);
+            uint4 o = now.x[u];
             if (!passes) o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-            if (on[u]) *reinterpret_cast<uint4*>(out + (int64_t)(h0 + u * rows) * head_dim) = o;
+            if (sub < rows && h0 + u * rows < set.heads) *reinterpret_cast<uint4*>(out + (int64_t)(h0 + u * rows) * head_dim) = o;
         }
     }
 }
@@ -136,10 +144,17 @@ extern "C" int asynclm_rope_apply(const asynclm_rope_table* table, const int32_t
     }
     if (tokens == 0) return ASYNCLM_OK;
     if (!positions || ((uintptr_t)positions & 3) != 0) return ASYNCLM_ERR_INVALID_ARG;
-    const int per_cta = rope_row_tokens(tokens);
+    const int per_cta = rope_row_tokens(tokens, rope_form(turns));
     const int block = 32 / (head_dim / 8) * kRopeUnroll;
     const int blocks = (sets.set[0].heads + block - 1) / block + (sets.set[1].heads + block - 1) / block;
     const int threads = 32 * std::min(kRopeRowThreads / 32, per_cta * blocks);
-    return cuda_status(launch_pdl(rope_apply_kernel, dim3((tokens + per_cta - 1) / per_cta), dim3(threads), rope_row_smem(per_cta),
-                                  (cudaStream_t)stream, turns, sets, positions, tokens, head_dim, per_cta));
+    const auto launch = [&](auto kernel) {
+        return cuda_status(launch_pdl(kernel, dim3((tokens + per_cta - 1) / per_cta), dim3(threads), rope_row_smem(per_cta), (cudaStream_t)stream, turns, sets,
+                                      positions, tokens, head_dim, per_cta));
+    };
+    switch (rope_form(turns)) {
+        case kRopeHalves: return launch(rope_apply_kernel<kRopeHalves>);
+        case kRopePairs: return launch(rope_apply_kernel<kRopePairs>);
+        default: return launch(rope_apply_kernel<kRopeOddHalves>);
+    }
 }

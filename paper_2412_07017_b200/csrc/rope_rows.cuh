@@ -26,7 +26,6 @@ constexpr int kRopeRowThreads = 256;
 constexpr int kRopeUnroll = 4;
 constexpr int kRopeMaxPairs = 128;
 constexpr int kRopeEntries = kRopeMaxPairs + 8;      // of a token's table, see rope_entry
-constexpr int kRopeMaxTokens = 8;                    // of a CTA
 
 // Heads [T][heads][head_dim] of one tensor, rows `stride` values apart.
 struct RowSet {
@@ -44,11 +43,20 @@ struct RopeTurns {
     int32_t layout;
 };
 
-// Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8 (halves of whole vectors), 4 (interleaved) or each by itself, and lanes
-// next to each other then read entries next to each other.
-__device__ __forceinline__ int rope_group(int rotary_dim, int layout) {
-    return layout == ASYNCLM_ROPE_INTERLEAVED ? 4 : rotary_dim % 16 == 0 ? 8 : 1;
+// The kernels' forms: halves of whole 16-byte vectors, interleaved pairs, halves that begin inside a vector.
+enum RopeForm { kRopeHalves, kRopePairs, kRopeOddHalves };
+inline RopeForm rope_form(const RopeTurns& r) {
+    return r.layout == ASYNCLM_ROPE_INTERLEAVED ? kRopePairs : r.rotary_dim % 16 == 0 ? kRopeHalves : kRopeOddHalves;
 }
+// CTAs of an SM and the most tokens of a CTA, by form.  The sines and cosines of a lane are 16 registers for pairs and 32 for halves, and rows in flight are
+// worth more than registers for pairs only (8192 tokens of 32/8 heads, pairs, append: 54.5 us with two CTAs to an SM, 47.7 with three;
+// 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3 with three, 21.2 with two and up to 16, where pairs take 56.9).
+constexpr int rope_ctas(int form) { return form == kRopePairs ? 3 : 2; }
+constexpr int rope_most_tokens(int form) { return form == kRopePairs ? 8 : 16; }
+// Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8, 4 or each by itself, and lanes next to each other then read
+// entries next to each other.
+template <int FORM>
+__device__ __forceinline__ constexpr int rope_group() { return FORM == kRopePairs ? 4 : FORM == kRopeHalves ? 8 : 1; }
 __device__ __forceinline__ int rope_entry(int j, int m, int per) { return m == 1 ? j : (j % m) * per + j / m; }
 
 // x c - y s with c = c.x + c.y, s = s.x + s.y, x and y of few bits: the first product's rounding error and the low parts are added last (the difference
@@ -62,11 +70,12 @@ __device__ __forceinline__ float rope_diff(float x, float2 c, float y, float2 s)
 
 // Fills table[i][...] with m cos and m sin (high parts, then low parts) of tokens 0 .. n - 1 of the CTA.  A thread keeps one pair, whose frequency it reads from the kernel's
 // parameters once (lanes that read different entries there take turns).
-template <typename Position>
+template <int FORM, typename Position>
 __device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kRopeEntries], int n, Position position) {
     const int pairs = r.rotary_dim / 2;
     if (pairs == 0) return;
-    const int m = rope_group(r.rotary_dim, r.layout), per = (pairs + m - 1) / m;
+    constexpr int m = rope_group<FORM>();
+    const int per = (pairs + m - 1) / m;
     const int at_once = max(1, (int)blockDim.x / pairs);
     for (int a = threadIdx.x; a < at_once * pairs; a += blockDim.x) {      // (blocks of fewer threads than pairs: several pairs a thread)
         const int j = a % pairs;
@@ -85,17 +94,20 @@ __device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kR
 }
 
 // This lane's sines and cosines: of its 8 values (halves), or of its 4 pairs (interleaved; c[k], s[k] for k < 4).
-struct RopeLane { float2 c[8], s[8]; };
+template <int FORM>
+struct RopeLane { float2 c[FORM == kRopePairs ? 4 : 8], s[FORM == kRopePairs ? 4 : 8]; };
 
-__device__ __forceinline__ RopeLane rope_lane(const RopeTurns& r, const float4* table, int v) {
-    RopeLane x;
-    const int rd = r.rotary_dim, pairs = rd / 2, m = rope_group(rd, r.layout), per = (pairs + m - 1) / m;
+template <int FORM>
+__device__ __forceinline__ RopeLane<FORM> rope_lane(const RopeTurns& r, const float4* table, int v) {
+    RopeLane<FORM> x;
+    constexpr int m = rope_group<FORM>();
+    const int rd = r.rotary_dim, pairs = rd / 2, per = (pairs + m - 1) / m;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < (FORM == kRopePairs ? 4 : 8); ++k) {
         float4 cs = make_float4(1.f, 0.f, 0.f, 0.f);
         const int dim = 8 * v + k;
-        if (r.layout == ASYNCLM_ROPE_INTERLEAVED) {
-            if (k < 4 && 4 * v + k < pairs) cs = table[k * per + v];
+        if (FORM == kRopePairs) {
+            if (4 * v + k < pairs) cs = table[k * per + v];
         } else if (dim < rd) {
             const bool second = dim >= pairs;
             const int j = second ? dim - pairs : dim;
@@ -109,13 +121,14 @@ __device__ __forceinline__ RopeLane rope_lane(const RopeTurns& r, const float4* 
 }
 
 // y = the lane's 8 values of a row, turned.  All lanes of the warp take part.  `stage`: 512 bytes of the warp's own.
-__device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane& cs, int v, int lane, uint4* stage, const uint4& x, float (&y)[8]) {
+template <int FORM>
+__device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane<FORM>& cs, int v, int lane, uint4* stage, const uint4& x, float (&y)[8]) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     float own[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) { own[2 * k] = bf16_lo(w[k]); own[2 * k + 1] = bf16_hi(w[k]); }
     const int rd = r.rotary_dim, pairs = rd / 2;
-    if (r.layout == ASYNCLM_ROPE_INTERLEAVED) {
+    if constexpr (FORM == kRopePairs) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float a = own[2 * k], b = own[2 * k + 1];
@@ -123,7 +136,7 @@ __device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane& cs
             y[2 * k] = on ? rope_diff(a, cs.c[k], b, cs.s[k]) : a;
             y[2 * k + 1] = on ? rope_diff(b, cs.c[k], a, make_float2(-cs.s[k].x, -cs.s[k].y)) : b;
         }
-    } else if (rd % 16 == 0) {
+    } else if constexpr (FORM == kRopeHalves) {
         // whole vectors: the pairs' other values are those of one other lane
         const int off = pairs / 8, other = v < off ? lane + off : v < 2 * off ? lane - off : lane;
 #pragma unroll
@@ -147,10 +160,10 @@ __device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane& cs
     }
 }
 
-// Tokens of a CTA: one while that leaves SMs without a CTA, up to eight, whose angles are then worked out beside each other.
-inline int rope_row_tokens(int total) {
-    int t = (total + 148 * 4 - 1) / (148 * 4);
-    return t < 1 ? 1 : t > kRopeMaxTokens ? kRopeMaxTokens : t;
+// Tokens of a CTA: one while that leaves SMs without a CTA; more are worked on beside each other.
+inline int rope_row_tokens(int total, int form) {
+    const int wave = 148 * (form == kRopePairs ? 4 : 2), t = (total + wave - 1) / wave;
+    return t < 1 ? 1 : t > rope_most_tokens(form) ? rope_most_tokens(form) : t;
 }
 // A warp's stage (512 bytes each) and the tables.
 inline size_t rope_row_smem(int tokens) { return (size_t)kRopeRowThreads * sizeof(uint4) + (size_t)tokens * kRopeEntries * sizeof(float4); }
