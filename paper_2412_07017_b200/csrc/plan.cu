@@ -316,6 +316,26 @@ constexpr int64_t kDivideMargin64 = 72;
 constexpr int64_t kStreamShare64 = 58;
 constexpr int64_t kStartNs = 3000;
 
+// The costs that a plan is made with: the above for the bf16 cache, and for the 8-bit one (ASYNCLM_PLAN_KV8) these.  Its
+// warp body takes, per 128 keys, 0.78 us when all SMs stream (6.3 TB/s) and 0.66 on a CTA alone (a warp's work on two
+// pages), half of what 16 bits take, while an item's boundary costs as much as there.  Its span body takes, per 128 keys
+// with one | two row tiles, 1.9 | 3.0 us on a CTA alone and 2.6 | 3.3 on all.  An item of it is taken as longer than it
+// is, 8 us, which keeps spans in longer pieces: with 6 us, 32 decode rows of 0.5-4 K keys beside 8 spans of 8-64 tokens
+// took 106.7 us and with 8 80.9; with the 16-bit cache's costs 79.8, but 64 beside 12 114.8 | 94.2, 24 spans of
+// 33-96 tokens 131 | 112.
+struct Model {
+    PathCost tensor, tensor_only, warp;
+    int64_t dual_ns, dual_only_ns;
+    StreamCost stream;
+    bool kv8;
+};
+constexpr Model model_of(int head_dim, bool kv8) {
+    if (!kv8) return Model{kTensorCost, kTensorOnlyCost, kWarpCost, kTensorDualTileNs, kTensorOnlyDualTileNs, stream_cost(head_dim), false};
+    const bool narrow = head_dim == 64;
+    return Model{PathCost{128, 2200, 8000, 10000}, PathCost{128, 2580, 8000, 2400}, PathCost{128, narrow ? 540 : 720, 1200, 2000}, 3200, 3270,
+                 narrow ? StreamCost{850, 750, 2500} : StreamCost{780, 660, 2500}, true};
+}
+
 // Sorts `v` by falling key, equal keys in the order they stand in.  What stands here comes in runs of equal keys (the
 // kv heads of a sequence, a unit's pieces), so the runs are sorted and written out again.
 template <typename T, typename Key>
@@ -348,8 +368,8 @@ struct CutPolicy {
 // (the others are there from the start), each takes the next item as soon as it is through with one, and those that are
 // still busy when nothing is left stream faster.  Time runs in steps of 1/1024 of the mean (longer ones where
 // an item or a join is very long); *mean_ns, the mean finish, is what no other order of the same items ends before.
-int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joins, int n_ctas, int head_dim, int64_t* mean_ns) {
-    const StreamCost cost = stream_cost(head_dim);
+int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joins, int n_ctas, const Model& model, int64_t* mean_ns) {
+    const StreamCost cost = model.stream;
     auto tile_ns = [&](int64_t ctas) { return std::max(cost.least_tile_ns, cost.tile_ns * ctas / kStreamCtas); };
     const int64_t tile = tile_ns(n_ctas);
     struct Run { int64_t ns, count; };      // items of equal cost
@@ -357,7 +377,7 @@ int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joi
     int64_t sum = 0, tiles_before = -1, longest = 0;
     for (const Item& it : queue) {
         const int64_t tiles = ((int64_t)it.kv1 - it.kv0 + kWarpCost.gran - 1) / kWarpCost.gran;
-        if (tiles != tiles_before) runs.push_back(Run{kWarpCost.item_ns + tiles * tile, 0});
+        if (tiles != tiles_before) runs.push_back(Run{model.warp.item_ns + tiles * tile, 0});
         tiles_before = tiles;
         ++runs.back().count;
         sum += runs.back().ns;
@@ -414,14 +434,15 @@ int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joi
 //   Returns false, with only the units (their division and n_chunks) filled in, if the cuts leave more than
 // max_partial_rows partial rows.
 bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp,
-                  std::vector<UnitBuild>& units, int group, int head_dim, int64_t kv_bytes, int n_ctas, const CutPolicy& policy,
+                  std::vector<UnitBuild>& units, int group, int head_dim, const Model& model, int64_t kv_bytes, int n_ctas, const CutPolicy& policy,
                   int64_t max_partial_rows, std::vector<Item>& items,
                   std::vector<int32_t>& cta_indptr_warp, std::vector<int32_t>& cta_indptr_tensor,
                   std::vector<int32_t>& item_cta, int32_t* queue_first, int32_t* queue_count) {
     struct Piece { Item it; int32_t cta; };
     const bool tensor_only = ids_warp.empty();
-    const PathCost tc = tensor_only ? kTensorOnlyCost : kTensorCost;
-    const int64_t dual_tile_ns = tensor_only ? kTensorOnlyDualTileNs : kTensorDualTileNs;
+    const PathCost tc = tensor_only ? model.tensor_only : model.tensor;
+    const PathCost kWarpCost = model.warp;
+    const int64_t dual_tile_ns = tensor_only ? model.dual_only_ns : model.dual_ns;
     auto tiles_of = [](int64_t keys, int gran) { return (keys + gran - 1) / gran; };
 
     // ---- warp-body work as the model sees it (the chunks are cut below, once the number of CTAs
@@ -637,6 +658,63 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
         chunks.insert(chunks.end(), tail.begin(), tail.end());
         queued = true;
     };
+    // The 8-bit cache: an item takes half the time and its boundary no less, so short chunks for the end of the queue cost
+    // more than they even out.  Units are cut into pieces of one length, the least that makes at most 1, 2, 3 or 4 pieces
+    // for a CTA, or not at all, whichever the model of the queue has end first, with what joining the pieces of a unit
+    // takes behind it.  (us of attention, cut as the 16-bit cache's | so: one sequence of 60 K keys, 8 kv heads, 56.7 |
+    // 30.9; 16 of 4 K 35.3 | 31.1; 5 of 32-110 K 166 | 144.8; 64 of 1-3 K 52.6 | 51.2.)  Not at head_dim 64 with a unit
+    // or more for every CTA: 32 sequences of 0.5-8 K keys, 8 kv heads, 47.9 | 54.3, 64 of 1-3 K 40.6 | 40.1.
+    const bool even = model.kv8 && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
+    if (even) {
+        std::vector<int64_t> joins;
+        for (int k = 0; k < used; ++k) joins.push_back(ctas[(size_t)k].load);
+        int64_t longest = 0;
+        for (int id : warp_order) longest = std::max(longest, tiles_of(units[id].n_keys, kWarpCost.gran));
+        // pieces of `most` tiles; of a unit: its tiles in equal parts
+        auto pieces_of = [&](int64_t t, int64_t most) { return (t + most - 1) / most; };
+        auto cut_even = [&](int64_t most) {
+            chunks.clear();
+            int64_t worst = 1;
+            for (int id : warp_order) {
+                const int64_t t = tiles_of(units[id].n_keys, kWarpCost.gran), pieces = pieces_of(t, most);
+                int64_t k0 = 0;
+                for (int64_t c = 0; c < pieces; ++c) {
+                    const int64_t take = t / pieces + (c < t % pieces ? 1 : 0);
+                    const int64_t k1 = std::min<int64_t>(units[id].n_keys, k0 + take * kWarpCost.gran);
+                    chunks.push_back(Item{id, (int32_t)k0, (int32_t)k1, (int32_t)c});
+                    k0 = k1;
+                }
+                units[id].u.n_chunks = (int32_t)pieces;
+                worst = std::max(worst, pieces);
+            }
+            sort_falling(chunks, [](const Item& x) { return (int64_t)x.kv1 - x.kv0; });
+            return worst;
+        };
+        int64_t best_most = longest, best_ns = -1, tried = -1;
+        for (int per_cta = 0; per_cta <= 4 && longest > 0; ++per_cta) {
+            int64_t most = longest;
+            if (per_cta > 0) {
+                int64_t lo = kMinChunkTiles - 1, hi = longest;      // (lo: too many pieces, or too short)
+                while (hi - lo > 1) {
+                    const int64_t mid = (lo + hi) / 2;
+                    int64_t n = 0;
+                    for (int id : warp_order) n += pieces_of(tiles_of(units[id].n_keys, kWarpCost.gran), mid);
+                    if (n <= (int64_t)per_cta * n_ctas) hi = mid; else lo = mid;
+                }
+                most = hi;
+            }
+            if (most == tried) continue;
+            tried = most;
+            const int64_t worst = cut_even(most);
+            int64_t mean = 0;
+            const int64_t ns = queue_ns(chunks, joins, n_ctas, model, &mean) + (worst > 1 ? 1500 + 250 * worst : 0);
+            if (best_ns < 0 || ns < best_ns) best_ns = ns, best_most = most;
+            if (per_cta == 0 && (int64_t)chunks.size() > 12 * (int64_t)n_ctas) break;      // (many units: nothing to gain)
+        }
+        if (longest > 0) cut_even(best_most);
+        tail.clear();
+        queued = true;
+    }
     bool cut_tail = n_ctas < kSaturatingCtas;
     int64_t shortest = 0;
     for (size_t i = warp_order.size(); i-- > 0 && shortest < tail_target && !cut_tail;) {
@@ -648,12 +726,12 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     for (int id : ids_warp)
         if (units[(size_t)id].u.ntok == 1) decode_tiles += tiles_of(units[(size_t)id].n_keys, kWarpCost.gran);
     cut_tail = cut_tail || 2 * decode_tiles < warp_tiles;      // (spans on the warp body: not measured without)
-    cut(cut_tail);
+    if (!even) cut(cut_tail);
     // Two fifths of the limit were chosen when the span CTAs had a margin of 88 and the limit came out that much higher. Where
     // pieces of that length leave no queue, they are taken: a CTA that comes from span tiles passes through the warp
     // body's start and end (3 us) to find a queue empty.  (us of attention a layer, with a queue | without: 4 sequences of 4/2
     // heads over 5-7 K keys, one with 75 tokens, 41 pieces on 40 CTAs 29.3 | 26.1; 23 of 4/2 heads with 2-44 tokens 30.3 | 23.2.)
-    if (used > 0 && chunks.size() + tail.size() > (size_t)(n_ctas - used) && warp_order.size() <= (size_t)(n_ctas - used)) {
+    if (!even && used > 0 && chunks.size() + tail.size() > (size_t)(n_ctas - used) && warp_order.size() <= (size_t)(n_ctas - used)) {
         const int64_t shorter = bulk_max;
         bulk_max = longest_piece(hi * 88 / span_margin64(head_dim));
         cut(cut_tail);
@@ -662,20 +740,20 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
             cut(cut_tail);
         }
     }
-    if (!cut_tail && chunks.size() > (size_t)(n_ctas - used)) {      // (else every CTA has one to begin with and nothing is left)
+    if (!even && !cut_tail && chunks.size() > (size_t)(n_ctas - used)) {      // (else every CTA has one to begin with and nothing is left)
         std::vector<int64_t> joins;
         for (int k = 0; k < used; ++k) joins.push_back(ctas[(size_t)k].load);
         int64_t mean = 0;
         queue_up();
-        const int64_t whole = queue_ns(chunks, joins, n_ctas, head_dim, &mean);
+        const int64_t whole = queue_ns(chunks, joins, n_ctas, model, &mean);
         // (Span CTAs join at times of their own, which evens the waves out better than modelled: where a gain of 6 to 11 % of the
         // mean was predicted, cutting was 1 to 7 % slower; where 20 %, 6 % faster.)
-        const int64_t cut_ns = std::max(stream_cost(head_dim).cut_ns, used > 0 ? mean / 8 : 0);
+        const int64_t cut_ns = std::max(model.stream.cut_ns, used > 0 ? mean / 8 : 0);
         if (whole - mean > cut_ns) {
             const std::vector<Item> uncut(chunks);
             cut(true);
             queue_up();
-            if (whole - queue_ns(chunks, joins, n_ctas, head_dim, &mean) <= cut_ns) {
+            if (whole - queue_ns(chunks, joins, n_ctas, model, &mean) <= cut_ns) {
                 chunks = uncut;
                 for (int id : warp_order) units[(size_t)id].u.n_chunks = 1;
                 for (const Item& it : chunks) units[(size_t)it.unit].u.n_chunks = std::max(units[(size_t)it.unit].u.n_chunks, it.chunk + 1);
@@ -806,6 +884,7 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     const bool tensor_wanted = !(opts && (opts->flags & ASYNCLM_PLAN_NO_TENSOR_PATH));
     const int tensor_min_rows =
         (opts && opts->tensor_min_rows > 0) ? opts->tensor_min_rows : default_tensor_min_rows(shape->head_dim);
+    const bool kv8 = opts && (opts->flags & ASYNCLM_PLAN_KV8);
     const int TQ = tensor_tile_tokens(G);
     const int fixed_chunk = opts ? opts->kv_chunk_tokens : 0;
     const int ctas_cuda = n_sms * kCudaSlotsPerSm;
@@ -861,8 +940,8 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
                          cta_indptr_tensor, item_cta);
         } else {
             // bytes of K and V the step has to read, each (sequence, kv head) counted once
-            const int64_t kv_bytes = total_kv * Hkv * 4 * shape->head_dim;
-            too_many = !deal_dynamic(ids_tensor, ids_cuda, units, G, shape->head_dim, kv_bytes, ctas_cuda, policy, max_partial_rows, items,
+            const int64_t kv_bytes = total_kv * Hkv * (kv8 ? 2 * ((int64_t)shape->head_dim + 1) : 4 * (int64_t)shape->head_dim);
+            too_many = !deal_dynamic(ids_tensor, ids_cuda, units, G, shape->head_dim, model_of(shape->head_dim, kv8), kv_bytes, ctas_cuda, policy, max_partial_rows, items,
                                      cta_indptr_cuda, cta_indptr_tensor, item_cta, &queue_first, &queue_count);
             if (too_many) return ASYNCLM_OK;
             n_items_cuda = queue_first + queue_count;
