@@ -4,8 +4,9 @@
 //     x_j ~ c_j * 2^e,   c_j = e4m3 nearest to x_j * 2^-e,   e = the least integer >= -100 with max|x_j| <= 448 * 2^e.
 // Why a power of two: e4m3 is a floating-point format, whose relative step is 2^-4 wherever a value lies, so a scale that brings
 // the maximum to 448 exactly gains nothing but up to one more bit at the subnormal end (values below 2^-6 * 2^e).  For it, x * 2^-e and
-// c * 2^e are exact (the only rounding is that of the code), c * 2^e is a bf16 value, so that tensor cores take the cache
-// as bf16 without a second rounding, and a scale is one byte (e8m0: e + 127), 1/128 of its row at head_dim 128.
+// c * 2^e are exact (the only rounding is that of the code) and c * 2^e is a bf16 value, so reading back rounds nothing; scores are
+// taken on the codes, whose 2^e of K multiplies the finished product; V is taken times 2^(e - a reference's), which shifts
+// exponents alone; and a scale is one byte (e8m0: e + 127), 1/128 of its row at head_dim 128.
 // Why e >= -100: c * 2^e then stays clear of fp32's and bf16's subnormal numbers, which these kernels flush; values below 2^-110
 // become zeros.
 #pragma once
