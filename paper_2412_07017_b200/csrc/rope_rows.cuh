@@ -8,7 +8,8 @@
 // rounding errors (rope_diff): a value that is left over from two that cancel is as exact, relatively, as any other, and is rounded
 // once, to what is written.  That takes six fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
 //
-// What bounds it: memory (8 bytes of traffic for each pair's eight flops) or, for few tokens, the latency of one chain: positions, angles, rows, stores.
+// What bounds it: instructions more than memory (4097 tokens of 32 + 8 heads of 128 take 21-22.5 us, 3.8-4 TB/s, with 59 % of the issue slots taken) or, for few
+// tokens, the latency of one chain: positions, angles, rows, stores (3.4 us in a graph).
 // A thread holds 8 values of a row, 16 bytes; head_dim / 8 lanes hold a row, so a pair's other half comes by shuffle, and so does a row's
 // maximum.  A warp takes kRopeUnroll times as many rows of ONE token as it has room for and requests them together: the sines and cosines of a
 // lane's values are the same for all heads and are read from shared memory once.
