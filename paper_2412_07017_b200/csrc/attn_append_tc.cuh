@@ -77,10 +77,10 @@ constexpr long long kGroupSkewCycles = 600;
 // 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest e) is an f16 number exactly (the least code
 // is 2^-9, the least f16 number 2^-24), and the softmax has one eV for the tile.  (A row's exponent follows its largest value; in a
 // trained model's cache they differ by a few.)  Otherwise the tile holds the codes alone, and the softmax takes an eV for every key: right for any, but
-// 32 more 16-byte reads of shared memory a warp and tile, at 4 cycles each.
+// it passes through the scores twice more.
 constexpr int kNearExponents = 15;
-// Of the latter, V rows whose exponents lie further apart than this take the softmax sum of their tile by exponentials of its own.  (The weight of a
-// key is exp2(s + eV - reference), and the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
+// So it does where a tile's eV lies further below the largest of its item so far than this.  (The weight of a key is exp2(s + eV - reference), and
+// the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
 constexpr int kFarExponents = 95;
 
 // Per head_dim: shared memory map (offsets from a 1024-byte aligned base) and barriers.
@@ -101,14 +101,15 @@ struct Geometry {
     static __host__ __device__ constexpr int slot(int which, int t) { return (which ? RING_K : 0) + ring_slot(0, t, ring(which)); }      // of tile t, K ring first
     static constexpr uint32_t OFF_Q = 0;                                   // Q[0], Q[1]
     static constexpr uint32_t OFF_RING = OFF_Q + 2 * QTILE_BYTES;
-    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^-eV of all its keys and 0, or 1 (2: far apart) in the third place; behind them
-    // 2^eK of each of its 64 keys, and eV and 2^-eV of each where they differ
+    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^-eV of all its keys and 0, behind them 2^eK of each of its 64 keys; or, with 1 in the
+    // third place, 0, 0, 64 ones, eV of each and 2^eK of each
     static constexpr uint32_t K_SLOT_BYTES = KV8 ? (uint32_t)(kTile * D) : SLOT_BYTES;
     static __host__ __device__ constexpr uint32_t slot_offset(int which, int s) {      // of the s-th slot of a ring
         return OFF_RING + (which ? RING_K * K_SLOT_BYTES + (uint32_t)s * SLOT_BYTES : (uint32_t)s * K_SLOT_BYTES);
     }
     static constexpr uint32_t OFF_SCALE = OFF_RING + RING_K * K_SLOT_BYTES + RING_V * SLOT_BYTES;
     static constexpr int SCALE_SLOTS = KV8 ? scale_slots(RING_K) : 0;
+    static_assert(!KV8 || RING_K % 2 == 0, "a K slot's tile before was the same group's (alternate tiles), or an earlier item's");
     static constexpr uint32_t SCALE_BYTES = 3 * kTile * 4 + 16;
     // The barriers lie behind everything the warp body uses when the CTA goes on to it: arrivals that nobody
     // waits for (an item's last on kOFree and on the ring's empty barriers) may still be queued in the shared
@@ -467,34 +468,29 @@ __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorM
         if (begins) most = -1000;
         take();
         float* v = reinterpret_cast<float*>(smem + Geo::OFF_SCALE + (uint32_t)(n % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
-        float ks[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t bk = k_now >> (8 * e) & 0xffu, bv = v_now >> (8 * e) & 0xffu;
-            ks[e] = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);
-        }
-        *reinterpret_cast<float2*>(v + 4 + key) = make_float2(ks[0], ks[1]);
+        float2 ks;
+        ks.x = (v_now & 0xffu) == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(k_now & 0xffu);
+        ks.y = v_now >> 8 == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(k_now >> 8);
         int top;
         const bool near = tile_exponents(v_now, key, rows_now, top);
         if (near) most = max(most, top);
-        if (near && most - top <= kFarExponents) {
+        const bool one = near && most - top <= kFarExponents;      // one eV for the tile
+        *reinterpret_cast<float2*>(v + 4 + key) = one ? ks : make_float2(1.f, 1.f);
+        if (one) {
             if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4((float)top, two_to(-top), 0.f, 0.f);
         } else {
-            int lo = 1000;
-            float ev[2], iv[2];
+            float ev[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint32_t bv = v_now >> (8 * e) & 0xffu;
                 const int x = near ? top : bv == kKv8NanByte ? kKv8LeastExponent : max((int)bv - 127, -126);
                 ev[e] = (float)x;
-                iv[e] = two_to(-x);
-                if (key + e < rows_now) lo = min(lo, x), most = max(most, x);
+                if (key + e < rows_now) most = max(most, x);
             }
-            lo = __reduce_min_sync(0xffffffffu, lo);
             most = __reduce_max_sync(0xffffffffu, most);
             *reinterpret_cast<float2*>(v + 4 + kTile + key) = make_float2(ev[0], ev[1]);
-            *reinterpret_cast<float2*>(v + 4 + 2 * kTile + key) = make_float2(iv[0], iv[1]);
-            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4(0.f, 0.f, most - lo > kFarExponents ? 2.f : 1.f, 0.f);
+            *reinterpret_cast<float2*>(v + 4 + 2 * kTile + key) = ks;
+            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4(0.f, 0.f, 1.f, 0.f);
         }
         __syncwarp();
         if (lane == 0 && !stall) mbar_arrive(full);
@@ -1019,6 +1015,19 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const int j = dual ? u : 2 * u + b, ct = cnt + u;
                 const int npg = (min(kTile, it.kv_end - (it.kv0 + j * kTile)) + kPage - 1) / kPage;
                 const uint32_t sb = s_addr + 64u * (uint32_t)(ct & 1);
+                // (8 bits) the tile's scales were written before its K tile was handed over, which is waited for here, too, in front of its
+                // scores: the slot is this tile's until the release below, and the tile it held before was this group's or an earlier item's, so the
+                // phase before is over
+                const float* tile_scales = nullptr;
+                float4 tile = make_float4(0.f, 0.f, 0.f, 0.f);
+                float x_scale = row_scale;
+                if constexpr (KV8) {
+                    const RingPlace x = ring_place(kv_base + j, Geo::RING_K);
+                    ok = __all_sync(0xffffffffu, mbar_wait_spin(bar(Geo::kRingFull0 + x.slot), x.parity, abort_flag, p.status, 33));
+                    if (!ok) break;
+                    tile_scales = reinterpret_cast<const float*>(smem + Geo::OFF_SCALE + (uint32_t)((kv_base + j) % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
+                    tile = *reinterpret_cast<const float4*>(tile_scales);
+                }
                 const long long tw = trace_clock();
                 if (lane == 0) trace_event(1 + warp, ev, 30);
                 ok = __all_sync(0xffffffffu, mbar_wait_spin(bar(Geo::kSFull0 + 2 * b + (ct & 1)), (uint32_t)(ct >> 1) & 1u, abort_flag, p.status, 31));
@@ -1030,30 +1039,35 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 tc_fence_after();
                 const int base = it.kv0 + j * kTile;
                 const int vis = max(0, min(kTile, lim_row - base));      // visible columns of this row
+                if constexpr (KV8) {
+                    if (__builtin_expect(tile.z != 0.f, 0)) {
+                        x_scale = 1.f;
+#pragma unroll 1
+                        for (int cc = 0; cc < 4; ++cc) {
+                            uint32_t x[16];
+                            tmem_ld16(sb + 16u * cc, x);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                x[e] = __float_as_uint(fmaf(__uint_as_float(x[e]) * tile_scales[4 + 2 * kTile + 16 * cc + e], row_scale, tile_scales[4 + kTile + 16 * cc + e]));
+                            tmem_st16(sb + 16u * cc, x);
+                        }
+                        tmem_wait_st();
+                    }
+                }
                 uint32_t rr[64];
                 tmem_ld32(sb, *reinterpret_cast<uint32_t(*)[32]>(&rr[0]));
                 tmem_ld32(sb + 32u, *reinterpret_cast<uint32_t(*)[32]>(&rr[32]));
-                // (8 bits) the tile's scales were written before its K tile was handed over, which this wait sees once more: the slot is this
-                // tile's until the release below
-                const float* tile_scales = nullptr;
-                if constexpr (KV8) {
-                    const RingPlace x = ring_place(kv_base + j, Geo::RING_K);
-                    ok = __all_sync(0xffffffffu, mbar_wait_spin(bar(Geo::kRingFull0 + x.slot), x.parity, abort_flag, p.status, 33));
-                    if (!ok) break;
-                    tile_scales = reinterpret_cast<const float*>(smem + Geo::OFF_SCALE + (uint32_t)((kv_base + j) % Geo::SCALE_SLOTS) * Geo::SCALE_BYTES);
-                }
                 // This S complete means every MMA issued for the group before it is complete: the ring slots they
                 // read go back to the producers, the K tile of j now, and the V tile of j - lead (its P V was
                 // issued in front of this Q K^T).
                 if (KV8 ? lane == 0 : m == 0) release(0, kv_base + j, dual);
                 if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
                 tmem_wait_ld();
-                // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V, whose tile leaves eV out: the tile's eV, which
-                // comes in below, or each key's
-                float4 tile = make_float4(0.f, 0.f, 0.f, 0.f);
-                float x_scale = row_scale;
+                // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V, whose tile leaves eV out: the tile's
+                // eV, which comes in below, or each key's, which has been added above and written back (in a loop over tensor memory: as a branch on the
+                // values in registers, with one like it for the sum, this rare path slowed the usual one down, a prompt of 7777 tokens 735 | 684 us)
                 if constexpr (KV8) {
-                    tile = *reinterpret_cast<const float4*>(tile_scales);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float4 ks = *reinterpret_cast<const float4*>(tile_scales + 4 + 4 * e);
@@ -1063,11 +1077,6 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                         rr[4 * e + 1] = __float_as_uint(a.y);
                         rr[4 * e + 2] = __float_as_uint(c.x);
                         rr[4 * e + 3] = __float_as_uint(c.y);
-                    }
-                    if (__builtin_expect(tile.z != 0.f, 0)) {
-                        x_scale = 1.f;
-#pragma unroll
-                        for (int e = 0; e < 64; ++e) rr[e] = __float_as_uint(fmaf(__uint_as_float(rr[e]), row_scale, tile_scales[4 + kTile + e]));
                     }
                 }
                 if (!__all_sync(0xffffffffu, vis == kTile)) {
@@ -1131,37 +1140,33 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float2 nm2 = make_float2(-m_use, -m_use);
                 uint32_t pk[32];
                 if constexpr (KV8) {
-                    // P' = exp2(x - m_ref) as f16 (11 bits); the sum takes it without the scale of V, 2^-eV times it
-                    if (__builtin_expect(tile.z == 0.f, 1)) {
-                        const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(tile.x - m_use, tile.x - m_use);
-                        float2 s2 = make_float2(0.f, 0.f), s2b = s2;
+                    // P' = exp2(x - m_ref) as f16 (11 bits); the sum takes it without the scale of V: 2^-eV times it, or, where every key has
+                    // its own, by exponentials of its own (and 0 times it)
+                    const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(tile.x - m_use, tile.x - m_use);
+                    float2 s2 = make_float2(0.f, 0.f), s2b = s2;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), scale2, b2);
-                            const float2 pe = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-                            if (e & 1) s2b = __fadd2_rn(s2b, pe); else s2 = __fadd2_rn(s2, pe);
-                            const __half2 h = __floats2half2_rn(pe.x, pe.y);
-                            pk[e] = *reinterpret_cast<const uint32_t*>(&h);
-                        }
-                        const float2 iv2 = make_float2(tile.y, tile.y);
-                        l2 = __ffma2_rn(s2, iv2, l2);
-                        l2b = __ffma2_rn(s2b, iv2, l2b);
-                    } else {
-                        const bool far = tile.z == 2.f;
+                    for (int e = 0; e < 32; ++e) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), scale2, b2);
+                        const float2 pe = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                        if (e & 1) s2b = __fadd2_rn(s2b, pe); else s2 = __fadd2_rn(s2, pe);
+                        const __half2 h = __floats2half2_rn(pe.x, pe.y);
+                        pk[e] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                    const float2 iv2 = make_float2(tile.y, tile.y);
+                    l2 = __ffma2_rn(s2, iv2, l2);
+                    l2b = __ffma2_rn(s2b, iv2, l2b);
+                    if (__builtin_expect(tile.z != 0.f, 0)) {
+                        float sum = 0.f;
+#pragma unroll 1
+                        for (int cc = 0; cc < 4; ++cc) {
+                            uint32_t x[16];
+                            tmem_ld16(sb + 16u * cc, x);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float2 ev = *reinterpret_cast<const float2*>(tile_scales + 4 + kTile + 2 * e), iv = *reinterpret_cast<const float2*>(tile_scales + 4 + 2 * kTile + 2 * e);
-                            const float2 x = __fadd2_rn(make_float2(__uint_as_float(rr[2 * e]), __uint_as_float(rr[2 * e + 1])), nm2);
-                            const float2 pe = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-                            if (far) {
-                                l2.x += fast_exp2(x.x - ev.x);
-                                l2.y += fast_exp2(x.y - ev.y);
-                            } else {
-                                l2 = __ffma2_rn(pe, iv, l2);
-                            }
-                            const __half2 h = __floats2half2_rn(pe.x, pe.y);
-                            pk[e] = *reinterpret_cast<const uint32_t*>(&h);
+                            for (int e = 0; e < 16; ++e)
+                                if (16 * cc + e < vis) sum += fast_exp2(__uint_as_float(x[e]) - (m_use + tile_scales[4 + kTile + 16 * cc + e]));
                         }
+                        l2.x += sum;
                     }
                 } else
 #pragma unroll
