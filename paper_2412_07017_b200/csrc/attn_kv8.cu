@@ -6,8 +6,8 @@
 // 5 of 32-110 K 145-153 (5.5-5.8 TB/s).
 // Spans are bound by the softmax warps: 64 keys and two row tiles take a CTA alone 1.43 us, 0.94 in 16 bits.  Of these 960 cycles, reading the keys' scales
 // from shared memory takes 400 (64 values to each of eight warps, 128 bytes a cycle), multiplying by them and the wait that they are there
-// 200, the producers' instructions the rest.  8 spans of 8-64 tokens beside 24 decode rows over 0.5-4 K keys 76-81 us (a batch of the
-// same kind in 16 bits 64), a prompt of 7777 tokens 684 us, 724 TFLOP/s.
+// 200, the producers' instructions the rest.  8 spans of 8-64 tokens beside 24 decode rows over 0.5-4 K keys 75-81 us (a batch of the
+// same kind in 16 bits 64), a prompt of 7777 tokens 684-712 us, 696-724 TFLOP/s.
 #include "asynclm.h"
 #include "attn_append_tc.cuh"
 #include "attn_decode.cuh"
