@@ -193,6 +193,9 @@ int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
 
 int asynclm_plan_get_info(const asynclm_plan_t* plan, asynclm_plan_info* info);
 
+/* What the plan was made for, and what a call's tensors have to fit: the shape, the number of sequences and that of new tokens. */
+int asynclm_plan_get_shape(const asynclm_plan_t* plan, asynclm_shape* shape, int32_t* batch, int32_t* total_q);
+
 /* Copies up to `capacity` items into `items` (host); returns the number of items, or < 0. */
 int asynclm_plan_get_items(const asynclm_plan_t* plan, asynclm_item_view* items, int32_t capacity);
 

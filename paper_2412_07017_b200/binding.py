@@ -25,7 +25,7 @@ EXPORTS = [
     "asynclm_kv_swap_out", "asynclm_kv_swap_in", "asynclm_trap_decide", "asynclm_latency_model",
     "asynclm_async_latency_of_order", "asynclm_token_monitor_step", "asynclm_token_monitor_workspace_bytes",
     "asynclm_kv_append_rope", "asynclm_rope_table_init", "asynclm_rope_apply", "asynclm_kv8_append", "asynclm_kv8_attn_mixed",
-    "asynclm_kv8_gather",
+    "asynclm_kv8_gather", "asynclm_plan_get_shape",
 ]
 
 TRAP_KEEP, TRAP_SWAP, TRAP_RECOMPUTE = 0, 1, 2
@@ -162,6 +162,7 @@ def load(rebuild_if_stale: bool = True):
     lib.asynclm_kv8_append.argtypes = [vp, ctypes.POINTER(CKv8Rows), vp, vp, ctypes.POINTER(CRopeTable), vp]
     lib.asynclm_kv8_attn_mixed.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     lib.asynclm_kv8_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.asynclm_plan_get_shape.argtypes = [vp, ctypes.POINTER(CShape), ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
     lib.asynclm_static_scratch_bytes.argtypes = []
     lib.asynclm_last_device_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     for name in EXPORTS:
@@ -199,8 +200,8 @@ def _calls():
                                                                             lib.asynclm_attn_mixed, lib.asynclm_step)),
                          torch.cuda.current_device, raw)
                 ext.bind_kv8(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.asynclm_kv8_append, lib.asynclm_kv8_attn_mixed, lib.asynclm_kv8_gather,
-                                                                               lib.asynclm_rope_apply)),
-                             torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.uint8, torch.int32, torch.int64)
+                                                                               lib.asynclm_rope_apply, lib.asynclm_plan_get_shape)),
+                             torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.uint8, torch.int32, torch.int64, torch.float32)
         except (ImportError, OSError, RuntimeError, AttributeError, TypeError) as e:
             ext = False
             warnings.warn(f"the per-layer calls go through ctypes, because their extension cannot be built or loaded: {e}", RuntimeWarning, stacklevel=3)
@@ -457,37 +458,59 @@ def asynclm_async_latency_of_order(gen, exe, order):
     return float(lat.value), done[:len(g)]
 
 
-def _rows_of(t, name: str, dtype=None, dense=False):
-    """(address, row stride in values) of a tensor [tokens][heads][head_dim] whose heads lie next to each other.  What the C call cannot see
-    (types, inner strides, devices) is checked here."""
+def _sizes(plan: Plan):
+    """(shape, sequences, new tokens) that the plan was made for."""
+    shape, batch, tokens = CShape(), ctypes.c_int32(), ctypes.c_int32()
+    _check(load().asynclm_plan_get_shape(plan.handle, ctypes.byref(shape), ctypes.byref(batch), ctypes.byref(tokens)), "asynclm_plan_get_shape")
+    return shape, batch.value, tokens.value
+
+
+def _rows_of(t, name: str, dense=False):
+    """(address, row stride in values) of a bf16 tensor [tokens][heads][head_dim] whose heads lie next to each other.  What the C call cannot see
+    (types, inner strides, devices; a stride of 0, which says "dense" there) is checked here."""
     import torch
-    if t.dim() != 3 or t.dtype != (dtype or torch.bfloat16) or not t.is_cuda:
-        raise ValueError(f"{name}: a CUDA tensor [tokens][heads][head_dim] of {dtype or torch.bfloat16} is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.dim() != 3 or t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor [tokens][heads][head_dim] of {torch.bfloat16} is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
     n, h, d = t.shape
     if n == 0:
         return t.data_ptr(), 0
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (dense and n > 1 and t.stride(0) != h * d):
-        raise ValueError(f"{name}: {'rows' if dense else 'the heads of a row'} have to lie next to each other in memory (strides {t.stride()})")
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or (n > 1 and (t.stride(0) != h * d if dense else t.stride(0) < h * d)):
+        raise ValueError(f"{name}: {'rows' if dense else 'the heads of a row'} have to lie next to each other in memory, {'' if dense else 'and rows must not overlap '}"
+                         f"(strides {t.stride()})")
     return t.data_ptr(), t.stride(0) if n > 1 else 0
 
 
-def _flat(t, name: str, what: str, dtypes=None):
+def _fits(t, name: str, tokens: int, heads: int, d: int) -> None:
+    if tuple(t.shape) != (tokens, heads, d):
+        raise ValueError(f"{name}: {tuple(t.shape)}, but tokens, heads and head_dim are {(tokens, heads, d)} for the plan and the other tensors")
+
+
+def _flat(t, name: str, what: str, dtypes=None, numel=None):
     if not t.is_cuda or not t.is_contiguous() or (dtypes is not None and t.dtype not in dtypes):
         raise ValueError(f"{name}: {what} is wanted, not {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name}: {t.numel()} elements, the plan is for {numel}")
     return t.data_ptr()
 
 
 _kv8_dtypes = None
 
 
-def _cache8(pool, scales):
-    """Addresses of a quantised cache's two tensors: one byte each (float8_e4m3fn and float8_e8m0fnu, or uint8)."""
+def _cache8(pool, scales, shape: Optional[CShape] = None):
+    """Addresses of a quantised cache's two tensors: one byte each (float8_e4m3fn and float8_e8m0fnu, or uint8).  (A misaligned one is the C call's to refuse,
+    whatever its size.)"""
     global _kv8_dtypes
     if _kv8_dtypes is None:
         import torch
         _kv8_dtypes = ((torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8))
-    return (_flat(pool, "kv8_pool", "a contiguous CUDA tensor of float8_e4m3fn or uint8", _kv8_dtypes[0]),
-            _flat(scales, "kv8_scales", "a contiguous CUDA tensor of float8_e8m0fnu or uint8", _kv8_dtypes[1]))
+    got = (_flat(pool, "kv8_pool", "a contiguous CUDA tensor of float8_e4m3fn or uint8", _kv8_dtypes[0]),
+           _flat(scales, "kv8_scales", "a contiguous CUDA tensor of float8_e8m0fnu or uint8", _kv8_dtypes[1]))
+    if shape is not None:
+        rows = shape.num_pages * 2 * shape.num_kv_heads * shape.page_size
+        for t, address, name, n in ((pool, got[0], "kv8_pool", rows * shape.head_dim), (scales, got[1], "kv8_scales", rows)):
+            if address % 16 == 0 and t.numel() != n:
+                raise ValueError(f"{name}: {t.numel()} bytes, the plan's cache has {n}")
+    return got
 
 
 def asynclm_rope_table(head_dim: int, theta: float = 500000.0, rotary_dim: int = 0, layout: str = "half", scaling=None, factor: float = 1.0,
@@ -536,26 +559,35 @@ def asynclm_kv8_append(plan: Plan, k_new, v_new, kv8_pool, kv8_scales, rope: Opt
         if rc is not None:
             return _check(rc, "asynclm_kv8_append")
     (ka, ks), (va, vs) = _rows_of(k_new, "k_new"), _rows_of(v_new, "v_new")
+    shape, _, tokens = _sizes(plan)
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        _fits(t, name, tokens, shape.num_kv_heads, shape.head_dim)
     (qa, qs), qo = (None, 0), None
     if q is not None:
         qa, qs = _rows_of(q, "q")
+        _fits(q, "q", tokens, shape.num_q_heads, shape.head_dim)
         if q_out is None or q_out.shape != q.shape:
             raise ValueError("q_out: a tensor of q's shape is wanted")
         qo = _rows_of(q_out, "q_out", dense=True)[0]
     rows = CKv8Rows(ka, va, qa, qo, ks, vs, qs)
-    pool, scales = _cache8(kv8_pool, kv8_scales)
+    pool, scales = _cache8(kv8_pool, kv8_scales, shape)
     _check(load().asynclm_kv8_append(plan.handle, ctypes.byref(rows), pool, scales, None if rope is None else ctypes.byref(rope),
                                      _stream_ptr(stream)), "asynclm_kv8_append")
 
 
 def asynclm_kv8_attn_mixed(plan: Plan, q, kv8_pool, kv8_scales, out, lse=None, stream=None) -> None:
-    """asynclm_attn_mixed over the quantised cache."""
+    """asynclm_attn_mixed over the quantised cache.  q and out are dense bf16 tensors of the plan's new tokens, lse a dense fp32 one or None."""
     if ext := _calls():
         rc = ext.kv8_attn(plan.handle, q, kv8_pool, kv8_scales, out, lse, stream)
         if rc is not None:
             return _check(rc, "asynclm_kv8_attn_mixed")
-    pool, scales = _cache8(kv8_pool, kv8_scales)
-    _check(load().asynclm_kv8_attn_mixed(plan.handle, q.data_ptr(), pool, scales, out.data_ptr(), None if lse is None else lse.data_ptr(),
+    import torch
+    shape, _, tokens = _sizes(plan)
+    pool, scales = _cache8(kv8_pool, kv8_scales, shape)
+    rows = tokens * shape.num_q_heads
+    qa, oa = (_flat(t, name, "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), rows * shape.head_dim) for t, name in ((q, "q"), (out, "out")))
+    la = None if lse is None else _flat(lse, "lse", "a contiguous CUDA tensor of float32", (torch.float32,), rows)
+    _check(load().asynclm_kv8_attn_mixed(plan.handle, qa, pool, scales, oa, la,
                                          _stream_ptr(stream)), "asynclm_kv8_attn_mixed")
 
 
@@ -568,11 +600,13 @@ def asynclm_kv8_gather(plan: Plan, out_indptr, first, kv8_pool, kv8_scales, k_ou
             return _check(rc, "asynclm_kv8_gather")
     import torch
     k, v = _rows_of(k_out, "k_out", dense=True)[0], _rows_of(v_out, "v_out", dense=True)[0]
+    shape, batch, _ = _sizes(plan)
     if k_out.shape != v_out.shape:
         raise ValueError(f"k_out, v_out: {tuple(k_out.shape)} and {tuple(v_out.shape)}")
-    pool, scales = _cache8(kv8_pool, kv8_scales)
-    _check(load().asynclm_kv8_gather(plan.handle, _flat(out_indptr, "out_indptr", "a contiguous CUDA tensor of int64", (torch.int64,)),
-                                     _flat(first, "first", "a contiguous CUDA tensor of int32", (torch.int32,)), k_out.shape[0], pool, scales, k, v,
+    _fits(k_out, "k_out, v_out", k_out.shape[0], shape.num_kv_heads, shape.head_dim)
+    pool, scales = _cache8(kv8_pool, kv8_scales, shape)
+    _check(load().asynclm_kv8_gather(plan.handle, _flat(out_indptr, "out_indptr", "a contiguous CUDA tensor of int64", (torch.int64,), batch + 1),
+                                     _flat(first, "first", "a contiguous CUDA tensor of int32", (torch.int32,), batch), k_out.shape[0], pool, scales, k, v,
                                      _stream_ptr(stream)), "asynclm_kv8_gather")
 
 

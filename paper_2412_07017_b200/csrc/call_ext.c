@@ -19,12 +19,13 @@ static int (*fn_step)(const asynclm_plan_t*, const void*, const void*, const voi
 static int (*fn_kv8_append)(const asynclm_plan_t*, const asynclm_kv8_rows*, void*, void*, const asynclm_rope_table*, void*);
 static int (*fn_kv8_attn)(const asynclm_plan_t*, const void*, const void*, const void*, void*, float*, void*);
 static int (*fn_kv8_gather)(const asynclm_plan_t*, const int64_t*, const int32_t*, int64_t, const void*, const void*, void*, void*, void*);
+static int (*fn_plan_shape)(const asynclm_plan_t*, asynclm_shape*, int32_t*, int32_t*);
 static int (*fn_rope)(const asynclm_rope_table*, const int32_t*, int32_t, int32_t, const asynclm_rope_rows*, int32_t, void*);
 static PyObject *current_device, *raw_stream;      /* callables: () -> device, (device) -> stream handle */
 static PyObject *s_data_ptr, *s_numel, *s_cuda_stream, *s_num_q_heads, *s_num_kv_heads, *s_head_dim, *s_page_size;
 /* what a tensor is asked for, and the dtypes of rows, of a quantised cache's tensors and of indices */
 static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous;
-static PyObject *t_bf16, *t_e4m3, *t_e8m0, *t_u8, *t_i32, *t_i64;
+static PyObject *t_bf16, *t_e4m3, *t_e8m0, *t_u8, *t_i32, *t_i64, *t_f32;
 
 /* (these return -1 with an exception set on failure) */
 static int address(PyObject* tensor, void** out) {
@@ -193,19 +194,21 @@ static PyObject* py_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 static PyObject* py_bind_kv8(PyObject* self, PyObject* args) {
-    Py_ssize_t append, attn, gather, rope;
-    PyObject *bf16, *e4m3, *e8m0, *u8, *i32, *i64;
-    if (!PyArg_ParseTuple(args, "nnnnOOOOOO", &append, &attn, &gather, &rope, &bf16, &e4m3, &e8m0, &u8, &i32, &i64)) return NULL;
+    Py_ssize_t append, attn, gather, rope, shape;
+    PyObject *bf16, *e4m3, *e8m0, *u8, *i32, *i64, *f32;
+    if (!PyArg_ParseTuple(args, "nnnnnOOOOOOO", &append, &attn, &gather, &rope, &shape, &bf16, &e4m3, &e8m0, &u8, &i32, &i64, &f32)) return NULL;
     fn_kv8_append = (void*)append;
     fn_kv8_attn = (void*)attn;
     fn_kv8_gather = (void*)gather;
     fn_rope = (void*)rope;
+    fn_plan_shape = (void*)shape;
     Py_XSETREF(t_bf16, Py_NewRef(bf16));
     Py_XSETREF(t_e4m3, Py_NewRef(e4m3));
     Py_XSETREF(t_e8m0, Py_NewRef(e8m0));
     Py_XSETREF(t_u8, Py_NewRef(u8));
     Py_XSETREF(t_i32, Py_NewRef(i32));
     Py_XSETREF(t_i64, Py_NewRef(i64));
+    Py_XSETREF(t_f32, Py_NewRef(f32));
     Py_RETURN_NONE;
 }
 
@@ -223,7 +226,8 @@ static int is_cuda_of(PyObject* t, PyObject* type, PyObject* or_type) {
     return right;
 }
 
-static int flat(PyObject* t, PyObject* type, PyObject* or_type, void** out) {
+/* The address of a contiguous tensor of `numel` elements.  1, 0 or -1 as above. */
+static int flat(PyObject* t, PyObject* type, PyObject* or_type, Py_ssize_t numel, void** out) {
     const int right = is_cuda_of(t, type, or_type);
     if (right <= 0) return right;
     PyObject* v = PyObject_CallMethodNoArgs(t, s_is_contiguous);
@@ -231,10 +235,29 @@ static int flat(PyObject* t, PyObject* type, PyObject* or_type, void** out) {
     const int whole = v == Py_True;
     Py_DECREF(v);
     if (!whole) return 0;
+    v = PyObject_CallMethodNoArgs(t, s_numel);
+    if (!v) return -1;
+    const Py_ssize_t got = PyLong_AsSsize_t(v);
+    Py_DECREF(v);
+    if (got == -1 && PyErr_Occurred()) return -1;
+    if (got != numel) return 0;
     return address(t, out) ? -1 : 1;
 }
 
-/* Rows [n][heads][d] of bf16 whose heads lie next to each other: address, shape and row stride.  1, 0 or -1 as above. */
+/* What a call's tensors have to fit; 0 if there is no such plan. */
+typedef struct plan_sizes {
+    asynclm_shape shape;
+    int32_t batch, tokens;
+    Py_ssize_t cache_rows;      /* rows of a quantised cache */
+} plan_sizes;
+static int sizes_of(const void* plan, plan_sizes* s) {
+    if (!plan || fn_plan_shape(plan, &s->shape, &s->batch, &s->tokens) != 0) return 0;
+    s->cache_rows = (Py_ssize_t)s->shape.num_pages * 2 * s->shape.num_kv_heads * s->shape.page_size;
+    return 1;
+}
+
+/* Rows [n][heads][d] of bf16 whose heads lie next to each other and which do not overlap: address, shape and row stride.  (A stride of 0 says "dense" to the C
+ * call.)  1, 0 or -1 as above. */
 typedef struct rows_view {
     void* ptr;
     Py_ssize_t n, heads, d, stride;
@@ -255,12 +278,14 @@ static int rows_of(PyObject* t, rows_view* r) {
         if (PyErr_Occurred()) return -1;
     }
     if (dim[0] > 0 && ((dim[2] > 1 && step[2] != 1) || (dim[1] > 1 && step[1] != dim[2]))) return 0;
+    if (dim[0] > 1 && step[0] < dim[1] * dim[2]) return 0;
     r->n = dim[0];
     r->heads = dim[1];
     r->d = dim[2];
     r->stride = dim[0] > 1 ? step[0] : 0;
     return address(t, &r->ptr) ? -1 : 1;
 }
+static int rows_are(const rows_view* r, Py_ssize_t n, Py_ssize_t heads, Py_ssize_t d) { return r->n == n && r->heads == heads && r->d == d; }
 static int dense(const rows_view* r) { return r->n <= 1 || r->stride == r->heads * r->d; }
 
 /* The calls of the quantised cache and of rotary rows: status, or None where an argument is not of the kind that needs no conversion
@@ -272,16 +297,19 @@ static PyObject* py_kv8_append(PyObject* self, PyObject* const* a, Py_ssize_t n)
     if (n != 9) return PyErr_Format(PyExc_TypeError, "9 arguments expected");
     rows_view k, v, q = {0}, qo = {0};
     void *plan, *pool, *scales, *rope, *stream;
+    plan_sizes s;
     if (handle_of(a[0], &plan) || handle_of(a[5], &rope)) return NULL;
+    TAKE(sizes_of(plan, &s));
     TAKE(rows_of(a[1], &k));
     TAKE(rows_of(a[2], &v));
-    TAKE(flat(a[3], t_e4m3, t_u8, &pool));
-    TAKE(flat(a[4], t_e8m0, t_u8, &scales));
+    TAKE(rows_are(&k, s.tokens, s.shape.num_kv_heads, s.shape.head_dim) && rows_are(&v, k.n, k.heads, k.d));
+    TAKE(flat(a[3], t_e4m3, t_u8, s.cache_rows * s.shape.head_dim, &pool));
+    TAKE(flat(a[4], t_e8m0, t_u8, s.cache_rows, &scales));
     if (a[6] != Py_None) {
         if (a[7] == Py_None) Py_RETURN_NONE;
         TAKE(rows_of(a[6], &q));
         TAKE(rows_of(a[7], &qo));
-        if (q.n != qo.n || q.heads != qo.heads || q.d != qo.d || !dense(&qo)) Py_RETURN_NONE;
+        TAKE(rows_are(&q, s.tokens, s.shape.num_q_heads, s.shape.head_dim) && rows_are(&qo, q.n, q.heads, q.d) && dense(&qo));
     }
     if (stream_of(a[8], &stream)) return NULL;
     const asynclm_kv8_rows rows = {k.ptr, v.ptr, q.ptr, qo.ptr, k.stride, v.stride, q.stride};
@@ -295,11 +323,17 @@ static PyObject* py_kv8_append(PyObject* self, PyObject* const* a, Py_ssize_t n)
 /* kv8_attn(handle, q, kv8_pool, kv8_scales, out, lse, stream) */
 static PyObject* py_kv8_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (n != 7) return PyErr_Format(PyExc_TypeError, "7 arguments expected");
-    void *plan, *q, *pool, *scales, *out, *lse, *stream;
-    if (handle_of(a[0], &plan) || address(a[1], &q)) return NULL;
-    TAKE(flat(a[2], t_e4m3, t_u8, &pool));
-    TAKE(flat(a[3], t_e8m0, t_u8, &scales));
-    if (address(a[4], &out) || address_or_null(a[5], &lse) || stream_of(a[6], &stream)) return NULL;
+    void *plan, *q, *pool, *scales, *out, *lse = NULL, *stream;
+    plan_sizes s;
+    if (handle_of(a[0], &plan)) return NULL;
+    TAKE(sizes_of(plan, &s));
+    const Py_ssize_t rows = (Py_ssize_t)s.tokens * s.shape.num_q_heads;
+    TAKE(flat(a[1], t_bf16, NULL, rows * s.shape.head_dim, &q));
+    TAKE(flat(a[2], t_e4m3, t_u8, s.cache_rows * s.shape.head_dim, &pool));
+    TAKE(flat(a[3], t_e8m0, t_u8, s.cache_rows, &scales));
+    TAKE(flat(a[4], t_bf16, NULL, rows * s.shape.head_dim, &out));
+    if (a[5] != Py_None) TAKE(flat(a[5], t_f32, NULL, rows, &lse));
+    if (stream_of(a[6], &stream)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = fn_kv8_attn(plan, q, pool, scales, out, lse, stream);
@@ -312,14 +346,16 @@ static PyObject* py_kv8_gather(PyObject* self, PyObject* const* a, Py_ssize_t n)
     if (n != 8) return PyErr_Format(PyExc_TypeError, "8 arguments expected");
     rows_view k, v;
     void *plan, *indptr, *first, *pool, *scales, *stream;
+    plan_sizes s;
     if (handle_of(a[0], &plan)) return NULL;
-    TAKE(flat(a[1], t_i64, NULL, &indptr));
-    TAKE(flat(a[2], t_i32, NULL, &first));
-    TAKE(flat(a[3], t_e4m3, t_u8, &pool));
-    TAKE(flat(a[4], t_e8m0, t_u8, &scales));
+    TAKE(sizes_of(plan, &s));
+    TAKE(flat(a[1], t_i64, NULL, (Py_ssize_t)s.batch + 1, &indptr));
+    TAKE(flat(a[2], t_i32, NULL, s.batch, &first));
+    TAKE(flat(a[3], t_e4m3, t_u8, s.cache_rows * s.shape.head_dim, &pool));
+    TAKE(flat(a[4], t_e8m0, t_u8, s.cache_rows, &scales));
     TAKE(rows_of(a[5], &k));
     TAKE(rows_of(a[6], &v));
-    if (k.n != v.n || k.heads != v.heads || k.d != v.d || !dense(&k) || !dense(&v)) Py_RETURN_NONE;
+    TAKE(rows_are(&k, k.n, s.shape.num_kv_heads, s.shape.head_dim) && rows_are(&v, k.n, k.heads, k.d) && dense(&k) && dense(&v));
     if (stream_of(a[7], &stream)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -344,17 +380,11 @@ static PyObject* py_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         if (in[k].n > INT32_MAX || in[k].heads > INT32_MAX || in[k].d > INT32_MAX) Py_RETURN_NONE;
         rows[k] = (asynclm_rope_rows){in[k].ptr, out[k].ptr, in[k].stride, out[k].stride, (int32_t)in[k].heads, 0};
     }
-    TAKE(flat(a[1], t_i32, NULL, &positions));
-    PyObject* count = PyObject_CallMethodNoArgs(a[1], s_numel);
-    if (!count) return NULL;
-    const Py_ssize_t tokens = PyLong_AsSsize_t(count);
-    Py_DECREF(count);
-    if (PyErr_Occurred()) return NULL;
-    if (tokens != in[0].n) Py_RETURN_NONE;
+    TAKE(flat(a[1], t_i32, NULL, in[0].n, &positions));
     if (stream_of(a[6], &stream)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = fn_rope(table, positions, (int32_t)tokens, (int32_t)in[0].d, rows, sets, stream);
+    rc = fn_rope(table, positions, (int32_t)in[0].n, (int32_t)in[0].d, rows, sets, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
@@ -365,7 +395,7 @@ static PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, "bind(plan, appe
                                 {"append_rope", (PyCFunction)(void*)py_append_rope, METH_FASTCALL, NULL},
                                 {"attn", (PyCFunction)(void*)py_attn, METH_FASTCALL, NULL},
                                 {"step", (PyCFunction)(void*)py_step, METH_FASTCALL, NULL},
-                                {"bind_kv8", py_bind_kv8, METH_VARARGS, "bind_kv8(append, attn, gather, rope, bf16, e4m3, e8m0, uint8, int32, int64)"},
+                                {"bind_kv8", py_bind_kv8, METH_VARARGS, "bind_kv8(append, attn, gather, rope, plan_get_shape, bf16, e4m3, e8m0, uint8, int32, int64, float32)"},
                                 {"kv8_append", (PyCFunction)(void*)py_kv8_append, METH_FASTCALL, NULL},
                                 {"kv8_attn", (PyCFunction)(void*)py_kv8_attn, METH_FASTCALL, NULL},
                                 {"kv8_gather", (PyCFunction)(void*)py_kv8_gather, METH_FASTCALL, NULL},

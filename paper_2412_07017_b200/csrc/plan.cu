@@ -1183,6 +1183,14 @@ extern "C" int asynclm_plan_get_info(const asynclm_plan_t* plan, asynclm_plan_in
     return ASYNCLM_OK;
 }
 
+extern "C" int asynclm_plan_get_shape(const asynclm_plan_t* plan, asynclm_shape* shape, int32_t* batch, int32_t* total_q) {
+    if (!plan || !shape || !batch || !total_q || plan->magic != kPlanMagic) return ASYNCLM_ERR_INVALID_ARG;
+    *shape = plan->shape;
+    *batch = plan->dev.batch;
+    *total_q = plan->dev.total_q;
+    return ASYNCLM_OK;
+}
+
 extern "C" int asynclm_plan_get_items(const asynclm_plan_t* plan, asynclm_item_view* out,
                                       int32_t capacity) {
     if (!plan || plan->magic != kPlanMagic || capacity < 0 || (capacity > 0 && !out))
