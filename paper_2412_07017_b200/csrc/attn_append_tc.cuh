@@ -74,11 +74,12 @@ constexpr int kTile = 64;                        // keys per KV tile: a K or V r
 constexpr float kRescaleThreshold = 8.f;
 constexpr long long kWaitCycles = 2000000000ll;
 constexpr long long kGroupSkewCycles = 600;
-// 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest e) is an f16 number exactly (the least code
-// is 2^-9, the least f16 number 2^-24), and the softmax has one eV for the tile.  (A row's exponent follows its largest value; in a
-// trained model's cache they differ by a few.)  Otherwise the tile holds the codes alone, and the softmax takes an eV for every key: right for any, but
-// it passes through the scores twice more.
-constexpr int kNearExponents = 15;
+// 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest e) is an f16 number exactly, and the
+// softmax has one eV for the tile.  A row counts in the reference as if it were as large as the tile's largest, then, so weights that count as
+// zero lie 2^-24 below the largest instead of 2^-32 (kKv8WeightShift).  (A row's exponent follows its largest value; in a
+// trained model's cache they differ by a few, but for a token that takes weight without having a value.)  Otherwise the tile holds the codes alone, and the
+// softmax takes an eV for every key: right for any, but it passes through the scores twice more.
+constexpr int kNearExponents = 8;
 // So it does where a tile's eV lies further below the largest of its item so far than this.  (The weight of a key is exp2(s + eV - reference), and
 // the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
 constexpr int kFarExponents = 95;
@@ -101,7 +102,7 @@ struct Geometry {
     static __host__ __device__ constexpr int slot(int which, int t) { return (which ? RING_K : 0) + ring_slot(0, t, ring(which)); }      // of tile t, K ring first
     static constexpr uint32_t OFF_Q = 0;                                   // Q[0], Q[1]
     static constexpr uint32_t OFF_RING = OFF_Q + 2 * QTILE_BYTES;
-    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^-eV of all its keys and 0, behind them 2^eK of each of its 64 keys; or, with 1 in the
+    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^(-eV - 7) of all its keys and 0, behind them 2^eK of each of its 64 keys; or, with 1 in the
     // third place, 0, 0, 64 ones, eV of each and 2^eK of each
     static constexpr uint32_t K_SLOT_BYTES = KV8 ? (uint32_t)(kTile * D) : SLOT_BYTES;
     static __host__ __device__ constexpr uint32_t slot_offset(int which, int s) {      // of the s-th slot of a ring
@@ -353,7 +354,7 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 // The largest exponent of a tile's rows, `bytes` being the scale bytes of this lane's rows key and key + 1; whether the others lie at most kNearExponents
-// below it.  Rows of the least exponent are left out: those of zeros have it, and what else has it is below 2^-91.  False where a row
+// below it.  (Rows of zeros, which have the least exponent, are no exception: what their keys weigh must not stand in the others' way.)  False where a row
 // is not finite.
 __device__ __forceinline__ bool tile_exponents(uint32_t bytes, int key, int rows, int& top) {
     int hi = kKv8LeastExponent, lo = 1000;
@@ -362,18 +363,15 @@ __device__ __forceinline__ bool tile_exponents(uint32_t bytes, int key, int rows
         const int b = (int)(bytes >> (8 * e) & 0xffu) - 127;
         if (key + e < rows) {
             hi = max(hi, b);
-            if (b > kKv8LeastExponent) lo = min(lo, b);
+            lo = min(lo, b);
         }
     }
     top = __reduce_max_sync(0xffffffffu, hi);
     lo = __reduce_min_sync(0xffffffffu, lo);
     return top <= 127 && top - lo <= kNearExponents;      // (the byte 255 is 128)
 }
-// 2^(byte - 127 - top) as f16, zero where it is below 2^-15.
-__device__ __forceinline__ uint32_t near_factor(uint32_t byte, int top) {
-    const int e = (int)byte - 127 - top + 15;
-    return e > 0 ? (uint32_t)min(e, 15) << 10 : e == 0 ? 0x200u : 0u;
-}
+// 2^(byte - 127 - top) as f16, of a row that is near (others, behind the sequence's end, get something finite).
+__device__ __forceinline__ uint32_t near_factor(uint32_t byte, int top) { return (uint32_t)min(max((int)byte - 127 - top + 15, 1), 15) << 10; }
 
 // How a producer of the 8-bit cache goes through a CTA's tiles: the item at hand and the one behind it, the place in it, the page ids of the tile's group (one to a
 // lane) and of the group behind (or of the next item's first).
@@ -462,7 +460,7 @@ __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorM
         if (lane < npages && !stall)
             asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                          ::"r"(sbase + Geo::slot_offset(0, s) + (uint32_t)lane * (kPage * D)), "l"(map), "r"(0), "r"(0), "r"(kv_head), "r"(2 * id), "r"(full) : "memory");
-        // What the softmax needs of the tile: every key's 2^eK; the tile's eV and 2^-eV, or every key's.  A row of V that is not finite (its codes are
+        // What the softmax needs of the tile: every key's 2^eK; the tile's eV and 2^(-eV - 7), or every key's eV.  A row of V that is not finite (its codes are
         // zeros) makes its key's score NaN, so that only those who see it are hit.  Keys behind the end are masked, whatever stands here.
         const uint32_t k_now = bytes_k, v_now = bytes_v;
         if (begins) most = -1000;
@@ -474,10 +472,10 @@ __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorM
         int top;
         const bool near = tile_exponents(v_now, key, rows_now, top);
         if (near) most = max(most, top);
-        const bool one = near && most - top <= kFarExponents;      // one eV for the tile
+        const bool one = near && most - top <= kFarExponents && top <= 126 - kKv8WeightShift;      // one eV for the tile
         *reinterpret_cast<float2*>(v + 4 + key) = one ? ks : make_float2(1.f, 1.f);
         if (one) {
-            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4((float)top, two_to(-top), 0.f, 0.f);
+            if (lane == 0) *reinterpret_cast<float4*>(v) = make_float4((float)top, two_to(-top - kKv8WeightShift), 0.f, 0.f);
         } else {
             float ev[2];
 #pragma unroll
@@ -1140,9 +1138,10 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float2 nm2 = make_float2(-m_use, -m_use);
                 uint32_t pk[32];
                 if constexpr (KV8) {
-                    // P' = exp2(x - m_ref) as f16 (11 bits); the sum takes it without the scale of V: 2^-eV times it, or, where every key has
-                    // its own, by exponentials of its own (and 0 times it)
-                    const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(tile.x - m_use, tile.x - m_use);
+                    // P' = exp2(x - m_ref + 7) as f16 (11 bits; see kKv8WeightShift); the sum takes it without the scale of V: 2^(-eV - 7) times it, or,
+                    // where every key has its own, by exponentials of its own (and 0 times it)
+                    const float bias = tile.x - (m_use - (float)kKv8WeightShift);
+                    const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(bias, bias);
                     float2 s2 = make_float2(0.f, 0.f), s2b = s2;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
@@ -1212,12 +1211,13 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             if (lane == 0) trace_event(1 + warp, ev, 35);
             const size_t hq = (size_t)it.kv_head * G + g;
             const size_t prow = it.partial_row0 < 0 ? 0 : (size_t)it.partial_row0 + t;
+            constexpr float unshift = KV8 ? 1.f / (1 << kKv8WeightShift) : 1.f;      // (8 bits: O is held times 2^7)
             float w0, w1, lse2;          // weights of O[0] and O[1] in this thread's output row
             int c_begin, c_end;          // 32-column chunks of the row this thread writes
             if (dual) {
                 const float inv = l_sum > 0.f ? 1.f / l_sum : KV8 ? l_sum : 0.f;      // (8 bits: a sum that is not a number stays one)
-                w0 = b == 0 ? inv : 0.f;
-                w1 = b == 1 ? inv : 0.f;
+                w0 = b == 0 ? inv * unshift : 0.f;
+                w1 = b == 1 ? inv * unshift : 0.f;
                 lse2 = l_sum > 0.f ? m_ref + log2f(l_sum) : KV8 && l_sum != 0.f ? l_sum : -INFINITY;
                 c_begin = 0; c_end = D / 32;
             } else {
@@ -1234,8 +1234,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float a1 = l1 > 0.f ? fast_exp2(m1 - M) : KV8 ? l1 : 0.f;
                 const float L = a0 * l0 + a1 * l1;
                 const float inv = L > 0.f ? 1.f / L : KV8 ? L : 0.f;
-                w0 = a0 * inv;
-                w1 = a1 * inv;
+                w0 = a0 * (inv * unshift);
+                w1 = a1 * (inv * unshift);
                 lse2 = L > 0.f ? M + log2f(L) : KV8 && L != 0.f ? L : -INFINITY;
                 c_begin = 2 * b; c_end = min(2 * b + 2, D / 32);
             }

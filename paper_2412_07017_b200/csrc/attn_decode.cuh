@@ -276,7 +276,8 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
             for (int off = 1; off < kWarps; off <<= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
             inv[q4] = L > 0.f ? 1.f / L : 0.f;
             lse2[q4] = L > 0.f ? M + log2f(L) : -INFINITY;
-            if constexpr (KV8) {      // a sum that is not a number stays one
+            if constexpr (KV8) {      // O is held times 2^7 (kKv8WeightShift); a sum that is not a number stays one
+                inv[q4] *= 1.f / (1 << kKv8WeightShift);
                 if (!(L >= 0.f)) inv[q4] = lse2[q4] = L;
             }
         }
@@ -448,9 +449,9 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
 // One consumer warp's two pages of a stage of the 8-bit cache, as two independent chains.
 //   A code is at most 448 and exact in f16, and so are the products of an f16 MMA, so both contractions take the codes as they are:
 //       x = (sum_i cK_i q'_i) * (query scale * 2^eK) + eV      in fp32: the score, and the V row's scale as an exponent
-//       O += P' cV,  P' = p * 2^eV = exp2(x - ref)
-// P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere, and none is lost that matters
-// beside the largest.  The softmax sum is that of P' 2^-eV in fp32, against the same reference; where an eV lies outside a
+//       O += P' cV,  P' = p * 2^eV * 2^7 = exp2(x - ref + 7)
+// P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere; one that counts as zero lies 2^-32 below
+// the largest x (kKv8WeightShift).  The softmax sum is that of P' 2^(-eV - 7) in fp32, against the same reference; where an eV lies outside a
 // window within which P' cannot have vanished and yet count (kLeastWindow; rows of zeros have the least exponent of all), the pages' sums take
 // exponentials of their own.  Against two references, one for sums and one for weights, this saves half of the exponentials.
 //   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes of a row, values 4 t .. 4 t + 3 of a
@@ -512,7 +513,7 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             const uint32_t bk = sb8[8 * hh], bv = sb8[kPage + 8 * hh];
             const float ek = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
             ev[pp][hh] = __uint_as_float(0x4b000000u | bv) - (8388608.f + 127.f);                   // bv - 127
-            iv[pp][hh] = __uint_as_float((254u - bv) << 23);                                        // 2^-eV inside the window
+            iv[pp][hh] = __uint_as_float((254u - kKv8WeightShift - bv) << 23);                      // 2^(-eV - 7) inside the window
             far = far || bv - kLeastWindow > kWindow;
             x[pp][2 * hh] = fmaf(sa[pp][2 * hh] + sb[pp][2 * hh], qs0 * ek, ev[pp][hh]);            // log2 domain
             x[pp][2 * hh + 1] = fmaf(sa[pp][2 * hh + 1] + sb[pp][2 * hh + 1], qs1 * ek, ev[pp][hh]);
@@ -549,7 +550,8 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1;
         }
     }
-    const float u0 = m0 == -INFINITY ? 0.f : m0, u1 = m1 == -INFINITY ? 0.f : m1;
+    constexpr float kShift = kKv8WeightShift;
+    const float u0 = (m0 == -INFINITY ? 0.f : m0) - kShift, u1 = (m1 == -INFINITY ? 0.f : m1) - kShift;
     far = __any_sync(0xffffffffu, far);
     uint32_t b0[WP], b1[WP];
 #pragma unroll
@@ -560,8 +562,9 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             l0 = fmaf(p2, iv[pp][1], fmaf(p0, iv[pp][0], l0));
             l1 = fmaf(p3, iv[pp][1], fmaf(p1, iv[pp][0], l1));
         } else {
-            l0 += fast_exp2(x[pp][0] - u0 - ev[pp][0]) + fast_exp2(x[pp][2] - u0 - ev[pp][1]);
-            l1 += fast_exp2(x[pp][1] - u1 - ev[pp][0]) + fast_exp2(x[pp][3] - u1 - ev[pp][1]);
+            const float e0 = ev[pp][0] + kShift, e1 = ev[pp][1] + kShift;
+            l0 += fast_exp2(x[pp][0] - u0 - e0) + fast_exp2(x[pp][2] - u0 - e1);
+            l1 += fast_exp2(x[pp][1] - u1 - e0) + fast_exp2(x[pp][3] - u1 - e1);
         }
         // P' (keys x columns, f16) -> its transpose as the B operand: two 8x8 transposes in registers
         b0[pp] = movmatrix_t(pack_f16x2(p0, p1));

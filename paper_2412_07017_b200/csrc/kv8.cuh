@@ -21,6 +21,9 @@ constexpr int kKv8LeastExponent = -100;
 constexpr uint32_t kKv8NanByte = 255;      // scale of a row with a value that is not finite; its codes are zeros
 constexpr int kKv8ScaleBytes = 2 * kPage;  // of one (page, kv head): 16 K rows, 16 V rows
 constexpr int kStatusBadGather = 45;
+// The attention kernels hold a key's weight, exp2(score + eV - reference), as an f16 number, times 2^kKv8WeightShift: the reference may be exceeded by 2^8, so
+// they stay below 2^15, and one loses bits only where it is below 2^-21 of the reference's weight and counts as zero below 2^-32.
+constexpr int kKv8WeightShift = 7;
 
 // Byte offset of the codes of (page, K|V, kv head, slot), and of its scale byte.
 __device__ __forceinline__ size_t kv8_row_offset(int64_t page, int which, int kv_head, int slot, int num_kv_heads, int head_dim) {
