@@ -1102,12 +1102,17 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                     // key's): rescale the running sum and O[b].  O[b] is at rest once the P V of the group's
                     // previous tile is done, which its commit tells: the next S of the other buffer, or kPvDone.
                     const float m_new = fmaxf(m_ref, cmax);
-                    const float scale = m_new == -INFINITY ? 1.f : fast_exp2(m_ref - m_new);
+                    // (8 bits: the sum's factor in two steps of its root, see dec::pages_kv8)
+                    const float step = m_new == -INFINITY ? 1.f : fast_exp2(KV8 ? 0.5f * (m_ref - m_new) : m_ref - m_new);
+                    const float scale = KV8 ? step * step : step;
                     m_ref = m_new;
-                    l2.x *= scale;
-                    l2.y *= scale;
-                    l2b.x *= scale;
-                    l2b.y *= scale;
+#pragma unroll
+                    for (int k = 0; k < (KV8 ? 2 : 1); ++k) {
+                        l2.x *= step;
+                        l2.y *= step;
+                        l2b.x *= step;
+                        l2b.y *= step;
+                    }
                     if (u > 0) {
                         const int ob = (ct + 1) & 1, pb = (u + 1 < mine ? Geo::kSFull0 : Geo::kPvDone0) + 2 * b + ob;
                         const uint32_t pp = u + 1 < mine ? (uint32_t)((ct + 1) >> 1) & 1u : (pv_phase >> ob) & 1u;
@@ -1230,12 +1235,13 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float m0 = __uint_as_float(x0), l0 = __uint_as_float(y0);
                 const float m1 = __uint_as_float(x1), l1 = __uint_as_float(y1);
                 const float M = fmaxf(m0, m1);
-                const float a0 = l0 > 0.f ? fast_exp2(m0 - M) : KV8 ? l0 : 0.f;
-                const float a1 = l1 > 0.f ? fast_exp2(m1 - M) : KV8 ? l1 : 0.f;
-                const float L = a0 * l0 + a1 * l1;
+                constexpr float root = KV8 ? 0.5f : 1.f;      // (8 bits: in two steps, as above)
+                const float a0 = l0 > 0.f ? fast_exp2(root * (m0 - M)) : KV8 ? l0 : 0.f;
+                const float a1 = l1 > 0.f ? fast_exp2(root * (m1 - M)) : KV8 ? l1 : 0.f;
+                const float L = KV8 ? a0 * l0 * a0 + a1 * l1 * a1 : a0 * l0 + a1 * l1;
                 const float inv = L > 0.f ? 1.f / L : KV8 ? L : 0.f;
-                w0 = a0 * (inv * unshift);
-                w1 = a1 * (inv * unshift);
+                w0 = KV8 ? a0 * (a0 * (inv * unshift)) : a0 * inv;
+                w1 = KV8 ? a1 * (a1 * (inv * unshift)) : a1 * inv;
                 lse2 = L > 0.f ? M + log2f(L) : KV8 && L != 0.f ? L : -INFINITY;
                 c_begin = 2 * b; c_end = min(2 * b + 2, D / 32);
             }

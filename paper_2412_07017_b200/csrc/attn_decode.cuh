@@ -267,11 +267,13 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
             float M = m;
 #pragma unroll
             for (int off = 1; off < kWarps; off <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-            wgt[q4] = m == -INFINITY ? 0.f : fast_exp2(m - M);
-            if constexpr (KV8) {      // (a warp all of whose visible keys are NaN has no maximum)
-                if (!(l >= 0.f)) wgt[q4] = l;
-            }
+            wgt[q4] = m == -INFINITY ? 0.f : fast_exp2(KV8 ? 0.5f * (m - M) : m - M);
             float L = wgt[q4] != 0.f ? l * wgt[q4] : 0.f;
+            if constexpr (KV8) {      // the factor in two steps, see pages_kv8 (and a warp all of whose visible keys are NaN has no maximum)
+                L *= wgt[q4];
+                wgt[q4] *= wgt[q4];
+                if (!(l >= 0.f)) wgt[q4] = L = l;
+            }
 #pragma unroll
             for (int off = 1; off < kWarps; off <<= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
             inv[q4] = L > 0.f ? 1.f / L : 0.f;
@@ -453,7 +455,12 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
 // P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere; one that counts as zero lies 2^-32 below
 // the largest x (kKv8WeightShift).  The softmax sum is that of P' 2^(-eV - 7) in fp32, against the same reference; where an eV lies outside a
 // window within which P' cannot have vanished and yet count (kLeastWindow; rows of zeros have the least exponent of all), the pages' sums take
-// exponentials of their own.  Against two references, one for sums and one for weights, this saves half of the exponentials.
+// exponentials of their own; from an eV above it on, all pages of the item do.  Against two references, one for sums and one for weights, this saves half of the
+// exponentials.
+//   The sum is in units of 2^ref, which follows x, not the score: where the first keys' V are zeros (eV = -100) and later ones large, it is near 2^100 when
+// the reference moves by more than 2^126, and counts for as much as before.  So it takes that factor in two steps of its root.  (O, whose
+// units are those of x, loses nothing that counts.)  Beside a row of V with an eV above 95 (values of 10^31) weights below 2^(eV - 126) of its own are missing
+// from the sum.
 //   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes of a row, values 4 t .. 4 t + 3 of a
 // 16-value piece: the first two are one k step's low half, the others its high half, and Q is laid out alike.  V (transposed): two neighbouring
 // values of two neighbouring keys; a byte permutation pairs the keys, and value 2 g becomes row g of the piece's MMA, 2 g + 1 row g + 8.
@@ -463,7 +470,8 @@ constexpr uint32_t kLeastWindow = 87, kWindow = 95;      // scale bytes 87 .. 18
 
 template <int D, int G>
 __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, const uint8_t* stage_scales, int warp, int lane, const uint32_t (&qb)[D / 16][2],
-                                          float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1) {
+                                          float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1,
+                                          bool& large) {
     using Geo = Geometry<D, true>;
     constexpr int WP = Geo::WARP_PAGES, PIECES = D / 16;
     const int g = lane >> 2, t4 = lane & 3;
@@ -508,13 +516,14 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
     for (int pp = 0; pp < WP; ++pp) {
         const int key0 = (pp * kWarps + warp) * kPage;
         const uint8_t* sb8 = stage_scales + key0 / kPage * kKv8ScaleBytes + g;
+        bool out[2];      // outside the window
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {      // keys g and g + 8
             const uint32_t bk = sb8[8 * hh], bv = sb8[kPage + 8 * hh];
             const float ek = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
             ev[pp][hh] = __uint_as_float(0x4b000000u | bv) - (8388608.f + 127.f);                   // bv - 127
             iv[pp][hh] = __uint_as_float((254u - kKv8WeightShift - bv) << 23);                      // 2^(-eV - 7) inside the window
-            far = far || bv - kLeastWindow > kWindow;
+            out[hh] = bv - kLeastWindow > kWindow;
             x[pp][2 * hh] = fmaf(sa[pp][2 * hh] + sb[pp][2 * hh], qs0 * ek, ev[pp][hh]);            // log2 domain
             x[pp][2 * hh + 1] = fmaf(sa[pp][2 * hh + 1] + sb[pp][2 * hh + 1], qs1 * ek, ev[pp][hh]);
         }
@@ -525,7 +534,14 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             if (g >= lim_b) x[pp][1] = -INFINITY;
             if (g + 8 >= lim_a) x[pp][2] = -INFINITY;
             if (g + 8 >= lim_b) x[pp][3] = -INFINITY;
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+                if (g + 8 * hh >= d.rows - key0) {      // (whatever the scales there are)
+                    ev[pp][hh] = iv[pp][hh] = 0.f;
+                    out[hh] = false;
+                }
         }
+        far = far || out[0] || out[1];
     }
     // ---- softmax against the lazily moved reference maxima of this thread's two columns
     float c0 = fmaxf(x[0][0], x[0][2]), c1 = fmaxf(x[0][1], x[0][3]);
@@ -541,10 +557,11 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, off));
         }
         const float n0 = fmaxf(m0, c0), n1 = fmaxf(m1, c1);
-        const float f0 = n0 == -INFINITY ? 1.f : fast_exp2(m0 - n0);
-        const float f1 = n1 == -INFINITY ? 1.f : fast_exp2(m1 - n1);
+        const float h0 = n0 == -INFINITY ? 1.f : fast_exp2(0.5f * (m0 - n0));
+        const float h1 = n1 == -INFINITY ? 1.f : fast_exp2(0.5f * (m1 - n1));
+        const float f0 = h0 * h0, f1 = h1 * h1;
         m0 = n0; m1 = n1;
-        l0 *= f0; l1 *= f1;
+        l0 = l0 * h0 * h0; l1 = l1 * h1 * h1;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             o[i][0] *= f0; o[i][1] *= f1; o[i][2] *= f0; o[i][3] *= f1;
@@ -552,7 +569,13 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
     }
     constexpr float kShift = kKv8WeightShift;
     const float u0 = (m0 == -INFINITY ? 0.f : m0) - kShift, u1 = (m1 == -INFINITY ? 0.f : m1) - kShift;
-    far = __any_sync(0xffffffffu, far);
+    far = __any_sync(0xffffffffu, far) || large;
+    if (far && !large) {      // an eV above the window: the reference may lie so far up that P' of later pages vanishes
+        bool above = false;
+#pragma unroll
+        for (int pp = 0; pp < WP; ++pp) above = above || fmaxf(ev[pp][0], ev[pp][1]) > (float)(kLeastWindow + kWindow) - 127.f;
+        large = __any_sync(0xffffffffu, above);
+    }
     uint32_t b0[WP], b1[WP];
 #pragma unroll
     for (int pp = 0; pp < WP; ++pp) {
@@ -893,6 +916,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     float o[Geo::KSTEPS][4];          // O^T: rows d = 16 i + g (+8), columns 2 t4, 2 t4 + 1
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;      // of columns 2 t4 and 2 t4 + 1
     float qs0 = 0.f, qs1 = 0.f;      // 8 bits: the columns' query scales
+    bool large = false;              // and whether the item has had an eV above the window of pages_kv8
     int item_count = 0;
 
     for (int n = 0;; ++n) {
@@ -947,6 +971,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             }
             m0 = m1 = -INFINITY;
             l0 = l1 = 0.f;
+            large = false;
         }
         // This warp's pages inside the stage: `warp` and, at head_dim 64, the one kWarps behind it.  Two pages at once are two
         // independent chains of loads, MMAs and exponentials: with one, a warp took as long for a page as at head_dim 128, for half the
@@ -956,7 +981,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         constexpr int WP = Geo::WARP_PAGES;
         if constexpr (KV8) {
             if (warp * kPage < d.rows)
-                pages_kv8<D, G>(d, stage, scale_base + (size_t)s * Geo::SCALE_BYTES, warp, lane, qb, o, qs0, qs1, m0, m1, l0, l1);
+                pages_kv8<D, G>(d, stage, scale_base + (size_t)s * Geo::SCALE_BYTES, warp, lane, qb, o, qs0, qs1, m0, m1, l0, l1, large);
         } else if (warp * kPage < d.rows) {
             bool on[WP];
             float sc[WP][4];

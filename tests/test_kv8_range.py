@@ -108,3 +108,19 @@ def test_a_sink_without_any_value(body, chunk):
         k, v = r.standard_normal((n, HKV, d)) * 0.4, 1.0 + r.standard_normal((n, HKV, d))
         k[at], v[at] = gap * d ** -0.5, 0.0
         check(np.ones((tokens, HQ, d)), rounded(k), rounded(v), body, f"{gap} nats, key {at}", kv_chunk_tokens=chunk)
+
+
+@pytest.mark.parametrize("body", BODIES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("first,second", [(None, 27), (None, 40), (27, None), (40, None), (-30, 100), (100, -30), (110, -28), (-90, 30), (60, -60)])
+def test_scales_of_v_that_change_along_a_sequence(body, d, first, second):
+    """Scores alike, the first half of the keys with V's rows at 2^first (None: zeros), the second half at 2^second: whichever comes first, each half has half
+    of the weight."""
+    r = np.random.default_rng(77)
+    n, tokens = 1530, BODIES[body][0]
+    q, k = (rounded(r.standard_normal((m, h, d)) * 0.5) for m, h in ((tokens, HQ), (n, HKV)))
+    v = 1.0 + r.standard_normal((n, HKV, d))
+    v[:n // 2] *= 0.0 if first is None else 2.0 ** first
+    v[n // 2:] *= 0.0 if second is None else 2.0 ** second
+    for chunk in (0, 1 << 20):
+        check(q, k, rounded(v), body, f"chunk {chunk}", kv_chunk_tokens=chunk)
