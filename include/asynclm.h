@@ -477,7 +477,8 @@ int asynclm_kv8_append(const asynclm_plan_t* plan, const asynclm_kv8_rows* rows,
 
 /*
  * asynclm_attn_mixed over the quantised cache: same plan, queries, masks, results and formulas, with K_j and V_j the values that codes and
- * scales stand for.  bf16 queries, fp32 accumulation and statistics, bf16 output.
+ * scales stand for.  bf16 queries, fp32 accumulation and statistics, bf16 output.  A query row (token, head) with a value that is not finite has NaN in its
+ * output and log-sum-exp; others are untouched.
  * Errors: INVALID_ARG, CUDA.
  */
 int asynclm_kv8_attn_mixed(const asynclm_plan_t* plan, const void* q, const void* kv8_pool, const void* kv8_scales, void* out, float* lse,

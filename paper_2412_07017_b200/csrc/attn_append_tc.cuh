@@ -928,8 +928,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             for (int c = 0; c < kQV; ++c) w[c] = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
         };
         // and as e4m3, scaled by a power of two to a largest value in 2^7 .. 2^8, in two parts: bf16's eight bits are those of a code and of the code of what
-        // is left, exactly down to 2^-9 of the largest value, and off by 2^-18 of it below.  Puts the thread's share (all of the row, or value half b) into the
-        // Q tile and returns the factor on the scores.
+        // is left, exactly down to 2^-9 of the largest value, and off by 2^-17 of it at most below.  Puts the thread's share (all of the row, or value half b) into
+        // the Q tile and returns the factor on the scores: NaN for a row with a value that is not finite (whose codes are the largest ones).
         auto f8_row = [&](const uint4 (&w)[kQV], bool dual) {
             uint32_t most = 0;
 #pragma unroll
@@ -966,6 +966,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 *reinterpret_cast<uint4*>(smem + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 *reinterpret_cast<uint4*>(smem + at + kRows * D) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
+            if (most >= 0x7f80u) return __uint_as_float(0x7fffffffu);
             return fmaxf(__uint_as_float((e - 7u) << 23) * qscale, FLT_MIN);      // (a masked score is -inf, and stays it)
         };
         // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.  (8 bits: a K slot

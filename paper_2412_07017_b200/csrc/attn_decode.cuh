@@ -937,7 +937,8 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             const bool col_valid = g < d.ntok * G;
             if constexpr (KV8) {
                 // The codes go to the tensor core as f16, which holds them exactly; so does the query row, by an f16 copy divided by the
-                // power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value).
+                // power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value).  A row with a value that is not
+                // finite has NaN for its scale, and so for its scores.
                 // Thread (g, t4) holds values 16 ks + 4 t4 .. + 3: the order in which ldmatrix deals out a row's bytes.
                 uint2 w[Geo::KSTEPS];
                 uint32_t most = 0;
@@ -949,7 +950,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 const uint32_t e = min(max(most >> 7, 1u), 253u);
-                const float down = __uint_as_float((254u - e) << 23), up = __uint_as_float(e << 23) * qscale;
+                const float down = __uint_as_float((254u - e) << 23), up = most >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float(e << 23) * qscale;
 #pragma unroll
                 for (int ks = 0; ks < Geo::KSTEPS; ++ks) {
                     qb[ks][0] = pack_f16x2(bf16_lo(w[ks].x) * down, bf16_hi(w[ks].x) * down);

@@ -124,3 +124,25 @@ def test_scales_of_v_that_change_along_a_sequence(body, d, first, second):
     v[n // 2:] *= 0.0 if second is None else 2.0 ** second
     for chunk in (0, 1 << 20):
         check(q, k, rounded(v), body, f"chunk {chunk}", kv_chunk_tokens=chunk)
+
+
+@pytest.mark.parametrize("body", BODIES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_that_are_not_finite_give_nan_and_only_their_own_rows(body, d):
+    r = np.random.default_rng(5)
+    n, tokens = 500, BODIES[body][0]
+    q, k, v = (rounded(r.standard_normal((m, h, d))) for m, h in ((tokens, HQ), (n, HKV), (n, HKV)))
+    for bad in (np.inf, -np.inf, np.nan):
+        x = q.copy()
+        rows = np.ones((tokens, HQ), bool)
+        for t, h, j in ((0, 2, 5), (tokens - 1, 0, d - 1), (tokens // 2, 7, 0)):
+            x[t, h, j], rows[t, h] = bad, False
+        got, lse = check(x, k, v, body, f"{bad}", rows=rows)
+        assert np.isnan(got[~rows]).all() and np.isnan(lse[~rows]).all(), bad
+        # keys of one sign: every score of such a row is infinite, and of one sign; small keys, and keys without those channels: a largest number in its place
+        # would not overflow
+        none = k.copy()
+        none[..., [0, 5, d - 1]] = 0.0
+        for what, other in (("positive", np.abs(k) + 0.1), ("small", k * 0.02), ("sparse", none)):
+            got, lse = check(x, rounded(other), v, body, f"{bad}, {what} keys", rows=rows)
+            assert np.isnan(got[~rows]).all() and np.isnan(lse[~rows]).all(), (bad, what)
