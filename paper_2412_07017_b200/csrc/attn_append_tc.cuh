@@ -938,7 +938,7 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
                 for (int e = 0; e < 4; ++e) most = max(most, max(x[e] & 0x7fffu, x[e] >> 16 & 0x7fffu));
             }
-            const uint32_t e = min(max(most >> 7, 8u), 253u);
+            const uint32_t e = min(max(most >> 7, 8u), 254u);
             const float up = __uint_as_float((261u - e) << 23);
             auto split = [&](uint32_t x, uint32_t& hi, uint32_t& lo) {      // two values -> two codes and two of the rest
                 const float a = bf16_lo(x) * up, c = bf16_hi(x) * up;

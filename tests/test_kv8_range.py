@@ -146,3 +146,15 @@ def test_queries_that_are_not_finite_give_nan_and_only_their_own_rows(body, d):
         for what, other in (("positive", np.abs(k) + 0.1), ("small", k * 0.02), ("sparse", none)):
             got, lse = check(x, rounded(other), v, body, f"{bad}, {what} keys", rows=rows)
             assert np.isnan(got[~rows]).all() and np.isnan(lse[~rows]).all(), (bad, what)
+
+
+@pytest.mark.parametrize("body", BODIES)
+def test_the_largest_finite_queries(body):
+    """Up to the largest bf16 number, against keys near 2^-100 under a scale that brings the scores to a few nats."""
+    r = np.random.default_rng(6)
+    n, d, tokens = 700, 64, BODIES[body][0]
+    big = W.bf16_bits_to_f64(np.array([0x7F7F], np.uint16))[0]
+    q = r.choice([0.9, 0.95, 1.0], (tokens, HQ, d)) * big
+    q[:, :, 1:] *= 2.0 ** -9
+    k = r.standard_normal((n, HKV, d)) * 2.0 ** -99
+    check(rounded(q), rounded(k), rounded(r.standard_normal((n, HKV, d))), body, "largest", sm_scale=2.0 ** -28)
