@@ -42,8 +42,8 @@ kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __gr
         const __nv_bfloat16* in = set.in + (int64_t)(r0 + i) * set.in_stride + 8 * v;
 #pragma unroll
         for (int u = 0; u < kRopeUnroll; ++u)
-            l.x[u] = item < n * blocks && h0 + u * rows < set.heads ? ldg_nc_v4(in + (int64_t)(h0 + u * rows) * d) : make_uint4(0, 0, 0, 0);
-        return l;
+            l.x[u] = item < n * blocks && h0 + u * rows < set.heads ? __ldcg(reinterpret_cast<const uint4*>(in + (int64_t)(h0 + u * rows) * d)) : make_uint4(0, 0, 0, 0);
+        return l;      // (not through the read-only path: q_out may be q itself)
     };
     // The angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the kernels in front until those
     // have completed.  Where all CTAs start at once the angles overlap the tail of the kernel in front; in a longer grid the first rows are
