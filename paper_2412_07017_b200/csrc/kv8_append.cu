@@ -89,8 +89,7 @@ kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __gr
             }
             if (which == 2) {
                 if (on) {
-                    uint4 o = x;
-                    if (8 * v < turns.rotary_dim) o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    const uint4 o = rope_words<FORM>(turns, v, x, y);
                     *reinterpret_cast<uint4*>(set.out + (int64_t)(r0 + i) * set.out_stride + (int64_t)h * d + 8 * v) = o;
                 }
                 continue;
@@ -148,6 +147,7 @@ extern "C" int asynclm_kv8_append(const asynclm_plan_t* plan, const asynclm_kv8_
     switch (rope_form(turns)) {
         case kRopeHalves: return launch(kv8_append_kernel<kRopeHalves>);
         case kRopePairs: return launch(kv8_append_kernel<kRopePairs>);
+        case kRopeOddPairs: return launch(kv8_append_kernel<kRopeOddPairs>);
         default: return launch(kv8_append_kernel<kRopeOddHalves>);
     }
 }

@@ -47,7 +47,6 @@ rope_apply_kernel(const __grid_constant__ RopeTurns turns, const __grid_constant
     Block next = load(warp);
     rope_fill<FORM>(turns, table, n, [&](int i) { return __ldcg(positions + r0 + i); });
     __syncthreads();
-    const bool passes = 8 * v >= turns.rotary_dim;      // none of the lane's values turns: they are copied as they are
     for (int item = warp; item < n * blocks; item += warps) {
         const Block now = next;
         next = load(item + warps);
@@ -60,8 +59,7 @@ rope_apply_kernel(const __grid_constant__ RopeTurns turns, const __grid_constant
         for (int u = 0; u < kRopeUnroll; ++u) {
             float y[8];
             rope_turn<FORM>(turns, cs, v, lane, smem + warp * 32, now.x[u], y);
-            uint4 o = now.x[u];
-            if (!passes) o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+            const uint4 o = rope_words<FORM>(turns, v, now.x[u], y);
             if (sub < rows && h0 + u * rows < set.heads) *reinterpret_cast<uint4*>(out + (int64_t)(h0 + u * rows) * head_dim) = o;
         }
     }
@@ -155,6 +153,7 @@ extern "C" int asynclm_rope_apply(const asynclm_rope_table* table, const int32_t
     switch (rope_form(turns)) {
         case kRopeHalves: return launch(rope_apply_kernel<kRopeHalves>);
         case kRopePairs: return launch(rope_apply_kernel<kRopePairs>);
+        case kRopeOddPairs: return launch(rope_apply_kernel<kRopeOddPairs>);
         default: return launch(rope_apply_kernel<kRopeOddHalves>);
     }
 }

@@ -44,20 +44,25 @@ struct RopeTurns {
     int32_t layout;
 };
 
-// The kernels' forms: halves of whole 16-byte vectors, interleaved pairs, halves that begin inside a vector.
-enum RopeForm { kRopeHalves, kRopePairs, kRopeOddHalves };
+// The kernels' forms: halves of whole 16-byte vectors, interleaved pairs that fill such vectors, halves that begin inside a vector, interleaved pairs that end
+// inside one.  (Sorting the values of a cut vector where none is cut would cost the append of a prompt 3 %.)
+enum RopeForm { kRopeHalves, kRopePairs, kRopeOddHalves, kRopeOddPairs };
+constexpr bool rope_in_pairs(int form) { return form == kRopePairs || form == kRopeOddPairs; }
+template <int FORM>
+constexpr bool kInPairs = rope_in_pairs(FORM);
 inline RopeForm rope_form(const RopeTurns& r) {
-    return r.layout == ASYNCLM_ROPE_INTERLEAVED ? kRopePairs : r.rotary_dim % 16 == 0 ? kRopeHalves : kRopeOddHalves;
+    if (r.layout == ASYNCLM_ROPE_INTERLEAVED) return r.rotary_dim % 8 == 0 ? kRopePairs : kRopeOddPairs;
+    return r.rotary_dim % 16 == 0 ? kRopeHalves : kRopeOddHalves;
 }
 // CTAs of an SM and the most tokens of a CTA, by form.  The sines and cosines of a lane are 16 registers for pairs and 32 for halves, and rows in flight are
 // worth more than registers for pairs only (8192 tokens of 32/8 heads, pairs, append: 54.5 us with two CTAs to an SM, 47.7 with three;
 // 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3 with three, 21.2 with two and up to 16, where pairs take 56.9).
-constexpr int rope_ctas(int form) { return form == kRopePairs ? 3 : 2; }
-constexpr int rope_most_tokens(int form) { return form == kRopePairs ? 8 : 16; }
+constexpr int rope_ctas(int form) { return rope_in_pairs(form) ? 3 : 2; }
+constexpr int rope_most_tokens(int form) { return rope_in_pairs(form) ? 8 : 16; }
 // Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8, 4 or each by itself, and lanes next to each other then read
 // entries next to each other.
 template <int FORM>
-__device__ __forceinline__ constexpr int rope_group() { return FORM == kRopePairs ? 4 : FORM == kRopeHalves ? 8 : 1; }
+__device__ __forceinline__ constexpr int rope_group() { return kInPairs<FORM> ? 4 : FORM == kRopeHalves ? 8 : 1; }
 __device__ __forceinline__ int rope_entry(int j, int m, int per) { return m == 1 ? j : (j % m) * per + j / m; }
 
 // x c - y s with c = c.x + c.y, s = s.x + s.y, x and y of few bits: the first product's rounding error and the low parts are added last (the difference
@@ -96,7 +101,7 @@ __device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kR
 
 // This lane's sines and cosines: of its 8 values (halves), or of its 4 pairs (interleaved; c[k], s[k] for k < 4).
 template <int FORM>
-struct RopeLane { float2 c[FORM == kRopePairs ? 4 : 8], s[FORM == kRopePairs ? 4 : 8]; };
+struct RopeLane { float2 c[kInPairs<FORM> ? 4 : 8], s[kInPairs<FORM> ? 4 : 8]; };
 
 template <int FORM>
 __device__ __forceinline__ RopeLane<FORM> rope_lane(const RopeTurns& r, const float4* table, int v) {
@@ -104,10 +109,10 @@ __device__ __forceinline__ RopeLane<FORM> rope_lane(const RopeTurns& r, const fl
     constexpr int m = rope_group<FORM>();
     const int rd = r.rotary_dim, pairs = rd / 2, per = (pairs + m - 1) / m;
 #pragma unroll
-    for (int k = 0; k < (FORM == kRopePairs ? 4 : 8); ++k) {
+    for (int k = 0; k < (kInPairs<FORM> ? 4 : 8); ++k) {
         float4 cs = make_float4(1.f, 0.f, 0.f, 0.f);
         const int dim = 8 * v + k;
-        if (FORM == kRopePairs) {
+        if (kInPairs<FORM>) {
             if (4 * v + k < pairs) cs = table[k * per + v];
         } else if (dim < rd) {
             const bool second = dim >= pairs;
@@ -129,22 +134,25 @@ __device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane<FOR
 #pragma unroll
     for (int k = 0; k < 4; ++k) { own[2 * k] = bf16_lo(w[k]); own[2 * k + 1] = bf16_hi(w[k]); }
     const int rd = r.rotary_dim, pairs = rd / 2;
-    if constexpr (FORM == kRopePairs) {
+    if constexpr (kInPairs<FORM>) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float a = own[2 * k], b = own[2 * k + 1];
-            const bool on = 4 * v + k < pairs;      // (0 * infinity is not to reach a value that passes through)
+            const bool on = 4 * v + (FORM == kRopePairs ? 0 : k) < pairs;      // (0 * infinity is not to reach a value that passes through)
             y[2 * k] = on ? rope_diff(a, cs.c[k], b, cs.s[k]) : a;
             y[2 * k + 1] = on ? rope_diff(b, cs.c[k], a, make_float2(-cs.s[k].x, -cs.s[k].y)) : b;
         }
     } else if constexpr (FORM == kRopeHalves) {
         // whole vectors: the pairs' other values are those of one other lane
         const int off = pairs / 8, other = v < off ? lane + off : v < 2 * off ? lane - off : lane;
+        uint32_t p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(0xffffffffu, w[k], other);
+        const bool on = v < 2 * off;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t p = __shfl_sync(0xffffffffu, w[k], other);
-            y[2 * k] = rope_diff(own[2 * k], cs.c[2 * k], bf16_lo(p), cs.s[2 * k]);
-            y[2 * k + 1] = rope_diff(own[2 * k + 1], cs.c[2 * k + 1], bf16_hi(p), cs.s[2 * k + 1]);
+            y[2 * k] = on ? rope_diff(own[2 * k], cs.c[2 * k], bf16_lo(p[k]), cs.s[2 * k]) : own[2 * k];
+            y[2 * k + 1] = on ? rope_diff(own[2 * k + 1], cs.c[2 * k + 1], bf16_hi(p[k]), cs.s[2 * k + 1]) : own[2 * k + 1];
         }
     } else {
         // halves that do not begin on a vector: through shared memory, value by value
@@ -156,14 +164,29 @@ __device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane<FOR
         for (int k = 0; k < 8; ++k) {
             const int dim = 8 * v + k;
             const float p = dim < rd ? __uint_as_float((uint32_t)row[dim < pairs ? dim + pairs : dim - pairs] << 16) : 0.f;
-            y[k] = rope_diff(own[k], cs.c[k], p, cs.s[k]);
+            y[k] = dim < rd ? rope_diff(own[k], cs.c[k], p, cs.s[k]) : own[k];
         }
     }
 }
 
+// The lane's 8 values as they are written: turned ones rounded, the others as they came, bit for bit (fp32 has no bf16 NaN's payload and these kernels flush
+// subnormal numbers). rotary_dim is even, so a word of two values is of one kind.
+template <int FORM>
+__device__ __forceinline__ uint4 rope_words(const RopeTurns& r, int v, const uint4& x, const float (&y)[8]) {
+    const int left = r.rotary_dim - 8 * v;      // values of the lane that turn
+    if (left <= 0) return x;
+    uint4 o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+    if (FORM == kRopeOddHalves || FORM == kRopeOddPairs) {
+        if (left <= 2) o.y = x.y;
+        if (left <= 4) o.z = x.z;
+        if (left <= 6) o.w = x.w;
+    }
+    return o;
+}
+
 // Tokens of a CTA: one while that leaves SMs without a CTA; more are worked on beside each other.
 inline int rope_row_tokens(int total, int form) {
-    const int wave = 148 * (form == kRopePairs ? 4 : 2), t = (total + wave - 1) / wave;
+    const int wave = 148 * (rope_in_pairs(form) ? 4 : 2), t = (total + wave - 1) / wave;
     return t < 1 ? 1 : t > rope_most_tokens(form) ? rope_most_tokens(form) : t;
 }
 // A warp's stage (512 bytes each) and the tables.

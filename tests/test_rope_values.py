@@ -28,6 +28,18 @@ def turned_both_ways(q, ctx, table):
     return to_bits(alone), to_bits(appended)
 
 
+@pytest.mark.parametrize("d,layout,rotary", ROTARY)
+def test_what_lies_behind_rotary_dim_passes_through_bit_for_bit(d, layout, rotary):
+    q = np.random.default_rng(rotary).integers(0, 1 << 16, (7, 4, d)).astype(np.uint16)
+    q[..., :rotary] = bits_of(np.random.default_rng(1).standard_normal(q[..., :rotary].shape))
+    special = np.array([0x7F80, 0xFF80, 0x7FC1, 0xFFBF, 0x0001, 0x8003, 0x007F, 0x8000], np.uint16)      # infinities, NaN, subnormal numbers, -0
+    if rotary < d:
+        q[0, 0, rotary:] = np.resize(special, d - rotary)
+        q[3, 2, rotary:] = np.resize(special[::-1], d - rotary)
+    for got in turned_both_ways(q, 11, B.asynclm_rope_table(d, 10000.0, rotary, layout)):
+        assert np.array_equal(got[..., rotary:], q[..., rotary:])
+
+
 @pytest.mark.parametrize("d,layout,rotary", [(128, "half", 128), (64, "interleaved", 32), (64, "half", 20)])
 @pytest.mark.parametrize("T", [1, 40, 1500])
 def test_queries_turned_where_they_lie(d, layout, rotary, T):
