@@ -396,8 +396,8 @@ int asynclm_async_latency_of_order(const double* gen, const double* exec, const 
  *             context, from = max(floor j(beta_fast), 0), to = min(ceil j(beta_slow), rotary_dim - 1) and
  *             t = (j - from) / (to - from) held to [0, 1]: t f_j / factor + (1 - t) f_j; m = attention_factor, or 0.1 ln(factor) + 1 if it is 0
  * asynclm_rope_table_init works the frequencies out on the host, once for a model; the calls below take the table (host memory, read
- * at the call).  Angles, sines and cosines are fp64, a rotated value is within 2^-22 of itself before it is rounded, once, to what
- * is written.
+ * at the call).  Angles, sines and cosines are fp64, a rotated value is within 2^-22 of itself, or 2^-38 of its pair, before it is rounded, once,
+ * to what is written; infinities and NaN come out as the formula has them.
  * Errors: INVALID_ARG (NULL; head_dim not a multiple of 8 in 8 .. 256; rotary_dim odd or above head_dim; theta <= 1; factor < 1;
  * parameters of the chosen scaling that are missing or out of order).
  */

@@ -4,9 +4,9 @@
 //     (x, y) -> m (x cos a - y sin a, y cos a + x sin a),
 // the pairs being (j, j + rotary_dim / 2) or (2j, 2j + 1), the others passing through.  The frequencies come as turns (f_j / 2 pi) in
 // fp64, where position * turns is reduced to [-1/2, 1/2] and its sine and cosine are taken: an fp32 angle is off by thousandths of a radian at
-// positions of 10^5.  Both are kept as two fp32 numbers, high and low part, and a product difference x c - y s is evaluated with its
-// rounding errors (rope_diff): a value that is left over from two that cancel is as exact, relatively, as any other, and is rounded
-// once, to what is written.  That takes six fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
+// positions of 10^5.  Both are kept as two fp32 numbers, a high part of 16 bits, whose products with bf16 values are exact, and a low part, and a product
+// difference x c - y s is evaluated from these (rope_diff): a value that is left over from two that cancel is as exact as any other down to 2^-18 of
+// them, and is rounded once, to what is written.  That takes five fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
 //
 // What bounds it: instructions more than memory (4097 tokens of 32 + 8 heads of 128 take 21-22.5 us, 3.8-4 TB/s, with 59 % of the issue slots taken) or, for few
 // tokens, the latency of one chain: positions, angles, rows, stores (3.4 us in a graph).
@@ -65,12 +65,19 @@ template <int FORM>
 __device__ __forceinline__ constexpr int rope_group() { return kInPairs<FORM> ? 4 : FORM == kRopeHalves ? 8 : 1; }
 __device__ __forceinline__ int rope_entry(int j, int m, int per) { return m == 1 ? j : (j % m) * per + j / m; }
 
-// x c - y s with c = c.x + c.y, s = s.x + s.y, x and y of few bits: the first product's rounding error and the low parts are added last (the difference
-// of products by fused multiply-adds is W. Kahan's).
+// c as a high part of 16 bits and the rest, which has c's sign, and is not zero unless c is: see rope_diff.
+__device__ __forceinline__ float2 rope_split(double c) {
+    const float high = __uint_as_float(__float_as_uint(__double2float_rz(c)) & 0xffffff00u);
+    const float low = (float)(c - (double)high);
+    return make_float2(high, c != 0.0 && low == 0.f ? copysignf(1e-30f, high) : low);
+}
+
+// x c - y s with c = c.x + c.y, s = s.x + s.y, x and y bf16 numbers: their products with the high parts are exact, so the difference of these has one rounding, and
+// the low parts are added last.  An infinite x or y makes the same infinity (or NaN) of both, because the parts have one sign: the sum is what
+// the formula has.
 __device__ __forceinline__ float rope_diff(float x, float2 c, float y, float2 s) {
     const float p = __fmul_rn(y, s.x);
-    const float err = __fmaf_rn(y, s.x, -p);                       // y s.x = p + err, exactly
-    const float low = __fmaf_rn(x, c.y, -__fmaf_rn(y, s.y, err));
+    const float low = __fmaf_rn(x, c.y, -__fmul_rn(y, s.y));
     return __fadd_rn(__fmaf_rn(x, c.x, -p), low);
 }
 
@@ -93,8 +100,8 @@ __device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kR
             sincospi(2.0 * (t - rint(t)), &s, &c);
             c *= r.factor;
             s *= r.factor;
-            const float ch = (float)c, sh = (float)s;
-            table[i][e] = make_float4(ch, sh, (float)(c - (double)ch), (float)(s - (double)sh));
+            const float2 cc = rope_split(c), ss = rope_split(s);
+            table[i][e] = make_float4(cc.x, ss.x, cc.y, ss.y);
         }
     }
 }

@@ -40,6 +40,30 @@ def test_what_lies_behind_rotary_dim_passes_through_bit_for_bit(d, layout, rotar
         assert np.array_equal(got[..., rotary:], q[..., rotary:])
 
 
+@pytest.mark.parametrize("d,layout,rotary", ROTARY)
+def test_values_that_are_not_finite_turn_as_the_formula_has_it(d, layout, rotary):
+    """x cos a - y sin a with an infinite x is infinite (NaN beside 0 * infinity, at position 0, or beside another infinity), and the other pairs of the row
+    are what they are without it, bit for bit."""
+    r = np.random.default_rng(rotary + d)
+    T, H = 6, 4
+    x = W.bf16_bits_to_f64(bits_of(r.standard_normal((T, H, d))))
+    table = B.asynclm_rope_table(d, 10000.0, rotary, layout)
+    f, m = kv8.frequencies(rotary, 10000.0)
+    clean = turned_both_ways(bits_of(x), 0, table)
+    for t in range(T):
+        for h in range(H):
+            x[t, h, r.integers(rotary)] = r.choice([np.inf, -np.inf, np.nan])
+    x[5, 3, :rotary] = np.where(r.random(rotary) < 0.3, np.inf, x[5, 3, :rotary])
+    with np.errstate(invalid="ignore"):
+        want = kv8.turn(x, np.arange(T), f, m, layout)
+    odd = ~np.isfinite(want)
+    assert odd.any() and np.isinf(want).any() and np.isnan(want[0]).any()
+    for got, without in zip(turned_both_ways(bits_of(x), 0, table), clean):
+        value = W.bf16_bits_to_f64(got)
+        assert np.array_equal(value[odd], want[odd], equal_nan=True)
+        assert np.array_equal(got[~odd], without[~odd])
+
+
 @pytest.mark.parametrize("d,layout,rotary", [(128, "half", 128), (64, "interleaved", 32), (64, "half", 20)])
 @pytest.mark.parametrize("T", [1, 40, 1500])
 def test_queries_turned_where_they_lie(d, layout, rotary, T):
