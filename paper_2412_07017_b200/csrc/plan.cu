@@ -276,24 +276,24 @@ void cut_and_deal(const std::vector<int>& unit_ids, std::vector<UnitBuild>& unit
 // alone and 1.4 | 2.4 on all 148, where memory and power bound it (with 900 | 1800 here, 48 sequences with 6 spans took
 // 120 us instead of 112).  At head_dim 64 it takes 0.93 | 1.55 alone and 1.0 | 1.9 on all.
 struct PathCost {
-    int gran;            // tokens per tile of the path (cuts fall on multiples of it)
+    static constexpr int gran = kKvTile;      // tokens per tile of every path (cuts fall on multiples of it); a constant, because planning divides by it a lot
     int64_t tile_ns;     // one tile in steady state
     int64_t item_ns;     // starting and finishing an item (pipeline fill and drain, merge, write)
     int64_t phase_ns;    // first item of the path on a CTA (descriptor chain, first loads)
 };
 // Span body: a KV tile of 128 keys against one row tile, an item, the body's start on a CTA.
-constexpr PathCost kTensorCost{128, 1170, 8000, 11800};
+constexpr PathCost kTensorCost{1170, 8000, 11800};
 constexpr int64_t kTensorDualTileNs = 2435;   // a KV tile of an item with two row tiles (more than 128 rows)
 // When every unit runs on the span body all SMs stream K/V tiles at once and the tile time is set by
 // the memory system (64 KB per tile and SM); the producers run ahead across item boundaries.
-constexpr PathCost kTensorOnlyCost{128, 1543, 8000, 2400};
+constexpr PathCost kTensorOnlyCost{1543, 8000, 2400};
 constexpr int64_t kTensorOnlyDualTileNs = 3126;
 // Warp body: 64 KB per 128-key tile (32 KB at head_dim 64).  It is bound by memory, so its tile time depends on
 // how many SMs stream at once: 1.39 us when all 148 do, 1.05 us (62 KB/us) when half of them run span tiles,
 // which draw some bandwidth too, 0.79 us for 74 and 0.73 for one by themselves; at head_dim 64 0.64, 0.58 for 37 to
 // 100 and 0.53 for one.  The model takes the second figure for both.  (At head_dim 64 900 here gives layers of 0.88 to 1.08 of the time
 // with 1050, 750 of 0.90 to 1.11, without a rule to tell which batch gains.)
-constexpr PathCost kWarpCost{128, 1050, 400, 2000};
+constexpr PathCost kWarpCost{1050, 400, 2000};
 // No step ends before its bytes have crossed the memory bus: K/V pages stream at about 6 bytes per
 // nanosecond on this access pattern (4 KB runs through a shuffled page table), after about 3 us in
 // which the CTAs start.  Without this floor the model would spread the span units over so many CTAs
@@ -332,7 +332,7 @@ struct Model {
 constexpr Model model_of(int head_dim, bool kv8) {
     if (!kv8) return Model{kTensorCost, kTensorOnlyCost, kWarpCost, kTensorDualTileNs, kTensorOnlyDualTileNs, stream_cost(head_dim), false};
     const bool narrow = head_dim == 64;
-    return Model{PathCost{128, 2200, 8000, 10000}, PathCost{128, 2580, 8000, 2400}, PathCost{128, narrow ? 540 : 720, 1200, 2000}, 3200, 3270,
+    return Model{PathCost{2200, 8000, 10000}, PathCost{2580, 8000, 2400}, PathCost{narrow ? 540 : 720, 1200, 2000}, 3200, 3270,
                  narrow ? StreamCost{850, 750, 2500} : StreamCost{780, 660, 2500}, true};
 }
 
