@@ -469,7 +469,7 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
 constexpr uint32_t kLeastWindow = 87, kWindow = 95;      // scale bytes 87 .. 182: 2^-40 .. 2^55
 
 template <int D, int G>
-__device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, const uint8_t* stage_scales, int warp, int lane, const uint32_t (&qb)[D / 16][2],
+__device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, uint8_t* stage_scales, int warp, int lane, const uint32_t (&qb)[D / 16][2],
                                           float (&o)[D / 16][4], float qs0, float qs1, float& m0, float& m1, float& l0, float& l1,
                                           bool& large) {
     using Geo = Geometry<D, true>;
@@ -481,7 +481,11 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
     const uint32_t page0 = smem_u32(stage) + (uint32_t)Geo::page_slot(warp) * Geo::PAGE_BYTES;      // the other page follows
     if ((WP - 1) * kWarps * kPage + (warp + 1) * kPage > d.rows) {
         // Slots past the sequence's end hold whatever was there before, NaN codes included: their scores are masked below, but 0 * NaN would still poison
-        // P V, so their V rows are cleared.  That goes for a whole page behind the end, too.
+        // P V, so their V rows are cleared, and whatever their scales are, they are not to have a say in which form the sums take.  That goes for a whole page behind
+        // the end, too.
+        static_assert(WP * kPage == 32, "a slot to a lane");
+        const int page = (lane / kPage) * kWarps + warp;
+        if (page * kPage + lane % kPage >= d.rows) stage_scales[page * kKv8ScaleBytes + kPage + lane % kPage] = 127;
 #pragma unroll
         for (int pp = 0; pp < WP; ++pp)
             for (int i = max(d.rows - (pp * kWarps + warp) * kPage, 0) * (D / 16) + lane; i < kPage * (D / 16); i += 32)
@@ -516,14 +520,13 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
     for (int pp = 0; pp < WP; ++pp) {
         const int key0 = (pp * kWarps + warp) * kPage;
         const uint8_t* sb8 = stage_scales + key0 / kPage * kKv8ScaleBytes + g;
-        bool out[2];      // outside the window
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {      // keys g and g + 8
             const uint32_t bk = sb8[8 * hh], bv = sb8[kPage + 8 * hh];
             const float ek = bv == kKv8NanByte ? __uint_as_float(0x7fffffffu) : kv8_scale(bk);      // a row that is not finite: see the header
             ev[pp][hh] = __uint_as_float(0x4b000000u | bv) - (8388608.f + 127.f);                   // bv - 127
             iv[pp][hh] = __uint_as_float((254u - kKv8WeightShift - bv) << 23);                      // 2^(-eV - 7) inside the window
-            out[hh] = bv - kLeastWindow > kWindow;
+            far = far || bv - kLeastWindow > kWindow;
             x[pp][2 * hh] = fmaf(sa[pp][2 * hh] + sb[pp][2 * hh], qs0 * ek, ev[pp][hh]);            // log2 domain
             x[pp][2 * hh + 1] = fmaf(sa[pp][2 * hh + 1] + sb[pp][2 * hh + 1], qs1 * ek, ev[pp][hh]);
         }
@@ -534,14 +537,7 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, con
             if (g >= lim_b) x[pp][1] = -INFINITY;
             if (g + 8 >= lim_a) x[pp][2] = -INFINITY;
             if (g + 8 >= lim_b) x[pp][3] = -INFINITY;
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh)
-                if (g + 8 * hh >= d.rows - key0) {      // (whatever the scales there are)
-                    ev[pp][hh] = iv[pp][hh] = 0.f;
-                    out[hh] = false;
-                }
         }
-        far = far || out[0] || out[1];
     }
     // ---- softmax against the lazily moved reference maxima of this thread's two columns
     float c0 = fmaxf(x[0][0], x[0][2]), c1 = fmaxf(x[0][1], x[0][3]);

@@ -46,14 +46,15 @@ def definition(q, k, v, ctx, scale):
     return out, a, top, lse
 
 
-def attend(q, k, v, tokens, sm_scale=0.0, **opts):
-    """Rows k, v (fp64 [n][Hkv][d], bf16 values), of which the last `tokens` are new, appended and attended to.  -> out fp64, lse, plan, K's and V's values."""
+def attend(q, k, v, tokens, sm_scale=0.0, stale=130, **opts):
+    """Rows k, v (fp64 [n][Hkv][d], bf16 values), of which the last `tokens` are new, appended and attended to; scales of unused slots are
+    `stale`.  -> out fp64, lse, plan, K's and V's values."""
     n, d = len(k), k.shape[-1]
     wl = W.make_single_step("range", W.Shape(q.shape[1], HKV, d, 16), [n - tokens], [tokens], seed=51)
     st = wl.steps[0]
     (kc, kb), (vc, vb) = kv8.quantise(k), kv8.quantise(v)
     codes = np.full((wl.num_pages, 2, HKV, 16, d), 0x7F, np.uint8)
-    byte = np.full((wl.num_pages, HKV, 2, 16), 130, np.uint8)
+    byte = np.full((wl.num_pages, HKV, 2, 16), stale, np.uint8)
     pos = np.arange(n - tokens)
     pages, slots = np.asarray(st.page_indices)[pos // 16], pos % 16
     for which, c, b in ((0, kc, kb), (1, vc, vb)):
@@ -158,3 +159,15 @@ def test_the_largest_finite_queries(body):
     q[:, :, 1:] *= 2.0 ** -9
     k = r.standard_normal((n, HKV, d)) * 2.0 ** -99
     check(rounded(q), rounded(k), rounded(r.standard_normal((n, HKV, d))), body, "largest", sm_scale=2.0 ** -28)
+
+
+@pytest.mark.parametrize("body", BODIES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_behind_the_end_have_no_say(body, d):
+    """Bit for bit: neither in the values nor in the form that a page's sums take."""
+    r = np.random.default_rng(8)
+    tokens, flags, _ = BODIES[body]
+    for n in (75, 403, 2005):
+        q, k, v = (rounded(r.standard_normal((m, h, d))) for m, h in ((tokens, HQ), (n, HKV), (n, HKV)))
+        one, *others = (attend(q, k, v, tokens, stale=stale, flags=flags)[:2] for stale in (130, 0, 27, 254, 255))
+        assert all(np.array_equal(a, b) for other in others for a, b in zip(one, other))
