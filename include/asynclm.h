@@ -451,8 +451,9 @@ int asynclm_rope_apply(const asynclm_rope_table* table, const int32_t* positions
  * and one byte a row.  A row is the head_dim values of one (token, kv head, K or V); it is held as
  *     codes   e4m3, x_j * 2^-e rounded to nearest even          standing for code * 2^e
  *     scale   one byte e + 127 (e8m0), e the least integer >= -100 with max|x_j| <= 448 * 2^e
- * (values below 2^-110 become zeros).  A row with a value that is not finite gets the byte 255, which stands for NaN, and codes of zero; a
- * token that sees such a row has NaN in its outputs and its log-sum-exp, tokens that do not see it are untouched.
+ * (values below 2^-110 become zeros, values from 248 * 2^120 = 3.3e38 on round to 2^128, which reads back as infinity).  A row with a value that is
+ * not finite gets the byte 255, which stands for NaN, and codes of zero; a token that sees such a row has NaN in its outputs and its log-sum-exp,
+ * tokens that do not see it are untouched.
  *     kv8_pool    device, 1 byte a value: [num_pages][2 (0 = K, 1 = V)][num_kv_heads][page_size][head_dim]
  *     kv8_scales  device, 1 byte a row:   [num_pages][num_kv_heads][2 (0 = K, 1 = V)][page_size]
  * both 16-byte aligned.  Shapes, plans, page tables and the rules on streams are those of the bf16 cache.  A pool that something else has

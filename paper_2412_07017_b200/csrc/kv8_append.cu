@@ -5,7 +5,7 @@
 // that the planner resolved.  A row is read once, turned in fp32 (rope_rows.cuh), its largest magnitude found by shuffles over the
 // head_dim / 8 lanes that hold it, and its codes and scale written (kv8.cuh): there is one rounding between the projection's bf16 and the code.
 // It moves 3 d bytes for a K or V row and 4 d for a query row, in whole 128-byte lines at head_dim 128.  8192 tokens of 32 / 8 heads of 128,
-// queries too, 64 values of a row rotated, take 48 us, 3.8 TB/s: bound by instructions (72 % of the issue slots; the compensated rotation, maxima and
+// queries too, 64 values of a row rotated, take 46.7 us, 4.0 TB/s: bound by instructions (72 % of the issue slots; the rotation in two parts, maxima and
 // conversions); few tokens by launch and latency, 3.6 us in a graph.
 #include <algorithm>
 

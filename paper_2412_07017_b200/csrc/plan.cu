@@ -319,10 +319,10 @@ constexpr int64_t kStartNs = 3000;
 // The costs that a plan is made with: the above for the bf16 cache, and for the 8-bit one (ASYNCLM_PLAN_KV8) these.  Its
 // warp body takes, per 128 keys, 0.78 us when all SMs stream (6.3 TB/s) and 0.66 on a CTA alone (a warp's work on two
 // pages), half of what 16 bits take, while an item's boundary costs as much as there.  Its span body takes, per 128 keys
-// with one | two row tiles, 1.9 | 3.0 us on a CTA alone and 2.6 | 3.3 on all.  An item of it is taken as longer than it
-// is, 8 us, which keeps spans in longer pieces: with 6 us, 32 decode rows of 0.5-4 K keys beside 8 spans of 8-64 tokens
-// took 106.7 us and with 8 80.9; with the 16-bit cache's costs 79.8, but 64 beside 12 114.8 | 94.2, 24 spans of
-// 33-96 tokens 131 | 112.
+// with one | two row tiles, 1.7 | 2.7 us on a CTA alone and 2.3 | 2.7 on all (1.9 | 3.0 and 2.6 | 3.3 when these costs were
+// chosen).  An item of it is taken as longer than it is, 8 us, which keeps spans in longer pieces.  (18 mixed batches at 6 | 8 | 10
+// us: 12 within 2 %; 128 sequences with 6 spans 81 | 75.6 | 76, 32 with 24 of 33-96 tokens 169 | 166 | 165, 32 with 8 61 | 63 |
+// 63 and 76 | 76 | 82, 48 with 3 97 | 97 | 86, 16 with 4 of 100-300 tokens 214 | 215 | 211.)
 struct Model {
     PathCost tensor, tensor_only, warp;
     int64_t dual_ns, dual_only_ns;
@@ -662,8 +662,10 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // more than they even out.  Units are cut into pieces of one length, the least that makes at most 1, 2, 3 or 4 pieces
     // for a CTA, or not at all, whichever the model of the queue has end first, with what joining the pieces of a unit
     // takes behind it.  (us of attention, cut as the 16-bit cache's | so: one sequence of 60 K keys, 8 kv heads, 56.7 |
-    // 30.9; 16 of 4 K 35.3 | 31.1; 5 of 32-110 K 166 | 144.8; 64 of 1-3 K 52.6 | 51.2.)  Not at head_dim 64 with a unit
-    // or more for every CTA: 32 sequences of 0.5-8 K keys, 8 kv heads, 47.9 | 54.3, 64 of 1-3 K 40.6 | 40.1.
+    // 30.9; 16 of 4 K 35.3 | 31.1; 5 of 32-110 K 166 | 144.8; 64 of 1-3 K 52.6 | 51.2.)  The search costs the host 50 to 80 us at such
+    // sizes.  Not at head_dim 64 with a unit or more for every CTA, where it is worth 2 % on average over 20 batches, 0.91 to 1.2 of the time by turns: 40
+    // sequences of 2-6 K keys, 8 kv heads, 58-60 | 53-55, 20 of 4-30 K 104-109 | 96-101, 64 of 1-3 K 42-43 | 41-43, 32 of 0.5-8 K 47, 56 | 57,
+    // 54, 100 of 1-10 K, 2 kv heads, 44-51 | 45-56, short ones and 128 of 16 kv heads equal.
     const bool even = model.kv8 && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
     if (even) {
         std::vector<int64_t> joins;

@@ -8,8 +8,9 @@
 // difference x c - y s is evaluated from these (rope_diff): a value that is left over from two that cancel is as exact as any other down to 2^-18 of
 // them, and is rounded once, to what is written.  That takes five fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
 //
-// What bounds it: instructions more than memory (4097 tokens of 32 + 8 heads of 128 take 21-22.5 us, 3.8-4 TB/s, with 59 % of the issue slots taken) or, for few
-// tokens, the latency of one chain: positions, angles, rows, stores (3.4 us in a graph).
+// What bounds it: instructions and their latency more than memory (4097 tokens of 32 + 8 heads of 128 take 21.0 us, 4 TB/s, with 62 % of the issue slots
+// taken by two CTAs to an SM, which is what their registers leave room for) or, for few tokens, the latency of one chain: positions, angles, rows, stores
+// (3.4 us in a graph).
 // A thread holds 8 values of a row, 16 bytes; head_dim / 8 lanes hold a row, so a pair's other half comes by shuffle, and so does a row's
 // maximum.  A warp takes kRopeUnroll times as many rows of ONE token as it has room for and requests them together: the sines and cosines of a
 // lane's values are the same for all heads and are read from shared memory once.
@@ -56,7 +57,8 @@ inline RopeForm rope_form(const RopeTurns& r) {
 }
 // CTAs of an SM and the most tokens of a CTA, by form.  The sines and cosines of a lane are 16 registers for pairs and 32 for halves, and rows in flight are
 // worth more than registers for pairs only (8192 tokens of 32/8 heads, pairs, append: 54.5 us with two CTAs to an SM, 47.7 with three;
-// 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3 with three, 21.2 with two and up to 16, where pairs take 56.9).
+// 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3 with three, 21.2 with two and up to 16, where pairs take 56.9; all with one instruction
+// a value more than now, 46.7 and 21.0).
 constexpr int rope_ctas(int form) { return rope_in_pairs(form) ? 3 : 2; }
 constexpr int rope_most_tokens(int form) { return rope_in_pairs(form) ? 8 : 16; }
 // Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8, 4 or each by itself, and lanes next to each other then read
