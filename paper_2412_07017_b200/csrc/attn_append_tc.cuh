@@ -1,13 +1,12 @@
 // Tensor-core attention for interrupt spans (tcgen05 MMA, accumulators and P in tensor memory).
 //
-// An interrupt span is a block of new tokens appended to one sequence (paper Section 3.2); in the
-// next decoding step (Section 5.3) every token of the span attends to the whole cached context and
-// causally to the span itself.  With G query heads per kv head, a span of q tokens gives G*q query
-// rows against the same K/V, which is a dense contraction: rows are packed 128 to a tile
-// (row r = token r / G, head r % G) and S = Q K^T and O += P V run on the tensor cores.
+// An interrupt span is a block of new tokens appended to one sequence (paper Section 3.2); in the next decoding step
+// (Section 5.3) every token of the span attends to the whole cached context and causally to the span itself.  With G
+// query heads per kv head, a span of q tokens gives G*q query rows against the same K/V, which is a dense contraction:
+// rows are packed 128 to a tile (row r = token r / G, head r % G) and S = Q K^T and O += P V run on the tensor cores.
 //
-// A work item covers up to 256 query rows (two row tiles) of one (sequence, kv head) and a range of
-// keys, 64 to a KV tile.  One persistent CTA per SM, twelve warps:
+// A work item covers up to 256 query rows (two row tiles) of one (sequence, kv head) and a range of keys, 64 to a KV
+// tile.  One persistent CTA per SM, twelve warps:
 //   warps 0-3, 4-7  two softmax groups, one thread per query row of a tile.  Each group owns two S
 //                   accumulators (64 fp32 columns of tensor memory each) and one O accumulator.
 //                     * items with more than 128 rows ("dual"): group b owns row tile b and both
@@ -26,23 +25,22 @@
 //                   unfinished last V page goes row by row through cp.async, with zeros behind the end).  K and V
 //                   have a ring of 80 KiB each (see span_ring.h).
 //   warps 9, 11     issue the MMAs, one warp per softmax group, by turns.  Warp 9 owns the tensor-memory allocation.
-// Why tiles of 64 keys: with two S buffers per group, the Q K^T of the tile after next is issued behind the
-// P V of the current one, and the softmax of the next tile, whose S is complete, runs meanwhile; with
-// 128-key tiles tensor memory holds one S per group (at head_dim 128) and each group's softmax and MMAs
-// took turns.  Per 64 keys of both row tiles (cycles, head_dim 128): the exponential unit needs 1024, the tensor pipe
-// 1280 (64-column Q K^T is bound by its operands in shared memory), a lone group's softmax about 1150.
-// Why the MMA warps take turns: the pipe serves two warps that issue at once in turn about, so both were done
-// at the same time, and then both waited for tiles and scores while the pipe ran dry; the groups' exponentials
-// fell together as well.  Turns keep the groups half a period apart.  What a turn has to work out in
-// front of its first MMA counts, too: positions in the rings are carried along instead of divided out.
-// A tile pair takes 1500-1640 cycles on a CTA alone (2050 with both warps issuing at once and cp.async copies), a
-// tile of one row tile 890 (1250; with a copy for each half of a page 1150: see tma_page); at head_dim 64 1520
-// (1700) and 900-940 (1070).  When all CTAs stream, the power limit leaves a clock of 1.5-1.7 GHz: attention of 8192 tokens
-// of one sequence (32 / 8 heads, head_dim 128) 530-570 -> 490-520 us, 24 sequences with spans of 33-96 tokens over 1-3 K keys
+// Why tiles of 64 keys: with two S buffers per group, the Q K^T of the tile after next is issued behind the P V of the
+// current one, and the softmax of the next tile, whose S is complete, runs meanwhile; with 128-key tiles tensor memory
+// holds one S per group (at head_dim 128) and each group's softmax and MMAs took turns.  Per 64 keys of both row tiles
+// (cycles, head_dim 128): the exponential unit needs 1024, the tensor pipe 1280 (64-column Q K^T is bound by its
+// operands in shared memory), a lone group's softmax about 1150.
+// Why the MMA warps take turns: the pipe serves two warps that issue at once in turn about, so both were done at the
+// same time, and then both waited for tiles and scores while the pipe ran dry; the groups' exponentials fell together
+// as well.  Turns keep the groups half a period apart.  What a turn has to work out in front of its first MMA counts,
+// too: positions in the rings are carried along instead of divided out.
+// A tile pair takes 1500-1640 cycles on a CTA alone (2050 with both warps issuing at once and cp.async copies), a tile
+// of one row tile 890 (1250; with a copy for each half of a page 1150: see tma_page); at head_dim 64 1520 (1700) and
+// 900-940 (1070).  When all CTAs stream, the power limit leaves a clock of 1.5-1.7 GHz: attention of 8192 tokens of one
+// sequence (32 / 8 heads, head_dim 128) 530-570 -> 490-520 us, 24 sequences with spans of 33-96 tokens over 1-3 K keys
 // 82 -> 71-74 us a layer.
-// All hand-offs are mbarriers with bounded waits; a wait that runs out sets the plan's status word
-// and a CTA-wide abort flag, every role falls through to the common exit, and the tensor memory is
-// released there.
+// All hand-offs are mbarriers with bounded waits; a wait that runs out sets the plan's status word and a CTA-wide abort
+// flag, every role falls through to the common exit, and the tensor memory is released there.
 #pragma once
 #include <cuda.h>
 
@@ -60,8 +58,9 @@ namespace tc {
 
 constexpr int kThreads = 384;
 constexpr int kProducerWarpK = 8, kMmaWarp = 9, kProducerWarpV = 10;      // 11: the second MMA warp
-// 8-bit cache: warp 8 brings K tiles, warps 10, 12, 13 and 15 turn V tiles, a page each, so that each of the four schedulers has one (14 is idle).  An SM has 128
-// registers for each thread of sixteen warps; the eight softmax (or consumer) warps take 32 more each from the others, at the start, for the whole kernel.
+// 8-bit cache: warp 8 brings K tiles, warps 10, 12, 13 and 15 turn V tiles, a page each, so that each of the four
+// schedulers has one (14 is idle).  An SM has 128 registers for each thread of sixteen warps; the eight softmax (or
+// consumer) warps take 32 more each from the others, at the start, for the whole kernel.
 constexpr int kThreadsKv8 = 512, kLaunchRegs = 128, kLowRegs = 160, kHighRegs = 96;
 static_assert(2 * kLowRegs + 2 * kHighRegs <= 4 * kLaunchRegs, "no more registers than the launch has");
 template <int ROLE>
@@ -74,14 +73,16 @@ constexpr int kTile = 64;                        // keys per KV tile: a K or V r
 constexpr float kRescaleThreshold = 8.f;
 constexpr long long kWaitCycles = 2000000000ll;
 constexpr long long kGroupSkewCycles = 600;
-// 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest e) is an f16 number exactly, and the
-// softmax has one eV for the tile.  A row counts in the reference as if it were as large as the tile's largest, then, so weights that count as
-// zero lie 2^-24 below the largest instead of 2^-32 (kKv8WeightShift).  (A row's exponent follows its largest value; in a
-// trained model's cache they differ by a few, but for a token that takes weight without having a value.)  Otherwise the tile holds the codes alone, and the
-// softmax takes an eV for every key: right for any, but it passes through the scores twice more.
+// 8 bits: the exponents of a tile's rows of V are near if they are at most this far apart: then code * 2^(e - largest
+// e) is an f16 number exactly, and the softmax has one eV for the tile.  A row counts in the reference as if it were as
+// large as the tile's largest, then, so weights that count as zero lie 2^-24 below the largest instead of 2^-32
+// (kKv8WeightShift).  (A row's exponent follows its largest value; in a trained model's cache they differ by a few, but
+// for a token that takes weight without having a value.)  Otherwise the tile holds the codes alone, and the softmax
+// takes an eV for every key: right for any, but it passes through the scores twice more.
 constexpr int kNearExponents = 8;
-// So it does where a tile's eV lies further below the largest of its item so far than this.  (The weight of a key is exp2(s + eV - reference), and
-// the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to 2^-31.)
+// So it does where a tile's eV lies further below the largest of its item so far than this.  (The weight of a key is
+// exp2(s + eV - reference), and the sum takes 2^-eV times it; below 2^-126 it is zero, which has to leave sums right to
+// 2^-31.)
 constexpr int kFarExponents = 95;
 
 // Per head_dim: shared memory map (offsets from a 1024-byte aligned base) and barriers.
@@ -102,8 +103,8 @@ struct Geometry {
     static __host__ __device__ constexpr int slot(int which, int t) { return (which ? RING_K : 0) + ring_slot(0, t, ring(which)); }      // of tile t, K ring first
     static constexpr uint32_t OFF_Q = 0;                                   // Q[0], Q[1]
     static constexpr uint32_t OFF_RING = OFF_Q + 2 * QTILE_BYTES;
-    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^(-eV - 7) of all its keys and 0, behind them 2^eK of each of its 64 keys; or, with 1 in the
-    // third place, 0, 0, 64 ones, eV of each and 2^eK of each
+    // 8 bits: a tile's scales as the softmax takes them, fp32: eV and 2^(-eV - 7) of all its keys and 0, behind them
+    // 2^eK of each of its 64 keys; or, with 1 in the third place, 0, 0, 64 ones, eV of each and 2^eK of each
     static constexpr uint32_t K_SLOT_BYTES = KV8 ? (uint32_t)(kTile * D) : SLOT_BYTES;
     static __host__ __device__ constexpr uint32_t slot_offset(int which, int s) {      // of the s-th slot of a ring
         return OFF_RING + (which ? RING_K * K_SLOT_BYTES + (uint32_t)s * SLOT_BYTES : (uint32_t)s * K_SLOT_BYTES);
@@ -353,9 +354,9 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
-// The largest exponent of a tile's rows, `bytes` being the scale bytes of this lane's rows key and key + 1; whether the others lie at most kNearExponents
-// below it.  (Rows of zeros, which have the least exponent, are no exception: what their keys weigh must not stand in the others' way.)  False where a row
-// is not finite.
+// The largest exponent of a tile's rows, `bytes` being the scale bytes of this lane's rows key and key + 1; whether the
+// others lie at most kNearExponents below it.  (Rows of zeros, which have the least exponent, are no exception: what
+// their keys weigh must not stand in the others' way.)  False where a row is not finite.
 __device__ __forceinline__ bool tile_exponents(uint32_t bytes, int key, int rows, int& top) {
     int hi = kKv8LeastExponent, lo = 1000;
 #pragma unroll
@@ -373,8 +374,8 @@ __device__ __forceinline__ bool tile_exponents(uint32_t bytes, int key, int rows
 // 2^(byte - 127 - top) as f16, of a row that is near (others, behind the sequence's end, get something finite).
 __device__ __forceinline__ uint32_t near_factor(uint32_t byte, int top) { return (uint32_t)min(max((int)byte - 127 - top + 15, 1), 15) << 10; }
 
-// How a producer of the 8-bit cache goes through a CTA's tiles: the item at hand and the one behind it, the place in it, the page ids of the tile's group (one to a
-// lane) and of the group behind (or of the next item's first).
+// How a producer of the 8-bit cache goes through a CTA's tiles: the item at hand and the one behind it, the place in
+// it, the page ids of the tile's group (one to a lane) and of the group behind (or of the next item's first).
 struct TileCursor {
     TItem cur, nxt;
     int pages, pages_nxt, ii, t;
@@ -418,8 +419,9 @@ struct TileCursor {
     }
 };
 
-// Producer of K tiles out of the 8-bit cache, one warp.  The MMAs take the codes as they are (kind::f8f6f4; Q is the sum of two rows of e4m3, see f8_row), so a tile is four
-// TMA copies; what the warp has to work out is the tile's scales for the softmax.  Their bytes come one tile ahead, two rows to a lane.
+// Producer of K tiles out of the 8-bit cache, one warp.  The MMAs take the codes as they are (kind::f8f6f4; Q is the
+// sum of two rows of e4m3, see f8_row), so a tile is four TMA copies; what the warp has to work out is the tile's
+// scales for the softmax.  Their bytes come one tile ahead, two rows to a lane.
 template <int D>
 __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorMap* map, const uint8_t* __restrict__ scales, int lane, int i0, int i1, const int32_t* head,
                                                uint32_t bar0, uint32_t sbase, uint8_t* smem, volatile int* abort_flag) {
@@ -460,8 +462,9 @@ __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorM
         if (lane < npages && !stall)
             asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                          ::"r"(sbase + Geo::slot_offset(0, s) + (uint32_t)lane * (kPage * D)), "l"(map), "r"(0), "r"(0), "r"(kv_head), "r"(2 * id), "r"(full) : "memory");
-        // What the softmax needs of the tile: every key's 2^eK; the tile's eV and 2^(-eV - 7), or every key's eV.  A row of V that is not finite (its codes are
-        // zeros) makes its key's score NaN, so that only those who see it are hit.  Keys behind the end are masked, whatever stands here.
+        // What the softmax needs of the tile: every key's 2^eK; the tile's eV and 2^(-eV - 7), or every key's eV.  A
+        // row of V that is not finite (its codes are zeros) makes its key's score NaN, so that only those who see it
+        // are hit.  Keys behind the end are masked, whatever stands here.
         const uint32_t k_now = bytes_k, v_now = bytes_v;
         if (begins) most = -1000;
         take();
@@ -499,9 +502,10 @@ __device__ __forceinline__ void kv8_k_producer(const DevPlan& p, const CUtensorM
         while (!mbar_try_wait(bar(Geo::kRingFull0 + Geo::slot(0, k)), (uint32_t)ring_use(k, Geo::RING_K) & 1u) && clock64() - t0 < kWaitCycles) {}
 }
 
-// Producer of one page of every V tile out of the 8-bit cache, one warp: the P V MMAs read the codes as f16, which holds them exactly, in the layout
-// that the TMA copies of the bf16 cache leave, with their scales as far as these are near each other (see kNearExponents).  A lane holds D / 32 pieces of
-// 16 codes of its page, for two tiles: the piece of the tile after next is requested when that of the one at hand has been turned and stored.
+// Producer of one page of every V tile out of the 8-bit cache, one warp: the P V MMAs read the codes as f16, which
+// holds them exactly, in the layout that the TMA copies of the bf16 cache leave, with their scales as far as these are
+// near each other (see kNearExponents).  A lane holds D / 32 pieces of 16 codes of its page, for two tiles: the piece
+// of the tile after next is requested when that of the one at hand has been turned and stored.
 template <int D>
 __device__ __forceinline__ void kv8_v_producer(const DevPlan& p, const uint8_t* __restrict__ pool8, const uint8_t* __restrict__ scales, int part, int lane, int i0, int i1,
                                                const int32_t* head, uint32_t bar0, uint8_t* smem, volatile int* abort_flag) {
@@ -510,13 +514,14 @@ __device__ __forceinline__ void kv8_v_producer(const DevPlan& p, const uint8_t* 
     constexpr int kMine = kPage * kPieces / 32;           // a lane's pieces of a page: 4 or 2
     constexpr int kRowsPerOp = 32 / kPieces;              // rows that a warp instruction moves
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    // The row of a lane's first piece, and which piece of the row it is.  Eight lanes take four pieces of two rows next to each other, so that
-    // the 16 bytes that each of them stores at once, at an even piece of an even row or an odd one of an odd row, meet all banks.
+    // The row of a lane's first piece, and which piece of the row it is.  Eight lanes take four pieces of two rows next
+    // to each other, so that the 16 bytes that each of them stores at once, at an even piece of an even row or an odd
+    // one of an odd row, meet all banks.
     const int piece = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
     const int row0 = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
     static_assert(kRowsPerOp == 4 || kRowsPerOp == 8, "rows of a warp instruction");
-    // Where the two 16-byte halves of a piece go inside a page (pieces XOR-swizzled by row): those of row0; four rows further on it is the same place with bit 6
-    // turned, 512 bytes on.
+    // Where the two 16-byte halves of a piece go inside a page (pieces XOR-swizzled by row): those of row0; four rows
+    // further on it is the same place with bit 6 turned, 512 bytes on.
     const uint32_t at_row = (uint32_t)part * Geo::PAGE_BYTES + (uint32_t)(piece >> 2) * Geo::ATOM_BYTES + (uint32_t)row0 * 128u +
                             ((uint32_t)(2 * (piece & 3)) ^ (uint32_t)row0) * 16u;
     const uint32_t src_lane = (uint32_t)row0 * D + (uint32_t)piece * 16u;
@@ -582,15 +587,16 @@ __device__ __forceinline__ void kv8_v_producer(const DevPlan& p, const uint8_t* 
 }
 
 // The whole kernel body, called by all twelve warps with `smem` 1024-byte aligned.
-// ALONE: in the kernel of steps that have span tiles only.  A launch starts on cold instruction caches, and there every line
-// of code that is fetched for the first time stands in the way: the P V of an unfinished last tile is a loop, and the output rows
-// go out in two passes of four at head_dim 128 (at 64, where a warp has one or two slices, two passes are slower).  us of
-// attention, unrolled | so, before the tiles came by TMA in brackets: 4 sequences of 100-300 keys with spans of 20-60 tokens
-// 14.04 | 13.68 (14.04), one span over 2000 keys 15.6 | 15.1 (15.2), head_dim 64 9.57 | 9.47 (9.18), 24 sequences with spans of 33-96
-// tokens 70.3 | 69.1, 8192 tokens 545 | 528.  Beside the warp body's code it is a loss: 8 sequences of 32-131 K keys with two
-// 256-token spans 917 | 925.
-// KV8: the cache is the 8-bit one, at `pool8` and `scales`, span_map is that of its K blocks (pool is not used): kv8_k_producer and kv8_v_producer.  ROLE: this call is
-// warps 0-7's (0) or those behind (1), whose registers differ, or everybody's (-1).
+// ALONE: in the kernel of steps that have span tiles only.  A launch starts on cold instruction caches, and there every
+// line of code that is fetched for the first time stands in the way: the P V of an unfinished last tile is a loop, and
+// the output rows go out in two passes of four at head_dim 128 (at 64, where a warp has one or two slices, two passes
+// are slower).  us of attention, unrolled | so, before the tiles came by TMA in brackets: 4 sequences of 100-300 keys
+// with spans of 20-60 tokens 14.04 | 13.68 (14.04), one span over 2000 keys 15.6 | 15.1 (15.2), head_dim 64 9.57 | 9.47
+// (9.18), 24 sequences with spans of 33-96 tokens 70.3 | 69.1, 8192 tokens 545 | 528.  Beside the warp body's code it
+// is a loss: 8 sequences of 32-131 K keys with two 256-token spans 917 | 925.
+// KV8: the cache is the 8-bit one, at `pool8` and `scales`, span_map is that of its K blocks (pool is not used):
+// kv8_k_producer and kv8_v_producer.  ROLE: this call is warps 0-7's (0) or those behind (1), whose registers differ,
+// or everybody's (-1).
 template <int D, int G, bool ALONE, bool KV8 = false, int ROLE = -1>
 __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* span_map, const __nv_bfloat16* __restrict__ q,
                                         const __nv_bfloat16* pool,
@@ -606,8 +612,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
     const int lane = threadIdx.x & 31;
     const int warp = threadIdx.x >> 5;
     const int Hq = p.num_q_heads, Hkv = p.num_kv_heads;
-    // The plan is there when this kernel starts (behind an upload by kernel the first launch starts when that has completed: PlanUse),
-    // so it may be read before pdl_wait(); everything else (pool, q, outputs) is touched only after it.
+    // The plan is there when this kernel starts (behind an upload by kernel the first launch starts when that has
+    // completed: PlanUse), so it may be read before pdl_wait(); everything else (pool, q, outputs) is touched only
+    // after it.
     const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
     const int i0 = head[0], i1 = head[1];
     const Work* head_work = reinterpret_cast<const Work*>(head + kHeadWorkTensor);      // = p.works[i0]
@@ -706,7 +713,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                     }
                     __syncwarp();
                     int page = __shfl_sync(0xffffffffu, pages_cur, (t - t0) * kPagesPerTile + min(lane, npages - 1));
-                    // checked build only: a bad id is replaced by page 0 (the copy must happen: the barrier counts its bytes)
+                    // checked build only: a bad id is replaced by page 0 (the copy must happen: the barrier counts its
+                    // bytes)
                     if (lane < npages && !page_ok(page, p.num_pages, p.status, kStatusBadPageSpan)) page = 0;
                     if (lane < npages_tma && !stall)
                         tma_page(slot_addr + (uint32_t)lane * Geo::PAGE_BYTES, span_map, (2 * page + which) * Hkv + cur.kv_head, full);
@@ -753,9 +761,10 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
         int base = 0;             // KV tiles before this item
         int cnt = 0;              // tiles of the group before this item: S buffer and phase of the hand-offs
         int item_no = 0;
-        // The warps take turns, group 0 first, whether they have MMAs to issue or not: turn n of warp 1 follows turn n of
-        // warp 0, turn n of warp 0 follows turn n - 1 of warp 1.  Not only for speed: a turn's waits for tiles stand in front of its
-        // token, and that order is what makes the parities of the ring's full barriers unambiguous (see span_ring.h).
+        // The warps take turns, group 0 first, whether they have MMAs to issue or not: turn n of warp 1 follows turn n
+        // of warp 0, turn n of warp 0 follows turn n - 1 of warp 1.  Not only for speed: a turn's waits for tiles stand
+        // in front of its token, and that order is what makes the parities of the ring's full barriers unambiguous (see
+        // span_ring.h).
         int turn_no = 0;
         auto take_token = [&](bool& good) {
             good = good && (b + turn_no == 0 || mbar_wait_spin(bar(Geo::kToken0 + b), (uint32_t)(turn_no + b + 1) & 1u, abort_flag, p.status, 28));
@@ -812,9 +821,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 if (lane == 0) trace_event(b ? 10 : 0, ev, 20 + b);
                 if (pv) wait_tile(1, vp, 24);
                 if (qk) wait_tile(0, kp, 21);
-                // The tiles were written by TMA copies, but for the rows of an unfinished last V page: those came by cp.async,
-                // through the generic proxy, and the MMAs read through the asynchronous one.  The full barrier orders
-                // the two, the fence makes the bytes visible across.
+                // The tiles were written by TMA copies, but for the rows of an unfinished last V page: those came by
+                // cp.async, through the generic proxy, and the MMAs read through the asynchronous one.  The full
+                // barrier orders the two, the fence makes the bytes visible across.
                 if (pv && last_page_by_rows(it.kv_end, j == ntiles - 1, kPage)) fence_async_smem();
                 const uint32_t buf = tmem + kColS + 128u * (uint32_t)b + 64u * (uint32_t)(c & 1);      // S and P
                 const uint64_t vd = smem_desc(tile_addr(1, vp), Geo::ATOM_BYTES, Geo::GROUP_BYTES);
@@ -851,7 +860,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                     for (int ks = 0; ks < D / 16; ++ks) {
                         if (ks == D / 16 - 2) pass_token();      // the other warp's first MMA queues behind the last two
                         if constexpr (KV8) {
-                            // Q is hi + lo, a tile each of one byte a value; a step is 32 values, and K's are the same for both
+                            // Q is hi + lo, a tile each of one byte a value; a step is 32 values, and K's are the same
+                            // for both
                             constexpr int kSteps = D / 32;
                             const uint64_t step = (uint64_t)((uint32_t)(ks % kSteps) * 32u >> 4);
                             mma_f8(el, buf, qd + (uint64_t)((uint32_t)(ks / kSteps) * (uint32_t)(kRows * D) >> 4) + step, kd + step, idesc_qk, ks > 0);
@@ -927,9 +937,10 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
 #pragma unroll
             for (int c = 0; c < kQV; ++c) w[c] = valid ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
         };
-        // and as e4m3, scaled by a power of two to a largest value in 2^7 .. 2^8, in two parts: bf16's eight bits are those of a code and of the code of what
-        // is left, exactly down to 2^-9 of the largest value, and off by 2^-17 of it at most below.  Puts the thread's share (all of the row, or value half b) into
-        // the Q tile and returns the factor on the scores: NaN for a row with a value that is not finite (whose codes are the largest ones).
+        // and as e4m3, scaled by a power of two to a largest value in 2^7 .. 2^8, in two parts: bf16's eight bits are
+        // those of a code and of the code of what is left, exactly down to 2^-9 of the largest value, and off by 2^-17
+        // of it at most below.  Puts the thread's share (all of the row, or value half b) into the Q tile and returns
+        // the factor on the scores: NaN for a row with a value that is not finite (whose codes are the largest ones).
         auto f8_row = [&](const uint4 (&w)[kQV], bool dual) {
             uint32_t most = 0;
 #pragma unroll
@@ -969,8 +980,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             if (most >= 0x7f80u) return __uint_as_float(0x7fffffffu);
             return fmaxf(__uint_as_float((e - 7u) << 23) * qscale, FLT_MIN);      // (a masked score is -inf, and stays it)
         };
-        // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.  (8 bits: a K slot
-        // after two of each of four warps, all of which wait for the tile themselves: one that came late would find the slot's next phase over.)
+        // A ring slot is free again after two arrivals: one of each group in a dual item, else two of its only reader.
+        // (8 bits: a K slot after two of each of four warps, all of which wait for the tile themselves: one that came
+        // late would find the slot's next phase over.)
         auto release = [&](int which, int t, bool dual) { mbar_arrive_n(bar(Geo::kRingEmpty0 + Geo::slot(which, t)), dual ? 1u : 2u); };
         TItem it_next = load_titem(head_work, i0 < i1);
         uint4 q_next[kQV];
@@ -1014,9 +1026,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const int j = dual ? u : 2 * u + b, ct = cnt + u;
                 const int npg = (min(kTile, it.kv_end - (it.kv0 + j * kTile)) + kPage - 1) / kPage;
                 const uint32_t sb = s_addr + 64u * (uint32_t)(ct & 1);
-                // (8 bits) the tile's scales were written before its K tile was handed over, which is waited for here, too, in front of its
-                // scores: the slot is this tile's until the release below, and the tile it held before was this group's or an earlier item's, so the
-                // phase before is over
+                // (8 bits) the tile's scales were written before its K tile was handed over, which is waited for here,
+                // too, in front of its scores: the slot is this tile's until the release below, and the tile it held
+                // before was this group's or an earlier item's, so the phase before is over
                 const float* tile_scales = nullptr;
                 float4 tile = make_float4(0.f, 0.f, 0.f, 0.f);
                 float x_scale = row_scale;
@@ -1063,9 +1075,11 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 if (KV8 ? lane == 0 : m == 0) release(0, kv_base + j, dual);
                 if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
                 tmem_wait_ld();
-                // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V, whose tile leaves eV out: the tile's
-                // eV, which comes in below, or each key's, which has been added above and written back (in a loop over tensor memory: as a branch on the
-                // values in registers, with one like it for the sum, this rare path slowed the usual one down, a prompt of 7777 tokens 735 | 684 us)
+                // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V,
+                // whose tile leaves eV out: the tile's eV, which comes in below, or each key's, which has been added
+                // above and written back (in a loop over tensor memory: as a branch on the values in registers, with
+                // one like it for the sum, this rare path slowed the usual one down, a prompt of 7777 tokens 735 | 684
+                // us)
                 if constexpr (KV8) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -1144,8 +1158,9 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 const float2 nm2 = make_float2(-m_use, -m_use);
                 uint32_t pk[32];
                 if constexpr (KV8) {
-                    // P' = exp2(x - m_ref + 7) as f16 (11 bits; see kKv8WeightShift); the sum takes it without the scale of V: 2^(-eV - 7) times it, or,
-                    // where every key has its own, by exponentials of its own (and 0 times it)
+                    // P' = exp2(x - m_ref + 7) as f16 (11 bits; see kKv8WeightShift); the sum takes it without the
+                    // scale of V: 2^(-eV - 7) times it, or, where every key has its own, by exponentials of its own
+                    // (and 0 times it)
                     const float bias = tile.x - (m_use - (float)kKv8WeightShift);
                     const float2 scale2 = make_float2(x_scale, x_scale), b2 = make_float2(bias, bias);
                     float2 s2 = make_float2(0.f, 0.f), s2b = s2;

@@ -140,8 +140,9 @@ __device__ __forceinline__ void tma_page_kv(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(0), "r"(kv_head), "r"(2 * page), "r"(bar) : "memory");
 }
 
-// The same for the 8-bit cache: a 4-D tensor of bytes (d values, 16 slots, Hkv heads, 2 * pages) and a box of (d, 16, 1, 2), rows swizzled over 128 bytes at
-// head_dim 128 and over 64 at head_dim 64 (piece c of slot s at c ^ (s & 7), or c ^ (s / 2 & 3)).
+// The same for the 8-bit cache: a 4-D tensor of bytes (d values, 16 slots, Hkv heads, 2 * pages) and a box of (d, 16,
+// 1, 2), rows swizzled over 128 bytes at head_dim 128 and over 64 at head_dim 64 (piece c of slot s at c ^ (s & 7), or
+// c ^ (s / 2 & 3)).
 __device__ __forceinline__ void tma_page_kv8(uint32_t dst, const CUtensorMap* map, int kv_head, int page, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -199,7 +200,8 @@ struct Geometry {
     static constexpr int STAGE_BYTES = STAGE_PAGES * PAGE_BYTES;      // 64 KiB; 8 bits at head_dim 64: 32 KiB
     static constexpr int KV8_STAGES = D == 128 ? 3 : 6;         // as many as fit
     static constexpr int SCALE_BYTES = KV8 ? STAGE_PAGES * kKv8ScaleBytes : 0;      // of a stage, behind all stages' pages
-    // Where page i of a stage lies in it.  8 bits: the two pages of a warp side by side, so that its merge state fits into their place.
+    // Where page i of a stage lies in it.  8 bits: the two pages of a warp side by side, so that its merge state fits
+    // into their place.
     static __device__ __forceinline__ int page_slot(int i) { return KV8 ? i % kWarps * 2 + i / kWarps : i; }
     static constexpr int WARP_BYTES = KV8 ? WARP_PAGES * PAGE_BYTES : PAGE_BYTES;      // from one warp's merge state to the next one's
     static constexpr int Q_BYTES = kCols * D * 2;               // the unit's query rows, [column][d]
@@ -252,11 +254,11 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
         }
         const uint8_t* stage = stage_base + (size_t)d.stage * Geo::STAGE_BYTES;
         const int ncols = d.ntok * G;
-        // The weights first, a (column, warp) pair to a lane (four columns at once, the other four of a unit with more behind
-        // them); the passes over the values get them by shuffle.  With weights worked out in every lane and pass, this stood between an
-        // item's last page and its result for 1.95 us at 4 columns of 128, 1.15 now (us a layer from a graph: 4 decoding sequences
-        // 12.66 -> 11.83, 64 over 1-3 K keys 82.6 -> 80.9, 32 with 8 spans 58.6 -> 57.0).  Unrolled passes are slower (12.02): a CTA
-        // of a short step fetches this code once.
+        // The weights first, a (column, warp) pair to a lane (four columns at once, the other four of a unit with more
+        // behind them); the passes over the values get them by shuffle.  With weights worked out in every lane and
+        // pass, this stood between an item's last page and its result for 1.95 us at 4 columns of 128, 1.15 now (us a
+        // layer from a graph: 4 decoding sequences 12.66 -> 11.83, 64 over 1-3 K keys 82.6 -> 80.9, 32 with 8 spans
+        // 58.6 -> 57.0).  Unrolled passes are slower (12.02): a CTA of a short step fetches this code once.
         auto state = [&](int w) { return reinterpret_cast<const float*>(stage + (size_t)w * Geo::WARP_BYTES); };
         float wgt[2] = {0.f, 0.f}, inv[2] = {0.f, 0.f}, lse2[2] = {0.f, 0.f};
 #pragma unroll
@@ -324,9 +326,9 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
         if (lane == 0) mbar_arrive_n(empty0 + 8 * d.stage, kWarps);
         if (d.partial_row < 0) continue;
         // ---- a chunk of a split unit: count it in; the CTA that completes the unit merges it
-        // This warp's partial rows are visible device-wide before the count moves, and the others' once it has: the merge warp gets the
-        // request through shared memory behind it and reads past L1.  (A fence here and one there took 0.5 us each: 4
-        // decoding sequences 11.41 -> 11.13 us a layer.)
+        // This warp's partial rows are visible device-wide before the count moves, and the others' once it has: the
+        // merge warp gets the request through shared memory behind it and reads past L1.  (A fence here and one there
+        // took 0.5 us each: 4 decoding sequences 11.41 -> 11.13 us a layer.)
         __syncwarp();
         int last = 0;
         if (lane == 0) {
@@ -338,11 +340,11 @@ __device__ __forceinline__ void epilogue_loop(const DevPlan& p, __nv_bfloat16* _
     }
 }
 
-// The merge warp's loop: LSE = log sum_c exp(LSE_c), O = sum_c exp(LSE_c - LSE) O_c over the chunks
-// of a completed split unit, in chunk order.  All chunks are read back from memory (this CTA's own
-// included), so the result does not depend on which CTA finished the unit.
-// PARTS = 2: two warps merge every unit, half of the passes each and twice as many chunks at once, so that up to eight chunks of
-// 128 values a head cost one round trip.
+// The merge warp's loop: LSE = log sum_c exp(LSE_c), O = sum_c exp(LSE_c - LSE) O_c over the chunks of a completed
+// split unit, in chunk order.  All chunks are read back from memory (this CTA's own included), so the result does not
+// depend on which CTA finished the unit.
+// PARTS = 2: two warps merge every unit, half of the passes each and twice as many chunks at once, so that up to eight
+// chunks of 128 values a head cost one round trip.
 template <int D, int G, int PARTS>
 __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __restrict__ out,
                                            float* __restrict__ lse, const TileDesc* merge_req,
@@ -356,9 +358,9 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
         constexpr int kPasses = 4 * D / 128 / PARTS, kAtOnce = 16 / kPasses;      // of four columns; chunks requested together
         const int value0 = 128 * kPasses * part;      // of the four columns' values: this warp's first
         // Four columns at a time, in passes of 128 values, four consecutive ones to a lane.  The weights come from one
-        // (column, chunk) pair to a lane, eight chunks at once; values and log-sum-exps are requested together, so that a unit of up to
-        // kAtOnce chunks costs one round trip to L2.  (Four columns of 128, up to eight chunks: 2.2 us with weights in every lane and
-        // pass, 1.8 so; 4 decoding sequences 11.83 -> 11.41 us a layer.)
+        // (column, chunk) pair to a lane, eight chunks at once; values and log-sum-exps are requested together, so that
+        // a unit of up to kAtOnce chunks costs one round trip to L2.  (Four columns of 128, up to eight chunks: 2.2 us
+        // with weights in every lane and pass, 1.8 so; 4 decoding sequences 11.83 -> 11.41 us a layer.)
         for (int c4 = 0; c4 < ncols; c4 += 4) {
             float4 acc[kPasses];
             bool on[kPasses];
@@ -449,23 +451,27 @@ __device__ __forceinline__ void merge_loop(const DevPlan& p, __nv_bfloat16* __re
 }
 
 // One consumer warp's two pages of a stage of the 8-bit cache, as two independent chains.
-//   A code is at most 448 and exact in f16, and so are the products of an f16 MMA, so both contractions take the codes as they are:
+//   A code is at most 448 and exact in f16, and so are the products of an f16 MMA, so both contractions take the codes
+// as they are:
 //       x = (sum_i cK_i q'_i) * (query scale * 2^eK) + eV      in fp32: the score, and the V row's scale as an exponent
 //       O += P' cV,  P' = p * 2^eV * 2^7 = exp2(x - ref + 7)
-// P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere; one that counts as zero lies 2^-32 below
-// the largest x (kKv8WeightShift).  The softmax sum is that of P' 2^(-eV - 7) in fp32, against the same reference; where an eV lies outside a
-// window within which P' cannot have vanished and yet count (kLeastWindow; rows of zeros have the least exponent of all), the pages' sums take
-// exponentials of their own; from an eV above it on, all pages of the item do.  Against two references, one for sums and one for weights, this saves half of the
-// exponentials.
-//   The sum is in units of 2^ref, which follows x, not the score: where the first keys' V are zeros (eV = -100) and later ones large, it is near 2^100 when
-// the reference moves by more than 2^126, and counts for as much as before.  So it takes that factor in two steps of its root.  (O, whose
-// units are those of x, loses nothing that counts.)  Beside a row of V with an eV above 95 (values of 10^31) weights below 2^(eV - 126) of its own are missing
-// from the sum.
-//   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes of a row, values 4 t .. 4 t + 3 of a
-// 16-value piece: the first two are one k step's low half, the others its high half, and Q is laid out alike.  V (transposed): two neighbouring
-// values of two neighbouring keys; a byte permutation pairs the keys, and value 2 g becomes row g of the piece's MMA, 2 g + 1 row g + 8.
-//   Cycles of a warp's two pages at head_dim 128 (64): 2030 (1480), of which the K and V parts with their 64 (32) cvt each 550 (290).  Turning codes into f16 with
-// integer instructions, seven for four codes, takes the K part to 1100 (570).
+// P' is rounded to f16 (11 bits) against the running maximum of x, so weights and scales may lie anywhere; one that
+// counts as zero lies 2^-32 below the largest x (kKv8WeightShift).  The softmax sum is that of P' 2^(-eV - 7) in fp32,
+// against the same reference; where an eV lies outside a window within which P' cannot have vanished and yet count
+// (kLeastWindow; rows of zeros have the least exponent of all), the pages' sums take exponentials of their own; from an
+// eV above it on, all pages of the item do.  Against two references, one for sums and one for weights, this saves half
+// of the exponentials.
+//   The sum is in units of 2^ref, which follows x, not the score: where the first keys' V are zeros (eV = -100) and
+// later ones large, it is near 2^100 when the reference moves by more than 2^126, and counts for as much as before.  So
+// it takes that factor in two steps of its root.  (O, whose units are those of x, loses nothing that counts.)  Beside a
+// row of V with an eV above 95 (values of 10^31) weights below 2^(eV - 126) of its own are missing from the sum.
+//   ldmatrix moves 16-bit units, so a thread gets the codes in pairs of bytes.  K (A operand, rows = keys): four bytes
+// of a row, values 4 t .. 4 t + 3 of a 16-value piece: the first two are one k step's low half, the others its high
+// half, and Q is laid out alike.  V (transposed): two neighbouring values of two neighbouring keys; a byte permutation
+// pairs the keys, and value 2 g becomes row g of the piece's MMA, 2 g + 1 row g + 8.
+//   Cycles of a warp's two pages at head_dim 128 (64): 2030 (1480), of which the K and V parts with their 64 (32) cvt
+// each 550 (290).  Turning codes into f16 with integer instructions, seven for four codes, takes the K part to 1100
+// (570).
 constexpr uint32_t kLeastWindow = 87, kWindow = 95;      // scale bytes 87 .. 182: 2^-40 .. 2^55
 
 template <int D, int G>
@@ -480,9 +486,9 @@ __device__ __forceinline__ void pages_kv8(const TileDesc& d, uint8_t* stage, uin
     const uint32_t row = (uint32_t)key * D, swz = D == 128 ? (uint32_t)(key & 7) : (uint32_t)(key >> 1 & 3);
     const uint32_t page0 = smem_u32(stage) + (uint32_t)Geo::page_slot(warp) * Geo::PAGE_BYTES;      // the other page follows
     if ((WP - 1) * kWarps * kPage + (warp + 1) * kPage > d.rows) {
-        // Slots past the sequence's end hold whatever was there before, NaN codes included: their scores are masked below, but 0 * NaN would still poison
-        // P V, so their V rows are cleared, and whatever their scales are, they are not to have a say in which form the sums take.  That goes for a whole page behind
-        // the end, too.
+        // Slots past the sequence's end hold whatever was there before, NaN codes included: their scores are masked
+        // below, but 0 * NaN would still poison P V, so their V rows are cleared, and whatever their scales are, they
+        // are not to have a say in which form the sums take.  That goes for a whole page behind the end, too.
         static_assert(WP * kPage == 32, "a slot to a lane");
         const int page = (lane / kPage) * kWarps + warp;
         if (page * kPage + lane % kPage >= d.rows) stage_scales[page * kKv8ScaleBytes + kPage + lane % kPage] = 127;
@@ -707,8 +713,9 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             pages_cur = head[kHeadPagesCuda + lane];
             if constexpr (APPEND) unappended_from = cur.kv_limit0 - 1 - (cur.q_row0 - cur.q_seq0);
         }
-        // The plan is there when this kernel starts (behind an upload by kernel the first launch starts when that has completed: PlanUse),
-        // so all of the above overlaps the tail of the kernel in front; the pool, Q and the queue are touched only from here on.
+        // The plan is there when this kernel starts (behind an upload by kernel the first launch starts when that has
+        // completed: PlanUse), so all of the above overlaps the tail of the kernel in front; the pool, Q and the queue
+        // are touched only from here on.
         pdl_wait();
         if (cur.kv_end == 0) cur = take();      // a CTA that came from span tiles starts on the queue
         while (cur.kv_end > 0 && ok) {
@@ -757,8 +764,8 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                     if (lane < npages && !page_ok(page, p.num_pages, p.status, kStatusBadPageWarp)) page = 0;
                     if (lane == 0) { if (n == 0) trace_mark(2); trace_add(6, 1); if (first) trace_add(5, 1); }
                     if constexpr (KV8) {
-                        // The pages, one TMA copy each, and their 32 scale bytes, by cp.async, 16 bytes a lane: another TMA copy for them
-                        // would cost the copy unit more than their bytes do.
+                        // The pages, one TMA copy each, and their 32 scale bytes, by cp.async, 16 bytes a lane: another
+                        // TMA copy for them would cost the copy unit more than their bytes do.
                         const int scale_page = __shfl_sync(0xffffffffu, page, lane >> 1);
                         if (lane < npages)
                             tma_page_kv8(smem_u32(stage_base + (size_t)s * Geo::STAGE_BYTES + (size_t)Geo::page_slot(lane) * Geo::PAGE_BYTES),
@@ -814,8 +821,9 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         epilogue_loop<D, G, KV8>(p, out, lse, stage_base, handoff, merge_req, empty0, done0, req0, reqfree0, abort_flag);
         return;
     }
-    // Where nothing is queued and a CTA has one item at most, the fetch warp has nothing to fetch and is a second merge warp.  (Such a
-    // step is short and ends on its merges: 4 decoding sequences over 0.5-4 K keys 11.14 -> 10.69 us a layer.)
+    // Where nothing is queued and a CTA has one item at most, the fetch warp has nothing to fetch and is a second merge
+    // warp.  (Such a step is short and ends on its merges: 4 decoding sequences over 0.5-4 K keys 11.14 -> 10.69 us a
+    // layer.)
     auto two_mergers = [&]() {
         const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
         return p.queue_count == 0 && head[3] - head[2] <= 1;
@@ -887,10 +895,11 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
 
     if constexpr (ROLE == 1) return;
     // ---------------------------------------------------------------------- consumer warps
-    // Pages ahead of the ring, only where they pay: in the kernel of steps without span tiles, and for items that are not all latency.
-    // (us a layer from a graph, without | with: 4 decoding sequences over 0.5-4 K keys 13.6 | 12.6, 64 over 1-3 K 87.3 | 85.7; with
-    // span tiles, where a longer append kernel in front competes for the memory, 32 sequences with 8 spans 69.9 |
-    // 70.6, and for the span tiles themselves 24 sequences with a span each 74.6 | 78.9; 4 sequences of 100-300 keys 8.4 | 8.7.)
+    // Pages ahead of the ring, only where they pay: in the kernel of steps without span tiles, and for items that are
+    // not all latency. (us a layer from a graph, without | with: 4 decoding sequences over 0.5-4 K keys 13.6 | 12.6, 64
+    // over 1-3 K 87.3 | 85.7; with span tiles, where a longer append kernel in front competes for the memory, 32
+    // sequences with 8 spans 69.9 | 70.6, and for the span tiles themselves 24 sequences with a span each 74.6 | 78.9;
+    // 4 sequences of 100-300 keys 8.4 | 8.7.)
     if constexpr (PREFETCH) {
         const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
         const Work* w = reinterpret_cast<const Work*>(head + kHeadWorkCuda);
@@ -932,9 +941,10 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             const uint8_t* qs = q_base + (size_t)s * Geo::Q_BYTES;
             const bool col_valid = g < d.ntok * G;
             if constexpr (KV8) {
-                // The codes go to the tensor core as f16, which holds them exactly; so does the query row, by an f16 copy divided by the
-                // power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25 below that value).  A row with a value that is not
-                // finite has NaN for its scale, and so for its scores.
+                // The codes go to the tensor core as f16, which holds them exactly; so does the query row, by an f16
+                // copy divided by the power of two of its largest value (bf16's eight bits fit; what is lost lies 2^-25
+                // below that value).  A row with a value that is not finite has NaN for its scale, and so for its
+                // scores.
                 // Thread (g, t4) holds values 16 ks + 4 t4 .. + 3: the order in which ldmatrix deals out a row's bytes.
                 uint2 w[Geo::KSTEPS];
                 uint32_t most = 0;
@@ -970,11 +980,12 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
             l0 = l1 = 0.f;
             large = false;
         }
-        // This warp's pages inside the stage: `warp` and, at head_dim 64, the one kWarps behind it.  Two pages at once are two
-        // independent chains of loads, MMAs and exponentials: with one, a warp took as long for a page as at head_dim 128, for half the
-        // bytes, and that time bound a CTA.  (ns for 128 keys of head_dim 64, one page | two: one CTA alone 710 | 528, 56 of them 730 |
-        // 577, 148, which memory bounds, 768 | 644; us of attention a layer: 64 decoding sequences of 32/8 heads over 1-3 K keys
-        // 47.8 -> 44.6, 256 of 8/2 heads 29.9 -> 27.8, 32 with 8 spans 49.1 -> 46.3, 100 of 8/2 heads with 20 spans 49.2 -> 42.0.)
+        // This warp's pages inside the stage: `warp` and, at head_dim 64, the one kWarps behind it.  Two pages at once
+        // are two independent chains of loads, MMAs and exponentials: with one, a warp took as long for a page as at
+        // head_dim 128, for half the bytes, and that time bound a CTA.  (ns for 128 keys of head_dim 64, one page |
+        // two: one CTA alone 710 | 528, 56 of them 730 | 577, 148, which memory bounds, 768 | 644; us of attention a
+        // layer: 64 decoding sequences of 32/8 heads over 1-3 K keys 47.8 -> 44.6, 256 of 8/2 heads 29.9 -> 27.8, 32
+        // with 8 spans 49.1 -> 46.3, 100 of 8/2 heads with 20 spans 49.2 -> 42.0.)
         constexpr int WP = Geo::WARP_PAGES;
         if constexpr (KV8) {
             if (warp * kPage < d.rows)

@@ -1,15 +1,17 @@
-// Attention over the 8-bit cache: the entry point, its kernels and launcher.  The bodies are those of the bf16 cache, with the cache's
-// format as a template parameter (attn_decode.cuh: what a consumer warp does with a page; attn_append_tc.cuh: how tiles get into shared
-// memory).  Which kernel runs follows the same rules as there (attn_kernels.cu).
+// Attention over the 8-bit cache: the entry point, its kernels and launcher.  The bodies are those of the bf16 cache,
+// with the cache's format as a template parameter (attn_decode.cuh: what a consumer warp does with a page;
+// attn_append_tc.cuh: how tiles get into shared memory).  Which kernel runs follows the same rules as there
+// (attn_kernels.cu).
 //
 // Decode is bound by memory, at half the bytes: 64 sequences of 1-3 K keys, 32 / 8 heads of 128, 51-53 us (4.9-5 TB/s),
 // 5 of 32-110 K 145-154 (5.5-5.8 TB/s).
-// Spans are bound by the softmax warps' chain: 64 keys take a CTA alone, at head_dim 128, 0.85 us with one row tile and 1.35
-// with two (0.46 | 0.81 in 16 bits), with all SMs at work 1.16 | 1.37 (0.73 | 1.19).  Without the conversion of V 0.82 | 1.26 alone, without
-// the reading of the keys' scales (64 values to each of eight warps, from shared memory) 0.81 | 1.20: neither is the bound by itself.
-// 8 spans of 8-64 tokens beside 24 decode rows over 0.5-4 K keys 75-81 us (a batch of the same kind in 16 bits 64; without either of
-// the two, other such batches take 0.95 to 1 of their time), a prompt of 7777 tokens 684-707 us, 701-724 TFLOP/s.  The kernel of both bodies spills: an
-// 88-byte frame at four heads of 128, because its registers are split once for both.
+// Spans are bound by the softmax warps' chain: 64 keys take a CTA alone, at head_dim 128, 0.85 us with one row tile and
+// 1.35 with two (0.46 | 0.81 in 16 bits), with all SMs at work 1.16 | 1.37 (0.73 | 1.19).  Without the conversion of V
+// 0.82 | 1.26 alone, without the reading of the keys' scales (64 values to each of eight warps, from shared memory)
+// 0.81 | 1.20: neither is the bound by itself. 8 spans of 8-64 tokens beside 24 decode rows over 0.5-4 K keys 75-81 us
+// (a batch of the same kind in 16 bits 64; without either of the two, other such batches take 0.95 to 1 of their time),
+// a prompt of 7777 tokens 684-707 us, 701-724 TFLOP/s.  The kernel of both bodies spills: an 88-byte frame at four
+// heads of 128, because its registers are split once for both.
 #include "asynclm.h"
 #include "attn_append_tc.cuh"
 #include "attn_decode.cuh"

@@ -1,4 +1,5 @@
-// Host side that the attention kernels' launchers share: tensor maps of the pools, the shared-memory attribute, the warp body's stages.
+// Host side that the attention kernels' launchers share: tensor maps of the pools, the shared-memory attribute, the
+// warp body's stages.
 #pragma once
 #include <cuda.h>
 
@@ -27,8 +28,10 @@ typedef CUresult (*ReplaceAddressFn)(CUtensorMap*, void*);
 // The pool as the two bodies read it, landed with the 128-byte swizzle:
 //   kv    (64 values, 16 slots, d / 64 row halves, Hkv, pages x K|V), a box is one page's K and V blocks of one kv head
 //         (dec::tma_page_kv)
-//   span  (64 values, 8 slots, d / 64 row halves, 2 groups of 8 slots, pages x K|V x Hkv), a box is one block (tc::tma_page)
-//   kv8   the 8-bit cache: (d bytes, 16 slots, Hkv, pages x K|V), a box as kv's; at head_dim 64 with the 64-byte swizzle (dec::tma_page_kv8)
+//   span  (64 values, 8 slots, d / 64 row halves, 2 groups of 8 slots, pages x K|V x Hkv), a box is one block
+// (tc::tma_page)
+//   kv8   the 8-bit cache: (d bytes, 16 slots, Hkv, pages x K|V), a box as kv's; at head_dim 64 with the 64-byte
+// swizzle (dec::tma_page_kv8)
 //   k8    the same, a box is one block (tc::kv8_k_producer)
 enum PoolMap { kKvMap, kSpanMap, kKv8Map, kK8Map };
 

@@ -1,12 +1,13 @@
-// The append of the 8-bit cache: the step's new K and V rows, quantised as they are written into their page slots, the keys (and, if
-// asked, the queries) turned by their positions on the way.
+// The append of the 8-bit cache: the step's new K and V rows, quantised as they are written into their page slots, the
+// keys (and, if asked, the queries) turned by their positions on the way.
 //
-// The interrupt block goes to the end of the context (paper Section 3.2): new token i of sequence b sits at position ctx_b + i, in the slot
-// that the planner resolved.  A row is read once, turned in fp32 (rope_rows.cuh), its largest magnitude found by shuffles over the
-// head_dim / 8 lanes that hold it, and its codes and scale written (kv8.cuh): there is one rounding between the projection's bf16 and the code.
-// It moves 3 d bytes for a K or V row and 4 d for a query row, in whole 128-byte lines at head_dim 128.  8192 tokens of 32 / 8 heads of 128,
-// queries too, 64 values of a row rotated, take 46.7 us, 4.0 TB/s: bound by instructions (72 % of the issue slots; the rotation in two parts, maxima and
-// conversions); few tokens by launch and latency, 3.6 us in a graph.
+// The interrupt block goes to the end of the context (paper Section 3.2): new token i of sequence b sits at position
+// ctx_b + i, in the slot that the planner resolved.  A row is read once, turned in fp32 (rope_rows.cuh), its largest
+// magnitude found by shuffles over the head_dim / 8 lanes that hold it, and its codes and scale written (kv8.cuh):
+// there is one rounding between the projection's bf16 and the code. It moves 3 d bytes for a K or V row and 4 d for a
+// query row, in whole 128-byte lines at head_dim 128.  8192 tokens of 32 / 8 heads of 128, queries too, 64 values of a
+// row rotated, take 46.7 us, 4.0 TB/s: bound by instructions (72 % of the issue slots; the rotation in two parts,
+// maxima and conversions); few tokens by launch and latency, 3.6 us in a graph.
 #include <algorithm>
 
 #include "kernels.h"
@@ -45,9 +46,9 @@ kv8_append_kernel(DevPlan p, const __grid_constant__ RopeTurns turns, const __gr
             l.x[u] = item < n * blocks && h0 + u * rows < set.heads ? __ldcg(reinterpret_cast<const uint4*>(in + (int64_t)(h0 + u * rows) * d)) : make_uint4(0, 0, 0, 0);
         return l;      // (not through the read-only path: q_out may be q itself)
     };
-    // The angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the kernels in front until those
-    // have completed.  Where all CTAs start at once the angles overlap the tail of the kernel in front; in a longer grid the first rows are
-    // requested in front of them.
+    // The angles come from the plan, which is there when this kernel starts (see PlanUse); rows and pool belong to the
+    // kernels in front until those have completed.  Where all CTAs start at once the angles overlap the tail of the
+    // kernel in front; in a longer grid the first rows are requested in front of them.
     const bool rows_first = gridDim.x > 148 * 2;
     Block next;
     if (rows_first) {

@@ -1,11 +1,12 @@
 // The 8-bit cache read back: ranges of sequences as dense bf16 rows.
 //
-// Output row out_indptr[b] + i is position first[b] + i of sequence b, found through the plan's page table; its values are code * 2^e, exact in
-// bf16.  Bound by memory: d + 1 bytes read and 2 d written for each K or V row.  A thread turns 8 codes into 16 bytes; head_dim / 8
-// lanes take a row, a warp 2 or 4 rows that follow each other, which in the pool are next to each other inside a page (and in the output Hkv rows
-// apart, whole 128-byte lines each). (With 16 codes to a thread
-// every store instruction leaves half of each 32-byte sector to the next one.)  The row's place is looked up once, by bisection over
-// out_indptr, and serves all its heads.  133 K tokens of 8 heads of 128 take 129-136 us, 6.0-6.3 TB/s; 700 of 2 heads of 64 2.4 in a graph.
+// Output row out_indptr[b] + i is position first[b] + i of sequence b, found through the plan's page table; its values
+// are code * 2^e, exact in bf16.  Bound by memory: d + 1 bytes read and 2 d written for each K or V row.  A thread
+// turns 8 codes into 16 bytes; head_dim / 8 lanes take a row, a warp 2 or 4 rows that follow each other, which in the
+// pool are next to each other inside a page (and in the output Hkv rows apart, whole 128-byte lines each). (With 16
+// codes to a thread every store instruction leaves half of each 32-byte sector to the next one.)  The row's place is
+// looked up once, by bisection over out_indptr, and serves all its heads.  133 K tokens of 8 heads of 128 take 129-136
+// us, 6.0-6.3 TB/s; 700 of 2 heads of 64 2.4 in a graph.
 #include <algorithm>
 
 #include "kernels.h"
@@ -38,8 +39,8 @@ kv8_gather_kernel(DevPlan p, const int64_t* out_indptr, const int32_t* first, co
     const int64_t i = row - __ldg(out_indptr + b), pos = __ldg(first + b) + i;
     const int64_t length = (int64_t)__ldg(p.kv_len_before + b) + __ldg(p.q_indptr + b + 1) - __ldg(p.q_indptr + b);
     const int64_t at = (int64_t)__ldg(p.page_indptr + b) + pos / kPage;
-    // Ranges come from device memory and the planner does not look at the pages of sequences without new tokens: whatever lies outside the sequence,
-    // its pages or the pool is reported and left out.
+    // Ranges come from device memory and the planner does not look at the pages of sequences without new tokens:
+    // whatever lies outside the sequence, its pages or the pool is reported and left out.
     int64_t page = -1;
     if (i >= 0 && row < __ldg(out_indptr + b + 1) && pos >= 0 && pos < length && at < __ldg(p.page_indptr + b + 1)) page = __ldg(p.page_indices + at);
     if (page < 0 || page >= p.num_pages) {

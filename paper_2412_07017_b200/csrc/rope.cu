@@ -1,5 +1,6 @@
-// Rotary positions of query and key rows, for caches that stay in bf16 (the fused form for the 8-bit cache is kv8_append.cu; the
-// mathematics and the division among threads are in rope_rows.cuh), and the table of frequencies that both take.
+// Rotary positions of query and key rows, for caches that stay in bf16 (the fused form for the 8-bit cache is
+// kv8_append.cu; the mathematics and the division among threads are in rope_rows.cuh), and the table of frequencies
+// that both take.
 #include <math.h>
 
 #include <algorithm>
@@ -17,7 +18,8 @@ constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 struct RopeSets { RowSet set[2]; };
 
-// Grid: one CTA for `tokens` tokens; its warps take blocks of rows of one token, and request the next block's rows before they turn one's.
+// Grid: one CTA for `tokens` tokens; its warps take blocks of rows of one token, and request the next block's rows
+// before they turn one's.
 template <int FORM>
 __global__ void __launch_bounds__(kRopeRowThreads, rope_ctas(FORM))
 rope_apply_kernel(const __grid_constant__ RopeTurns turns, const __grid_constant__ RopeSets sets, const int32_t* positions, int total, int head_dim, int tokens) {

@@ -1,19 +1,23 @@
-// Rows of heads, turned by their tokens' positions and written as bf16 (rope.cu) or as rows of the 8-bit cache (kv8_append.cu).
+// Rows of heads, turned by their tokens' positions and written as bf16 (rope.cu) or as rows of the 8-bit cache
+// (kv8_append.cu).
 //
 // Rotary positions: pair j of a head's first rotary_dim values turns by the angle position * f_j,
 //     (x, y) -> m (x cos a - y sin a, y cos a + x sin a),
-// the pairs being (j, j + rotary_dim / 2) or (2j, 2j + 1), the others passing through.  The frequencies come as turns (f_j / 2 pi) in
-// fp64, where position * turns is reduced to [-1/2, 1/2] and its sine and cosine are taken: an fp32 angle is off by thousandths of a radian at
-// positions of 10^5.  Both are kept as two fp32 numbers, a high part of 16 bits, whose products with bf16 values are exact, and a low part, and a product
-// difference x c - y s is evaluated from these (rope_diff): a value that is left over from two that cancel is as exact as any other down to 2^-18 of
-// them, and is rounded once, to what is written.  That takes five fp32 instructions a value, without conversions to fp64, which run at an eighth of the rate of these.
+// the pairs being (j, j + rotary_dim / 2) or (2j, 2j + 1), the others passing through.  The frequencies come as turns
+// (f_j / 2 pi) in fp64, where position * turns is reduced to [-1/2, 1/2] and its sine and cosine are taken: an fp32
+// angle is off by thousandths of a radian at positions of 10^5.  Both are kept as two fp32 numbers, a high part of 16
+// bits, whose products with bf16 values are exact, and a low part, and a product difference x c - y s is evaluated from
+// these (rope_diff): a value that is left over from two that cancel is as exact as any other down to 2^-18 of them, and
+// is rounded once, to what is written.  That takes five fp32 instructions a value, without conversions to fp64, which
+// run at an eighth of the rate of these.
 //
-// What bounds it: instructions and their latency more than memory (4097 tokens of 32 + 8 heads of 128 take 21.0 us, 4 TB/s, with 62 % of the issue slots
-// taken by two CTAs to an SM, which is what their registers leave room for) or, for few tokens, the latency of one chain: positions, angles, rows, stores
-// (3.4 us in a graph).
-// A thread holds 8 values of a row, 16 bytes; head_dim / 8 lanes hold a row, so a pair's other half comes by shuffle, and so does a row's
-// maximum.  A warp takes kRopeUnroll times as many rows of ONE token as it has room for and requests them together: the sines and cosines of a
-// lane's values are the same for all heads and are read from shared memory once.
+// What bounds it: instructions and their latency more than memory (4097 tokens of 32 + 8 heads of 128 take 21.0 us, 4
+// TB/s, with 62 % of the issue slots taken by two CTAs to an SM, which is what their registers leave room for) or, for
+// few tokens, the latency of one chain: positions, angles, rows, stores (3.4 us in a graph).
+// A thread holds 8 values of a row, 16 bytes; head_dim / 8 lanes hold a row, so a pair's other half comes by shuffle,
+// and so does a row's maximum.  A warp takes kRopeUnroll times as many rows of ONE token as it has room for and
+// requests them together: the sines and cosines of a lane's values are the same for all heads and are read from shared
+// memory once.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -45,8 +49,9 @@ struct RopeTurns {
     int32_t layout;
 };
 
-// The kernels' forms: halves of whole 16-byte vectors, interleaved pairs that fill such vectors, halves that begin inside a vector, interleaved pairs that end
-// inside one.  (Sorting the values of a cut vector where none is cut would cost the append of a prompt 3 %.)
+// The kernels' forms: halves of whole 16-byte vectors, interleaved pairs that fill such vectors, halves that begin
+// inside a vector, interleaved pairs that end inside one.  (Sorting the values of a cut vector where none is cut would
+// cost the append of a prompt 3 %.)
 enum RopeForm { kRopeHalves, kRopePairs, kRopeOddHalves, kRopeOddPairs };
 constexpr bool rope_in_pairs(int form) { return form == kRopePairs || form == kRopeOddPairs; }
 template <int FORM>
@@ -55,14 +60,15 @@ inline RopeForm rope_form(const RopeTurns& r) {
     if (r.layout == ASYNCLM_ROPE_INTERLEAVED) return r.rotary_dim % 8 == 0 ? kRopePairs : kRopeOddPairs;
     return r.rotary_dim % 16 == 0 ? kRopeHalves : kRopeOddHalves;
 }
-// CTAs of an SM and the most tokens of a CTA, by form.  The sines and cosines of a lane are 16 registers for pairs and 32 for halves, and rows in flight are
-// worth more than registers for pairs only (8192 tokens of 32/8 heads, pairs, append: 54.5 us with two CTAs to an SM, 47.7 with three;
-// 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3 with three, 21.2 with two and up to 16, where pairs take 56.9; all with one instruction
-// a value more than now, 46.7 and 21.0).
+// CTAs of an SM and the most tokens of a CTA, by form.  The sines and cosines of a lane are 16 registers for pairs and
+// 32 for halves, and rows in flight are worth more than registers for pairs only (8192 tokens of 32/8 heads, pairs,
+// append: 54.5 us with two CTAs to an SM, 47.7 with three; 4097 tokens, halves: 23.3 with two and up to 8 tokens, 30.3
+// with three, 21.2 with two and up to 16, where pairs take 56.9; all with one instruction a value more than now, 46.7
+// and 21.0).
 constexpr int rope_ctas(int form) { return rope_in_pairs(form) ? 3 : 2; }
 constexpr int rope_most_tokens(int form) { return rope_in_pairs(form) ? 8 : 16; }
-// Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8, 4 or each by itself, and lanes next to each other then read
-// entries next to each other.
+// Where pair j lies in a token's table: a lane reads `m` consecutive pairs, 8, 4 or each by itself, and lanes next to
+// each other then read entries next to each other.
 template <int FORM>
 __device__ __forceinline__ constexpr int rope_group() { return kInPairs<FORM> ? 4 : FORM == kRopeHalves ? 8 : 1; }
 __device__ __forceinline__ int rope_entry(int j, int m, int per) { return m == 1 ? j : (j % m) * per + j / m; }
@@ -74,17 +80,18 @@ __device__ __forceinline__ float2 rope_split(double c) {
     return make_float2(high, c != 0.0 && low == 0.f ? copysignf(1e-30f, high) : low);
 }
 
-// x c - y s with c = c.x + c.y, s = s.x + s.y, x and y bf16 numbers: their products with the high parts are exact, so the difference of these has one rounding, and
-// the low parts are added last.  An infinite x or y makes the same infinity (or NaN) of both, because the parts have one sign: the sum is what
-// the formula has.
+// x c - y s with c = c.x + c.y, s = s.x + s.y, x and y bf16 numbers: their products with the high parts are exact, so
+// the difference of these has one rounding, and the low parts are added last.  An infinite x or y makes the same
+// infinity (or NaN) of both, because the parts have one sign: the sum is what the formula has.
 __device__ __forceinline__ float rope_diff(float x, float2 c, float y, float2 s) {
     const float p = __fmul_rn(y, s.x);
     const float low = __fmaf_rn(x, c.y, -__fmul_rn(y, s.y));
     return __fadd_rn(__fmaf_rn(x, c.x, -p), low);
 }
 
-// Fills table[i][...] with m cos and m sin (high parts, then low parts) of tokens 0 .. n - 1 of the CTA.  A thread keeps one pair, whose frequency it reads from the kernel's
-// parameters once (lanes that read different entries there take turns).
+// Fills table[i][...] with m cos and m sin (high parts, then low parts) of tokens 0 .. n - 1 of the CTA.  A thread
+// keeps one pair, whose frequency it reads from the kernel's parameters once (lanes that read different entries there
+// take turns).
 template <int FORM, typename Position>
 __device__ __forceinline__ void rope_fill(const RopeTurns& r, float4 (*table)[kRopeEntries], int n, Position position) {
     const int pairs = r.rotary_dim / 2;
@@ -178,8 +185,8 @@ __device__ __forceinline__ void rope_turn(const RopeTurns& r, const RopeLane<FOR
     }
 }
 
-// The lane's 8 values as they are written: turned ones rounded, the others as they came, bit for bit (fp32 has no bf16 NaN's payload and these kernels flush
-// subnormal numbers). rotary_dim is even, so a word of two values is of one kind.
+// The lane's 8 values as they are written: turned ones rounded, the others as they came, bit for bit (fp32 has no bf16
+// NaN's payload and these kernels flush subnormal numbers). rotary_dim is even, so a word of two values is of one kind.
 template <int FORM>
 __device__ __forceinline__ uint4 rope_words(const RopeTurns& r, int v, const uint4& x, const float (&y)[8]) {
     const int left = r.rotary_dim - 8 * v;      // values of the lane that turn

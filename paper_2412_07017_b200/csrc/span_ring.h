@@ -31,12 +31,14 @@ namespace tc {
 
 // Slots of one ring: 80 KiB of 64-key tiles.
 ASYNCLM_HD constexpr int ring_slots(int head_dim) { return 640 / head_dim; }
-// The same for the 8-bit cache, whose K tiles are the codes themselves (8 KB, 4 KB at head_dim 64) and whose V tiles are f16, with room for the tiles' scales.
+// The same for the 8-bit cache, whose K tiles are the codes themselves (8 KB, 4 KB at head_dim 64) and whose V tiles
+// are f16, with room for the tiles' scales.
 ASYNCLM_HD constexpr int ring_slots_kv8(int which, int head_dim) { return head_dim == 128 ? 6 : which ? 11 : 10; }
-// Slots for those scales, which every warp of a softmax group reads until it hands its weights over.  When the producer fills tile t, every warp of its
-// group has released tile t - slots, at the start of its softmax, so it is through with the group's tile before that, t - slots - 1 (both groups on every
-// tile) or t - slots - 2 (alternate tiles), and the other group's warps, which have released t - slots - 1, are through with t - slots - 3.  So
-// t - slots - 3 may be overwritten; one more makes the number even.
+// Slots for those scales, which every warp of a softmax group reads until it hands its weights over.  When the producer
+// fills tile t, every warp of its group has released tile t - slots, at the start of its softmax, so it is through with
+// the group's tile before that, t - slots - 1 (both groups on every tile) or t - slots - 2 (alternate tiles), and the
+// other group's warps, which have released t - slots - 1, are through with t - slots - 3.  So t - slots - 3 may be
+// overwritten; one more makes the number even.
 ASYNCLM_HD constexpr int scale_slots(int slots) { return slots + 4; }
 // Slot (K ring first, then V ring) of the CTA's t-th K (which = 0) or V (which = 1) tile.
 ASYNCLM_HD constexpr int ring_slot(int which, int t, int slots) { return which * slots + t % slots; }
@@ -51,8 +53,9 @@ ASYNCLM_HD constexpr RingPlace ring_next(RingPlace x, int step, int slots) {
     if (x.slot >= slots) { x.slot -= slots; x.parity ^= 1u; }
     return x;
 }
-// Whether an item's last tile has a last page that is not full (`page`: a power of two; items begin on a page boundary).
-// V's is copied row by row through the generic proxy, with zeros behind the end, and the MMAs that read it need a proxy fence.
+// Whether an item's last tile has a last page that is not full (`page`: a power of two; items begin on a page
+// boundary). V's is copied row by row through the generic proxy, with zeros behind the end, and the MMAs that read it
+// need a proxy fence.
 ASYNCLM_HD constexpr bool last_page_by_rows(int kv_end, bool last_tile, int page) { return last_tile && (kv_end & (page - 1)) != 0; }
 
 }  // namespace tc
