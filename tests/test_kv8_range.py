@@ -113,7 +113,7 @@ def test_a_sink_without_any_value(body, chunk):
 
 @pytest.mark.parametrize("body", BODIES)
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("first,second", [(None, 27), (None, 40), (27, None), (40, None), (-30, 100), (100, -30), (110, -28), (-90, 30), (60, -60)])
+@pytest.mark.parametrize("first,second", [(None, 27), (None, 40), (27, None), (40, None), (-30, 100), (100, -30), (110, -28), (-90, 30), (60, -60), (None, 125), (125, None), (125, 3)])
 def test_scales_of_v_that_change_along_a_sequence(body, d, first, second):
     """Scores alike, the first half of the keys with V's rows at 2^first (None: zeros), the second half at 2^second: whichever comes first, each half has half
     of the weight."""
