@@ -794,7 +794,8 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
             const int last_pages = (it.kv_end - (it.kv0 + (ntiles - 1) * kTile) + kPage - 1) / kPage;      // of the item's last tile
             const uint32_t idesc_last = instr_desc<KV8>(16u * (uint32_t)last_pages, 0);      // (8 bits: e4m3, whose number is f16's)
             // where the group's next K and V tile lie
-            RingPlace kp = ring_place(base + (dual ? 0 : b), Geo::RING_K), vp = ring_place(base + (dual ? 0 : b), Geo::RING_V);
+            RingPlace kp = ring_place(base + (dual ? 0 : b), Geo::RING_K), vp = kp;
+            if constexpr (KV8) vp = ring_place(base + (dual ? 0 : b), Geo::RING_V);
             auto next_place = [&](int which, RingPlace& x) { x = ring_next(x, dual ? 1 : 2, Geo::ring(which)); };
             auto wait_tile = [&](int which, const RingPlace& x, int code) {
                 const long long tw = trace_clock();
@@ -1072,8 +1073,13 @@ __device__ __forceinline__ void tc_body(const DevPlan& p, const CUtensorMap* spa
                 // This S complete means every MMA issued for the group before it is complete: the ring slots they
                 // read go back to the producers, the K tile of j now, and the V tile of j - lead (its P V was
                 // issued in front of this Q K^T).
-                if (KV8 ? lane == 0 : m == 0) release(0, kv_base + j, dual);
-                if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
+                if constexpr (KV8) {
+                    if (lane == 0) release(0, kv_base + j, dual);
+                    if (m == 0 && u >= 2) release(1, kv_base + j - lead, dual);
+                } else if (m == 0) {
+                    release(0, kv_base + j, dual);
+                    if (u >= 2) release(1, kv_base + j - lead, dual);
+                }
                 tmem_wait_ld();
                 // score * 2^eK; with the row's scale and eV (log2 domain) it is the exponent of a key's weight of V,
                 // whose tile leaves eV out: the tile's eV, which comes in below, or each key's, which has been added

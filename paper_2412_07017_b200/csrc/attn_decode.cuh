@@ -802,7 +802,8 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                 landing = max(0, n - S + 1);      // stage s has been used and is given away again below
                 if (lane == 0) {
                     desc[s].flags = kFlagEnd;
-                    mbar_arrive_n(full0 + 8 * s, KV8 ? 33 : 1);
+                    if constexpr (KV8) mbar_arrive_n(full0 + 8 * s, 33);
+                    else mbar_arrive(full0 + 8 * s);
                 }
             }
         }

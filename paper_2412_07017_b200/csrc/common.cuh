@@ -140,7 +140,9 @@ __device__ __forceinline__ void prefetch_first_pages(const DevPlan& p, const __n
         if (page < 0 || page >= p.num_pages) continue;      // (the checked build reports it where it is copied)
 #pragma unroll
         for (int l = lane; l < 2 * kLines; l += 32) {
-            const uint8_t* line = reinterpret_cast<const uint8_t*>(pool) + pool_row_offset(page, l / kLines, kv_head, 0, p.num_kv_heads, D) * (KV8 ? 1 : 2) + (l % kLines) * 128;
+            const size_t block = pool_row_offset(page, l / kLines, kv_head, 0, p.num_kv_heads, D);
+            const void* line = pool + block + (l % kLines) * 64;
+            if constexpr (KV8) line = reinterpret_cast<const uint8_t*>(pool) + block + (l % kLines) * 128;
             asm volatile("prefetch.global.L2 [%0];" ::"l"(line));
         }
     }
