@@ -88,6 +88,8 @@ typedef struct asynclm_plan_options {
 #define ASYNCLM_PLAN_NO_TENSOR_PATH        2  /* keep every row on the warp body              */
 #define ASYNCLM_PLAN_KV8                   4  /* balance for asynclm_kv8_attn_mixed; either kind of plan serves
                                                  either kind of cache                         */
+#define ASYNCLM_PLAN_SHARE_ALL             8  /* asynclm_plan_prefix: share every prefix that two sequences have, whatever it
+                                                 saves (for measurements and tests)           */
 
 /* Host-side description of one step's batch (all arrays on the host, int32). */
 typedef struct asynclm_batch {
@@ -130,7 +132,8 @@ typedef struct asynclm_item_view {
     int32_t kv_head;
     int32_t tok0;       /* first new token of the unit, index i inside the sequence's span */
     int32_t ntok;       /* tokens of the span covered by the unit */
-    int32_t kv0, kv1;   /* key positions [kv0, kv1) the item reads (before causal clipping) */
+    int32_t kv0, kv1;   /* key positions [kv0, kv1) the item reads (before causal clipping).  A shared prefix: seq and tok0 are those of
+                           the first row of the group that the unit holds.  Selected pages: positions among the selected keys */
     int32_t path;       /* 0 = warp body, 1 = span body */
     int32_t cta;        /* persistent CTA that processes the item; -1 = handed out at run time to
                            whichever CTA is free (items are listed in hand-out order) */
@@ -191,10 +194,53 @@ int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
                  const asynclm_batch* batch, void* host_ws, size_t host_bytes,
                  void* dev_ws, size_t dev_bytes, void* stream, asynclm_plan_t** out_plan);
 
+/*
+ * asynclm_plan for a batch whose sequences begin with the same pages, as those of one server do: the descriptions of the functions
+ * that a model may call stand in front of every conversation.  The sequences [first_seq, first_seq + n_seqs) of a group have the same pages for
+ * their first prefix_tokens tokens (whole pages); a plan made here lets the step read those once for the group instead of once for every
+ * sequence: their keys become units whose query rows are those of all the group's sequences, each sequence's own keys units of their own, and
+ * a kernel behind the attention joins each row's partial results.  Everything else is as with asynclm_plan: batch, lengths and page lists are given in
+ * full, and the plan serves the same calls (append, attention over either cache, the static form, the read-back) with the same results to rounding.
+ *   Groups rise in first_seq and do not overlap; sequences may be in none.  Every sequence with new tokens has kv_len_before >= prefix_tokens.
+ *   What is not worth sharing is planned as if it were not shared: a sequence with more than 128 rows (G * q_len) keeps its prefix to itself, and
+ * so does the batch where little would be saved (ASYNCLM_PLAN_SHARE_ALL shares that, too).
+ *   Workspaces: make the plan without a device workspace first (asynclm_plan_info then says what is needed) or retry on WORKSPACE_TOO_SMALL;
+ * asynclm_plan_workspace_size does not cover these plans.
+ * Errors: those of asynclm_plan; INVALID_ARG (groups out of order or outside the batch, a prefix that is not whole pages or longer than a
+ * sequence's context), PAGE_TABLE (sequences of a group differ in the pages of their prefix).
+ */
+typedef struct asynclm_prefix_group {
+    int32_t first_seq, n_seqs;
+    int32_t prefix_tokens;        /* a multiple of page_size */
+    int32_t reserved;             /* 0 */
+} asynclm_prefix_group;
+int asynclm_plan_prefix(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch, const asynclm_prefix_group* groups,
+                        int32_t n_groups, void* host_ws, size_t host_bytes, void* dev_ws, size_t dev_bytes, void* stream, asynclm_plan_t** out_plan);
+
+/*
+ * asynclm_plan for attention over selected pages: every (new token, kv head) attends to at most budget_pages of the pages that hold the keys it
+ * sees, the first first_pages and the last last_pages (its own key's among them) and, for the rest, those that asynclm_select_pages chooses.  A step is
+ *     append, asynclm_kv_bounds, asynclm_select_pages, asynclm_attn_mixed (or the quantised cache's calls)
+ * for every layer; the attention reads the lists that the selection left in the plan's device workspace, and is refused (INVALID_ARG) before the first
+ * one.  Meant for decoding sequences and short spans (every token's lists and scores have room in the device workspace) over long contexts; out
+ * and lse are those of the softmax over the keys attended to.  asynclm_step refuses such a plan (the selection comes between its halves).
+ *   Workspaces: as for asynclm_plan_prefix.
+ * Errors: those of asynclm_plan; INVALID_ARG (first_pages < 0, last_pages < 1, first_pages + last_pages > budget_pages, kv_chunk_tokens set).
+ */
+typedef struct asynclm_sparse {
+    int32_t budget_pages, first_pages, last_pages;
+    int32_t reserved;             /* 0 */
+} asynclm_sparse;
+int asynclm_plan_sparse(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch, const asynclm_sparse* sparse, void* host_ws,
+                        size_t host_bytes, void* dev_ws, size_t dev_bytes, void* stream, asynclm_plan_t** out_plan);
+
 int asynclm_plan_get_info(const asynclm_plan_t* plan, asynclm_plan_info* info);
 
 /* What the plan was made for, and what a call's tensors have to fit: the shape, the number of sequences and that of new tokens. */
 int asynclm_plan_get_shape(const asynclm_plan_t* plan, asynclm_shape* shape, int32_t* batch, int32_t* total_q);
+
+/* The page numbers that a plan of asynclm_plan_sparse was made with; INVALID_ARG for any other. */
+int asynclm_plan_get_sparse(const asynclm_plan_t* plan, asynclm_sparse* sparse);
 
 /* Copies up to `capacity` items into `items` (host); returns the number of items, or < 0. */
 int asynclm_plan_get_items(const asynclm_plan_t* plan, asynclm_item_view* items, int32_t capacity);
@@ -273,7 +319,7 @@ int asynclm_step(const asynclm_plan_t* plan, const void* q, const void* k_new, c
  * A library built with -DASYNCLM_DEBUG (build.py --debug) also checks, on the device, every page id
  * it is about to turn into an address and reports the first bad one here instead of using it:
  * 41 the append's row slot, 42 a span tile's page, 43 a decode chunk's page, 44 the append inside
- * asynclm_step; an append leaves the row out, span tiles and decode chunks read page 0 in its place, nothing
+ * asynclm_step, 46 asynclm_kv_bounds; an append leaves the row out and bounds the page, span tiles and decode chunks read page 0 in its place, nothing
  * faults.  The ordinary build relies on asynclm_plan, which validates every id on the host.
  * Returns ASYNCLM_OK or ASYNCLM_ERR_DEVICE_STATUS / ASYNCLM_ERR_CUDA.
  */
@@ -499,6 +545,59 @@ int asynclm_kv8_attn_mixed(const asynclm_plan_t* plan, const void* q, const void
  */
 int asynclm_kv8_gather(const asynclm_plan_t* plan, const int64_t* out_indptr, const int32_t* first, int64_t total_rows, const void* kv8_pool,
                        const void* kv8_scales, void* k_out, void* v_out, void* stream);
+
+/*
+ * Bounds of a page's keys: for every channel the least and the largest value over the page's slots in use,
+ *     key_bounds   device, bf16 [num_pages][num_kv_heads][2 (least, largest)][head_dim], 16-byte aligned
+ * exact, as they are values of the cache (of a quantised one, as asynclm_kv8_gather reads them); a channel with a NaN gets -infinity and +infinity.
+ * Taken of the plan's sequences that have new tokens: of the pages with a new token (from_start == 0: behind every append, on the same stream), or of all
+ * pages up to ctx_b + q_len_b (from_start != 0: for a cache whose bounds nothing has kept).  Any kind of plan.  Other pages' bounds are left alone.
+ * One kernel.  Errors: INVALID_ARG, CUDA.
+ */
+int asynclm_kv_bounds(const asynclm_plan_t* plan, const void* kv_pool, void* key_bounds, int32_t from_start, void* stream);
+int asynclm_kv8_bounds(const asynclm_plan_t* plan, const void* kv8_pool, const void* kv8_scales, void* key_bounds, int32_t from_start, void* stream);
+
+/*
+ * Selects the pages of a plan of asynclm_plan_sparse.  The score of a page for a token and a kv head is
+ *     max over the head's G queries q of sum_c max(q_c * least_c, q_c * largest_c),
+ * which no key in the page exceeds (before sm_scale).  Of the pages with keys that the token sees, the first and last ones of the plan are taken, and those
+ * of the others with the largest scores, the lowest page among equals.  Scores are held in 64 bits, so that the choice does not hang on
+ * the order of additions; infinities and NaN in q or bounds count as 2^128 and more, with their sign, subnormal values as zero.
+ *
+ *   q          device, bf16 [T][num_q_heads][head_dim], as the attention takes it
+ *   pages_out  device, int32 [T][num_kv_heads][budget_pages], or NULL: the chosen pages as numbers inside the sequence, rising, -1 behind the last
+ * One kernel.  Errors: INVALID_ARG (also: the plan is of another kind), CUDA.
+ */
+int asynclm_select_pages(const asynclm_plan_t* plan, const void* q, const void* key_bounds, int32_t* pages_out, void* stream);
+
+/*
+ * Verification of drafted tokens (for steps whose spans are tokens that a cheaper model, or a search of the text, proposed) with given random numbers:
+ * what is emitted is distributed as the target's own tokens would be.  Sequence b has n = draft_indptr[b + 1] - draft_indptr[b] drafts; draft i of all is
+ * token x = draft_tokens[i], drawn from row i of `draft`; its target row is i + b, and row draft_indptr[b + 1] + b is the one behind the last draft.
+ *   Draft i is accepted if accept_u[i] * q(x) < p(x) and all drafts of its sequence in front of it are (draft == NULL: q(x) = 1, a proposal made with
+ * certainty).  The token behind the accepted ones has the weights w_t = max(p_t - q_t, 0) of the first rejected draft's rows, or w = p of the row behind
+ * the last draft: it is the least t with sum_{t' <= t} w > sample_u[b] * sum w, evaluated in 64 bits.  Where rounding has left no weight, w = p; where
+ * that has none either, the token is -1.  Weights that are NaN count as zero, negative probabilities as none; a draft outside the vocabulary is
+ * rejected.  Random numbers lie in [0, 1).
+ *
+ *   rows          host.  target [drafts + batch][vocab] and draft [drafts][vocab] or NULL: device, bf16 or fp32 (dtype), rows any stride >= vocab apart
+ *   draft_indptr  device, int32 [batch + 1], from 0, not falling, up to `drafts`
+ *   draft_tokens, accept_u [drafts]; sample_u [batch]: device
+ *   accepted      device, int32 [batch]: drafts accepted
+ *   tokens_out    device, int32 [drafts + batch]: from draft_indptr[b] + b on the accepted drafts, the next token, then -1 in the sequence's other places
+ *   workspace     device, 16-byte aligned, asynclm_draft_verify_workspace_bytes(batch, vocab) bytes, owned by the caller and all zero before the first call;
+ *                 every call leaves it fit for the next, of any batch and vocab that it is large enough for; calls that share it must not overlap on the GPU
+ * One kernel; one row of p and at most one of q are read a sequence; batch <= 65535.  Errors: INVALID_ARG, CUDA.
+ */
+typedef struct asynclm_draft_rows {
+    const void *target, *draft;
+    int64_t target_stride, draft_stride;      /* values */
+    int32_t vocab;
+    int32_t dtype;                            /* ASYNCLM_DTYPE_BF16 / F32 */
+} asynclm_draft_rows;
+size_t asynclm_draft_verify_workspace_bytes(int32_t batch, int32_t vocab);
+int asynclm_draft_verify(const asynclm_draft_rows* rows, const int32_t* draft_indptr, int32_t batch, int32_t drafts, const int32_t* draft_tokens,
+                         const float* accept_u, const float* sample_u, int32_t* accepted, int32_t* tokens_out, void* workspace, void* stream);
 
 /*
  * Measurement aid (no counterpart in the paper, none of the method's arithmetic): reads n_blocks

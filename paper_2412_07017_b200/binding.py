@@ -25,7 +25,8 @@ EXPORTS = [
     "asynclm_kv_swap_out", "asynclm_kv_swap_in", "asynclm_trap_decide", "asynclm_latency_model",
     "asynclm_async_latency_of_order", "asynclm_token_monitor_step", "asynclm_token_monitor_workspace_bytes",
     "asynclm_kv_append_rope", "asynclm_rope_table_init", "asynclm_rope_apply", "asynclm_kv8_append", "asynclm_kv8_attn_mixed",
-    "asynclm_kv8_gather", "asynclm_plan_get_shape",
+    "asynclm_kv8_gather", "asynclm_plan_get_shape", "asynclm_plan_prefix", "asynclm_plan_sparse", "asynclm_plan_get_sparse", "asynclm_kv_bounds", "asynclm_kv8_bounds",
+    "asynclm_select_pages", "asynclm_draft_verify", "asynclm_draft_verify_workspace_bytes",
 ]
 
 TRAP_KEEP, TRAP_SWAP, TRAP_RECOMPUTE = 0, 1, 2
@@ -33,6 +34,7 @@ TRAP_KEEP, TRAP_SWAP, TRAP_RECOMPUTE = 0, 1, 2
 PLAN_REJECT_ALIASED_WRITES = 1
 PLAN_NO_TENSOR_PATH = 2
 PLAN_KV8 = 4
+PLAN_SHARE_ALL = 8
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {None: 0, "none": 0, "linear": 1, "bands": 2, "yarn": 3}
@@ -114,6 +116,19 @@ class CKv8Rows(ctypes.Structure):
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64)]
 
 
+class CPrefixGroup(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("first_seq", "n_seqs", "prefix_tokens", "reserved")]
+
+
+class CSparse(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("budget_pages", "first_pages", "last_pages", "reserved")]
+
+
+class CDraftRows(ctypes.Structure):
+    _fields_ = [("target", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("target_stride", ctypes.c_int64), ("draft_stride", ctypes.c_int64),
+                ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -163,15 +178,25 @@ def load(rebuild_if_stale: bool = True):
     lib.asynclm_kv8_attn_mixed.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     lib.asynclm_kv8_gather.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp]
     lib.asynclm_plan_get_shape.argtypes = [vp, ctypes.POINTER(CShape), ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
+    planned = [vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
+    lib.asynclm_plan_prefix.argtypes = [ctypes.POINTER(CShape), ctypes.POINTER(CPlanOptions), ctypes.POINTER(CBatch), ctypes.POINTER(CPrefixGroup), i32] + planned
+    lib.asynclm_plan_sparse.argtypes = [ctypes.POINTER(CShape), ctypes.POINTER(CPlanOptions), ctypes.POINTER(CBatch), ctypes.POINTER(CSparse)] + planned
+    lib.asynclm_plan_get_sparse.argtypes = [vp, ctypes.POINTER(CSparse)]
+    lib.asynclm_kv_bounds.argtypes = [vp, vp, vp, i32, vp]
+    lib.asynclm_kv8_bounds.argtypes = [vp, vp, vp, vp, i32, vp]
+    lib.asynclm_select_pages.argtypes = [vp, vp, vp, vp, vp]
+    lib.asynclm_draft_verify.argtypes = [ctypes.POINTER(CDraftRows), vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.asynclm_draft_verify_workspace_bytes.argtypes = [i32, i32]
     lib.asynclm_static_scratch_bytes.argtypes = []
     lib.asynclm_last_device_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     for name in EXPORTS:
         if name not in ("asynclm_strerror", "asynclm_last_cuda_error", "asynclm_static_scratch_bytes",
-                        "asynclm_kv_swap_staging_bytes", "asynclm_token_monitor_workspace_bytes"):
+                        "asynclm_kv_swap_staging_bytes", "asynclm_token_monitor_workspace_bytes", "asynclm_draft_verify_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     lib.asynclm_static_scratch_bytes.restype = ctypes.c_size_t
     lib.asynclm_kv_swap_staging_bytes.restype = ctypes.c_size_t
     lib.asynclm_token_monitor_workspace_bytes.restype = ctypes.c_size_t
+    lib.asynclm_draft_verify_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -280,24 +305,60 @@ def _get_info(handle) -> dict:
     return info.as_dict()
 
 
-def plan_host(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, num_sms=148,
-              sm_scale=0.0, **opts) -> Plan:
-    """Host-only planning (no CUDA call): for inspection, sizing and CPU tests."""
-    lib = load()
-    cs, co = _cshape(shape, num_pages, sm_scale), _copts(num_sms=num_sms, **opts)
-    cb, keep = _cbatch(q_indptr, kv_len_before, page_indptr, page_indices)
-    T = int(keep[0][0][-1]) if len(keep[0][0]) else 0
-    hbytes = 1 << 16
+def _host_plan(make, hbytes=1 << 16) -> Plan:
+    """A plan without a device workspace; make(host address, bytes, out) calls the planner."""
     while True:
         ws = np.zeros(hbytes // 8, dtype=np.int64)
         out = ctypes.c_void_p()
-        rc = lib.asynclm_plan(ctypes.byref(cs), ctypes.byref(co), ctypes.byref(cb), ws.ctypes.data,
-                              ws.nbytes, None, 0, None, ctypes.byref(out))
+        rc, what, keep = make(ws.ctypes.data, ws.nbytes, None, 0, None, ctypes.byref(out))
         if rc == -4 and hbytes < (1 << 32):
             hbytes *= 4
             continue
-        _check(rc, "asynclm_plan")
+        _check(rc, what)
         return Plan(out.value, ws, None, keep)
+
+
+def plan_host(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, num_sms=148,
+              sm_scale=0.0, groups=None, sparse=None, **opts) -> Plan:
+    """Host-only planning (no CUDA call): for inspection, sizing and CPU tests.  groups: as in asynclm_plan_prefix; sparse: (budget_pages, first_pages,
+    last_pages) of asynclm_plan_sparse."""
+    return _host_plan(_planner(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, sm_scale, groups, sparse, num_sms=num_sms, **opts))
+
+
+def _planner(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, sm_scale, groups, sparse, **opts):
+    """make(host_ws, bytes, dev_ws, bytes, stream, out) -> (status, the call's name, what has to be kept) of the planner for these arguments."""
+    lib = load()
+    cs, co = _cshape(shape, num_pages, sm_scale), _copts(**opts)
+    cb, keep = _cbatch(q_indptr, kv_len_before, page_indptr, page_indices)
+    front = (ctypes.byref(cs), ctypes.byref(co), ctypes.byref(cb))
+    if groups is not None:
+        rows = [tuple(int(x) for x in g) for g in groups]
+        if any(len(g) != 3 for g in rows):
+            raise ValueError("groups: (first sequence, sequences, tokens of the prefix) of each is wanted")
+        arr = (CPrefixGroup * max(len(rows), 1))(*(CPrefixGroup(*g, 0) for g in rows))
+        return lambda *ws: (lib.asynclm_plan_prefix(*front, arr, len(rows), *ws), "asynclm_plan_prefix", keep)
+    if sparse is not None:
+        pages = CSparse(*(int(x) for x in sparse), 0)
+        return lambda *ws: (lib.asynclm_plan_sparse(*front, ctypes.byref(pages), *ws), "asynclm_plan_sparse", keep)
+    return lambda *ws: (lib.asynclm_plan(*front, *ws), "asynclm_plan", keep)
+
+
+def _device_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, stream, sm_scale, host_ws, dev_ws, groups=None, sparse=None, **opts) -> Plan:
+    import torch
+    if host_ws is None or dev_ws is None:
+        dry_opts = dict(opts)
+        sms = dry_opts.pop("num_sms", None) or torch.cuda.get_device_properties(torch.cuda.current_device()).multi_processor_count
+        dry = plan_host(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, num_sms=sms, sm_scale=sm_scale, groups=groups, sparse=sparse,
+                        **dry_opts)
+        if host_ws is None:
+            host_ws = torch.empty(dry.info["host_bytes_used"] + 256, dtype=torch.uint8).pin_memory()
+        if dev_ws is None:
+            dev_ws = torch.empty(dry.info["device_bytes_used"] + 256, dtype=torch.uint8, device="cuda")
+    make = _planner(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, sm_scale, groups, sparse, **opts)
+    out = ctypes.c_void_p()
+    rc, what, _ = make(host_ws.data_ptr(), host_ws.numel(), dev_ws.data_ptr(), dev_ws.numel(), _stream_ptr(stream), ctypes.byref(out))
+    _check(rc, what)
+    return Plan(out.value, host_ws, dev_ws, None)
 
 
 def asynclm_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices,
@@ -313,27 +374,22 @@ def asynclm_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_in
             if got[0] != 0:
                 _check(got[0], "asynclm_plan")
             return Plan(got[1], host_ws, dev_ws, None)
-    import torch
-    lib = load()
-    cs, co = _cshape(shape, num_pages, sm_scale), _copts(**opts)
-    cb, keep = _cbatch(q_indptr, kv_len_before, page_indptr, page_indices)
-    if host_ws is None or dev_ws is None:
-        sms = opts.get("num_sms") or torch.cuda.get_device_properties(
-            torch.cuda.current_device()).multi_processor_count
-        dry_opts = dict(opts)
-        dry_opts.pop("num_sms", None)
-        dry = plan_host(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices,
-                        num_sms=sms, sm_scale=sm_scale, **dry_opts)
-        if host_ws is None:
-            host_ws = torch.empty(dry.info["host_bytes_used"] + 256, dtype=torch.uint8).pin_memory()
-        if dev_ws is None:
-            dev_ws = torch.empty(dry.info["device_bytes_used"] + 256, dtype=torch.uint8, device="cuda")
-    s = _stream_ptr(stream)
-    out = ctypes.c_void_p()
-    _check(lib.asynclm_plan(ctypes.byref(cs), ctypes.byref(co), ctypes.byref(cb),
-                            host_ws.data_ptr(), host_ws.numel(), dev_ws.data_ptr(), dev_ws.numel(),
-                            s, ctypes.byref(out)), "asynclm_plan")
-    return Plan(out.value, host_ws, dev_ws, None)
+    return _device_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, stream, sm_scale, host_ws, dev_ws, **opts)
+
+
+def asynclm_plan_prefix(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, groups, stream=None, sm_scale=0.0, host_ws=None, dev_ws=None,
+                        **opts) -> Plan:
+    """asynclm_plan for a batch whose sequences begin with the same pages: `groups` lists (first sequence, sequences, tokens of the prefix), the tokens
+    being whole pages.  The plan serves the same calls as an ordinary one; the attention reads each group's prefix once."""
+    return _device_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, stream, sm_scale, host_ws, dev_ws, groups=groups, **opts)
+
+
+def asynclm_plan_sparse(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, budget_pages, first_pages=1, last_pages=1, stream=None,
+                        sm_scale=0.0, host_ws=None, dev_ws=None, **opts) -> Plan:
+    """asynclm_plan for attention over selected pages: of those that a token sees the first and last ones and, up to budget_pages, those that
+    asynclm_select_pages chooses."""
+    return _device_plan(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indices, stream, sm_scale, host_ws, dev_ws,
+                        sparse=(budget_pages, first_pages, last_pages), **opts)
 
 
 def _stream_ptr(stream):
@@ -608,6 +664,81 @@ def asynclm_kv8_gather(plan: Plan, out_indptr, first, kv8_pool, kv8_scales, k_ou
     _check(load().asynclm_kv8_gather(plan.handle, _flat(out_indptr, "out_indptr", "a contiguous CUDA tensor of int64", (torch.int64,), batch + 1),
                                      _flat(first, "first", "a contiguous CUDA tensor of int32", (torch.int32,), batch), k_out.shape[0], pool, scales, k, v,
                                      _stream_ptr(stream)), "asynclm_kv8_gather")
+
+
+def _bounds_of(key_bounds, shape: CShape):
+    import torch
+    return _flat(key_bounds, "key_bounds", "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), shape.num_pages * shape.num_kv_heads * 2 * shape.head_dim)
+
+
+def asynclm_kv_bounds(plan: Plan, kv_pool, key_bounds, from_start: bool = False, stream=None) -> None:
+    """Least and largest value of every key channel into key_bounds (bf16 [pages][kv heads][2][head_dim]): of the pages with the step's new tokens, or,
+    from_start, of all pages of the plan's sequences that have new tokens."""
+    import torch
+    shape = _sizes(plan)[0]
+    pool = _flat(kv_pool, "kv_pool", "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), shape.num_pages * 2 * shape.num_kv_heads * shape.page_size * shape.head_dim)
+    _check(load().asynclm_kv_bounds(plan.handle, pool, _bounds_of(key_bounds, shape), int(bool(from_start)), _stream_ptr(stream)), "asynclm_kv_bounds")
+
+
+def asynclm_kv8_bounds(plan: Plan, kv8_pool, kv8_scales, key_bounds, from_start: bool = False, stream=None) -> None:
+    """asynclm_kv_bounds of the quantised cache."""
+    shape = _sizes(plan)[0]
+    pool, scales = _cache8(kv8_pool, kv8_scales, shape)
+    _check(load().asynclm_kv8_bounds(plan.handle, pool, scales, _bounds_of(key_bounds, shape), int(bool(from_start)), _stream_ptr(stream)), "asynclm_kv8_bounds")
+
+
+def asynclm_select_pages(plan: Plan, q, key_bounds, pages_out=None, stream=None) -> None:
+    """Chooses the pages that the attention with this plan (of asynclm_plan_sparse) reads; pages_out (int32 [tokens][kv heads][budget_pages]) receives their
+    numbers inside the sequences, rising, -1 behind the last."""
+    import torch
+    shape, _, tokens = _sizes(plan)
+    qa = _flat(q, "q", "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), tokens * shape.num_q_heads * shape.head_dim)
+    oa = None
+    if pages_out is not None:
+        oa = _flat(pages_out, "pages_out", "a contiguous CUDA tensor of int32", (torch.int32,), tokens * shape.num_kv_heads * _budget(plan))
+    _check(load().asynclm_select_pages(plan.handle, qa, _bounds_of(key_bounds, shape), oa, _stream_ptr(stream)), "asynclm_select_pages")
+
+
+def _budget(plan: Plan) -> int:
+    pages = CSparse()
+    _check(load().asynclm_plan_get_sparse(plan.handle, ctypes.byref(pages)), "asynclm_plan_get_sparse")
+    return pages.budget_pages
+
+
+def draft_verify_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(load().asynclm_draft_verify_workspace_bytes(int(batch), int(vocab)))
+
+
+def _probabilities(t, name: str, rows: int, vocab: int, dtype):
+    """(address, row stride) of a tensor [rows][vocab] whose rows may be any distance apart."""
+    if t.dim() != 2 or t.dtype != dtype or not t.is_cuda or tuple(t.shape) != (rows, vocab):
+        raise ValueError(f"{name}: a CUDA tensor of {dtype}, {(rows, vocab)}, is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if (vocab > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < vocab):
+        raise ValueError(f"{name}: a row's values have to lie next to each other, and rows must not overlap (strides {t.stride()})")
+    return t.data_ptr(), t.stride(0) if rows > 1 else vocab
+
+
+def asynclm_draft_verify(draft_indptr, target, draft, draft_tokens, accept_u, sample_u, accepted, tokens_out, workspace, stream=None) -> None:
+    """Drafted tokens held against the target's probabilities (see include/asynclm.h).  draft_indptr int32 [batch + 1]; target [drafts + batch][vocab] and
+    draft [drafts][vocab] (or None: proposals made with certainty), bf16 or fp32; draft_tokens int32, accept_u fp32 [drafts]; sample_u fp32 [batch];
+    accepted int32 [batch]; tokens_out int32 [drafts + batch]; workspace: uint8, zeroed, of draft_verify_workspace_bytes(batch, vocab) bytes or more."""
+    import torch
+    batch, drafts = draft_indptr.numel() - 1, draft_tokens.numel()
+    if target.dim() != 2 or target.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"target: a CUDA tensor [drafts + batch][vocab] of bfloat16 or float32 is wanted, not {tuple(target.shape)} of {target.dtype}")
+    vocab = target.shape[1]
+    ta, ts = _probabilities(target, "target", drafts + batch, vocab, target.dtype)
+    da, ds = (None, 0) if draft is None else _probabilities(draft, "draft", drafts, vocab, target.dtype)
+    i32, f32 = (torch.int32,), (torch.float32,)
+    rows = CDraftRows(ta, da if drafts else None, ts, ds, vocab, 0 if target.dtype == torch.bfloat16 else 1)
+    flat = [_flat(t, name, f"a contiguous CUDA tensor of {'int32' if kind is i32 else 'float32'}", kind, n) for t, name, kind, n in (
+        (draft_indptr, "draft_indptr", i32, batch + 1), (draft_tokens, "draft_tokens", i32, drafts), (accept_u, "accept_u", f32, drafts),
+        (sample_u, "sample_u", f32, batch), (accepted, "accepted", i32, batch), (tokens_out, "tokens_out", i32, drafts + batch))]
+    wa = _flat(workspace, "workspace", "a contiguous CUDA tensor of uint8", (torch.uint8,))
+    if workspace.numel() < draft_verify_workspace_bytes(batch, vocab):
+        raise ValueError(f"workspace: {workspace.numel()} bytes, {draft_verify_workspace_bytes(batch, vocab)} are needed")
+    _check(load().asynclm_draft_verify(ctypes.byref(rows), flat[0], batch, drafts, flat[1], flat[2], flat[3], flat[4], flat[5], wa, _stream_ptr(stream)),
+           "asynclm_draft_verify")
 
 
 def asynclm_read_ceiling(kv_pool, k_block_offsets, v_delta_bytes: int, block_bytes: int, sink, stream=None) -> None:

@@ -71,8 +71,10 @@ extern "C" int asynclm_attn_mixed(const asynclm_plan_t* plan, const void* q, con
     if (!q || !kv_pool || !out || !aligned16(q) || !aligned16(kv_pool) || !aligned16(out))
         return ASYNCLM_ERR_INVALID_ARG;
     if (int rc = check_plan_device(plan->device)) return rc;
+    if (!asynclm::pages_chosen(plan)) return ASYNCLM_ERR_INVALID_ARG;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
+    use.reads_page_lists();
     int rc = cuda_status(use.launched(launch_attention(use.dev, q, kv_pool, out, lse, s)));
     if (rc != ASYNCLM_OK) return rc;
     return cuda_status(launch_lse_merge(use.dev, out, lse, s));
@@ -85,11 +87,13 @@ extern "C" int asynclm_step(const asynclm_plan_t* plan, const void* q, const voi
     if (!q || !k_new || !v_new || !kv_pool || !out || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new) ||
         !aligned16(kv_pool) || !aligned16(out))
         return ASYNCLM_ERR_INVALID_ARG;
+    if (plan->sparse) return ASYNCLM_ERR_INVALID_ARG;      // pages are selected between the append and the attention
     if (int rc = check_plan_device(plan->device)) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
     int rc;
-    if (plan->dev.num_items_tensor > 0 || plan->max_q_len > kStepFusedMaxSpan) {
+    // (rows that share a prefix: a unit's keys are not all of its sequence's, which the fused form counts on)
+    if (plan->shared || plan->dev.num_items_tensor > 0 || plan->max_q_len > kStepFusedMaxSpan) {
         // With the append fused in, every item copies the new rows it reads, so the units of one long span
         // copy its first rows again and again (quadratic in the span length), and in the span body the
         // copy stands in front of the loads: the separate append kernel, which copies every row once, is

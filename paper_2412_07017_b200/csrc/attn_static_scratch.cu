@@ -66,11 +66,13 @@ extern "C" int asynclm_attn_mixed_static(const asynclm_plan_t* plan, const void*
     const size_t o_bytes = align256(rows * (size_t)plan->dev.group * (size_t)plan->dev.head_dim * sizeof(float));
     const size_t l_bytes = align256(rows * (size_t)plan->dev.group * sizeof(float));
     if (o_bytes + l_bytes > kStaticScratchBytes) return ASYNCLM_ERR_STATIC_SCRATCH_TOO_SMALL;
+    if (!pages_chosen(plan)) return ASYNCLM_ERR_INVALID_ARG;
     if (int rc = check_plan_device(plan->device)) return rc;
     void* base = nullptr;
     if (int rc = cuda_status(scratch_address(&base))) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
+    use.reads_page_lists();
     DevPlan& d = use.dev;                        // same plan, partial results redirected
     d.partial_o = (float*)base;
     d.partial_lse = (float*)((unsigned char*)base + o_bytes);

@@ -56,12 +56,13 @@ static int default_tensor_min_rows(int head_dim) { return head_dim == 64 ? 64 : 
 struct BlobLayout {
     size_t off_q_indptr, off_kv_len, off_page_indptr, off_page_indices, off_row_seq, off_row_slot, off_units,
         off_items, off_works, off_heads, off_cta_cuda, off_cta_tensor, off_split, off_merge, off_status,
-        off_arrivals, blob_bytes;
+        off_arrivals, off_joins, off_join_blocks, off_select_chunks, off_select_base, blob_bytes;
 };
 
 static BlobLayout layout_blob(int batch, int total_q, int64_t total_pages, int64_t n_units,
                               int64_t n_items, int ctas_cuda, int ctas_tensor, int64_t n_split,
-                              int64_t n_merge_blocks) {
+                              int64_t n_merge_blocks, int64_t n_joins = 0, int64_t n_join_blocks = 0, int64_t n_select_chunks = 0,
+                              int64_t n_select_rows = 0) {
     BlobLayout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
@@ -81,6 +82,10 @@ static BlobLayout layout_blob(int batch, int total_q, int64_t total_pages, int64
     L.off_split = take(sizeof(int32_t) * (size_t)std::max<int64_t>(n_split, 1));
     L.off_merge = take(sizeof(int32_t) * (size_t)std::max<int64_t>(n_merge_blocks, 1));
     L.off_arrivals = take(sizeof(int32_t) * (size_t)std::max<int64_t>(n_units, 1));
+    L.off_joins = take(sizeof(Join) * (size_t)n_joins);
+    L.off_join_blocks = take(sizeof(int32_t) * (size_t)n_join_blocks);
+    L.off_select_chunks = take(sizeof(SelectChunk) * (size_t)n_select_chunks);
+    L.off_select_base = take(sizeof(int64_t) * (size_t)n_select_rows);
     L.blob_bytes = o;
     return L;
 }
@@ -192,6 +197,10 @@ struct UnitBuild {
     Unit u;
     int path;
     int64_t n_keys;   // keys visible to the unit's last token
+    int32_t run = -1;      // shared prefix: the run of sequences that the unit's rows belong to
+    bool flat = false;     // the unit holds the prefix that its run shares: all of its tokens see all of its keys
+    // its rows are written as partial rows, whatever the number of chunks
+    bool partial() const { return u.n_chunks > 1 || run >= 0; }
 };
 
 // Cuts the units of one path into items and deals them to `n_ctas` persistent CTAs.
@@ -431,11 +440,12 @@ int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joi
 // and merged in chunk order, so the output does not depend on which CTA ran what.
 //   The load limit is the smallest one under which the span units fit and the room left on all CTAs
 // covers the modelled time of the queue; it is found by bisection.
+//   queue_only: no CTA starts on a chunk of its own (its header would hold page ids, which selected pages have none of yet).
 //   Returns false, with only the units (their division and n_chunks) filled in, if the cuts leave more than
 // max_partial_rows partial rows.
 bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp,
                   std::vector<UnitBuild>& units, int group, int head_dim, const Model& model, int64_t kv_bytes, int n_ctas, const CutPolicy& policy,
-                  int64_t max_partial_rows, std::vector<Item>& items,
+                  int64_t max_partial_rows, bool queue_only, std::vector<Item>& items,
                   std::vector<int32_t>& cta_indptr_warp, std::vector<int32_t>& cta_indptr_tensor,
                   std::vector<int32_t>& item_cta, int32_t* queue_first, int32_t* queue_count) {
     struct Piece { Item it; int32_t cta; };
@@ -476,7 +486,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
         for (size_t i = 0; i < n0; ++i) {
             const int id = ids_tensor[i];
             UnitBuild& ub = units[(size_t)id];
-            if (ub.u.ntok * group <= 128) continue;
+            if (ub.u.ntok * group <= 128 || ub.flat) continue;      // (a shared prefix has partial rows anyway)
             if (tc.phase_ns + tc.item_ns + tiles_of(ub.n_keys, tc.gran) * dual_tile_ns <= limit0) continue;
             if (!by_keys.empty() && by_keys[(size_t)id]) continue;
             UnitBuild second = ub;
@@ -764,7 +774,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     }
     int64_t partial_rows = 0;
     for (const UnitBuild& ub : units)
-        if (ub.u.n_chunks > 1) partial_rows += (int64_t)ub.u.n_chunks * ub.u.ntok;
+        if (ub.partial()) partial_rows += (int64_t)ub.u.n_chunks * ub.u.ntok;
     if (partial_rows > max_partial_rows) return false;
     if (!queued) queue_up();
 
@@ -772,7 +782,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // queue), then the span items grouped by CTA
     cta_indptr_warp.assign((size_t)n_ctas + 1, 0);
     cta_indptr_tensor.assign((size_t)n_ctas + 1, 0);
-    const int n_start = (int)std::min<size_t>(chunks.size(), (size_t)(n_ctas - used));
+    const int n_start = queue_only ? 0 : (int)std::min<size_t>(chunks.size(), (size_t)(n_ctas - used));
     items.reserve(chunks.size() + pieces_out.size());
     item_cta.reserve(chunks.size() + pieces_out.size());
     for (size_t i = 0; i < chunks.size(); ++i) {
@@ -800,12 +810,67 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     return true;
 }
 
-}  // namespace
+// What a plan may have beyond the ordinary one.
+struct PlanExtra {
+    const asynclm_prefix_group* groups = nullptr;
+    int32_t n_groups = 0;
+    const asynclm_sparse* sparse = nullptr;
+};
 
-extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
-                            const asynclm_batch* batch, void* host_ws, size_t host_bytes,
-                            void* dev_ws, size_t dev_bytes, void* stream,
-                            asynclm_plan_t** out_plan) {
+// Sequences next to each other in the batch that share their first `tokens` keys: the units of `first` hold these for all rows
+// [row0, row0 + rows).
+struct Run {
+    int32_t first, tokens, row0, rows, seqs;
+};
+
+// A sequence with more rows of a kv head than a row tile keeps its prefix to itself: its items are bound by the products, of which
+// sharing saves none, and its partial rows would be many.
+constexpr int kMostSharedRows = 128;
+// Sharing costs partial rows and the join behind the attention; it has to save as many bytes of K and V as cross the bus in this time.
+constexpr int64_t kLeastSavedNs = 2500;
+
+// The runs of the groups (checked: ASYNCLM_OK, or what is wrong with them), and shared[b], the keys of sequence b that its run holds.
+int find_runs(const PlanExtra& extra, const asynclm_batch& batch, int B, int page, int group, int64_t bytes_per_key, bool all, std::vector<Run>& runs,
+              std::vector<int32_t>& shared) {
+    int end = 0;
+    int64_t saved = 0;
+    for (int g = 0; g < extra.n_groups; ++g) {
+        const asynclm_prefix_group& x = extra.groups[g];
+        if (x.first_seq < end || x.n_seqs < 1 || x.n_seqs > B - x.first_seq || x.prefix_tokens < 0 || x.prefix_tokens % page != 0 || x.reserved != 0)
+            return ASYNCLM_ERR_INVALID_ARG;
+        end = x.first_seq + x.n_seqs;
+        const size_t n_pages = (size_t)(x.prefix_tokens / page);
+        const int32_t* pages = nullptr;      // of the first sequence that has new tokens
+        bool open = false;                   // the last run may go on
+        for (int b = x.first_seq; b < end; ++b) {
+            const int ql = batch.q_indptr[b + 1] - batch.q_indptr[b];
+            if (ql == 0) continue;
+            if (batch.kv_len_before[b] < x.prefix_tokens) return ASYNCLM_ERR_INVALID_ARG;
+            const int32_t* own = batch.page_indices + batch.page_indptr[b];
+            if (pages == nullptr) pages = own;
+            else if (n_pages > 0 && std::memcmp(pages, own, n_pages * sizeof(int32_t)) != 0) return ASYNCLM_ERR_PAGE_TABLE;
+            if (n_pages == 0 || (int64_t)ql * group > kMostSharedRows) {
+                open = false;
+                continue;
+            }
+            if (!open) runs.push_back(Run{b, x.prefix_tokens, batch.q_indptr[b], 0, 0});
+            open = true;
+            runs.back().rows += ql;
+            ++runs.back().seqs;
+            shared[(size_t)b] = (int32_t)runs.size();
+        }
+    }
+    for (Run& r : runs) {
+        if (r.seqs < 2) r.tokens = 0;
+        saved += (int64_t)(r.seqs - 1) * r.tokens * bytes_per_key;
+    }
+    if (saved == 0 || (!all && saved * 1000 / kDramBytesPerUs < kLeastSavedNs)) runs.clear();
+    for (int32_t& at : shared) at = at > 0 && !runs.empty() && runs[(size_t)at - 1].tokens > 0 ? at : 0;
+    return ASYNCLM_OK;
+}
+
+int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch, const PlanExtra& extra, void* host_ws,
+              size_t host_bytes, void* dev_ws, size_t dev_bytes, void* stream, asynclm_plan_t** out_plan) {
     int rc = check_shape(shape);
     if (rc != ASYNCLM_OK) return rc;
     if (!batch || !host_ws || !out_plan || batch->batch < 0) return ASYNCLM_ERR_INVALID_ARG;
@@ -882,11 +947,40 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
             return ASYNCLM_ERR_PAGE_TABLE;
     }
 
+    // ---- what is shared, what is selected --------------------------------------------------------
+    const bool kv8 = opts && (opts->flags & ASYNCLM_PLAN_KV8);
+    const int64_t bytes_per_key = (int64_t)Hkv * (kv8 ? 2 * ((int64_t)shape->head_dim + 1) : 4 * (int64_t)shape->head_dim);
+    std::vector<Run> runs;
+    std::vector<int32_t> shared;      // 1 + the sequence's run, or 0
+    if (extra.n_groups > 0) {
+        shared.assign((size_t)B, 0);
+        rc = find_runs(extra, *batch, B, P, G, bytes_per_key, opts && (opts->flags & ASYNCLM_PLAN_SHARE_ALL), runs, shared);
+        if (rc != ASYNCLM_OK) return rc;
+    }
+    auto run_of = [&](int b) { return shared.empty() ? -1 : shared[(size_t)b] - 1; };
+    const asynclm_sparse* sparse = extra.sparse;
+    const int64_t n_select = sparse ? (int64_t)T * Hkv * sparse->budget_pages : 0;
+    std::vector<SelectChunk> select_chunks;
+    std::vector<int64_t> select_base;
+    int64_t select_keys = 0;      // scores of one kv head
+    if (sparse) {
+        select_base.reserve((size_t)T);
+        for (int b = 0; b < B; ++b)
+            for (int r = q_indptr[b]; r < q_indptr[b + 1]; ++r) {
+                const int64_t pages = (batch->kv_len_before[b] + (int64_t)(r - q_indptr[b])) / P + 1;
+                select_base.push_back(select_keys);
+                if (pages > sparse->budget_pages) select_keys += pages;
+                // (a row whose pages all fit has nothing scored: one chunk, which lists them)
+                const int64_t end = pages > sparse->budget_pages ? pages : 1;
+                for (int64_t j = 0; j < end; j += kSelectChunkPages) select_chunks.push_back(SelectChunk{r, (int32_t)j});
+            }
+        if ((int64_t)select_chunks.size() * Hkv > INT32_MAX || total_pages + n_select > (int64_t)1 << 40) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
+    }
+
     // ---- units ------------------------------------------------------------------------------
-    const bool tensor_wanted = !(opts && (opts->flags & ASYNCLM_PLAN_NO_TENSOR_PATH));
+    const bool tensor_wanted = !sparse && !(opts && (opts->flags & ASYNCLM_PLAN_NO_TENSOR_PATH));
     const int tensor_min_rows =
         (opts && opts->tensor_min_rows > 0) ? opts->tensor_min_rows : default_tensor_min_rows(shape->head_dim);
-    const bool kv8 = opts && (opts->flags & ASYNCLM_PLAN_KV8);
     const int TQ = tensor_tile_tokens(G);
     const int fixed_chunk = opts ? opts->kv_chunk_tokens : 0;
     const int ctas_cuda = n_sms * kCudaSlotsPerSm;
@@ -908,10 +1002,60 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
         split_units.clear(); merge_blocks.clear();
         n_items_cuda = queue_first = queue_count = 0;
         partial_rows = 0;
-        for (int b = 0; b < B; ++b) {
+        int64_t read_keys = total_kv;      // keys the step has to read, each (sequence, kv head) counted once
+        for (size_t k = 0; k < runs.size(); ++k) {
+            const Run& run = runs[k];
+            if (run.tokens == 0) continue;
+            read_keys -= (int64_t)(run.seqs - 1) * run.tokens;
+            const bool tensor = tensor_on && (int64_t)G * run.rows >= tensor_min_rows;
+            const int step = tensor ? TQ : warp_unit_tokens(G);
+            for (int h = 0; h < Hkv; ++h) {
+                for (int t0 = 0; t0 < run.rows; t0 += step) {
+                    UnitBuild ub{};
+                    ub.u.seq = run.first;
+                    ub.u.kv_head = h;
+                    ub.u.q_row0 = run.row0 + t0;
+                    ub.u.ntok = std::min(step, run.rows - t0);
+                    ub.u.kv_limit0 = run.tokens;      // of every token: no item reaches beyond
+                    ub.u.partial_base = -1;
+                    ub.u.page_base = page_indptr[run.first];
+                    ub.path = tensor ? kPathTensor : kPathCuda;
+                    ub.n_keys = run.tokens;
+                    ub.run = (int32_t)k;
+                    ub.flat = true;
+                    (tensor ? ids_tensor : ids_cuda).push_back((int)units.size());
+                    units.push_back(ub);
+                }
+            }
+        }
+        if (sparse) {
+            // A unit for every row and kv head, whose page list the selection writes: full pages, and the last one up to the row's own key.
+            read_keys = 0;
+            for (int b = 0; b < B; ++b)
+                for (int r = q_indptr[b]; r < q_indptr[b + 1]; ++r) {
+                    const int pos = batch->kv_len_before[b] + (r - q_indptr[b]);
+                    const int pages = std::min(pos / P + 1, (int)sparse->budget_pages);
+                    for (int h = 0; h < Hkv; ++h) {
+                        UnitBuild ub{};
+                        ub.u.seq = b;
+                        ub.u.kv_head = h;
+                        ub.u.q_row0 = r;
+                        ub.u.ntok = 1;
+                        ub.u.kv_limit0 = (pages - 1) * P + pos % P + 1;
+                        ub.u.partial_base = -1;
+                        ub.path = kPathCuda;
+                        ub.n_keys = ub.u.kv_limit0;
+                        ids_cuda.push_back((int)units.size());
+                        units.push_back(ub);
+                    }
+                    read_keys += units.back().n_keys;
+                }
+        }
+        for (int b = 0; b < B && !sparse; ++b) {
             const int ql = q_indptr[b + 1] - q_indptr[b];
             if (ql == 0) continue;
-            const int ctx = batch->kv_len_before[b];
+            const int run = run_of(b), front = run >= 0 ? runs[(size_t)run].tokens : 0;      // keys that the run holds
+            const int ctx = batch->kv_len_before[b] - front;
             const bool tensor = tensor_on && (int64_t)G * ql >= tensor_min_rows;
             const int step = tensor ? TQ : warp_unit_tokens(G);
             for (int h = 0; h < Hkv; ++h) {
@@ -924,9 +1068,10 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
                     ub.u.kv_limit0 = ctx + t0 + 1;
                     ub.u.n_chunks = 0;
                     ub.u.partial_base = -1;
-                    ub.u.page_base = page_indptr[b];
+                    ub.u.page_base = page_indptr[b] + front / P;
                     ub.path = tensor ? kPathTensor : kPathCuda;
                     ub.n_keys = (int64_t)ub.u.kv_limit0 + ub.u.ntok - 1;
+                    ub.run = run;
                     (tensor ? ids_tensor : ids_cuda).push_back((int)units.size());
                     units.push_back(ub);
                 }
@@ -934,33 +1079,32 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
         }
 
         // ---- items and CTA assignment --------------------------------------------------------------
-        if (fixed_chunk > 0 || ctas_cuda != ctas_tensor) {
+        if ((fixed_chunk > 0 && !sparse) || ctas_cuda != ctas_tensor) {
             cut_and_deal(ids_cuda, units, fixed_chunk, ctas_cuda, kCudaItemOverheadTiles, items,
                          cta_indptr_cuda, item_cta);
             n_items_cuda = (int)items.size();
             cut_and_deal(ids_tensor, units, fixed_chunk, ctas_tensor, kTensorItemOverheadTiles, items,
                          cta_indptr_tensor, item_cta);
         } else {
-            // bytes of K and V the step has to read, each (sequence, kv head) counted once
-            const int64_t kv_bytes = total_kv * Hkv * (kv8 ? 2 * ((int64_t)shape->head_dim + 1) : 4 * (int64_t)shape->head_dim);
-            too_many = !deal_dynamic(ids_tensor, ids_cuda, units, G, shape->head_dim, model_of(shape->head_dim, kv8), kv_bytes, ctas_cuda, policy, max_partial_rows, items,
-                                     cta_indptr_cuda, cta_indptr_tensor, item_cta, &queue_first, &queue_count);
+            too_many = !deal_dynamic(ids_tensor, ids_cuda, units, G, shape->head_dim, model_of(shape->head_dim, kv8), read_keys * bytes_per_key, ctas_cuda, policy,
+                                     max_partial_rows, sparse != nullptr, items, cta_indptr_cuda, cta_indptr_tensor, item_cta, &queue_first, &queue_count);
             if (too_many) return ASYNCLM_OK;
             n_items_cuda = queue_first + queue_count;
         }
 
         // ---- partial rows ------------------------------------------------------------------------
         for (size_t i = 0; i < units.size(); ++i) {
-            if (units[i].u.n_chunks > 1) {
+            if (units[i].partial()) {
                 units[i].u.partial_base = (int32_t)partial_rows;
                 partial_rows += (int64_t)units[i].u.n_chunks * units[i].u.ntok;
+                if (partial_rows > INT32_MAX / 2) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
+                if (units[i].run >= 0) continue;      // joined with the other unit of its rows, below
                 split_units.push_back((int32_t)i);
                 if (i >= (size_t)(INT32_MAX >> 6)) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
                 // split units of the warp body are merged inside the attention kernel; those of the span
                 // body by the merge kernel
                 if (units[i].path == kPathTensor)
                     for (int rb = 0; rb * 4 < units[i].u.ntok * G; ++rb) merge_blocks.push_back((int32_t)((i << 6) | (size_t)rb));
-                if (partial_rows > INT32_MAX / 2) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
             }
         }
         return ASYNCLM_OK;
@@ -979,9 +1123,9 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
         if (fixed_chunk == 0) {
             int64_t span_rows = 0, span_units = 0, warp_rows = 0;
             for (const UnitBuild& ub : units) {
-                const int64_t rows = ub.u.n_chunks > 1 ? (int64_t)ub.u.n_chunks * ub.u.ntok : 0;
+                const int64_t rows = ub.partial() ? (int64_t)ub.u.n_chunks * ub.u.ntok : 0;
                 if (ub.path != kPathTensor) warp_rows += rows;
-                else if (rows > 0) span_rows += rows, ++span_units;
+                else if (rows > 0 && !ub.flat) span_rows += rows, ++span_units;
             }
             const int64_t room = (int64_t)(ASYNCLM_STATIC_SCRATCH_BYTES / ((size_t)G * (shape->head_dim + 1) * sizeof(float))) - warp_rows;
             CutPolicy fewer;
@@ -999,6 +1143,27 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
 
     const int n_split = (int)split_units.size();
 
+    // ---- rows of a run: the unit with the sequence's own keys beside the one with the shared keys ----
+    std::vector<Join> joins;
+    std::vector<int32_t> join_blocks;
+    if (!runs.empty()) {
+        std::vector<std::vector<int32_t>> flat(runs.size() * (size_t)Hkv);      // a run's units with its prefix, by rows
+        for (size_t i = 0; i < units.size(); ++i)
+            if (units[i].flat) flat[(size_t)units[i].run * Hkv + units[i].u.kv_head].push_back((int32_t)i);
+        for (const UnitBuild& own : units) {
+            if (own.run < 0 || own.flat) continue;
+            for (int32_t id : flat[(size_t)own.run * Hkv + own.u.kv_head]) {
+                const Unit& pre = units[(size_t)id].u;
+                const int r0 = std::max(own.u.q_row0, pre.q_row0), r1 = std::min(own.u.q_row0 + own.u.ntok, pre.q_row0 + pre.ntok);
+                if (r0 >= r1) continue;
+                if (joins.size() >= (size_t)(INT32_MAX >> 6)) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
+                for (int rb = 0; rb * 4 < (r1 - r0) * G; ++rb) join_blocks.push_back((int32_t)((joins.size() << 6) | (size_t)rb));
+                joins.push_back(Join{r0, r1 - r0, own.u.kv_head, own.u.partial_base + r0 - own.u.q_row0, own.u.ntok, own.u.n_chunks,
+                                     pre.partial_base + r0 - pre.q_row0, pre.ntok, pre.n_chunks, {0, 0, 0}});
+            }
+        }
+    }
+
     // CTAs without an item, which stand at the end, have something to do only where there is a queue: else they are not
     // launched, and their headers (384 bytes each, of which a small plan mostly consists) are neither cleared nor uploaded.
     int grid_cuda = ctas_cuda, grid_tensor = ctas_tensor;
@@ -1010,11 +1175,20 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
 
     // ---- pack ---------------------------------------------------------------------------------
     BlobLayout L = layout_blob(B, T, total_pages, (int64_t)units.size(), n_items, grid_cuda,
-                               grid_tensor, (int64_t)n_split, (int64_t)merge_blocks.size());
+                               grid_tensor, (int64_t)n_split, (int64_t)merge_blocks.size(), (int64_t)joins.size(), (int64_t)join_blocks.size(),
+                               (int64_t)select_chunks.size(), (int64_t)select_base.size());
     const size_t plan_bytes = align_up(sizeof(asynclm_plan_s), 256);
     const size_t item_cta_bytes = align_up(sizeof(int32_t) * (size_t)std::max(n_items, 1), 256);
-    const size_t host_need = plan_bytes + L.blob_bytes + item_cta_bytes;
-    const size_t dev_need = L.blob_bytes + partial_bytes(partial_rows, G, shape->head_dim);
+    const size_t shift_bytes = runs.empty() ? 0 : align_up(sizeof(int32_t) * units.size(), 256);
+    const size_t host_need = plan_bytes + L.blob_bytes + item_cta_bytes + shift_bytes;
+    // behind the blob: partial rows, then a selection's counters, page lists and scores
+    const size_t off_arrived = L.blob_bytes + partial_bytes(partial_rows, G, shape->head_dim);
+    const size_t off_select = off_arrived + (sparse ? align_up(sizeof(int32_t) * (size_t)std::max(T, 1) * Hkv, 256) : 0);
+    const size_t off_keys = off_select + align_up(sizeof(int32_t) * (size_t)n_select, 256);
+    const size_t dev_need = off_keys + align_up(sizeof(uint64_t) * (size_t)select_keys * Hkv, 256);
+    // the lists as indices of the page table: 2^31 of them are 8 GB
+    const int64_t select_at = ((int64_t)off_select - (int64_t)L.off_page_indices) / (int64_t)sizeof(int32_t);
+    if (sparse && select_at + n_select > INT32_MAX) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
     if (host_bytes < host_need) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
     if (!host_only && dev_bytes < dev_need) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
 
@@ -1040,7 +1214,10 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
             row_slot[r] = (int64_t)batch->page_indices[page_indptr[b] + pos / P] * P + pos % P;
         }
     Unit* h_units = (Unit*)(hb + L.off_units);
-    for (size_t i = 0; i < units.size(); ++i) h_units[i] = units[i].u;
+    for (size_t i = 0; i < units.size(); ++i) {
+        if (sparse) units[i].u.page_base = (int32_t)(select_at + ((int64_t)units[i].u.q_row0 * Hkv + units[i].u.kv_head) * sparse->budget_pages);
+        h_units[i] = units[i].u;
+    }
     if (n_items > 0) std::memcpy(hb + L.off_items, items.data(), sizeof(Item) * (size_t)n_items);
     int32_t* h_heads = (int32_t*)(hb + L.off_heads);
     std::memset(h_heads, 0, sizeof(int32_t) * kHeadWords * (size_t)std::max(grid_cuda, grid_tensor));
@@ -1058,7 +1235,7 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
         w.partial_row0 = u.partial_base < 0 ? -1 : u.partial_base + it.chunk * u.ntok;
         w.page0 = u.page_base + it.kv0 / kPage;
         w.unit = it.unit;
-        w.n_chunks = u.n_chunks;
+        w.n_chunks = units[(size_t)it.unit].run >= 0 ? 0 : u.n_chunks;      // 0: the attention kernel merges none of them
         w.partial_base = u.partial_base;
         w.q_seq0 = q_indptr[u.seq];
         h_works[i] = w;
@@ -1086,7 +1263,18 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     if (n_split > 0) std::memcpy(hb + L.off_split, split_units.data(), sizeof(int32_t) * split_units.size());
     if (!merge_blocks.empty())
         std::memcpy(hb + L.off_merge, merge_blocks.data(), sizeof(int32_t) * merge_blocks.size());
+    if (!joins.empty()) {
+        std::memcpy(hb + L.off_joins, joins.data(), sizeof(Join) * joins.size());
+        std::memcpy(hb + L.off_join_blocks, join_blocks.data(), sizeof(int32_t) * join_blocks.size());
+    }
+    if (!select_chunks.empty()) {
+        std::memcpy(hb + L.off_select_chunks, select_chunks.data(), sizeof(SelectChunk) * select_chunks.size());
+        std::memcpy(hb + L.off_select_base, select_base.data(), sizeof(int64_t) * select_base.size());
+    }
     int32_t* h_item_cta = (int32_t*)(hb + L.blob_bytes);
+    int32_t* h_shift = runs.empty() ? nullptr : (int32_t*)(hb + L.blob_bytes + item_cta_bytes);
+    for (size_t i = 0; i < units.size() && h_shift; ++i)
+        h_shift[i] = units[i].flat ? -1 : units[i].run >= 0 ? runs[(size_t)units[i].run].tokens : 0;
     if (n_items > 0) std::memcpy(h_item_cta, item_cta.data(), sizeof(int32_t) * (size_t)n_items);
 
     asynclm_plan_s* plan = (asynclm_plan_s*)host_ws;
@@ -1098,8 +1286,11 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     plan->h_units = h_units;
     plan->h_items = (const Item*)(hb + L.off_items);
     plan->h_item_cta = h_item_cta;
-    plan->h_kv_len_before = (const int32_t*)(hb + L.off_kv_len);
+    plan->h_q_indptr = (const int32_t*)(hb + L.off_q_indptr);
+    plan->h_unit_shift = h_shift;
     plan->h_units_path_split = n_items_cuda;
+    plan->shared = runs.empty() ? 0 : 1;
+    plan->sparse = sparse ? 1 : 0;
     for (int b = 0; b < B; ++b) plan->max_q_len = std::max(plan->max_q_len, q_indptr[b + 1] - q_indptr[b]);
 
     char* db = (char*)dev_ws;
@@ -1127,6 +1318,21 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     d.partial_o = (float*)dp(L.blob_bytes);
     d.partial_lse = (float*)dp(L.blob_bytes + align_up((size_t)partial_rows * (size_t)G *
                                                            (size_t)shape->head_dim * sizeof(float), 256));
+    d.joins = (const Join*)dp(L.off_joins);
+    d.join_blocks = (const int32_t*)dp(L.off_join_blocks);
+    d.num_join_blocks = (int32_t)join_blocks.size();
+    d.total_pages = total_pages;
+    if (sparse) {
+        d.select_chunks = (const SelectChunk*)dp(L.off_select_chunks);
+        d.select_base = (const int64_t*)dp(L.off_select_base);
+        d.select_arrivals = (int32_t*)dp(off_arrived);
+        d.select_pages = (int32_t*)dp(off_select);
+        d.select_keys = (unsigned long long*)dp(off_keys);
+        d.num_select_chunks = (int32_t)select_chunks.size();
+        d.select_budget = sparse->budget_pages;
+        d.select_first = sparse->first_pages;
+        d.select_last = sparse->last_pages;
+    }
     d.batch = B;
     d.total_q = T;
     d.num_units = (int32_t)units.size();
@@ -1160,7 +1366,7 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
     info.num_items_tensor = d.num_items_tensor;
     info.launches_append = T > 0 ? 1 : 0;
     // span tiles and decode rows share one fused launch when a step has both
-    info.launches_attn = ((n_items_cuda > 0 || d.num_items_tensor > 0) ? 1 : 0) + (merge_blocks.empty() ? 0 : 1);
+    info.launches_attn = ((n_items_cuda > 0 || d.num_items_tensor > 0) ? 1 : 0) + (merge_blocks.empty() ? 0 : 1) + (joins.empty() ? 0 : 1);
     info.num_sms = n_sms;
     info.total_kv_tokens = total_kv;
     info.device_bytes_used = dev_need;
@@ -1173,10 +1379,42 @@ extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_optio
         cudaError_t e = by_kernel ? upload_plan(db, by_kernel, L.blob_bytes, (cudaStream_t)stream)
                                   : cudaMemcpyAsync(db, hb, L.blob_bytes, cudaMemcpyHostToDevice, (cudaStream_t)stream);
         if (int rc = cuda_status(e)) return rc;
+        // (no call may find anything but pages of the pool in the lists, and the counters start at zero)
+        if (sparse && T > 0) e = cudaMemsetAsync(db + off_arrived, 0, off_keys - off_arrived, (cudaStream_t)stream);
+        if (int rc = cuda_status(e)) return rc;
         plan->fresh = by_kernel ? 1 : 0;
     }
     *out_plan = plan;
     return ASYNCLM_OK;
+}
+
+}  // namespace
+
+extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
+                            const asynclm_batch* batch, void* host_ws, size_t host_bytes,
+                            void* dev_ws, size_t dev_bytes, void* stream,
+                            asynclm_plan_t** out_plan) {
+    return make_plan(shape, opts, batch, PlanExtra{}, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
+}
+
+extern "C" int asynclm_plan_prefix(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch,
+                                   const asynclm_prefix_group* groups, int32_t n_groups, void* host_ws, size_t host_bytes, void* dev_ws,
+                                   size_t dev_bytes, void* stream, asynclm_plan_t** out_plan) {
+    if (n_groups < 0 || (n_groups > 0 && !groups)) return ASYNCLM_ERR_INVALID_ARG;
+    PlanExtra extra;
+    extra.groups = groups;
+    extra.n_groups = n_groups;
+    return make_plan(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
+}
+
+extern "C" int asynclm_plan_sparse(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch, const asynclm_sparse* sparse,
+                                   void* host_ws, size_t host_bytes, void* dev_ws, size_t dev_bytes, void* stream, asynclm_plan_t** out_plan) {
+    if (!sparse || sparse->first_pages < 0 || sparse->last_pages < 1 || sparse->reserved != 0 ||
+        (int64_t)sparse->first_pages + sparse->last_pages > sparse->budget_pages || (opts && opts->kv_chunk_tokens != 0))
+        return ASYNCLM_ERR_INVALID_ARG;
+    PlanExtra extra;
+    extra.sparse = sparse;
+    return make_plan(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
 }
 
 extern "C" int asynclm_plan_get_info(const asynclm_plan_t* plan, asynclm_plan_info* info) {
@@ -1193,6 +1431,12 @@ extern "C" int asynclm_plan_get_shape(const asynclm_plan_t* plan, asynclm_shape*
     return ASYNCLM_OK;
 }
 
+extern "C" int asynclm_plan_get_sparse(const asynclm_plan_t* plan, asynclm_sparse* sparse) {
+    if (!plan || !sparse || plan->magic != kPlanMagic || !plan->sparse) return ASYNCLM_ERR_INVALID_ARG;
+    *sparse = asynclm_sparse{plan->dev.select_budget, plan->dev.select_first, plan->dev.select_last, 0};
+    return ASYNCLM_OK;
+}
+
 extern "C" int asynclm_plan_get_items(const asynclm_plan_t* plan, asynclm_item_view* out,
                                       int32_t capacity) {
     if (!plan || plan->magic != kPlanMagic || capacity < 0 || (capacity > 0 && !out))
@@ -1204,10 +1448,11 @@ extern "C" int asynclm_plan_get_items(const asynclm_plan_t* plan, asynclm_item_v
         asynclm_item_view v;
         v.seq = u.seq;
         v.kv_head = u.kv_head;
-        v.tok0 = u.kv_limit0 - 1 - plan->h_kv_len_before[u.seq];
+        const int32_t shift = plan->h_unit_shift ? plan->h_unit_shift[it.unit] : 0;
+        v.tok0 = u.q_row0 - plan->h_q_indptr[u.seq];
         v.ntok = u.ntok;
-        v.kv0 = it.kv0;
-        v.kv1 = it.kv1;
+        v.kv0 = it.kv0 + std::max(shift, 0);
+        v.kv1 = it.kv1 + std::max(shift, 0);
         v.path = i < plan->h_units_path_split ? kPathCuda : kPathTensor;
         v.cta = plan->h_item_cta[i];
         out[i] = v;

@@ -28,16 +28,22 @@ struct asynclm_plan_s {
     const asynclm::Unit* h_units;
     const asynclm::Item* h_items;
     const int32_t* h_item_cta;
-    const int32_t* h_kv_len_before;
+    const int32_t* h_q_indptr;
     int32_t h_units_path_split;   // items [0, this) are warp-body items, the rest span items
+    const int32_t* h_unit_shift;  // keys in front of the unit's first (a shared prefix's length), or -1: the unit holds a shared prefix itself
     int32_t device;
     int32_t host_only;
+    int32_t shared, sparse;       // made by asynclm_plan_prefix with something to share, by asynclm_plan_sparse
+    mutable int32_t selected;     // sparse: a call has chosen pages
     int32_t max_q_len;            // longest span of the step
     mutable int32_t fresh;        // the upload was a kernel, and no launch has been ordered behind it yet (see PlanUse)
     mutable unsigned long long captured_in;      // 1 + the id of the last stream capture that a launch of a fresh plan went into, or 0
 };
 
 namespace asynclm {
+
+// False: the plan is for selected pages, and none have been selected with it.
+inline bool pages_chosen(const asynclm_plan_s* plan) { return !plan->sparse || __atomic_load_n(&plan->selected, __ATOMIC_ACQUIRE) != 0; }
 
 // The device plan for one call.  The kernels read the plan ahead of their wait for the kernel in front, which may only be as far as its
 // trigger then: what a copy in the stream wrote is complete and in no cache by that time, what a kernel in front is
@@ -61,6 +67,12 @@ class PlanUse {
             status = cudaStreamCaptureStatusInvalidated;
         }
         dev.full_launch = status != cudaStreamCaptureStatusActive || __atomic_load_n(&plan->captured_in, __ATOMIC_ACQUIRE) != id + 1;
+    }
+
+    // For the attention: a plan for selected pages has its page lists written by the kernel in front (asynclm_select_pages), so this launch
+    // starts when that has completed.
+    void reads_page_lists() {
+        if (plan->sparse) dev.full_launch = 1;
     }
 
     // Takes and returns the outcome of the call's first launch with `dev`; what the call launches behind it starts early.

@@ -49,6 +49,22 @@ struct alignas(16) Work {
                            // ctx = kv_limit0 - 1 - (q_row0 - q_seq0))
 };
 
+// Rows of a sequence that shares a prefix, to be joined from two sets of partial rows: those of the unit that holds the sequence's own
+// keys and those of the unit that holds the shared ones (each chunk's rows are `stride` partial rows behind the last one's).
+struct alignas(16) Join {
+    int32_t q_row0, ntok;      // global token rows [q_row0, q_row0 + ntok)
+    int32_t kv_head;
+    int32_t own_row, own_stride, own_chunks;      // partial row of token q_row0 in chunk 0
+    int32_t pre_row, pre_stride, pre_chunks;
+    int32_t pad[3];
+};
+
+// Pages of one row of a plan for selected pages that one CTA and kv head scores; see select_pages.cu.
+struct SelectChunk {
+    int32_t row, page0;
+};
+constexpr int kSelectChunkPages = 64;
+
 // Per persistent CTA, one 384-byte header that holds everything the CTA needs to issue its first
 // loads after a single round trip to memory: words 0-3 its item ranges (span body first, last;
 // warp body first, last), words 8-19 the Work record of its first span item, words 20-31 that of
@@ -90,6 +106,16 @@ struct DevPlan {
     int32_t* status;                 // device status word
     int32_t* counters;               // [0] next chunk of the warp body's queue, [1] CTAs that are done with the
                                      // queue; both are zero between launches (the last CTA puts them back)
+    const Join* joins;               // plans with a shared prefix
+    const int32_t* join_blocks;      // [num_join_blocks] (join << 6) | row block: 4 (token, head) rows each
+    const SelectChunk* select_chunks;// plans for selected pages: the score kernel's work list
+    const int64_t* select_base;      // [T] pages in front of the row's in the score array (of one kv head)
+    int32_t* select_pages;           // [T][Hkv][budget] physical pages: what the units' page0 points at
+    unsigned long long* select_keys; // scores as ordered integers: [row][Hkv][pages of the row]
+    int32_t* select_arrivals;        // [T][Hkv] chunks that are scored; zero between launches
+    int32_t num_join_blocks, num_select_chunks;
+    int32_t select_budget, select_first, select_last;
+    int64_t total_pages;             // entries of the page table
     int32_t queue_first, queue_count;// items [queue_first, queue_first + queue_count) are handed out at run time
     int32_t batch, total_q, num_units, num_items, num_items_cuda, num_items_tensor;
     int32_t num_split_units, num_ctas_cuda, num_ctas_tensor;
