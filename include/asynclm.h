@@ -561,12 +561,12 @@ int asynclm_kv8_bounds(const asynclm_plan_t* plan, const void* kv8_pool, const v
  * Selects the pages of a plan of asynclm_plan_sparse.  The score of a page for a token and a kv head is
  *     max over the head's G queries q of sum_c max(q_c * least_c, q_c * largest_c),
  * which no key in the page exceeds (before sm_scale).  Of the pages with keys that the token sees, the first and last ones of the plan are taken, and those
- * of the others with the largest scores, the lowest page among equals.  Scores are held in 64 bits, so that the choice does not hang on
- * the order of additions; infinities and NaN in q or bounds count as 2^128 and more, with their sign, subnormal values as zero.
+ * of the others with the largest scores, the lowest page among equals.  Scores count as in 64 bits, so that the choice does not hang on
+ * the order of additions; values beyond +-2^56 in q or bounds, infinities and NaN among them, count as +-2^56.
  *
  *   q          device, bf16 [T][num_q_heads][head_dim], as the attention takes it
  *   pages_out  device, int32 [T][num_kv_heads][budget_pages], or NULL: the chosen pages as numbers inside the sequence, rising, -1 behind the last
- * One kernel.  Errors: INVALID_ARG (also: the plan is of another kind), CUDA.
+ * Two kernels, or one where all pages fit the budget.  Errors: INVALID_ARG (also: the plan is of another kind), CUDA.
  */
 int asynclm_select_pages(const asynclm_plan_t* plan, const void* q, const void* key_bounds, int32_t* pages_out, void* stream);
 

@@ -823,6 +823,9 @@ struct Run {
     int32_t first, tokens, row0, rows, seqs;
 };
 
+// Selected pages: a chunk of scores is a multiple of these pages, and there are about so many for an SM.
+constexpr int kSelectWarpPages = 64, kSelectCtasPerSm = 3;
+
 // A sequence with more rows of a kv head than a row tile keeps its prefix to itself: its items are bound by the products, of which
 // sharing saves none, and its partial rows would be many.
 constexpr int kMostSharedRows = 128;
@@ -963,18 +966,36 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     std::vector<SelectChunk> select_chunks;
     std::vector<int64_t> select_base;
     int64_t select_keys = 0;      // scores of one kv head
+    int32_t chunk_pages = kSelectWarpPages;
     if (sparse) {
+        auto pages_of = [&](int r, int b) { return (batch->kv_len_before[b] + (r - q_indptr[b])) / P + 1; };
+        // Rows that have more pages than the budget are scored, as many together as a chunk takes (they read the same bounds).
+        struct Group { int row0, rows, pages; };
+        std::vector<Group> groups;
+        int64_t scored = 0;
         select_base.reserve((size_t)T);
         for (int b = 0; b < B; ++b)
             for (int r = q_indptr[b]; r < q_indptr[b + 1]; ++r) {
-                const int64_t pages = (batch->kv_len_before[b] + (int64_t)(r - q_indptr[b])) / P + 1;
+                const int pages = pages_of(r, b);
                 select_base.push_back(select_keys);
-                if (pages > sparse->budget_pages) select_keys += pages;
-                // (a row whose pages all fit has nothing scored: one chunk, which lists them)
-                const int64_t end = pages > sparse->budget_pages ? pages : 1;
-                for (int64_t j = 0; j < end; j += kSelectChunkPages) select_chunks.push_back(SelectChunk{r, (int32_t)j});
+                if (pages <= sparse->budget_pages) continue;
+                select_keys += pages;
+                if (r > q_indptr[b] && !groups.empty() && groups.back().row0 + groups.back().rows == r && groups.back().rows < kSelectQueries / G) {
+                    ++groups.back().rows;
+                    scored += pages - groups.back().pages;
+                    groups.back().pages = pages;
+                } else {
+                    groups.push_back(Group{r, 1, pages});
+                    scored += pages;
+                }
             }
-        if ((int64_t)select_chunks.size() * Hkv > INT32_MAX || total_pages + n_select > (int64_t)1 << 40) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
+        // chunks of equal length, as many as make kSelectCtasPerSm CTAs for an SM
+        const int64_t share = (scored * Hkv + (int64_t)kSelectCtasPerSm * n_sms - 1) / ((int64_t)kSelectCtasPerSm * n_sms);
+        chunk_pages = (int32_t)std::min<int64_t>(std::max<int64_t>((share + kSelectWarpPages - 1) / kSelectWarpPages, 1) * kSelectWarpPages, 1 << 20);
+        for (const Group& g : groups)
+            for (int64_t j = 0; j < g.pages; j += chunk_pages) select_chunks.push_back(SelectChunk{g.row0, g.rows, (int32_t)j, 0});
+        if ((int64_t)select_chunks.size() * Hkv > INT32_MAX || (int64_t)T * Hkv > INT32_MAX || total_pages + n_select > (int64_t)1 << 40)
+            return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
     }
 
     // ---- units ------------------------------------------------------------------------------
@@ -1181,11 +1202,12 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     const size_t item_cta_bytes = align_up(sizeof(int32_t) * (size_t)std::max(n_items, 1), 256);
     const size_t shift_bytes = runs.empty() ? 0 : align_up(sizeof(int32_t) * units.size(), 256);
     const size_t host_need = plan_bytes + L.blob_bytes + item_cta_bytes + shift_bytes;
-    // behind the blob: partial rows, then a selection's counters, page lists and scores
-    const size_t off_arrived = L.blob_bytes + partial_bytes(partial_rows, G, shape->head_dim);
-    const size_t off_select = off_arrived + (sparse ? align_up(sizeof(int32_t) * (size_t)std::max(T, 1) * Hkv, 256) : 0);
+    // behind the blob: partial rows, then a selection's error bounds, page lists and scores
+    const size_t off_error = L.blob_bytes + partial_bytes(partial_rows, G, shape->head_dim);
+    const size_t off_select = off_error + (sparse ? align_up(sizeof(float) * (size_t)T * Hkv, 256) : 0);
     const size_t off_keys = off_select + align_up(sizeof(int32_t) * (size_t)n_select, 256);
-    const size_t dev_need = off_keys + align_up(sizeof(uint64_t) * (size_t)select_keys * Hkv, 256);
+    const size_t off_exact = off_keys + align_up(sizeof(uint32_t) * (size_t)select_keys * Hkv, 256);
+    const size_t dev_need = off_exact + align_up(sizeof(uint64_t) * (size_t)select_keys * Hkv, 256);
     // the lists as indices of the page table: 2^31 of them are 8 GB
     const int64_t select_at = ((int64_t)off_select - (int64_t)L.off_page_indices) / (int64_t)sizeof(int32_t);
     if (sparse && select_at + n_select > INT32_MAX) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
@@ -1325,10 +1347,12 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     if (sparse) {
         d.select_chunks = (const SelectChunk*)dp(L.off_select_chunks);
         d.select_base = (const int64_t*)dp(L.off_select_base);
-        d.select_arrivals = (int32_t*)dp(off_arrived);
         d.select_pages = (int32_t*)dp(off_select);
-        d.select_keys = (unsigned long long*)dp(off_keys);
+        d.select_keys = (unsigned*)dp(off_keys);
+        d.select_exact = (unsigned long long*)dp(off_exact);
+        d.select_error = (unsigned*)dp(off_error);
         d.num_select_chunks = (int32_t)select_chunks.size();
+        d.select_chunk_pages = chunk_pages;
         d.select_budget = sparse->budget_pages;
         d.select_first = sparse->first_pages;
         d.select_last = sparse->last_pages;
@@ -1379,8 +1403,8 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
         cudaError_t e = by_kernel ? upload_plan(db, by_kernel, L.blob_bytes, (cudaStream_t)stream)
                                   : cudaMemcpyAsync(db, hb, L.blob_bytes, cudaMemcpyHostToDevice, (cudaStream_t)stream);
         if (int rc = cuda_status(e)) return rc;
-        // (no call may find anything but pages of the pool in the lists, and the counters start at zero)
-        if (sparse && T > 0) e = cudaMemsetAsync(db + off_arrived, 0, off_keys - off_arrived, (cudaStream_t)stream);
+        // (no call may find anything but pages of the pool in the lists)
+        if (sparse && T > 0) e = cudaMemsetAsync(db + off_error, 0, off_keys - off_error, (cudaStream_t)stream);
         if (int rc = cuda_status(e)) return rc;
         plan->fresh = by_kernel ? 1 : 0;
     }

@@ -59,11 +59,12 @@ struct alignas(16) Join {
     int32_t pad[3];
 };
 
-// Pages of one row of a plan for selected pages that one CTA and kv head scores; see select_pages.cu.
+// Plans for selected pages: rows next to each other of one sequence, for which one CTA and kv head score DevPlan::select_chunk_pages pages (see
+// select_pages.cu).
 struct SelectChunk {
-    int32_t row, page0;
+    int32_t row0, rows, page0, pad;
 };
-constexpr int kSelectChunkPages = 64;
+constexpr int kSelectQueries = 16;      // (row, head) pairs of a chunk at most
 
 // Per persistent CTA, one 384-byte header that holds everything the CTA needs to issue its first
 // loads after a single round trip to memory: words 0-3 its item ranges (span body first, last;
@@ -111,10 +112,11 @@ struct DevPlan {
     const SelectChunk* select_chunks;// plans for selected pages: the score kernel's work list
     const int64_t* select_base;      // [T] pages in front of the row's in the score array (of one kv head)
     int32_t* select_pages;           // [T][Hkv][budget] physical pages: what the units' page0 points at
-    unsigned long long* select_keys; // scores as ordered integers: [row][Hkv][pages of the row]
-    int32_t* select_arrivals;        // [T][Hkv] chunks that are scored; zero between launches
+    unsigned* select_keys;           // scores in 32 bits, as ordered integers: [row][Hkv][pages of the row]
+    unsigned long long* select_exact;// the same in 64 bits, of pages whose 32 bits leave the choice open
+    unsigned* select_error;          // [T][Hkv] how far the 32 bits of a row's scores may be off (a float); zero between launches
     int32_t num_join_blocks, num_select_chunks;
-    int32_t select_budget, select_first, select_last;
+    int32_t select_chunk_pages, select_budget, select_first, select_last;
     int64_t total_pages;             // entries of the page table
     int32_t queue_first, queue_count;// items [queue_first, queue_first + queue_count) are handed out at run time
     int32_t batch, total_q, num_units, num_items, num_items_cuda, num_items_tensor;

@@ -2,15 +2,22 @@
 // could score highest.
 //
 // Score.  For a query q and a page whose keys lie between lo and hi, channel by channel, no key scores more than
-//     sum_c max(q_c lo_c, q_c hi_c) = sum_c q_c (q_c < 0 ? lo_c : hi_c);
-// a page's score is the largest over the G queries of the kv head.  Two sums of 32 bits in different orders differ in their last bits, and with
-// them the choice, wherever two pages are close.  So the sums are held in 64 bits, where a product of bf16 values is exact: the choice depends on
-// the values alone but for ties within 2^-45.  A bf16 value becomes an fp64 one by its bits (the upper word holds all of it), and which of lo and hi
-// is wanted is a bit operation on that word.
+//     sum_c max(q_c lo_c, q_c hi_c) = sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c;
+// a page's score is the largest over the G queries of the kv head.  As two products it is a matrix product of bf16 operands, pages x queries.  But sums
+// of 32 bits in different orders differ in their last bits, and with them the choice, wherever two pages are close; the choice shall depend on the
+// values alone.  So it is made in two steps: scores from the tensor cores with a bound of their error, e = 2^-14 sum_c |q_c| max(|lo_c|, |hi_c|), the
+// largest of the row; then, as the budget's last score t in 32 bits lies within e of the one in full, pages above t + 2e are in, pages below
+// t - 2e are out, and the few in between (one to five, where scores are not equal) are scored again in 64 bits, where a product of bf16 values is exact.
+//   (e: a score is 2 D / 16 instructions one after the other, each of which adds 16 exact products to the sum; with truncation to 2^-23 of the largest
+// for each of the 17 terms that is 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128.)
+//   In 64 bits for all pages the score kernel took 106 us for 48 sequences of 3-12 K tokens with 1-4 new ones each (451 K sums over 4 heads of 128):
+// for every product a bit operation, an fma and a move, 112 instructions a sum.
 //
-// A CTA scores kSelectChunkPages pages of one (row, kv head), a warp 16 / G of them at a time, four channels to a lane; the 16 sums are exchanged
-// and halved together.  Scores go to the workspace as ordered integers.  The CTA that finishes a row's last chunk selects: the 64-bit threshold
-// by histograms of eight bits, from the first bit in which the scores differ, then the pages in rising order, each thread a stretch of them.
+// select_score_kernel: a warp takes 16 pages, the M of its MMAs, a CTA a stretch of a sequence's pages for one kv head and all of the sequence's rows
+// (drafted tokens) at once.  Operands come from memory as they are: the k index may stand for any channel as long as it is the same for both
+// sides, so a thread's 16 bytes of a page's row are two steps' fragments.  Bound by the bytes of the bounds.
+// select_choose_kernel: a CTA for every (row, kv head).  A histogram of eight bits, from the first bit in which the scores differ, narrows t to one bin, whose
+// keys are ranked against each other; then the pages in rising order, each thread a stretch of them.
 #include <algorithm>
 
 #include "asynclm.h"
@@ -22,167 +29,253 @@ namespace asynclm {
 
 namespace {
 
-constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
-constexpr int kKeysInShared = 4096;      // of a row (65 536 tokens); longer ones are read from L2
-constexpr unsigned long long kAlways = ~0ull;      // key of a page that is taken whatever its score
+constexpr int kScoreThreads = 256, kScoreWarps = kScoreThreads / 32;
+constexpr int kTilePages = 16;
+constexpr int kChooseThreads = 512, kChooseWarps = kChooseThreads / 32;
+constexpr int kKeysInShared = 8192;                // of a row (131 072 tokens); longer ones are read from L2
+constexpr unsigned kAlways = 0xffffffffu;          // key of a page that is taken whatever its score
+constexpr unsigned kTaken = 0xfffffffeu;
 
-// Upper word of the fp64 number with a bf16 number's value (the lower word is zero).  Subnormal ones count as zero, infinities and NaN as 2^128 and
-// more, with their sign.
-__device__ __forceinline__ uint32_t f64_word(uint32_t bf16_bits) {
-    const uint32_t m = bf16_bits & 0x7fffu;
-    return m < 0x80u ? 0u : (bf16_bits & 0x8000u) << 16 | ((m << 13) + 0x38000000u);
+// Values beyond +-2^56, NaN among them, count as +-2^56 (so that no sum of products overflows).
+constexpr uint32_t kMostPair = 0x5b805b80u, kLeastPair = 0xdb80db80u;
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
-__device__ __forceinline__ double f64_of(uint32_t word) { return __hiloint2double((int)word, 0); }
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t held(uint32_t x) { return min2(max2(x, kLeastPair), kMostPair); }
 
+__device__ __forceinline__ unsigned ordered(float x) {
+    const unsigned u = __float_as_uint(x + 0.f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ unsigned long long ordered(double x) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-template <int D, int G>
-struct SelectShape {
-    static constexpr int LANES = D / 4;              // of a page: four channels to a lane
-    static constexpr int AT_ONCE = 32 / LANES;       // pages that a warp's load covers
-    static constexpr int LOADS = 16 / G;             // of them, together 16 sums a lane
-    static constexpr int PAGES = LOADS * AT_ONCE;
-};
+// D (16x8, fp32) += A (16x16, bf16, row) . B (16x8, bf16, col)
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 
-// Sums v[0 .. 15] over the lanes of a page (LANES of them, next to each other); lane l gets sum number index16(l).
-template <int LANES>
-__device__ __forceinline__ double reduce16(double (&v)[16], int lane) {
+// Pages that a row sees.
+__device__ __forceinline__ int pages_of_row(const DevPlan& p, int row, int seq) {
+    return (__ldg(p.kv_len_before + seq) + row - __ldg(p.q_indptr + seq)) / kPage + 1;
+}
+
+// Thread (g, t) = (lane / 4, lane % 4) of an MMA holds channels 32 j + 8 t .. + 7 of pages g and g + 8 (A) and of query g (B): a 16-byte vector's
+// first two words are the k columns 2t, 2t + 1 and 2t + 8, 2t + 9 of one instruction, its last two those of the next.
+template <int D, int G>
+__global__ void __launch_bounds__(kScoreThreads, 2)
+select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds) {
+    constexpr int J = D / 32, kColumns = 8, kGroups = kSelectQueries / kColumns;
+    __shared__ uint4 s_q[kGroups][J][2][32];      // max(q, 0) and min(q, 0) as the threads take them
+    __shared__ unsigned s_error[kSelectQueries];
+    pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int h = blockIdx.x % p.num_kv_heads;
+    const SelectChunk c = p.select_chunks[blockIdx.x / p.num_kv_heads];
+    const int seq = __ldg(p.row_seq + c.row0);
+    const int32_t* table = p.page_indices + __ldg(p.page_indptr + seq);
+    const int np0 = pages_of_row(p, c.row0, seq), pos0 = __ldg(p.kv_len_before + seq) + c.row0 - __ldg(p.q_indptr + seq);
+    const int end = min(c.page0 + p.select_chunk_pages, (pos0 + c.rows - 1) / kPage + 1);
+    const int queries = c.rows * G;
+    auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
+    int j0 = c.page0 + warp * kTilePages, ids = id_of(j0);
+    if (tid < kSelectQueries) s_error[tid] = 0;
+    pdl_wait();      // queries and bounds are the kernels' in front
+    for (int i = tid; i < kGroups * J * 32; i += kScoreThreads) {
+        const int l = i % 32, j = i / 32 % J, k = i / 32 / J * kColumns + l / 4;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (k < queries)
+            w = *reinterpret_cast<const uint4*>(q + (((size_t)(c.row0 + k / G) * p.num_q_heads + (size_t)h * G + k % G) * D + 32 * j + 8 * (l % 4)) * 2);
+        w = make_uint4(held(w.x), held(w.y), held(w.z), held(w.w));
+        s_q[i / 32 / J][j][0][l] = make_uint4(max2(w.x, 0), max2(w.y, 0), max2(w.z, 0), max2(w.w, 0));
+        s_q[i / 32 / J][j][1][l] = make_uint4(min2(w.x, 0), min2(w.y, 0), min2(w.z, 0), min2(w.w, 0));
+    }
+    __syncthreads();
+    float error[kGroups][2];
 #pragma unroll
-    for (int half = 8; half >= 1; half >>= 1) {
-        const int bit = LANES / 16 * half;
-        const bool upper = (lane & bit) != 0;
+    for (int k = 0; k < kGroups; ++k) error[k][0] = error[k][1] = 0.f;
+    for (; j0 < end; j0 += kScoreWarps * kTilePages) {
+        uint4 lo[J][2], hi[J][2];      // of pages g and g + 8
 #pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const double send = upper ? v[i] : v[i + half], keep = upper ? v[i + half] : v[i];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+        for (int half = 0; half < 2; ++half) {
+            const int64_t page = __shfl_sync(0xffffffffu, ids, g + 8 * half);
+            const uint4* src = reinterpret_cast<const uint4*>(bounds + ((max(page, (int64_t)0) * p.num_kv_heads + h) * 2) * D * 2) + t;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                lo[j][half] = hi[j][half] = make_uint4(0, 0, 0, 0);
+                if (page >= 0) {
+                    lo[j][half] = src[4 * j];
+                    hi[j][half] = src[4 * j + D / 8];
+                }
+            }
+        }
+        ids = id_of(j0 + kScoreWarps * kTilePages);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint4 &x = lo[j][half], &y = hi[j][half];
+                x = make_uint4(held(x.x), held(x.y), held(x.z), held(x.w));
+                y = make_uint4(held(y.x), held(y.y), held(y.z), held(y.w));
+            }
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            if (k * kColumns >= queries) break;
+            float s[4] = {0.f, 0.f, 0.f, 0.f}, a[4] = {0.f, 0.f, 0.f, 0.f};      // scores, sums of magnitudes
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const uint4 up = s_q[k][j][0][lane], down = s_q[k][j][1][lane];
+                mma16(s, hi[j][0].x, hi[j][1].x, hi[j][0].y, hi[j][1].y, up.x, up.y);
+                mma16(s, hi[j][0].z, hi[j][1].z, hi[j][0].w, hi[j][1].w, up.z, up.w);
+                mma16(s, lo[j][0].x, lo[j][1].x, lo[j][0].y, lo[j][1].y, down.x, down.y);
+                mma16(s, lo[j][0].z, lo[j][1].z, lo[j][0].w, lo[j][1].w, down.z, down.w);
+                constexpr uint32_t kAbs = 0x7fff7fffu;
+                auto most = [&](uint32_t x, uint32_t y) { return max2(x & kAbs, y & kAbs); };
+                mma16(a, most(lo[j][0].x, hi[j][0].x), most(lo[j][1].x, hi[j][1].x), most(lo[j][0].y, hi[j][0].y), most(lo[j][1].y, hi[j][1].y),
+                      (up.x | down.x) & kAbs, (up.y | down.y) & kAbs);
+                mma16(a, most(lo[j][0].z, hi[j][0].z), most(lo[j][1].z, hi[j][1].z), most(lo[j][0].w, hi[j][0].w), most(lo[j][1].w, hi[j][1].w),
+                      (up.z | down.z) & kAbs, (up.w | down.w) & kAbs);
+            }
+            // this thread: pages g (0, 1) and g + 8 (2, 3), queries 2 t and 2 t + 1 of the eight
+            error[k][0] = fmaxf(error[k][0], fmaxf(a[0], a[2]));
+            error[k][1] = fmaxf(error[k][1], fmaxf(a[1], a[3]));
+            // the largest over a row's heads
+            if constexpr (G >= 2) {
+                s[0] = fmaxf(s[0], s[1]);
+                s[2] = fmaxf(s[2], s[3]);
+#pragma unroll
+                for (int off = 1; off < G / 2; off <<= 1) {
+                    s[0] = fmaxf(s[0], __shfl_xor_sync(0xffffffffu, s[0], off));
+                    s[2] = fmaxf(s[2], __shfl_xor_sync(0xffffffffu, s[2], off));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < (G == 1 ? 2 : 1); ++e) {
+                const int query = k * kColumns + 2 * t + e, r = query / G;
+                if (query % G != 0 || r >= c.rows) continue;
+                const int row = c.row0 + r, np = (pos0 + r) / kPage + 1;
+                unsigned* keys = p.select_keys + p.select_base[row] * p.num_kv_heads + (size_t)h * np;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int j = j0 + g + 8 * half;
+                    if (j < min(end, np)) keys[j] = j < p.select_first || j >= np - p.select_last ? kAlways : ordered(s[2 * half + e]);
+                }
+            }
         }
     }
-    return LANES == 32 ? v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1) : v[0];
+    // ---- how far the scores may be off: a row's largest (positive floats compare as integers)
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float x = error[k][e];
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+            if (g == 0) atomicMax(&s_error[k * kColumns + 2 * t + e], __float_as_uint(x));
+        }
+    __syncthreads();
+    if (tid < queries) atomicMax(p.select_error + (size_t)(c.row0 + tid / G) * p.num_kv_heads + h, s_error[tid]);
+}
+
+// The score of a page in 64 bits, by a warp.
+template <int D, int G>
+__device__ __forceinline__ double exact_score(const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds, int lane) {
+    constexpr int N = D / 32;
+    auto value = [](const __nv_bfloat16* x) {
+        const float f = __bfloat162float(*x);
+        return (double)(f != f ? -0x1p56f : fminf(fmaxf(f, -0x1p56f), 0x1p56f));      // (as held() has it)
+    };
+    double lo[N], hi[N], best = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        lo[i] = value(reinterpret_cast<const __nv_bfloat16*>(bounds) + i * 32 + lane);
+        hi[i] = value(reinterpret_cast<const __nv_bfloat16*>(bounds) + D + i * 32 + lane);
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const double x = value(reinterpret_cast<const __nv_bfloat16*>(q) + g * D + i * 32 + lane);
+            s = fma(x, x < 0.0 ? lo[i] : hi[i], s);
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+        best = g == 0 ? s : fmax(best, s);
+    }
+    return best;
 }
 
 template <int D, int G>
-__global__ void __launch_bounds__(kSelectThreads)
-select_pages_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds, int32_t* __restrict__ pages_out) {
-    using S = SelectShape<D, G>;
-    __shared__ unsigned long long s_keys[kKeysInShared];
+__global__ void __launch_bounds__(kChooseThreads)
+select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds, int32_t* __restrict__ pages_out) {
+    __shared__ unsigned s_keys[kKeysInShared];
+    __shared__ unsigned s_some[kChooseThreads];               // the keys of t's bin; the pages that are scored again
+    __shared__ unsigned long long s_exact[kChooseThreads];
     __shared__ int s_hist[256];
-    __shared__ unsigned long long s_lo[kSelectWarps], s_hi[kSelectWarps];
-    __shared__ int s_count[kSelectWarps][2];
-    __shared__ int s_bin, s_above, s_in, s_last;
+    __shared__ unsigned s_lo[kChooseWarps], s_hi[kChooseWarps], s_threshold;
+    __shared__ int s_count[kChooseWarps][2];
+    __shared__ int s_bin, s_above, s_in, s_n, s_total;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int h = blockIdx.x % p.num_kv_heads;
-    const SelectChunk c = p.select_chunks[blockIdx.x / p.num_kv_heads];
-    const int row = c.row, seq = __ldg(p.row_seq + row);
-    const int np = (__ldg(p.kv_len_before + seq) + row - __ldg(p.q_indptr + seq)) / kPage + 1;      // pages that the token sees
+    const int row = blockIdx.x / p.num_kv_heads, h = blockIdx.x % p.num_kv_heads, seq = __ldg(p.row_seq + row);
+    const int np = pages_of_row(p, row, seq);
     const int32_t* table = p.page_indices + __ldg(p.page_indptr + seq);
     const int budget = p.select_budget;
-    const size_t pair = (size_t)row * p.num_kv_heads + h;
-    int32_t* list = p.select_pages + pair * budget;
-    int32_t* out = pages_out == nullptr ? nullptr : pages_out + pair * budget;
-    pdl_wait();      // queries and bounds are the kernels' in front, and so are the lists as long as the last attention reads them
+    int32_t* list = p.select_pages + (size_t)blockIdx.x * budget;
+    int32_t* out = pages_out == nullptr ? nullptr : pages_out + (size_t)blockIdx.x * budget;
+    const size_t keys_at = p.select_base[row] * p.num_kv_heads + (size_t)h * np;
+    unsigned* keys = p.select_keys + keys_at;
+    if (tid < 256) s_hist[tid] = 0;
+    if (tid == 0) s_n = s_total = 0;
+    pdl_wait();      // the scores; and the lists belong to the last attention as long as it runs
     if (np <= budget) {
-        for (int j = tid; j < budget; j += kSelectThreads) {
+        for (int j = tid; j < budget; j += kChooseThreads) {
             if (j < np) list[j] = __ldg(table + j);
             if (out != nullptr) out[j] = j < np ? j : -1;
         }
         return;
     }
-    unsigned long long* keys = p.select_keys + p.select_base[row] * p.num_kv_heads + (size_t)h * np;
-    // ---- scores
-    {
-        uint32_t qw[G][4], neg[G][4];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const uint2 w = *reinterpret_cast<const uint2*>(q + (((size_t)row * p.num_q_heads + (size_t)h * G + g) * D + (size_t)(lane % S::LANES) * 4) * 2);
-            const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                qw[g][i] = f64_word(x[i]);
-                neg[g][i] = (uint32_t)((int32_t)qw[g][i] >> 31);
-            }
-        }
-        const int end = min(c.page0 + kSelectChunkPages, np);
-        for (int j0 = c.page0 + warp * S::PAGES; j0 < end; j0 += kSelectWarps * S::PAGES) {
-            uint2 wl[S::LOADS], wh[S::LOADS];
-#pragma unroll
-            for (int u = 0; u < S::LOADS; ++u) {
-                const int j = min(j0 + u * S::AT_ONCE + lane / S::LANES, end - 1);
-                const uint8_t* src = bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D * 2 + (size_t)(lane % S::LANES) * 8;
-                wl[u] = *reinterpret_cast<const uint2*>(src);
-                wh[u] = *reinterpret_cast<const uint2*>(src + D * 2);
-            }
-            double v[16];
-#pragma unroll
-            for (int u = 0; u < S::LOADS; ++u) {
-#pragma unroll
-                for (int g = 0; g < G; ++g) v[u * G + g] = 0.0;
-                const uint32_t l[4] = {wl[u].x & 0xffffu, wl[u].x >> 16, wl[u].y & 0xffffu, wl[u].y >> 16};
-                const uint32_t t[4] = {wh[u].x & 0xffffu, wh[u].x >> 16, wh[u].y & 0xffffu, wh[u].y >> 16};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t lo = f64_word(l[i]), hi = f64_word(t[i]), differ = lo ^ hi;
-#pragma unroll
-                    for (int g = 0; g < G; ++g) v[u * G + g] = fma(f64_of(qw[g][i]), f64_of(hi ^ (differ & neg[g][i])), v[u * G + g]);
-                }
-            }
-            double s = reduce16<S::LANES>(v, lane);
-            // the largest over the heads: their number is the low bits of the sum's
-            constexpr int kUnit = S::LANES / 16;
-#pragma unroll
-            for (int off = kUnit; off < kUnit * G; off <<= 1) s = fmax(s, __shfl_xor_sync(0xffffffffu, s, off));
-            const int number = lane % S::LANES / kUnit, j = j0 + number / G * S::AT_ONCE + lane / S::LANES;
-            if (lane % kUnit == 0 && number % G == 0 && j < end) {
-                const bool always = j < p.select_first || j >= np - p.select_last;
-                keys[j] = always ? kAlways : ordered(s);
-            }
-        }
-    }
-    // ---- the CTA that completes the row goes on
-    __syncthreads();
-    if (tid == 0) {
-        __threadfence();
-        const int chunks = (np + kSelectChunkPages - 1) / kSelectChunkPages;
-        s_last = atomicAdd(p.select_arrivals + pair, 1) == chunks - 1;
-        if (s_last) {
-            p.select_arrivals[pair] = 0;      // ready for the next launch
-            __threadfence();
-        }
-    }
-    __syncthreads();
-    if (!s_last) return;
+    const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-100f;
     const bool shared = np <= kKeysInShared;
-    unsigned long long lo = ~0ull, hi = 0;      // of the scores
-    for (int j = tid; j < np; j += kSelectThreads) {
-        const unsigned long long k = __ldcg(keys + j);
+    unsigned lo = ~0u, hi = 0;      // of the scores
+#pragma unroll 4
+    for (int j = tid; j < np; j += kChooseThreads) {
+        const unsigned k = __ldcg(keys + j);
         if (shared) s_keys[j] = k;
         if (k != kAlways) lo = min(lo, k), hi = max(hi, k);
     }
     auto key = [&](int j) { return shared ? s_keys[j] : __ldcg(keys + j); };
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, off));
-        hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, off));
-    }
+    auto set_key = [&](int j, unsigned k) { (shared ? s_keys : keys)[j] = k; };
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
     if (lane == 0) s_lo[warp] = lo, s_hi[warp] = hi;
     __syncthreads();
+    if (tid == 0) p.select_error[blockIdx.x] = 0;      // (all have read it) ready for the next launch
 #pragma unroll
-    for (int w = 0; w < kSelectWarps; ++w) lo = min(lo, s_lo[w]), hi = max(hi, s_hi[w]);
-    // ---- threshold: keys above `hi` are in, below `lo` out, and of those in between the first `need` pages
+    for (int w = 0; w < kChooseWarps; ++w) lo = min(lo, s_lo[w]), hi = max(hi, s_hi[w]);
+    // ---- t: the need-th largest of the scores
     int need = budget - p.select_first - p.select_last;
     if (need == 0) {
         lo = kAlways, hi = kAlways - 1;
     } else {
-        int shift = lo == hi ? 0 : max(0, 56 - __clzll((long long)(lo ^ hi)));
+        const int all = need;
+        int shift = lo == hi ? 0 : max(0, 24 - __clz(lo ^ hi));
         while (true) {
-            const unsigned long long base = lo >> shift;
-            s_hist[tid] = 0;
-            __syncthreads();
-            for (int j = tid; j < np; j += kSelectThreads) {
-                const unsigned long long k = key(j);
-                if (k >= lo && k <= hi) atomicAdd(&s_hist[(int)((k >> shift) - base)], 1);
+            const unsigned base = lo >> shift;
+            for (int j = tid; j < np; j += kChooseThreads) {
+                const unsigned k = key(j);
+                if (k >= lo && k <= hi) atomicAdd(&s_hist[(k >> shift) - base], 1);
             }
             __syncthreads();
             if (warp == 0) {      // a lane takes eight bins, the highest lane the highest
@@ -197,28 +290,128 @@ select_pages_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
                 }
                 above -= sum;
                 if (above < need && need <= above + sum) {
-                    int i = 7;
-                    while (above + n[i] < need) above += n[i], --i;
-                    s_bin = 8 * lane + i;
+                    int bin = 0, in = 0;
+#pragma unroll
+                    for (int i = 7; i >= 0; --i)      // (from the highest: the first with which `need` is reached)
+                        if (in == 0) {
+                            if (above + n[i] >= need) bin = 8 * lane + i, in = n[i];
+                            else above += n[i];
+                        }
+                    s_bin = bin;
                     s_above = above;
-                    s_in = n[i];
+                    s_in = in;
                 }
             }
             __syncthreads();
+            const int in = s_in;
             need -= s_above;
-            const unsigned long long first = (base + (unsigned)s_bin) << shift, last = first + ((1ull << shift) - 1);
+            const unsigned first = (base + (unsigned)s_bin) << shift, last = first + ((1u << shift) - 1);
             lo = max(lo, first);
             hi = min(hi, last);
-            if (s_in == need || shift == 0) break;
+            if (shift == 0) break;
+            if (in <= kChooseThreads) {      // few: the need-th of them by rank
+                for (int j = tid; j < np; j += kChooseThreads) {
+                    const unsigned k = key(j);
+                    if (k >= lo && k <= hi) s_some[atomicAdd(&s_n, 1)] = k;
+                }
+                __syncthreads();
+                if (tid < in) {
+                    const unsigned k = s_some[tid];
+                    int above = 0, equal = 0;
+                    for (int i = 0; i < in; ++i) above += s_some[i] > k, equal += s_some[i] == k;
+                    if (above < need && need <= above + equal) s_threshold = k;      // (the same from all equal ones)
+                }
+                __syncthreads();
+                lo = s_threshold;
+                break;
+            }
             shift = max(0, shift - 8);
-            __syncthreads();      // (s_bin is read before it is written again)
+            if (tid < 256) s_hist[tid] = 0;
+            __syncthreads();
+        }
+        // ---- scores within 2 e of it decide nothing
+        const float t = unordered(lo);
+        lo = ordered(__fadd_rd(t, -2.f * error));
+        hi = ordered(__fadd_ru(t, 2.f * error));
+        if (tid == 0) s_n = 0;
+        __syncthreads();
+        int above = 0;
+        for (int j = tid; j < np; j += kChooseThreads) {
+            const unsigned k = key(j);
+            above += k > hi && k != kAlways;
+            if (k >= lo && k <= hi) {
+                const int at = atomicAdd(&s_n, 1);
+                if (at < kChooseThreads) s_some[at] = (unsigned)j;
+            }
+        }
+        above = __reduce_add_sync(0xffffffffu, above);
+        if (lane == 0) atomicAdd(&s_total, above);
+        __syncthreads();
+        need = all - s_total;      // to be taken of these
+        const int open = s_n;
+        if (open > need) {
+            const uint8_t* q_row = q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D * 2;
+            auto exact = [&](int j) {
+                return ordered(exact_score<D, G>(q_row, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D * 2, lane));
+            };
+            if (open <= kChooseThreads) {
+                for (int i = warp; i < open; i += kChooseWarps) {
+                    const unsigned long long x = exact((int)s_some[i]);
+                    if (lane == 0) s_exact[i] = x;
+                }
+                __syncthreads();
+                if (tid < open) {
+                    const unsigned long long x = s_exact[tid];
+                    const unsigned page = s_some[tid];
+                    int rank = 0;      // (of equal ones the lower page goes first)
+                    for (int i = 0; i < open; ++i) rank += s_exact[i] > x || (s_exact[i] == x && s_some[i] < page);
+                    set_key((int)page, rank < need ? kTaken : 0);
+                }
+                need = 0;
+            } else {
+                // many scores that are (nearly) equal: the least of those in, bit by bit
+                unsigned long long* all_exact = p.select_exact + keys_at;
+                for (int j = warp; j < np; j += kChooseWarps) {
+                    const unsigned k = key(j);
+                    if (k < lo || k > hi) continue;
+                    const unsigned long long x = exact(j);
+                    if (lane == 0) all_exact[j] = x;
+                }
+                auto count = [&](unsigned long long least) {      // of the open ones, with at least this
+                    __syncthreads();
+                    if (tid == 0) s_total = 0;
+                    __syncthreads();
+                    int n = 0;
+                    for (int j = tid; j < np; j += kChooseThreads) {
+                        const unsigned k = key(j);
+                        n += k >= lo && k <= hi && __ldcg(all_exact + j) >= least;
+                    }
+                    n = __reduce_add_sync(0xffffffffu, n);
+                    if (lane == 0) atomicAdd(&s_total, n);
+                    __syncthreads();
+                    return s_total;
+                };
+                unsigned long long least = 0;
+                for (int bit = 63; bit >= 0; --bit)
+                    if (count(least | 1ull << bit) >= need) least |= 1ull << bit;
+                need -= count(least + 1);      // (no score is the largest integer)
+                __syncthreads();
+                for (int j = tid; j < np; j += kChooseThreads) {
+                    const unsigned k = key(j);
+                    if (k < lo || k > hi) continue;
+                    const unsigned long long x = __ldcg(all_exact + j);
+                    set_key(j, x > least ? kTaken : x == least ? hi : 0);
+                }
+                lo = hi;
+            }
+            __syncthreads();
         }
     }
-    // ---- the list: a stretch of pages to a thread
-    const int per = (np + kSelectThreads - 1) / kSelectThreads, first = min(tid * per, np), last = min(first + per, np);
+    // ---- the list: pages with keys above `hi`, and the first `need` of those from `lo` to `hi`; a stretch of pages to a thread
+    const int per = (np + kChooseThreads - 1) / kChooseThreads, first = min(tid * per, np), last = min(first + per, np);
     int above = 0, among = 0;
     for (int j = first; j < last; ++j) {
-        const unsigned long long k = key(j);
+        const unsigned k = key(j);
         above += k > hi;
         among += k >= lo && k <= hi;
     }
@@ -234,7 +427,7 @@ select_pages_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     before_among -= among;
     for (int w = 0; w < warp; ++w) before_above += s_count[w][0], before_among += s_count[w][1];
     for (int j = first; j < last; ++j) {
-        const unsigned long long k = key(j);
+        const unsigned k = key(j);
         const bool in = k >= lo && k <= hi;
         if (k > hi || (in && before_among < need)) {
             const int at = before_above + min(before_among, need);
@@ -246,12 +439,31 @@ select_pages_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     }
 }
 
+template <int D, int G>
+cudaError_t launch_scores(const DevPlan& p, const void* q, const void* bounds, cudaStream_t s) {
+    return launch_when(!p.full_launch, select_score_kernel<D, G>, dim3((unsigned)(p.num_select_chunks * p.num_kv_heads)), dim3(kScoreThreads), 0, s, p,
+                      (const uint8_t*)q, (const uint8_t*)bounds);
+}
+
+template <int D, int G>
+cudaError_t launch_choice(const DevPlan& p, const void* q, const void* bounds, int32_t* pages_out, cudaStream_t s) {
+    return launch_when(!p.full_launch, select_choose_kernel<D, G>, dim3((unsigned)(p.total_q * p.num_kv_heads)), dim3(kChooseThreads), 0, s, p,
+                      (const uint8_t*)q, (const uint8_t*)bounds, pages_out);
+}
+
 template <int D>
-cudaError_t launch_select(const DevPlan& p, const void* q, const void* bounds, int32_t* pages_out, cudaStream_t s) {
-    const dim3 grid((unsigned)(p.num_select_chunks * p.num_kv_heads));
-    auto kernel = p.group == 1 ? select_pages_kernel<D, 1> : p.group == 2 ? select_pages_kernel<D, 2> : p.group == 4 ? select_pages_kernel<D, 4>
-                                                                                                                     : select_pages_kernel<D, 8>;
-    return launch_when(!p.full_launch, kernel, grid, dim3(kSelectThreads), 0, s, p, (const uint8_t*)q, (const uint8_t*)bounds, pages_out);
+int select_d(PlanUse& use, const void* q, const void* bounds, int32_t* pages_out, cudaStream_t s) {
+    auto run = [&](auto scores, auto choice) {
+        if (use.dev.num_select_chunks > 0)
+            if (int rc = cuda_status(use.launched(scores(use.dev, q, bounds, s)))) return rc;
+        return cuda_status(use.launched(choice(use.dev, q, bounds, pages_out, s)));
+    };
+    switch (use.dev.group) {
+        case 1: return run(launch_scores<D, 1>, launch_choice<D, 1>);
+        case 2: return run(launch_scores<D, 2>, launch_choice<D, 2>);
+        case 4: return run(launch_scores<D, 4>, launch_choice<D, 4>);
+        default: return run(launch_scores<D, 8>, launch_choice<D, 8>);
+    }
 }
 
 }  // namespace
@@ -266,8 +478,7 @@ extern "C" int asynclm_select_pages(const asynclm_plan_t* plan, const void* q, c
     if (int rc = check_plan_device(plan->device)) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
-    const cudaError_t e = use.dev.head_dim == 128 ? launch_select<128>(use.dev, q, key_bounds, pages_out, s) : launch_select<64>(use.dev, q, key_bounds, pages_out, s);
-    const int rc = cuda_status(use.launched(e));
+    const int rc = use.dev.head_dim == 128 ? select_d<128>(use, q, key_bounds, pages_out, s) : select_d<64>(use, q, key_bounds, pages_out, s);
     if (rc == ASYNCLM_OK) __atomic_store_n(&plan->selected, 1, __ATOMIC_RELEASE);
     return rc;
 }
