@@ -74,7 +74,6 @@ extern "C" int asynclm_attn_mixed(const asynclm_plan_t* plan, const void* q, con
     if (!asynclm::pages_chosen(plan)) return ASYNCLM_ERR_INVALID_ARG;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
-    use.reads_page_lists();
     int rc = cuda_status(use.launched(launch_attention(use.dev, q, kv_pool, out, lse, s)));
     if (rc != ASYNCLM_OK) return rc;
     return cuda_status(launch_lse_merge(use.dev, out, lse, s));

@@ -678,7 +678,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         auto load_pages = [&](const PItem& it, int first_page) {
             const int npg = (it.kv_end - it.kv0 + kPage - 1) / kPage;
             const int idx = first_page + lane;
-            return idx < npg ? __ldg(p.page_indices + it.page0 + idx) : 0;
+            return idx < npg ? __ldcg(p.page_indices + it.page0 + idx) : 0;      // (selected pages: the kernel in front writes them)
         };
         auto land_copies = [&](int k0, int k1) {
             const long long t0 = clock64();
@@ -870,7 +870,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
                 if (lane < 12) w = __ldg(rec + lane);
                 const int kv0 = __shfl_sync(0xffffffffu, w, 0), kv_end = __shfl_sync(0xffffffffu, w, 1);
                 const int page0 = __shfl_sync(0xffffffffu, w, 7);
-                if (lane < (kv_end - kv0 + kPage - 1) / kPage) pg = __ldg(p.page_indices + page0 + lane);
+                if (lane < (kv_end - kv0 + kPage - 1) / kPage) pg = __ldcg(p.page_indices + page0 + lane);
                 if constexpr (APPEND) {
                     // asynclm_step: the new K/V rows this item reads go into their page slots now; the
                     // producer's copies (asynchronous proxy) come after the hand-off below

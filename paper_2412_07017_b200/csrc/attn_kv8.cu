@@ -146,7 +146,6 @@ extern "C" int asynclm_kv8_attn_mixed(const asynclm_plan_t* plan, const void* q,
     if (int rc = check_plan_device(plan->device)) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
-    use.reads_page_lists();
     const cudaError_t e = use.dev.head_dim == 128 ? launch_kv8_d<128>(use.dev, q, kv8_pool, kv8_scales, out, lse, s)
                                                   : launch_kv8_d<64>(use.dev, q, kv8_pool, kv8_scales, out, lse, s);
     const int rc = cuda_status(use.launched(e));

@@ -72,7 +72,6 @@ extern "C" int asynclm_attn_mixed_static(const asynclm_plan_t* plan, const void*
     if (int rc = cuda_status(scratch_address(&base))) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     PlanUse use(plan, s);
-    use.reads_page_lists();
     DevPlan& d = use.dev;                        // same plan, partial results redirected
     d.partial_o = (float*)base;
     d.partial_lse = (float*)((unsigned char*)base + o_bytes);

@@ -823,8 +823,8 @@ struct Run {
     int32_t first, tokens, row0, rows, seqs;
 };
 
-// Selected pages: a chunk of scores is a multiple of these pages, and there are about so many for an SM.
-constexpr int kSelectWarpPages = 64, kSelectCtasPerSm = 3;
+// Selected pages: a chunk of scores is a multiple of these pages (16 for each warp of a CTA), and so many CTAs run on an SM.
+constexpr int kSelectChunkUnit = 64, kSelectCtasPerSm = 4;
 
 // A sequence with more rows of a kv head than a row tile keeps its prefix to itself: its items are bound by the products, of which
 // sharing saves none, and its partial rows would be many.
@@ -966,11 +966,11 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     std::vector<SelectChunk> select_chunks;
     std::vector<int64_t> select_base;
     int64_t select_keys = 0;      // scores of one kv head
-    int32_t chunk_pages = kSelectWarpPages;
+    int32_t chunk_pages = kSelectChunkUnit, most_pages = 0;
     if (sparse) {
         auto pages_of = [&](int r, int b) { return (batch->kv_len_before[b] + (r - q_indptr[b])) / P + 1; };
         // Rows that have more pages than the budget are scored, as many together as a chunk takes (they read the same bounds).
-        struct Group { int row0, rows, pages; };
+        struct Group { int seq, row0, rows, pages; };
         std::vector<Group> groups;
         int64_t scored = 0;
         select_base.reserve((size_t)T);
@@ -980,20 +980,22 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
                 select_base.push_back(select_keys);
                 if (pages <= sparse->budget_pages) continue;
                 select_keys += pages;
+                most_pages = std::max(most_pages, pages);
                 if (r > q_indptr[b] && !groups.empty() && groups.back().row0 + groups.back().rows == r && groups.back().rows < kSelectQueries / G) {
                     ++groups.back().rows;
                     scored += pages - groups.back().pages;
                     groups.back().pages = pages;
                 } else {
-                    groups.push_back(Group{r, 1, pages});
+                    groups.push_back(Group{b, r, 1, pages});
                     scored += pages;
                 }
             }
-        // chunks of equal length, as many as make kSelectCtasPerSm CTAs for an SM
-        const int64_t share = (scored * Hkv + (int64_t)kSelectCtasPerSm * n_sms - 1) / ((int64_t)kSelectCtasPerSm * n_sms);
-        chunk_pages = (int32_t)std::min<int64_t>(std::max<int64_t>((share + kSelectWarpPages - 1) / kSelectWarpPages, 1) * kSelectWarpPages, 1 << 20);
+        // chunks of one length, about two for each of the CTAs that run at once
+        const int64_t ctas = (int64_t)kSelectCtasPerSm * n_sms * 2;
+        chunk_pages = (int32_t)std::min<int64_t>(std::max<int64_t>((scored * Hkv + ctas * kSelectChunkUnit - 1) / (ctas * kSelectChunkUnit), 1) * kSelectChunkUnit, 1 << 24);
         for (const Group& g : groups)
-            for (int64_t j = 0; j < g.pages; j += chunk_pages) select_chunks.push_back(SelectChunk{g.row0, g.rows, (int32_t)j, 0});
+            for (int64_t j = 0; j < g.pages; j += chunk_pages)
+                select_chunks.push_back(SelectChunk{g.row0, g.rows, (int32_t)j, batch->kv_len_before[g.seq] + (g.row0 - q_indptr[g.seq]), page_indptr[g.seq], {0, 0, 0}});
         if ((int64_t)select_chunks.size() * Hkv > INT32_MAX || (int64_t)T * Hkv > INT32_MAX || total_pages + n_select > (int64_t)1 << 40)
             return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
     }
@@ -1353,6 +1355,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
         d.select_error = (unsigned*)dp(off_error);
         d.num_select_chunks = (int32_t)select_chunks.size();
         d.select_chunk_pages = chunk_pages;
+        d.select_most_pages = most_pages;
         d.select_budget = sparse->budget_pages;
         d.select_first = sparse->first_pages;
         d.select_last = sparse->last_pages;

@@ -69,12 +69,6 @@ class PlanUse {
         dev.full_launch = status != cudaStreamCaptureStatusActive || __atomic_load_n(&plan->captured_in, __ATOMIC_ACQUIRE) != id + 1;
     }
 
-    // For the attention: a plan for selected pages has its page lists written by the kernel in front (asynclm_select_pages), so this launch
-    // starts when that has completed.
-    void reads_page_lists() {
-        if (plan->sparse) dev.full_launch = 1;
-    }
-
     // Takes and returns the outcome of the call's first launch with `dev`; what the call launches behind it starts early.
     cudaError_t launched(cudaError_t e) {
         if (e != cudaSuccess || dev.full_launch == 0) return e;

@@ -61,8 +61,11 @@ struct alignas(16) Join {
 
 // Plans for selected pages: rows next to each other of one sequence, for which one CTA and kv head score DevPlan::select_chunk_pages pages (see
 // select_pages.cu).
-struct SelectChunk {
-    int32_t row0, rows, page0, pad;
+struct alignas(16) SelectChunk {
+    int32_t row0, rows, page0;
+    int32_t pos0;           // position of row0 in its sequence
+    int32_t page_base;      // page_indptr of the sequence
+    int32_t pad[3];
 };
 constexpr int kSelectQueries = 16;      // (row, head) pairs of a chunk at most
 
@@ -116,7 +119,8 @@ struct DevPlan {
     unsigned long long* select_exact;// the same in 64 bits, of pages whose 32 bits leave the choice open
     unsigned* select_error;          // [T][Hkv] how far the 32 bits of a row's scores may be off (a float); zero between launches
     int32_t num_join_blocks, num_select_chunks;
-    int32_t select_chunk_pages, select_budget, select_first, select_last;
+    int32_t select_chunk_pages, select_most_pages;      // (the longest row's)
+    int32_t select_budget, select_first, select_last;
     int64_t total_pages;             // entries of the page table
     int32_t queue_first, queue_count;// items [queue_first, queue_first + queue_count) are handed out at run time
     int32_t batch, total_q, num_units, num_items, num_items_cuda, num_items_tensor;

@@ -29,15 +29,14 @@ namespace asynclm {
 
 namespace {
 
-constexpr int kScoreThreads = 256, kScoreWarps = kScoreThreads / 32;
+constexpr int kScoreThreads = 128, kScoreWarps = kScoreThreads / 32;
 constexpr int kTilePages = 16;
-constexpr int kChooseThreads = 512, kChooseWarps = kChooseThreads / 32;
-constexpr int kKeysInShared = 8192;                // of a row (131 072 tokens); longer ones are read from L2
+constexpr int kThreadKeys = 8;                     // of a row's keys in a thread's registers
 constexpr unsigned kAlways = 0xffffffffu;          // key of a page that is taken whatever its score
 constexpr unsigned kTaken = 0xfffffffeu;
 
 // Values beyond +-2^56, NaN among them, count as +-2^56 (so that no sum of products overflows).
-constexpr uint32_t kMostPair = 0x5b805b80u, kLeastPair = 0xdb80db80u;
+constexpr uint32_t kMostPair = 0x5b805b80u, kLeastPair = 0xdb80db80u, kAbs = 0x7fff7fffu;
 __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -66,15 +65,10 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Pages that a row sees.
-__device__ __forceinline__ int pages_of_row(const DevPlan& p, int row, int seq) {
-    return (__ldg(p.kv_len_before + seq) + row - __ldg(p.q_indptr + seq)) / kPage + 1;
-}
-
 // Thread (g, t) = (lane / 4, lane % 4) of an MMA holds channels 32 j + 8 t .. + 7 of pages g and g + 8 (A) and of query g (B): a 16-byte vector's
 // first two words are the k columns 2t, 2t + 1 and 2t + 8, 2t + 9 of one instruction, its last two those of the next.
 template <int D, int G>
-__global__ void __launch_bounds__(kScoreThreads, 2)
+__global__ void __launch_bounds__(kScoreThreads, 4)
 select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds) {
     constexpr int J = D / 32, kColumns = 8, kGroups = kSelectQueries / kColumns;
     __shared__ uint4 s_q[kGroups][J][2][32];      // max(q, 0) and min(q, 0) as the threads take them
@@ -83,9 +77,8 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int h = blockIdx.x % p.num_kv_heads;
     const SelectChunk c = p.select_chunks[blockIdx.x / p.num_kv_heads];
-    const int seq = __ldg(p.row_seq + c.row0);
-    const int32_t* table = p.page_indices + __ldg(p.page_indptr + seq);
-    const int np0 = pages_of_row(p, c.row0, seq), pos0 = __ldg(p.kv_len_before + seq) + c.row0 - __ldg(p.q_indptr + seq);
+    const int32_t* table = p.page_indices + c.page_base;
+    const int pos0 = c.pos0;
     const int end = min(c.page0 + p.select_chunk_pages, (pos0 + c.rows - 1) / kPage + 1);
     const int queries = c.rows * G;
     auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
@@ -121,32 +114,43 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
             }
         }
         ids = id_of(j0 + kScoreWarps * kTilePages);
+        const bool more = queries > kColumns;
+        float s_all[kGroups][4], a_all[kGroups][4];      // scores, sums of magnitudes
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+        for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_all[k][e] = a_all[k][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            uint32_t l[2][4], u[2][4], m[2][4];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                uint4 &x = lo[j][half], &y = hi[j][half];
-                x = make_uint4(held(x.x), held(x.y), held(x.z), held(x.w));
-                y = make_uint4(held(y.x), held(y.y), held(y.z), held(y.w));
+                const uint32_t x[4] = {lo[j][half].x, lo[j][half].y, lo[j][half].z, lo[j][half].w}, y[4] = {hi[j][half].x, hi[j][half].y, hi[j][half].z, hi[j][half].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    l[half][e] = held(x[e]);
+                    u[half][e] = held(y[e]);
+                    m[half][e] = max2(l[half][e] & kAbs, u[half][e] & kAbs);
+                }
             }
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                if (k > 0 && !more) break;
+                const uint4 up = s_q[k][j][0][lane], down = s_q[k][j][1][lane];
+                float(&s)[4] = s_all[k], (&a)[4] = a_all[k];
+                mma16(s, u[0][0], u[1][0], u[0][1], u[1][1], up.x, up.y);
+                mma16(s, u[0][2], u[1][2], u[0][3], u[1][3], up.z, up.w);
+                mma16(s, l[0][0], l[1][0], l[0][1], l[1][1], down.x, down.y);
+                mma16(s, l[0][2], l[1][2], l[0][3], l[1][3], down.z, down.w);
+                mma16(a, m[0][0], m[1][0], m[0][1], m[1][1], (up.x | down.x) & kAbs, (up.y | down.y) & kAbs);
+                mma16(a, m[0][2], m[1][2], m[0][3], m[1][3], (up.z | down.z) & kAbs, (up.w | down.w) & kAbs);
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
-            if (k * kColumns >= queries) break;
-            float s[4] = {0.f, 0.f, 0.f, 0.f}, a[4] = {0.f, 0.f, 0.f, 0.f};      // scores, sums of magnitudes
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const uint4 up = s_q[k][j][0][lane], down = s_q[k][j][1][lane];
-                mma16(s, hi[j][0].x, hi[j][1].x, hi[j][0].y, hi[j][1].y, up.x, up.y);
-                mma16(s, hi[j][0].z, hi[j][1].z, hi[j][0].w, hi[j][1].w, up.z, up.w);
-                mma16(s, lo[j][0].x, lo[j][1].x, lo[j][0].y, lo[j][1].y, down.x, down.y);
-                mma16(s, lo[j][0].z, lo[j][1].z, lo[j][0].w, lo[j][1].w, down.z, down.w);
-                constexpr uint32_t kAbs = 0x7fff7fffu;
-                auto most = [&](uint32_t x, uint32_t y) { return max2(x & kAbs, y & kAbs); };
-                mma16(a, most(lo[j][0].x, hi[j][0].x), most(lo[j][1].x, hi[j][1].x), most(lo[j][0].y, hi[j][0].y), most(lo[j][1].y, hi[j][1].y),
-                      (up.x | down.x) & kAbs, (up.y | down.y) & kAbs);
-                mma16(a, most(lo[j][0].z, hi[j][0].z), most(lo[j][1].z, hi[j][1].z), most(lo[j][0].w, hi[j][0].w), most(lo[j][1].w, hi[j][1].w),
-                      (up.z | down.z) & kAbs, (up.w | down.w) & kAbs);
-            }
+            if (k > 0 && !more) break;
+            float(&s)[4] = s_all[k];
+            const float(&a)[4] = a_all[k];
             // this thread: pages g (0, 1) and g + 8 (2, 3), queries 2 t and 2 t + 1 of the eight
             error[k][0] = fmaxf(error[k][0], fmaxf(a[0], a[2]));
             error[k][1] = fmaxf(error[k][1], fmaxf(a[1], a[3]));
@@ -188,82 +192,113 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     if (tid < queries) atomicMax(p.select_error + (size_t)(c.row0 + tid / G) * p.num_kv_heads + h, s_error[tid]);
 }
 
-// The score of a page in 64 bits, by a warp.
-template <int D, int G>
-__device__ __forceinline__ double exact_score(const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds, int lane) {
-    constexpr int N = D / 32;
-    auto value = [](const __nv_bfloat16* x) {
-        const float f = __bfloat162float(*x);
-        return (double)(f != f ? -0x1p56f : fminf(fmaxf(f, -0x1p56f), 0x1p56f));      // (as held() has it)
-    };
-    double lo[N], hi[N], best = 0.0;
+__device__ __forceinline__ double held_value(__nv_bfloat16 x) {      // (as held() has it)
+    const float f = __bfloat162float(x);
+    return (double)(f != f ? -0x1p56f : fminf(fmaxf(f, -0x1p56f), 0x1p56f));
+}
+
+// The score of a page in 64 bits, by a warp; the queries [group][head_dim] in shared memory.
+__device__ __forceinline__ double exact_score(const __nv_bfloat16* q, const __nv_bfloat16* __restrict__ bounds, int head_dim, int group, int lane) {
+    double lo[4], hi[4], s[8];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        lo[i] = value(reinterpret_cast<const __nv_bfloat16*>(bounds) + i * 32 + lane);
-        hi[i] = value(reinterpret_cast<const __nv_bfloat16*>(bounds) + D + i * 32 + lane);
+    for (int i = 0; i < 4; ++i) {
+        const bool on = 32 * i < head_dim;
+        lo[i] = on ? held_value(bounds[32 * i + lane]) : 0.0;
+        hi[i] = on ? held_value(bounds[head_dim + 32 * i + lane]) : 0.0;
     }
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        double s = 0.0;
+    for (int g = 0; g < 8; ++g) {
+        s[g] = 0.0;
+        if (g >= group) continue;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const double x = value(reinterpret_cast<const __nv_bfloat16*>(q) + g * D + i * 32 + lane);
-            s = fma(x, x < 0.0 ? lo[i] : hi[i], s);
+        for (int i = 0; i < 4; ++i) {
+            const double x = 32 * i < head_dim ? held_value(q[g * head_dim + 32 * i + lane]) : 0.0;
+            s[g] = fma(x, x < 0.0 ? lo[i] : hi[i], s[g]);
         }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        best = g == 0 ? s : fmax(best, s);
     }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            if (g < group) s[g] += __shfl_xor_sync(0xffffffffu, s[g], off);
+    double best = s[0];
+#pragma unroll
+    for (int g = 1; g < 8; ++g)
+        if (g < group) best = fmax(best, s[g]);
     return best;
 }
 
-template <int D, int G>
-__global__ void __launch_bounds__(kChooseThreads)
-select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds, int32_t* __restrict__ pages_out) {
-    __shared__ unsigned s_keys[kKeysInShared];
-    __shared__ unsigned s_some[kChooseThreads];               // the keys of t's bin; the pages that are scored again
-    __shared__ unsigned long long s_exact[kChooseThreads];
+// A warp has the keys of a stretch of pages, 32 of them at a time, in registers where the row has at most kThreadKeys for every thread.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ bounds, int32_t* __restrict__ pages_out) {
+    constexpr int kWarps = THREADS / 32;
+    __shared__ unsigned s_some[THREADS];               // the keys of t's bin; the pages that are scored again
+    __shared__ unsigned long long s_exact[THREADS];
     __shared__ int s_hist[256];
-    __shared__ unsigned s_lo[kChooseWarps], s_hi[kChooseWarps], s_threshold;
-    __shared__ int s_count[kChooseWarps][2];
-    __shared__ int s_bin, s_above, s_in, s_n, s_total;
+    __shared__ unsigned s_lo[kWarps], s_hi[kWarps], s_threshold;
+    __shared__ int s_count[kWarps][2];
+    __shared__ int s_bin, s_above, s_in, s_n, s_open, s_total;
+    __shared__ __align__(16) __nv_bfloat16 s_q[8 * 128];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = blockIdx.x / p.num_kv_heads, h = blockIdx.x % p.num_kv_heads, seq = __ldg(p.row_seq + row);
-    const int np = pages_of_row(p, row, seq);
+    const size_t row_keys = (size_t)__ldg(p.select_base + row) * p.num_kv_heads;
+    const int np = (__ldg(p.kv_len_before + seq) + row - __ldg(p.q_indptr + seq)) / kPage + 1;      // pages that the row sees
     const int32_t* table = p.page_indices + __ldg(p.page_indptr + seq);
     const int budget = p.select_budget;
     int32_t* list = p.select_pages + (size_t)blockIdx.x * budget;
     int32_t* out = pages_out == nullptr ? nullptr : pages_out + (size_t)blockIdx.x * budget;
-    const size_t keys_at = p.select_base[row] * p.num_kv_heads + (size_t)h * np;
-    unsigned* keys = p.select_keys + keys_at;
-    if (tid < 256) s_hist[tid] = 0;
-    if (tid == 0) s_n = s_total = 0;
+    unsigned* keys = p.select_keys + row_keys + (size_t)h * np;
+    for (int i = tid; i < 256; i += THREADS) s_hist[i] = 0;
+    if (tid == 0) s_n = s_open = s_total = 0;
+    pdl_trigger();
     pdl_wait();      // the scores; and the lists belong to the last attention as long as it runs
     if (np <= budget) {
-        for (int j = tid; j < budget; j += kChooseThreads) {
+        for (int j = tid; j < budget; j += THREADS) {
             if (j < np) list[j] = __ldg(table + j);
             if (out != nullptr) out[j] = j < np ? j : -1;
         }
         return;
     }
+    const int D = p.head_dim, G = p.group;
+    for (int i = tid; i < G * D / 8; i += THREADS)
+        reinterpret_cast<uint4*>(s_q)[i] = reinterpret_cast<const uint4*>(q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D)[i];
     const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-100f;
-    const bool shared = np <= kKeysInShared;
-    unsigned lo = ~0u, hi = 0;      // of the scores
-#pragma unroll 4
-    for (int j = tid; j < np; j += kChooseThreads) {
-        const unsigned k = __ldcg(keys + j);
-        if (shared) s_keys[j] = k;
-        if (k != kAlways) lo = min(lo, k), hi = max(hi, k);
+    // ---- this thread's keys: pages stretch0 + 32 i + lane
+    const int steps = (np + THREADS - 1) / THREADS, stretch0 = warp * steps * 32;
+    const bool resident = steps <= kThreadKeys;
+    unsigned mine[kThreadKeys];
+#pragma unroll
+    for (int i = 0; i < kThreadKeys; ++i) {
+        const int j = stretch0 + 32 * i + lane;
+        mine[i] = resident && i < steps && j < np ? __ldcg(keys + j) : 0;      // (0 is below any score's)
     }
-    auto key = [&](int j) { return shared ? s_keys[j] : __ldcg(keys + j); };
-    auto set_key = [&](int j, unsigned k) { (shared ? s_keys : keys)[j] = k; };
+    // use(page, key) for each of them, all lanes together; use returns the key, or another to put in its place
+    auto each = [&](auto use) {
+        if (resident) {
+#pragma unroll
+            for (int i = 0; i < kThreadKeys; ++i)
+                if (i < steps) mine[i] = use(stretch0 + 32 * i + lane, mine[i]);
+        } else {
+            for (int i = 0; i < steps; ++i) {
+                const int j = stretch0 + 32 * i + lane;
+                const unsigned k = j < np ? __ldcg(keys + j) : 0, now = use(j, k);
+                if (now != k && j < np) __stcg(keys + j, now);
+            }
+        }
+    };
+    unsigned lo = ~0u, hi = 0;      // of the scores
+    each([&](int, unsigned k) {
+        if (k != kAlways && k != 0) lo = min(lo, k), hi = max(hi, k);
+        return k;
+    });
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
     if (lane == 0) s_lo[warp] = lo, s_hi[warp] = hi;
     __syncthreads();
     if (tid == 0) p.select_error[blockIdx.x] = 0;      // (all have read it) ready for the next launch
 #pragma unroll
-    for (int w = 0; w < kChooseWarps; ++w) lo = min(lo, s_lo[w]), hi = max(hi, s_hi[w]);
+    for (int w = 0; w < kWarps; ++w) lo = min(lo, s_lo[w]), hi = max(hi, s_hi[w]);
     // ---- t: the need-th largest of the scores
     int need = budget - p.select_first - p.select_last;
     if (need == 0) {
@@ -273,10 +308,10 @@ select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __
         int shift = lo == hi ? 0 : max(0, 24 - __clz(lo ^ hi));
         while (true) {
             const unsigned base = lo >> shift;
-            for (int j = tid; j < np; j += kChooseThreads) {
-                const unsigned k = key(j);
+            each([&](int, unsigned k) {
                 if (k >= lo && k <= hi) atomicAdd(&s_hist[(k >> shift) - base], 1);
-            }
+                return k;
+            });
             __syncthreads();
             if (warp == 0) {      // a lane takes eight bins, the highest lane the highest
                 int n[8], sum = 0;
@@ -309,11 +344,11 @@ select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __
             lo = max(lo, first);
             hi = min(hi, last);
             if (shift == 0) break;
-            if (in <= kChooseThreads) {      // few: the need-th of them by rank
-                for (int j = tid; j < np; j += kChooseThreads) {
-                    const unsigned k = key(j);
+            if (in <= THREADS) {      // few: the need-th of them by rank
+                each([&](int, unsigned k) {
                     if (k >= lo && k <= hi) s_some[atomicAdd(&s_n, 1)] = k;
-                }
+                    return k;
+                });
                 __syncthreads();
                 if (tid < in) {
                     const unsigned k = s_some[tid];
@@ -326,66 +361,67 @@ select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __
                 break;
             }
             shift = max(0, shift - 8);
-            if (tid < 256) s_hist[tid] = 0;
+            for (int i = tid; i < 256; i += THREADS) s_hist[i] = 0;
             __syncthreads();
         }
         // ---- scores within 2 e of it decide nothing
         const float t = unordered(lo);
         lo = ordered(__fadd_rd(t, -2.f * error));
         hi = ordered(__fadd_ru(t, 2.f * error));
-        if (tid == 0) s_n = 0;
-        __syncthreads();
         int above = 0;
-        for (int j = tid; j < np; j += kChooseThreads) {
-            const unsigned k = key(j);
+        each([&](int j, unsigned k) {
             above += k > hi && k != kAlways;
             if (k >= lo && k <= hi) {
-                const int at = atomicAdd(&s_n, 1);
-                if (at < kChooseThreads) s_some[at] = (unsigned)j;
+                const int at = atomicAdd(&s_open, 1);
+                if (at < THREADS) s_some[at] = (unsigned)j;
             }
-        }
+            return k;
+        });
         above = __reduce_add_sync(0xffffffffu, above);
         if (lane == 0) atomicAdd(&s_total, above);
         __syncthreads();
         need = all - s_total;      // to be taken of these
-        const int open = s_n;
+        const int open = s_open;
         if (open > need) {
-            const uint8_t* q_row = q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D * 2;
-            auto exact = [&](int j) {
-                return ordered(exact_score<D, G>(q_row, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D * 2, lane));
-            };
-            if (open <= kChooseThreads) {
-                for (int i = warp; i < open; i += kChooseWarps) {
+            auto exact = [&](int j) { return ordered(exact_score(s_q, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D, D, G, lane)); };
+            if (open <= THREADS) {
+                for (int i = warp; i < open; i += kWarps) {
                     const unsigned long long x = exact((int)s_some[i]);
                     if (lane == 0) s_exact[i] = x;
                 }
                 __syncthreads();
-                if (tid < open) {
-                    const unsigned long long x = s_exact[tid];
-                    const unsigned page = s_some[tid];
-                    int rank = 0;      // (of equal ones the lower page goes first)
-                    for (int i = 0; i < open; ++i) rank += s_exact[i] > x || (s_exact[i] == x && s_some[i] < page);
-                    set_key((int)page, rank < need ? kTaken : 0);
-                }
+                // an open page is in if fewer than `need` go in front of it (of equal scores the lower page)
+                each([&](int j, unsigned k) {
+                    if (k < lo || k > hi) return k;
+                    unsigned long long x = 0;
+                    for (int i = 0; i < open; ++i)
+                        if (s_some[i] == (unsigned)j) x = s_exact[i];
+                    int rank = 0;
+                    for (int i = 0; i < open; ++i) rank += s_exact[i] > x || (s_exact[i] == x && s_some[i] < (unsigned)j);
+                    return rank < need ? kTaken : 0u;
+                });
                 need = 0;
             } else {
                 // many scores that are (nearly) equal: the least of those in, bit by bit
-                unsigned long long* all_exact = p.select_exact + keys_at;
-                for (int j = warp; j < np; j += kChooseWarps) {
-                    const unsigned k = key(j);
-                    if (k < lo || k > hi) continue;
-                    const unsigned long long x = exact(j);
-                    if (lane == 0) all_exact[j] = x;
-                }
+                unsigned long long* all_exact = p.select_exact + row_keys + (size_t)h * np;
+                each([&](int j, unsigned k) {
+                    unsigned which = __ballot_sync(0xffffffffu, k >= lo && k <= hi);
+                    for (; which; which &= which - 1) {
+                        const int at = __shfl_sync(0xffffffffu, j, __ffs(which) - 1);
+                        const unsigned long long x = exact(at);
+                        if (lane == 0) __stcg(all_exact + at, x);
+                    }
+                    return k;
+                });
                 auto count = [&](unsigned long long least) {      // of the open ones, with at least this
                     __syncthreads();
                     if (tid == 0) s_total = 0;
                     __syncthreads();
                     int n = 0;
-                    for (int j = tid; j < np; j += kChooseThreads) {
-                        const unsigned k = key(j);
-                        n += k >= lo && k <= hi && __ldcg(all_exact + j) >= least;
-                    }
+                    each([&](int j, unsigned k) {
+                        if (k >= lo && k <= hi) n += __ldcg(all_exact + j) >= least;
+                        return k;
+                    });
                     n = __reduce_add_sync(0xffffffffu, n);
                     if (lane == 0) atomicAdd(&s_total, n);
                     __syncthreads();
@@ -395,48 +431,39 @@ select_choose_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __
                 for (int bit = 63; bit >= 0; --bit)
                     if (count(least | 1ull << bit) >= need) least |= 1ull << bit;
                 need -= count(least + 1);      // (no score is the largest integer)
-                __syncthreads();
-                for (int j = tid; j < np; j += kChooseThreads) {
-                    const unsigned k = key(j);
-                    if (k < lo || k > hi) continue;
+                each([&](int j, unsigned k) {
+                    if (k < lo || k > hi) return k;
                     const unsigned long long x = __ldcg(all_exact + j);
-                    set_key(j, x > least ? kTaken : x == least ? hi : 0);
-                }
+                    return x > least ? kTaken : x == least ? hi : 0u;
+                });
                 lo = hi;
             }
-            __syncthreads();
         }
     }
-    // ---- the list: pages with keys above `hi`, and the first `need` of those from `lo` to `hi`; a stretch of pages to a thread
-    const int per = (np + kChooseThreads - 1) / kChooseThreads, first = min(tid * per, np), last = min(first + per, np);
-    int above = 0, among = 0;
-    for (int j = first; j < last; ++j) {
-        const unsigned k = key(j);
-        above += k > hi;
-        among += k >= lo && k <= hi;
-    }
-    int before_above = above, before_among = among;      // inclusive sums, then those of the threads in front
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int a = __shfl_up_sync(0xffffffffu, before_above, off), b = __shfl_up_sync(0xffffffffu, before_among, off);
-        if (lane >= off) before_above += a, before_among += b;
-    }
-    if (lane == 31) s_count[warp][0] = before_above, s_count[warp][1] = before_among;
+    // ---- the list: pages with keys above `hi`, and the first `need` of those from `lo` to `hi`
+    int above = 0, among = 0;      // of the warp's stretch
+    each([&](int, unsigned k) {
+        above += __popc(__ballot_sync(0xffffffffu, k > hi));
+        among += __popc(__ballot_sync(0xffffffffu, k >= lo && k <= hi));
+        return k;
+    });
+    if (lane == 0) s_count[warp][0] = above, s_count[warp][1] = among;
     __syncthreads();
-    before_above -= above;
-    before_among -= among;
-    for (int w = 0; w < warp; ++w) before_above += s_count[w][0], before_among += s_count[w][1];
-    for (int j = first; j < last; ++j) {
-        const unsigned k = key(j);
-        const bool in = k >= lo && k <= hi;
-        if (k > hi || (in && before_among < need)) {
-            const int at = before_above + min(before_among, need);
+    above = among = 0;      // in front of the stretch
+    for (int w = 0; w < warp; ++w) above += s_count[w][0], among += s_count[w][1];
+    const unsigned below = (1u << lane) - 1;
+    each([&](int j, unsigned k) {
+        const unsigned over = __ballot_sync(0xffffffffu, k > hi), in = __ballot_sync(0xffffffffu, k >= lo && k <= hi);
+        const int among_here = among + __popc(in & below);
+        if (k > hi || (k >= lo && k <= hi && among_here < need)) {
+            const int at = above + __popc(over & below) + min(among_here, need);
             list[at] = __ldg(table + j);
             if (out != nullptr) out[at] = j;
         }
-        before_above += k > hi;
-        before_among += in;
-    }
+        above += __popc(over);
+        among += __popc(in);
+        return k;
+    });
 }
 
 template <int D, int G>
@@ -445,25 +472,25 @@ cudaError_t launch_scores(const DevPlan& p, const void* q, const void* bounds, c
                       (const uint8_t*)q, (const uint8_t*)bounds);
 }
 
-template <int D, int G>
+// As many threads as hold the longest row's keys in registers, 128 to 512: a short row's steps are fewer barriers than work.
 cudaError_t launch_choice(const DevPlan& p, const void* q, const void* bounds, int32_t* pages_out, cudaStream_t s) {
-    return launch_when(!p.full_launch, select_choose_kernel<D, G>, dim3((unsigned)(p.total_q * p.num_kv_heads)), dim3(kChooseThreads), 0, s, p,
-                      (const uint8_t*)q, (const uint8_t*)bounds, pages_out);
+    const dim3 grid((unsigned)(p.total_q * p.num_kv_heads));
+    auto run = [&](auto kernel, int threads) {
+        return launch_when(!p.full_launch, kernel, grid, dim3(threads), 0, s, p, (const __nv_bfloat16*)q, (const __nv_bfloat16*)bounds, pages_out);
+    };
+    if (p.select_most_pages <= 128 * kThreadKeys) return run(select_choose_kernel<128>, 128);
+    if (p.select_most_pages <= 256 * kThreadKeys) return run(select_choose_kernel<256>, 256);
+    return run(select_choose_kernel<512>, 512);
 }
 
 template <int D>
 int select_d(PlanUse& use, const void* q, const void* bounds, int32_t* pages_out, cudaStream_t s) {
-    auto run = [&](auto scores, auto choice) {
-        if (use.dev.num_select_chunks > 0)
-            if (int rc = cuda_status(use.launched(scores(use.dev, q, bounds, s)))) return rc;
-        return cuda_status(use.launched(choice(use.dev, q, bounds, pages_out, s)));
-    };
-    switch (use.dev.group) {
-        case 1: return run(launch_scores<D, 1>, launch_choice<D, 1>);
-        case 2: return run(launch_scores<D, 2>, launch_choice<D, 2>);
-        case 4: return run(launch_scores<D, 4>, launch_choice<D, 4>);
-        default: return run(launch_scores<D, 8>, launch_choice<D, 8>);
+    if (use.dev.num_select_chunks > 0) {
+        auto scores = use.dev.group == 1 ? launch_scores<D, 1> : use.dev.group == 2 ? launch_scores<D, 2> : use.dev.group == 4 ? launch_scores<D, 4>
+                                                                                                                         : launch_scores<D, 8>;
+        if (int rc = cuda_status(use.launched(scores(use.dev, q, bounds, s)))) return rc;
     }
+    return cuda_status(use.launched(launch_choice(use.dev, q, bounds, pages_out, s)));
 }
 
 }  // namespace
