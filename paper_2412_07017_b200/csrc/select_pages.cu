@@ -84,7 +84,24 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
     int j0 = c.page0 + warp * kTilePages, ids = id_of(j0);
     if (tid < kSelectQueries) s_error[tid] = 0;
+    uint4 lo[J][2], hi[J][2];      // of pages g and g + 8
+    auto load = [&]() {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int64_t page = __shfl_sync(0xffffffffu, ids, g + 8 * half);
+            const uint4* src = reinterpret_cast<const uint4*>(bounds + ((max(page, (int64_t)0) * p.num_kv_heads + h) * 2) * D * 2) + t;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                lo[j][half] = hi[j][half] = make_uint4(0, 0, 0, 0);
+                if (page >= 0) {
+                    lo[j][half] = src[4 * j];
+                    hi[j][half] = src[4 * j + D / 8];
+                }
+            }
+        }
+    };
     pdl_wait();      // queries and bounds are the kernels' in front
+    load();
     for (int i = tid; i < kGroups * J * 32; i += kScoreThreads) {
         const int l = i % 32, j = i / 32 % J, k = i / 32 / J * kColumns + l / 4;
         uint4 w = make_uint4(0, 0, 0, 0);
@@ -99,20 +116,6 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) error[k][0] = error[k][1] = 0.f;
     for (; j0 < end; j0 += kScoreWarps * kTilePages) {
-        uint4 lo[J][2], hi[J][2];      // of pages g and g + 8
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t page = __shfl_sync(0xffffffffu, ids, g + 8 * half);
-            const uint4* src = reinterpret_cast<const uint4*>(bounds + ((max(page, (int64_t)0) * p.num_kv_heads + h) * 2) * D * 2) + t;
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                lo[j][half] = hi[j][half] = make_uint4(0, 0, 0, 0);
-                if (page >= 0) {
-                    lo[j][half] = src[4 * j];
-                    hi[j][half] = src[4 * j + D / 8];
-                }
-            }
-        }
         ids = id_of(j0 + kScoreWarps * kTilePages);
         const bool more = queries > kColumns;
         float s_all[kGroups][4], a_all[kGroups][4];      // scores, sums of magnitudes
@@ -177,6 +180,7 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
                 }
             }
         }
+        if (j0 + kScoreWarps * kTilePages < end) load();
     }
     // ---- how far the scores may be off: a row's largest (positive floats compare as integers)
 #pragma unroll
@@ -197,35 +201,19 @@ __device__ __forceinline__ double held_value(__nv_bfloat16 x) {      // (as held
     return (double)(f != f ? -0x1p56f : fminf(fmaxf(f, -0x1p56f), 0x1p56f));
 }
 
-// The score of a page in 64 bits, by a warp; the queries [group][head_dim] in shared memory.
-__device__ __forceinline__ double exact_score(const __nv_bfloat16* q, const __nv_bfloat16* __restrict__ bounds, int head_dim, int group, int lane) {
-    double lo[4], hi[4], s[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool on = 32 * i < head_dim;
-        lo[i] = on ? held_value(bounds[32 * i + lane]) : 0.0;
-        hi[i] = on ? held_value(bounds[head_dim + 32 * i + lane]) : 0.0;
+// The sum of one query in shared memory and a page's bounds in 64 bits, by a warp.
+__device__ __forceinline__ double exact_sum(const __nv_bfloat16* q, const __nv_bfloat16* __restrict__ bounds, int head_dim, int lane) {
+    double s = 0.0;
+#pragma unroll 1
+    for (int i = 2 * lane; i < head_dim; i += 64) {
+        const __nv_bfloat162 l = *reinterpret_cast<const __nv_bfloat162*>(bounds + i), u = *reinterpret_cast<const __nv_bfloat162*>(bounds + head_dim + i);
+        const double x = held_value(q[i]), y = held_value(q[i + 1]);
+        s = fma(x, held_value(x < 0.0 ? l.x : u.x), s);
+        s = fma(y, held_value(y < 0.0 ? l.y : u.y), s);
     }
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
-        s[g] = 0.0;
-        if (g >= group) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const double x = 32 * i < head_dim ? held_value(q[g * head_dim + 32 * i + lane]) : 0.0;
-            s[g] = fma(x, x < 0.0 ? lo[i] : hi[i], s[g]);
-        }
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-        for (int g = 0; g < 8; ++g)
-            if (g < group) s[g] += __shfl_xor_sync(0xffffffffu, s[g], off);
-    double best = s[0];
-#pragma unroll
-    for (int g = 1; g < 8; ++g)
-        if (g < group) best = fmax(best, s[g]);
-    return best;
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    return s;
 }
 
 // A warp has the keys of a stretch of pages, 32 of them at a time, in registers where the row has at most kThreadKeys for every thread.
@@ -383,11 +371,16 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         need = all - s_total;      // to be taken of these
         const int open = s_open;
         if (open > need) {
-            auto exact = [&](int j) { return ordered(exact_score(s_q, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D, D, G, lane)); };
+            auto exact = [&](int j, int g) {
+                return ordered(exact_sum(s_q + g * D, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D, D, lane));
+            };
             if (open <= THREADS) {
-                for (int i = warp; i < open; i += kWarps) {
-                    const unsigned long long x = exact((int)s_some[i]);
-                    if (lane == 0) s_exact[i] = x;
+                s_exact[tid] = 0;
+                __syncthreads();
+#pragma unroll 1
+                for (int i = warp; i < open * G; i += kWarps) {      // a page and head to a warp: the code is met once, and cold
+                    const unsigned long long x = exact((int)s_some[i / G], i % G);
+                    if (lane == 0) atomicMax(&s_exact[i / G], x);
                 }
                 __syncthreads();
                 // an open page is in if fewer than `need` go in front of it (of equal scores the lower page)
@@ -408,7 +401,8 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
                     unsigned which = __ballot_sync(0xffffffffu, k >= lo && k <= hi);
                     for (; which; which &= which - 1) {
                         const int at = __shfl_sync(0xffffffffu, j, __ffs(which) - 1);
-                        const unsigned long long x = exact(at);
+                        unsigned long long x = 0;
+                        for (int g = 0; g < G; ++g) x = max(x, exact(at, g));
                         if (lane == 0) __stcg(all_exact + at, x);
                     }
                     return k;
