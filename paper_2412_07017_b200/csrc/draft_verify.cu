@@ -9,10 +9,12 @@
 // exponents' difference in bias: all weights and sums are times 2^-896, which changes no comparison, and zeros and subnormal numbers are right as they
 // are.  (With conversions, of which an SM does 16 a cycle, a mean batch of 300 bf16 rows of 100 003 took 45.7 us, 26.4 for 64 pairs of fp32 rows of 128 256.)
 //
-// One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself), a warp kPiece values of it at a time, and
-// leaves each piece's sum in the workspace; the CTA that completes the row finds the piece by the sums, and reads that one again.  Every
-// value is read once, so the bytes of one row of p and one of q a sequence are what bounds a large batch, and a chain of round trips (bounds of the
-// sequence, tokens, their probabilities, values; count, sums, one piece) a small one.
+// One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself); a warp has pieces of 4 KB brought into shared memory, the
+// next one while it sums the last, and leaves each piece's sum in the workspace; the CTA that completes the row finds the piece by the sums, and brings
+// that one again.  Every value is read once, so the bytes of one row of p and one of q a sequence are what bounds a large batch, and a chain of
+// round trips (bounds of the sequence, tokens, their probabilities, values; count, sums, one piece) a small one.  Rows start anywhere: what is copied are
+// the 16-byte vectors that memory has them in, and shared memory is read value by value.  (Out of registers, by vectors, with the checks that the ends of
+// a row need, the loop outgrew the instruction cache or the registers: 300 bf16 rows of 100 003 took 33 to 126 us.)
 #include <algorithm>
 
 #include "asynclm.h"
@@ -23,9 +25,13 @@ namespace asynclm {
 
 namespace {
 
-constexpr int kVerifyThreads = 128, kVerifyWarps = kVerifyThreads / 32, kVerifyCtasPerSm = 8;
-constexpr int kLaneValues = 16, kPiece = 32 * kLaneValues;
-constexpr int kSharedPieces = 1024;
+constexpr int kVerifyThreads = 64, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kPieceBytes = 4096;
+template <typename T>
+constexpr int kPiece = kPieceBytes / (int)sizeof(T);
+constexpr int kSlots = 2;      // of a warp: a piece of p, and one of q with a vector more
+constexpr int kSlotBytes = kPieceBytes, kSlotBytesQ = 2 * kPieceBytes + 16;
+constexpr int kSharedPieces = kSlots * kSlotBytes / 8;
 constexpr int kMostSequences = 65535;
 constexpr size_t kArrivalBytes = 65536 * sizeof(int32_t);      // in front of the sums for any batch, so that calls of different sizes share a workspace
 
@@ -41,38 +47,75 @@ struct VerifyArgs {
     int32_t batch, drafts, vocab, pieces;
 };
 
+// The rows that a token's weight comes from.  A piece is so many values of p from a 16-byte boundary on; the first begins `lead` values in front of
+// the row.  q's values lie `apart` values further behind a boundary of theirs.
 template <typename T>
 struct Weights {
+    static constexpr int N = 16 / sizeof(T);
     const T *p, *q;      // q == nullptr: w = p
     int without;         // a token whose weight is zero (a draft proposed with certainty), or -1
     int vocab;
+    int lead, apart;
+
+    __device__ __forceinline__ Weights(const T* p_, const T* q_, int without_, int vocab_)
+        : p(p_), q(q_), without(without_), vocab(vocab_), lead((int)((uintptr_t)p_ % 16 / sizeof(T))),
+          apart((int)(((uintptr_t)q_ / sizeof(T) - (uintptr_t)p_ / sizeof(T)) % N)) {}
+
+    __device__ __forceinline__ int token0(int piece) const { return piece * kPiece<T> - lead; }
 };
 
-// The bits, as those of fp32 numbers, of the 16 bytes of values from `at` on of a row; zero behind its end.
-template <typename T, bool VEC, int N>
-__device__ __forceinline__ void load_values(const T* __restrict__ row, int at, int vocab, uint32_t (&x)[N]) {
-    static_assert(N == 16 / sizeof(T), "a vector at a time");
-    if (VEC && at + N <= vocab) {
-        const uint4 w = ldg_nc_v4(reinterpret_cast<const uint4*>(row + at));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ void copy_vec(uint32_t dst, uintptr_t src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// Requests a piece of a row, the first vector of which begins at value `from` (a boundary), and `more` vectors behind it into dst; zeros behind the row's
+// end.  (The first vector may begin in front of the row: what is read there lies in the 16 bytes of the row's first value.)
+template <typename T>
+__device__ __forceinline__ void request(T* dst, const T* row, int from, int more, int vocab, int lane) {
+    constexpr int N = 16 / sizeof(T), kVecs = kPieceBytes / 16;
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst) + 16 * lane;
+    if (from >= 0 && from + (kVecs + more) * N <= vocab) {
+        const uintptr_t src = (uintptr_t)(row + from) + 16 * lane;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (sizeof(T) == 4) x[i] = u[i];
-            else x[i] = i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16;
-        }
+        for (int k = 0; k < kVecs; k += 32) copy_vec(to + 16 * k, src + 16 * k, 16);
+        if (lane < more) copy_vec(to + 16 * kVecs, src + 16 * kVecs, 16);
         return;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = at + i < vocab ? __float_as_uint((float)row[at + i]) : 0u;
+#pragma unroll 1
+    for (int k = 0; k < kVecs + more; k += 32) {
+        const int at = from + (k + lane) * N, bytes = at + N <= 0 ? 0 : max(min(vocab - at, N), 0) * (int)sizeof(T);
+        if (k + lane < kVecs + more) copy_vec(to + 16 * k, (uintptr_t)(row + (bytes > 0 ? at : 0)) & ~(uintptr_t)15, bytes);      // (of no bytes: any address)
+    }
 }
+template <typename T>
+__device__ __forceinline__ void request_piece(const Weights<T>& w, T* slot, int piece, int lane) {
+    request(slot, w.p, w.token0(piece), 0, w.vocab, lane);
+    if (w.q != nullptr) request(slot + kPiece<T>, w.q, w.token0(piece) - w.apart, w.apart ? 1 : 0, w.vocab, lane);
+}
+// What has come of a piece is made fit to be summed: nothing in front of the row, no weight for `without`.
+template <typename T>
+__device__ __forceinline__ void clean_piece(const Weights<T>& w, T* slot, int piece, int lane) {
+    __syncwarp();      // (all lanes' copies are there)
+    if (piece == 0 && lane < w.lead) slot[lane] = (T)0.f;
+    const int at = w.without - w.token0(piece);
+    if (w.without >= 0 && at >= 0 && at < kPiece<T> && lane == 0) slot[at] = (T)0.f;
+    __syncwarp();
+}
+__device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
 
 // max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  NaN counts as zero, and so does a negative q.
 __device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
+template <bool WITH_Q>
 __device__ __forceinline__ double weight(uint32_t p, uint32_t q) {
+    if (!WITH_Q) return __uint_as_float(p) > 0.f ? scaled(p) : 0.0;
     const uint32_t from = (uint32_t)max((int)q, 0);
     return __uint_as_float(p) > __uint_as_float(from) ? scaled(p) - scaled(from) : 0.0;
 }
-__device__ __forceinline__ double weight(uint32_t p) { return __uint_as_float(p) > 0.f ? scaled(p) : 0.0; }
+// The weight of value j of a piece in its slot.
+template <typename T>
+__device__ __forceinline__ double weight_in(const Weights<T>& w, const T* slot, int j) {
+    return w.q != nullptr ? weight<true>(bits_of(slot[j]), bits_of(slot[kPiece<T> + w.apart + j])) : weight<false>(bits_of(slot[j]), 0u);
+}
 
 __device__ __forceinline__ double warp_sum(double x) {
 #pragma unroll
@@ -90,43 +133,75 @@ __device__ __forceinline__ double warp_scan(double x, int lane) {
     return x;
 }
 
-// The sums of pieces first, first + step, ... below `end` by this warp.
-template <typename T, bool VEC, bool WITH_Q>
-__device__ __forceinline__ void sum_pieces(const Weights<T>& w, int first, int step, int end, double* sums, int lane) {
-    constexpr int N = 16 / sizeof(T), kParts = kLaneValues / N;
-    for (int i = first; i < end; i += step) {
-        uint32_t a[kParts][N], b[kParts][N];
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            const int at = i * kPiece + (k * 32 + lane) * N;
-            load_values<T, VEC, N>(w.p, at, w.vocab, a[k]);
-            if (WITH_Q) load_values<T, VEC, N>(w.q, at, w.vocab, b[k]);
-        }
-        if (!WITH_Q && w.without / kPiece == i) {      // (-1 / kPiece is 0)
-#pragma unroll
-            for (int k = 0; k < kParts; ++k)
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (i * kPiece + (k * 32 + lane) * N + e == w.without) a[k][e] = 0;
-        }
-        double sum = 0.0;
-#pragma unroll
-        for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int e = 0; e < N; ++e) sum += WITH_Q ? weight(a[k][e], b[k][e]) : weight(a[k][e]);
-        sum = warp_sum(sum);
-        if (lane == 0) sums[i] = sum;
-    }
+// The sum of a piece in its slot, lane by lane: value by value, whatever the numbers and q's place.
+template <typename T, bool WITH_Q>
+__device__ __forceinline__ double sum_by_values(const T* slot, int apart, int lane) {
+    double sum = 0.0;
+#pragma unroll 4
+    for (int j = lane; j < kPiece<T>; j += 32) sum += weight<WITH_Q>(bits_of(slot[j]), WITH_Q ? bits_of(slot[kPiece<T> + apart + j]) : 0u);
+    return sum;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void sum_pieces(const Weights<T>& w, int first, int step, int end, double* sums, int lane) {
-    if (w.q != nullptr) sum_pieces<T, VEC, true>(w, first, step, end, sums, lane);
-    else sum_pieces<T, VEC, false>(w, first, step, end, sums, lane);
+// The same by vectors, where q's lie as p's do; `odd` is set where a number is no probability, and the sum is none then.
+template <typename T, bool WITH_Q>
+__device__ __forceinline__ double sum_by_vectors(const T* slot, int lane, bool& odd) {
+    constexpr int N = 16 / sizeof(T);
+    double sum[2] = {0.0, 0.0};
+    uint32_t signs = 0, most = 0;
+#pragma unroll 4
+    for (int k = lane; k < kPieceBytes / 16; k += 32) {
+        const uint4 v = reinterpret_cast<const uint4*>(slot)[k];
+        const uint4 u = WITH_Q ? reinterpret_cast<const uint4*>(slot + kPiece<T>)[k] : make_uint4(0, 0, 0, 0);
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w}, y[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (!WITH_Q) most = sizeof(T) == 4 ? max(most, x[i]) : __vmaxu2(most, x[i]);
+            signs |= y[i];
+#pragma unroll
+            for (int e = 0; e < N / 4; ++e) {
+                const uint32_t a = sizeof(T) == 4 ? x[i] : e ? x[i] & 0xffff0000u : x[i] << 16, b = sizeof(T) == 4 ? y[i] : e ? y[i] & 0xffff0000u : y[i] << 16;
+                if constexpr (!WITH_Q) sum[i & 1] += scaled(a);
+                else if (__uint_as_float(a) > __uint_as_float(b)) sum[i & 1] += scaled(a) - scaled(b);
+            }
+        }
+    }
+    if constexpr (sizeof(T) == 4) odd = most > 0x7f800000u || signs >> 31;
+    else odd = most >> 16 > 0x7f80u || (most & 0xffffu) > 0x7f80u || (signs & 0x80008000u);
+    return sum[0] + sum[1];
+}
+template <typename T, bool WITH_Q>
+__device__ __forceinline__ double sum_of_piece(const T* slot, int apart, int lane) {
+    if (!WITH_Q || apart == 0) {
+        bool odd;
+        const double sum = sum_by_vectors<T, WITH_Q>(slot, lane, odd);
+        if (!__any_sync(0xffffffffu, odd)) return sum;
+    }
+    return sum_by_values<T, WITH_Q>(slot, apart, lane);
+}
+
+// The sums of pieces first, first + step, ... below `end` by this warp, in its two slots.
+template <typename T>
+__device__ __forceinline__ void sum_pieces(const Weights<T>& w, T* slots, int slot_values, int first, int step, int end, double* sums, int lane) {
+    auto ask = [&](int i, int slot) {
+        if (i < end) request_piece(w, slots + slot * slot_values, i, lane);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    ask(first, 0);
+    int at = 0;
+    for (int i = first; i < end; i += step, at ^= 1) {
+        ask(i + step, at ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        T* slot = slots + at * slot_values;
+        clean_piece(w, slot, i, lane);
+        const double sum = warp_sum(w.q != nullptr ? sum_of_piece<T, true>(slot, w.apart, lane) : sum_of_piece<T, false>(slot, 0, lane));
+        if (lane == 0) sums[i] = sum;
+        __syncwarp();      // (the slot is free)
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // The least token whose inclusive sum of weights exceeds u * (sum of all); -1 if no weight is positive.  By one warp; sum_of(i): a piece's sum.
-template <typename T, bool VEC, typename SumOf>
-__device__ __forceinline__ int search(const Weights<T>& w, SumOf sum_of, int pieces, float u, int lane) {
+template <typename T, typename SumOf>
+__device__ __forceinline__ int search(const Weights<T>& w, T* slot, SumOf sum_of, int pieces, float u, int lane) {
     // a stretch of pieces to a lane, then the pieces of the stretch
     const int per = (pieces + 31) / 32, c0 = min(lane * per, pieces), c1 = min(c0 + per, pieces);
     double mine = 0.0;
@@ -153,42 +228,34 @@ __device__ __forceinline__ int search(const Weights<T>& w, SumOf sum_of, int pie
         before = end;
     }
     before = front;
-    // the token: kLaneValues next to each other to a lane
-    constexpr int N = 16 / sizeof(T);
-    const int t0 = piece * kPiece + lane * kLaneValues;
-    double x[kLaneValues], sum = 0.0;
-#pragma unroll
-    for (int k = 0; k < kLaneValues; k += N) {
-        uint32_t a[N], b[N];
-        load_values<T, VEC, N>(w.p, t0 + k, w.vocab, a);
-        if (w.q != nullptr) load_values<T, VEC, N>(w.q, t0 + k, w.vocab, b);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[k + e] = t0 + k + e == w.without ? 0.0 : w.q != nullptr ? weight(a[e], b[e]) : weight(a[e]);
-    }
-#pragma unroll
-    for (int k = 0; k < kLaneValues; ++k) sum += x[k];
-    const double through = before + warp_scan(sum, lane);
-    const unsigned past = __ballot_sync(0xffffffffu, sum > 0.0 && through > threshold), any = __ballot_sync(0xffffffffu, sum > 0.0);
+    // of the piece: a stretch of its values to a lane (each in an order of its own, so that lanes read different banks), then the values of the stretch
+    request_piece(w, slot, piece, lane);
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    clean_piece(w, slot, piece, lane);
+    constexpr int kStretch = kPiece<T> / 32;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int k = 0; k < kStretch; ++k) sum += weight_in(w, slot, lane * kStretch + (k + lane * (4 / (int)sizeof(T))) % kStretch);
+    const double end = before + warp_scan(sum, lane);
+    const unsigned past = __ballot_sync(0xffffffffu, sum > 0.0 && end > threshold), any = __ballot_sync(0xffffffffu, sum > 0.0);
     const int from = past ? __ffs(past) - 1 : 31 - __clz(any);
+    before = __shfl_sync(0xffffffffu, end - sum, from);
     int token = -1;
-    double run = through - sum;
-    bool found = false;
-#pragma unroll
-    for (int k = 0; k < kLaneValues; ++k) {
-        run += x[k];
-        if (!found && x[k] > 0.0) {
-            token = t0 + k;
-            found = run > threshold;
-        }
+    for (int k = 0; k < kStretch; k += 32) {
+        const double x = weight_in(w, slot, from * kStretch + k + lane), through = before + warp_scan(x, lane);
+        const unsigned over = __ballot_sync(0xffffffffu, x > 0.0 && through > threshold), some = __ballot_sync(0xffffffffu, x > 0.0);
+        if (some) token = w.token0(piece) + from * kStretch + k + (over ? __ffs(over) - 1 : 31 - __clz(some));
+        if (over) break;
+        before = __shfl_sync(0xffffffffu, through, 31);
     }
-    return __shfl_sync(0xffffffffu, token, from);
+    return token;
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kVerifyThreads, kVerifyCtasPerSm)
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads)
 draft_verify_kernel(VerifyArgs a) {
     __shared__ int s_last, s_again;
-    __shared__ double s_sums[kSharedPieces];
+    extern __shared__ __align__(16) uint8_t s_slots[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
     pdl_wait();
     pdl_trigger();
@@ -217,12 +284,14 @@ draft_verify_kernel(VerifyArgs a) {
         }
     }
     const bool rejected = accepted < n;
-    Weights<T> w{target + (int64_t)accepted * a.target_stride, rejected && draft != nullptr ? draft + (int64_t)accepted * a.draft_stride : nullptr,
-                 rejected && draft == nullptr ? rejected_token : -1, a.vocab};
+    Weights<T> w(target + (int64_t)accepted * a.target_stride, rejected && draft != nullptr ? draft + (int64_t)accepted * a.draft_stride : nullptr,
+                 rejected && draft == nullptr ? rejected_token : -1, a.vocab);
     // ---- this CTA's slice of the row's pieces
+    const int slot_values = (a.draft == nullptr ? kSlotBytes : kSlotBytesQ) / (int)sizeof(T);
+    T* slots = reinterpret_cast<T*>(s_slots) + (size_t)warp * kSlots * slot_values;
     double* sums = a.sums + (size_t)b * a.pieces;
     const int first = (int)((int64_t)a.pieces * blockIdx.x / gridDim.x), end = (int)((int64_t)a.pieces * (blockIdx.x + 1) / gridDim.x);
-    sum_pieces<T, VEC>(w, first + warp, kVerifyWarps, end, sums, lane);
+    sum_pieces(w, slots, slot_values, first + warp, kVerifyWarps, end, sums, lane);
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
@@ -236,6 +305,7 @@ draft_verify_kernel(VerifyArgs a) {
     if (!s_last) return;
     // ---- the CTA that completes the row
     const bool shared = a.pieces <= kSharedPieces;
+    double* s_sums = reinterpret_cast<double*>(s_slots + (size_t)kSlots * slot_values * sizeof(T));      // the second warp's slots
     int token = -1;
     for (int attempt = 0; attempt < 2; ++attempt) {
         if (shared) {
@@ -243,7 +313,7 @@ draft_verify_kernel(VerifyArgs a) {
             __syncthreads();
         }
         if (warp == 0) {
-            token = search<T, VEC>(w, [&](int i) { return shared ? s_sums[i] : __ldcg(sums + i); }, a.pieces, __ldg(a.sample_u + b), lane);
+            token = search(w, slots, [&](int i) { return shared ? s_sums[i] : __ldcg(sums + i); }, a.pieces, __ldg(a.sample_u + b), lane);
             if (lane == 0) s_again = token < 0 && rejected && attempt == 0;
         }
         __syncthreads();
@@ -251,7 +321,7 @@ draft_verify_kernel(VerifyArgs a) {
         // nothing is left of max(p - q, 0), as rounded probabilities may have it: the target's own
         w.q = nullptr;
         w.without = -1;
-        sum_pieces<T, VEC>(w, warp, kVerifyWarps, a.pieces, sums, lane);
+        sum_pieces(w, slots, slot_values, warp, kVerifyWarps, a.pieces, sums, lane);
         __syncthreads();      // (the sums are this CTA's own now)
     }
     if (warp != 0) return;
@@ -266,14 +336,14 @@ draft_verify_kernel(VerifyArgs a) {
 extern "C" size_t asynclm_draft_verify_workspace_bytes(int32_t batch, int32_t vocab) {
     using namespace asynclm;
     if (batch <= 0 || vocab <= 0) return 0;
-    const size_t pieces = ((size_t)vocab + kPiece - 1) / kPiece;
+    const size_t pieces = ((size_t)vocab + 3 + kPiece<float> - 1) / kPiece<float>;      // (rows may start 3 values behind a boundary; of bf16 there are no more)
     return kArrivalBytes + (size_t)batch * pieces * sizeof(double);
 }
 
 extern "C" int asynclm_draft_verify(const asynclm_draft_rows* rows, const int32_t* draft_indptr, int32_t batch, int32_t drafts, const int32_t* draft_tokens,
                                     const float* accept_u, const float* sample_u, int32_t* accepted, int32_t* tokens_out, void* workspace, void* stream) {
     using namespace asynclm;
-    if (!rows || batch < 0 || drafts < 0 || rows->vocab <= 0 || rows->vocab > INT32_MAX - kPiece || batch > kMostSequences) return ASYNCLM_ERR_INVALID_ARG;
+    if (!rows || batch < 0 || drafts < 0 || rows->vocab <= 0 || rows->vocab > INT32_MAX - 4096 || batch > kMostSequences) return ASYNCLM_ERR_INVALID_ARG;
     if (rows->dtype != ASYNCLM_DTYPE_BF16 && rows->dtype != ASYNCLM_DTYPE_F32) return ASYNCLM_ERR_INVALID_ARG;
     if (batch == 0) return drafts == 0 ? ASYNCLM_OK : ASYNCLM_ERR_INVALID_ARG;
     if (!rows->target || !draft_indptr || !sample_u || !accepted || !tokens_out || !workspace || (drafts > 0 && (!draft_tokens || !accept_u)))
@@ -299,12 +369,12 @@ extern "C" int asynclm_draft_verify(const asynclm_draft_rows* rows, const int32_
     a.batch = batch;
     a.drafts = drafts;
     a.vocab = rows->vocab;
-    a.pieces = (rows->vocab + kPiece - 1) / kPiece;
-    // as many CTAs as run at once, each with a piece or more for its warps
-    const int slices = std::max(1, std::min(kVerifyCtasPerSm * 148 / batch, (a.pieces + kVerifyWarps - 1) / kVerifyWarps));
-    // rows that all start on a 16-byte boundary are read by vectors
-    const bool vec = (((uintptr_t)a.target | (uintptr_t)a.draft | (uintptr_t)a.target_stride * size | (uintptr_t)a.draft_stride * size) & 15) == 0;
-    auto kernel = size == 4 ? (vec ? draft_verify_kernel<float, true> : draft_verify_kernel<float, false>)
-                            : (vec ? draft_verify_kernel<__nv_bfloat16, true> : draft_verify_kernel<__nv_bfloat16, false>);
-    return cuda_status(launch_pdl(kernel, dim3(slices, batch), dim3(kVerifyThreads), 0, (cudaStream_t)stream, a));
+    const int piece = size == 4 ? kPiece<float> : kPiece<__nv_bfloat16>;
+    a.pieces = (int)(((int64_t)rows->vocab + 16 / (int)size - 1 + piece - 1) / piece);      // wherever a row starts
+    // as many CTAs as run at once (by their shared memory), each with a piece or more for its warps
+    const size_t smem = (size_t)kVerifyWarps * kSlots * (rows->draft ? kSlotBytesQ : kSlotBytes);
+    const int resident = 148 * (int)((size_t)(227 << 10) / (smem + 1536));
+    const int slices = std::max(1, std::min(resident / batch, (a.pieces + kVerifyWarps - 1) / kVerifyWarps));
+    auto kernel = size == 4 ? draft_verify_kernel<float> : draft_verify_kernel<__nv_bfloat16>;
+    return cuda_status(launch_pdl(kernel, dim3(slices, batch), dim3(kVerifyThreads), smem, (cudaStream_t)stream, a));
 }
