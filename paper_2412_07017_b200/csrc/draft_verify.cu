@@ -9,7 +9,7 @@
 // exponents' difference in bias: all weights and sums are times 2^-896, which changes no comparison, and zeros and subnormal numbers are right as they
 // are.  (With conversions, of which an SM does 16 a cycle, a mean batch of 300 bf16 rows of 100 003 took 45.7 us, 26.4 for 64 pairs of fp32 rows of 128 256.)
 //
-// One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself); a warp has pieces of 4 KB brought into shared memory, the
+// One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself); a warp has pieces of 2 KB brought into shared memory, the
 // next one while it sums the last, and leaves each piece's sum in the workspace; the CTA that completes the row finds the piece by the sums, and brings
 // that one again.  Every value is read once, so the bytes of one row of p and one of q a sequence are what bounds a large batch, and a chain of
 // round trips (bounds of the sequence, tokens, their probabilities, values; count, sums, one piece) a small one.  Rows start anywhere: what is copied are
@@ -26,7 +26,7 @@ namespace asynclm {
 namespace {
 
 constexpr int kVerifyThreads = 64, kVerifyWarps = kVerifyThreads / 32;
-constexpr int kPieceBytes = 4096;
+constexpr int kPieceBytes = 2048;
 template <typename T>
 constexpr int kPiece = kPieceBytes / (int)sizeof(T);
 constexpr int kSlots = 2;      // of a warp: a piece of p, and one of q with a vector more
