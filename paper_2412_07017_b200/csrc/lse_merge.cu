@@ -13,6 +13,7 @@ namespace asynclm {
 // so small blocks that fit beside each other early do better.)
 constexpr int kMergeThreads = 128;
 constexpr int kMergeRows = 4;
+static_assert(kJoinRows == kMergeThreads / 32, "a row to a warp");
 
 // One row by a warp: chunks c < n, the partial row of chunk c being prow_of(c), for head `g` of kv head `kv_head`.
 template <int D, typename RowOf>
@@ -107,11 +108,10 @@ template <int D>
 __global__ void __launch_bounds__(kMergeThreads)
 lse_join_kernel(DevPlan p, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     const int G = p.group;
-    const int entry = p.join_blocks[blockIdx.x];
-    const Join j = p.joins[entry >> 6];
-    const int pair = (entry & 63) * kMergeRows + (threadIdx.x >> 5);
+    const Join j = p.joins[blockIdx.x];
+    const int pair = j.pair0 + (threadIdx.x >> 5);
     pdl_wait();     // as above
-    if (pair >= j.ntok * G) return;
+    if (pair >= j.pairs) return;
     const int t = pair / G;
     const size_t own = (size_t)j.own_row + t, pre = (size_t)j.pre_row + t;
     merge_row<D>(p, j.own_chunks + j.pre_chunks,

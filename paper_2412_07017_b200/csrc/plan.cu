@@ -56,12 +56,12 @@ static int default_tensor_min_rows(int head_dim) { return head_dim == 64 ? 64 : 
 struct BlobLayout {
     size_t off_q_indptr, off_kv_len, off_page_indptr, off_page_indices, off_row_seq, off_row_slot, off_units,
         off_items, off_works, off_heads, off_cta_cuda, off_cta_tensor, off_split, off_merge, off_status,
-        off_arrivals, off_joins, off_join_blocks, off_select_chunks, off_select_base, blob_bytes;
+        off_arrivals, off_joins, off_select_chunks, off_select_base, blob_bytes;
 };
 
 static BlobLayout layout_blob(int batch, int total_q, int64_t total_pages, int64_t n_units,
                               int64_t n_items, int ctas_cuda, int ctas_tensor, int64_t n_split,
-                              int64_t n_merge_blocks, int64_t n_joins = 0, int64_t n_join_blocks = 0, int64_t n_select_chunks = 0,
+                              int64_t n_merge_blocks, int64_t n_joins = 0, int64_t n_select_chunks = 0,
                               int64_t n_select_rows = 0) {
     BlobLayout L{};
     size_t o = 0;
@@ -83,7 +83,6 @@ static BlobLayout layout_blob(int batch, int total_q, int64_t total_pages, int64
     L.off_merge = take(sizeof(int32_t) * (size_t)std::max<int64_t>(n_merge_blocks, 1));
     L.off_arrivals = take(sizeof(int32_t) * (size_t)std::max<int64_t>(n_units, 1));
     L.off_joins = take(sizeof(Join) * (size_t)n_joins);
-    L.off_join_blocks = take(sizeof(int32_t) * (size_t)n_join_blocks);
     L.off_select_chunks = take(sizeof(SelectChunk) * (size_t)n_select_chunks);
     L.off_select_base = take(sizeof(int64_t) * (size_t)n_select_rows);
     L.blob_bytes = o;
@@ -445,7 +444,7 @@ int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joi
 // max_partial_rows partial rows.
 bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp,
                   std::vector<UnitBuild>& units, int group, int head_dim, const Model& model, int64_t kv_bytes, int n_ctas, const CutPolicy& policy,
-                  int64_t max_partial_rows, bool queue_only, std::vector<Item>& items,
+                  int64_t max_partial_rows, bool queue_only, int64_t* limit_ns, std::vector<Item>& items,
                   std::vector<int32_t>& cta_indptr_warp, std::vector<int32_t>& cta_indptr_tensor,
                   std::vector<int32_t>& item_cta, int32_t* queue_first, int32_t* queue_count) {
     struct Piece { Item it; int32_t cta; };
@@ -609,6 +608,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
         if (fill(mid, false)) hi = mid; else lo = mid;
     }
     fill(hi, true);
+    *limit_ns = hi;
     for (const Piece& pz : pieces_out) units[pz.it.unit].u.n_chunks = std::max(units[pz.it.unit].u.n_chunks, pz.it.chunk + 1);
 
     // ---- warp-body chunks.  An item boundary costs time and a split unit costs partial rows and a
@@ -826,15 +826,21 @@ struct Run {
 // Selected pages: a chunk of scores is a multiple of these pages (16 for each warp of a CTA), and so many CTAs run on an SM.
 constexpr int kSelectChunkUnit = 64, kSelectCtasPerSm = 4;
 
-// A sequence with more rows of a kv head than a row tile keeps its prefix to itself: its items are bound by the products, of which
-// sharing saves none, and its partial rows would be many.
-constexpr int kMostSharedRows = 128;
+// Rows of a kv head (G * q_len) up to which a sequence always shares its prefix.  Longer spans' items are bound by the products, of which sharing
+// saves none, and their partial rows are many, but their prefixes are cut by keys and evened out where they share it: for batches with such spans the planner
+// compares the ways by their modelled time.  (us of attention, unshared | shared by sequences of up to 128 rows | 512 | 1024 | 4096, 32/8 heads of 128 but
+// for the third: 30 sequences with 6 spans of 4-100 tokens 103 | 127 | 84 | 84 | 84; 8 spans of 100-200 177 | 179 | 119 | 104 | 109; 40 with 8 of 20-200 at
+// head_dim 64 134 | 124 | 112 | 93 | 93; 30 with 3 of 300-600 193 | 267 | 266 | 265 | 193; 6 of 250-500 alone 151 | 151 | 152 | 152 | 184; 4 prompts of
+// 500-1500 358-389 | 358 | 358 | 358 | 358, and 496 if all share.)
+constexpr int64_t kMostSharedRows = 1024;
 // Sharing costs partial rows and the join behind the attention; it has to save as many bytes of K and V as cross the bus in this time.
 constexpr int64_t kLeastSavedNs = 2500;
 
-// The runs of the groups (checked: ASYNCLM_OK, or what is wrong with them), and shared[b], the keys of sequence b that its run holds.
-int find_runs(const PlanExtra& extra, const asynclm_batch& batch, int B, int page, int group, int64_t bytes_per_key, bool all, std::vector<Run>& runs,
-              std::vector<int32_t>& shared) {
+// The runs of the groups (checked: ASYNCLM_OK, or what is wrong with them) of sequences with up to most_rows rows, and shared[b], 1 + sequence b's run or 0.
+int find_runs(const PlanExtra& extra, const asynclm_batch& batch, int B, int page, int group, int64_t bytes_per_key, bool all, int64_t most_rows,
+              std::vector<Run>& runs, std::vector<int32_t>& shared) {
+    runs.clear();
+    shared.assign((size_t)B, 0);
     int end = 0;
     int64_t saved = 0;
     for (int g = 0; g < extra.n_groups; ++g) {
@@ -852,7 +858,7 @@ int find_runs(const PlanExtra& extra, const asynclm_batch& batch, int B, int pag
             const int32_t* own = batch.page_indices + batch.page_indptr[b];
             if (pages == nullptr) pages = own;
             else if (n_pages > 0 && std::memcmp(pages, own, n_pages * sizeof(int32_t)) != 0) return ASYNCLM_ERR_PAGE_TABLE;
-            if (n_pages == 0 || (int64_t)ql * group > kMostSharedRows) {
+            if (n_pages == 0 || (int64_t)ql * group > most_rows) {
                 open = false;
                 continue;
             }
@@ -955,9 +961,10 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     const int64_t bytes_per_key = (int64_t)Hkv * (kv8 ? 2 * ((int64_t)shape->head_dim + 1) : 4 * (int64_t)shape->head_dim);
     std::vector<Run> runs;
     std::vector<int32_t> shared;      // 1 + the sequence's run, or 0
+    const bool share_all = opts && (opts->flags & ASYNCLM_PLAN_SHARE_ALL);
+    auto share = [&](int64_t most_rows) { return find_runs(extra, *batch, B, P, G, bytes_per_key, share_all, most_rows, runs, shared); };
     if (extra.n_groups > 0) {
-        shared.assign((size_t)B, 0);
-        rc = find_runs(extra, *batch, B, P, G, bytes_per_key, opts && (opts->flags & ASYNCLM_PLAN_SHARE_ALL), runs, shared);
+        rc = share(share_all ? INT64_MAX : kMostSharedRows);
         if (rc != ASYNCLM_OK) return rc;
     }
     auto run_of = [&](int b) { return shared.empty() ? -1 : shared[(size_t)b] - 1; };
@@ -1016,6 +1023,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     int32_t queue_first = 0, queue_count = 0;
     std::vector<int32_t> split_units, merge_blocks;   // merge block: 4 (token, head) rows of a split unit
     int64_t partial_rows = 0;
+    int64_t limit_ns = 0;             // the load limit that the cuts were made for: the step's modelled time
     // (too_many: the cuts leave more than max_partial_rows partial rows, and nothing is dealt)
     bool too_many = false;
     auto deal = [&](const CutPolicy& policy, bool tensor_on, int64_t max_partial_rows) -> int {
@@ -1110,7 +1118,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
                          cta_indptr_tensor, item_cta);
         } else {
             too_many = !deal_dynamic(ids_tensor, ids_cuda, units, G, shape->head_dim, model_of(shape->head_dim, kv8), read_keys * bytes_per_key, ctas_cuda, policy,
-                                     max_partial_rows, sparse != nullptr, items, cta_indptr_cuda, cta_indptr_tensor, item_cta, &queue_first, &queue_count);
+                                     max_partial_rows, sparse != nullptr, &limit_ns, items, cta_indptr_cuda, cta_indptr_tensor, item_cta, &queue_first, &queue_count);
             if (too_many) return ASYNCLM_OK;
             n_items_cuda = queue_first + queue_count;
         }
@@ -1141,8 +1149,29 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     while (partial_bytes(static_rows, G, shape->head_dim) > ASYNCLM_STATIC_SCRATCH_BYTES) --static_rows;
     auto fits_static = [&]() { return !too_many && partial_rows <= static_rows; };
     const CutPolicy fastest;
-    rc = deal(fastest, tensor_wanted, static_rows);
-    if (rc == ASYNCLM_OK && !fits_static()) {
+    if (!runs.empty() && !share_all && fixed_chunk == 0) {
+        int64_t longest = 0;      // rows of a sequence in a group
+        for (int g = 0; g < extra.n_groups; ++g)
+            for (int b = extra.groups[g].first_seq; b < extra.groups[g].first_seq + extra.groups[g].n_seqs; ++b)
+                longest = std::max<int64_t>(longest, (int64_t)(q_indptr[b + 1] - q_indptr[b]) * G);
+        if (longest > kMostSharedRows) {
+            // partial rows are written and read, past what the model has in its load limit
+            int64_t best = -1, best_ns = 0;
+            for (const int64_t most : {kMostSharedRows, INT64_MAX, (int64_t)0}) {
+                (void)share(most);
+                rc = deal(fastest, tensor_wanted, INT64_MAX);
+                if (rc != ASYNCLM_OK) continue;
+                const int64_t ns = limit_ns + partial_rows * G * (shape->head_dim + 1) * 8 * 1000 / kDramBytesPerUs;
+                if (best < 0 || ns < best_ns) best = most, best_ns = ns;
+            }
+            (void)share(best < 0 ? 0 : best);
+        }
+    }
+    // (rows that share a prefix have partial rows whatever the cuts: where those alone are too many, no other cuts are tried)
+    int64_t least_rows = 0;
+    for (const Run& r : runs) least_rows += r.tokens > 0 ? 2 * (int64_t)r.rows * Hkv : 0;
+    rc = deal(fastest, tensor_wanted, least_rows > static_rows ? INT64_MAX : static_rows);
+    if (rc == ASYNCLM_OK && !fits_static() && least_rows <= static_rows) {
         if (fixed_chunk == 0) {
             int64_t span_rows = 0, span_units = 0, warp_rows = 0;
             for (const UnitBuild& ub : units) {
@@ -1168,7 +1197,6 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
 
     // ---- rows of a run: the unit with the sequence's own keys beside the one with the shared keys ----
     std::vector<Join> joins;
-    std::vector<int32_t> join_blocks;
     if (!runs.empty()) {
         std::vector<std::vector<int32_t>> flat(runs.size() * (size_t)Hkv);      // a run's units with its prefix, by rows
         for (size_t i = 0; i < units.size(); ++i)
@@ -1179,10 +1207,10 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
                 const Unit& pre = units[(size_t)id].u;
                 const int r0 = std::max(own.u.q_row0, pre.q_row0), r1 = std::min(own.u.q_row0 + own.u.ntok, pre.q_row0 + pre.ntok);
                 if (r0 >= r1) continue;
-                if (joins.size() >= (size_t)(INT32_MAX >> 6)) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
-                for (int rb = 0; rb * 4 < (r1 - r0) * G; ++rb) join_blocks.push_back((int32_t)((joins.size() << 6) | (size_t)rb));
-                joins.push_back(Join{r0, r1 - r0, own.u.kv_head, own.u.partial_base + r0 - own.u.q_row0, own.u.ntok, own.u.n_chunks,
-                                     pre.partial_base + r0 - pre.q_row0, pre.ntok, pre.n_chunks, {0, 0, 0}});
+                if (joins.size() >= (size_t)(INT32_MAX / kJoinRows)) return ASYNCLM_ERR_WORKSPACE_TOO_SMALL;
+                for (int k = 0; k < (r1 - r0) * G; k += kJoinRows)
+                    joins.push_back(Join{r0, k, (r1 - r0) * G, own.u.kv_head, own.u.partial_base + r0 - own.u.q_row0, own.u.ntok, own.u.n_chunks,
+                                         pre.partial_base + r0 - pre.q_row0, pre.ntok, pre.n_chunks, {0, 0}});
             }
         }
     }
@@ -1198,7 +1226,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
 
     // ---- pack ---------------------------------------------------------------------------------
     BlobLayout L = layout_blob(B, T, total_pages, (int64_t)units.size(), n_items, grid_cuda,
-                               grid_tensor, (int64_t)n_split, (int64_t)merge_blocks.size(), (int64_t)joins.size(), (int64_t)join_blocks.size(),
+                               grid_tensor, (int64_t)n_split, (int64_t)merge_blocks.size(), (int64_t)joins.size(),
                                (int64_t)select_chunks.size(), (int64_t)select_base.size());
     const size_t plan_bytes = align_up(sizeof(asynclm_plan_s), 256);
     const size_t item_cta_bytes = align_up(sizeof(int32_t) * (size_t)std::max(n_items, 1), 256);
@@ -1287,10 +1315,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     if (n_split > 0) std::memcpy(hb + L.off_split, split_units.data(), sizeof(int32_t) * split_units.size());
     if (!merge_blocks.empty())
         std::memcpy(hb + L.off_merge, merge_blocks.data(), sizeof(int32_t) * merge_blocks.size());
-    if (!joins.empty()) {
-        std::memcpy(hb + L.off_joins, joins.data(), sizeof(Join) * joins.size());
-        std::memcpy(hb + L.off_join_blocks, join_blocks.data(), sizeof(int32_t) * join_blocks.size());
-    }
+    if (!joins.empty()) std::memcpy(hb + L.off_joins, joins.data(), sizeof(Join) * joins.size());
     if (!select_chunks.empty()) {
         std::memcpy(hb + L.off_select_chunks, select_chunks.data(), sizeof(SelectChunk) * select_chunks.size());
         std::memcpy(hb + L.off_select_base, select_base.data(), sizeof(int64_t) * select_base.size());
@@ -1343,8 +1368,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     d.partial_lse = (float*)dp(L.blob_bytes + align_up((size_t)partial_rows * (size_t)G *
                                                            (size_t)shape->head_dim * sizeof(float), 256));
     d.joins = (const Join*)dp(L.off_joins);
-    d.join_blocks = (const int32_t*)dp(L.off_join_blocks);
-    d.num_join_blocks = (int32_t)join_blocks.size();
+    d.num_join_blocks = (int32_t)joins.size();
     d.total_pages = total_pages;
     if (sparse) {
         d.select_chunks = (const SelectChunk*)dp(L.off_select_chunks);

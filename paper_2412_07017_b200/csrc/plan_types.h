@@ -49,15 +49,17 @@ struct alignas(16) Work {
                            // ctx = kv_limit0 - 1 - (q_row0 - q_seq0))
 };
 
-// Rows of a sequence that shares a prefix, to be joined from two sets of partial rows: those of the unit that holds the sequence's own
-// keys and those of the unit that holds the shared ones (each chunk's rows are `stride` partial rows behind the last one's).
+// (token, head) rows of sequences that share a prefix, to be joined by one block from two sets of partial rows: those of the unit that holds the
+// sequence's own keys and those of the unit that holds the shared ones (a chunk's rows are `stride` partial rows behind the last one's).
 struct alignas(16) Join {
-    int32_t q_row0, ntok;      // global token rows [q_row0, q_row0 + ntok)
+    int32_t q_row0;            // global token row of pair 0; pair k is head k % G of token k / G
+    int32_t pair0, pairs;      // the block's pairs [pair0, pair0 + kJoinRows), of `pairs`
     int32_t kv_head;
-    int32_t own_row, own_stride, own_chunks;      // partial row of token q_row0 in chunk 0
+    int32_t own_row, own_stride, own_chunks;      // partial row of token 0 in chunk 0
     int32_t pre_row, pre_stride, pre_chunks;
-    int32_t pad[3];
+    int32_t pad[2];
 };
+constexpr int kJoinRows = 4;
 
 // Plans for selected pages: rows next to each other of one sequence, for which one CTA and kv head score DevPlan::select_chunk_pages pages (see
 // select_pages.cu).
@@ -110,8 +112,7 @@ struct DevPlan {
     int32_t* status;                 // device status word
     int32_t* counters;               // [0] next chunk of the warp body's queue, [1] CTAs that are done with the
                                      // queue; both are zero between launches (the last CTA puts them back)
-    const Join* joins;               // plans with a shared prefix
-    const int32_t* join_blocks;      // [num_join_blocks] (join << 6) | row block: 4 (token, head) rows each
+    const Join* joins;               // [num_join_blocks] of plans with a shared prefix
     const SelectChunk* select_chunks;// plans for selected pages: the score kernel's work list
     const int64_t* select_base;      // [T] pages in front of the row's in the score array (of one kv head)
     int32_t* select_pages;           // [T][Hkv][budget] physical pages: what the units' page0 points at

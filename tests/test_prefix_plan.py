@@ -59,7 +59,7 @@ def test_every_key_once(heads, kv8, groups, own, new, alone):
 
 def test_nothing_worth_sharing_is_the_ordinary_plan():
     shape = Shape(32, 8, 128, PAGE)
-    for groups, own, new in (([(2, 16)], [4, 9], [1, 1]), ([(1, 8192)], [4], [1]), ([(3, 0)], [5, 6, 7], [1, 1, 1]), ([(3, 9600)], [5, 6, 7], [200, 300, 1])):
+    for groups, own, new in (([(2, 16)], [4, 9], [1, 1]), ([(1, 8192)], [4], [1]), ([(3, 0)], [5, 6, 7], [1, 1, 1]), ([(4, 3008)], [5, 6, 7, 8], [900, 1300, 1000, 700])):
         rows, args = batch(groups, own, new)
         a, b = B.plan_host(shape, 1 << 20, *args, groups=rows), B.plan_host(shape, 1 << 20, *args)
         assert (a.items() == b.items()).all() and a.info["partial_rows"] == b.info["partial_rows"]
