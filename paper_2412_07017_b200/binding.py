@@ -227,6 +227,9 @@ def _calls():
                 ext.bind_kv8(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.asynclm_kv8_append, lib.asynclm_kv8_attn_mixed, lib.asynclm_kv8_gather,
                                                                                lib.asynclm_rope_apply, lib.asynclm_plan_get_shape)),
                              torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.uint8, torch.int32, torch.int64, torch.float32)
+                ext.bind_pages(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.asynclm_kv_bounds, lib.asynclm_kv8_bounds, lib.asynclm_select_pages,
+                                                                                 lib.asynclm_plan_get_sparse, lib.asynclm_draft_verify,
+                                                                                 lib.asynclm_draft_verify_workspace_bytes)))
         except (ImportError, OSError, RuntimeError, AttributeError, TypeError) as e:
             ext = False
             warnings.warn(f"the per-layer calls go through ctypes, because their extension cannot be built or loaded: {e}", RuntimeWarning, stacklevel=3)
@@ -674,6 +677,10 @@ def _bounds_of(key_bounds, shape: CShape):
 def asynclm_kv_bounds(plan: Plan, kv_pool, key_bounds, from_start: bool = False, stream=None) -> None:
     """Least and largest value of every key channel into key_bounds (bf16 [pages][kv heads][2][head_dim]): of the pages with the step's new tokens, or,
     from_start, of all pages of the plan's sequences that have new tokens."""
+    if ext := _calls():
+        rc = ext.bounds(plan.handle, kv_pool, None, key_bounds, from_start, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_kv_bounds")
     import torch
     shape = _sizes(plan)[0]
     pool = _flat(kv_pool, "kv_pool", "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), shape.num_pages * 2 * shape.num_kv_heads * shape.page_size * shape.head_dim)
@@ -682,6 +689,10 @@ def asynclm_kv_bounds(plan: Plan, kv_pool, key_bounds, from_start: bool = False,
 
 def asynclm_kv8_bounds(plan: Plan, kv8_pool, kv8_scales, key_bounds, from_start: bool = False, stream=None) -> None:
     """asynclm_kv_bounds of the quantised cache."""
+    if ext := _calls():
+        rc = ext.bounds(plan.handle, kv8_pool, kv8_scales, key_bounds, from_start, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_kv8_bounds")
     shape = _sizes(plan)[0]
     pool, scales = _cache8(kv8_pool, kv8_scales, shape)
     _check(load().asynclm_kv8_bounds(plan.handle, pool, scales, _bounds_of(key_bounds, shape), int(bool(from_start)), _stream_ptr(stream)), "asynclm_kv8_bounds")
@@ -690,6 +701,10 @@ def asynclm_kv8_bounds(plan: Plan, kv8_pool, kv8_scales, key_bounds, from_start:
 def asynclm_select_pages(plan: Plan, q, key_bounds, pages_out=None, stream=None) -> None:
     """Chooses the pages that the attention with this plan (of asynclm_plan_sparse) reads; pages_out (int32 [tokens][kv heads][budget_pages]) receives their
     numbers inside the sequences, rising, -1 behind the last."""
+    if ext := _calls():
+        rc = ext.select(plan.handle, q, key_bounds, pages_out, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_select_pages")
     import torch
     shape, _, tokens = _sizes(plan)
     qa = _flat(q, "q", "a contiguous CUDA tensor of bfloat16", (torch.bfloat16,), tokens * shape.num_q_heads * shape.head_dim)
@@ -721,7 +736,11 @@ def _probabilities(t, name: str, rows: int, vocab: int, dtype):
 def asynclm_draft_verify(draft_indptr, target, draft, draft_tokens, accept_u, sample_u, accepted, tokens_out, workspace, stream=None) -> None:
     """Drafted tokens held against the target's probabilities (see include/asynclm.h).  draft_indptr int32 [batch + 1]; target [drafts + batch][vocab] and
     draft [drafts][vocab] (or None: proposals made with certainty), bf16 or fp32; draft_tokens int32, accept_u fp32 [drafts]; sample_u fp32 [batch];
-    accepted int32 [batch]; tokens_out int32 [drafts + batch]; workspace: uint8, zeroed, of draft_verify_workspace_bytes(batch, vocab) bytes or more."""
+    accepted int32 [batch]; tokens_out int32 [drafts + batch]; workspace: uint8, zeroed, of draft_verify_workspace_bytes(batch, vocab) bytes or more.  All on the current device."""
+    if ext := _calls():
+        rc = ext.verify(draft_indptr, target, draft, draft_tokens, accept_u, sample_u, accepted, tokens_out, workspace, stream)
+        if rc is not None:
+            return _check(rc, "asynclm_draft_verify")
     import torch
     batch, drafts = draft_indptr.numel() - 1, draft_tokens.numel()
     if target.dim() != 2 or target.dtype not in (torch.bfloat16, torch.float32):
@@ -737,6 +756,9 @@ def asynclm_draft_verify(draft_indptr, target, draft, draft_tokens, accept_u, sa
     wa = _flat(workspace, "workspace", "a contiguous CUDA tensor of uint8", (torch.uint8,))
     if workspace.numel() < draft_verify_workspace_bytes(batch, vocab):
         raise ValueError(f"workspace: {workspace.numel()} bytes, {draft_verify_workspace_bytes(batch, vocab)} are needed")
+    for t in (draft_indptr, target, draft, draft_tokens, accept_u, sample_u, accepted, tokens_out, workspace):
+        if t is not None and t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"a tensor on {t.device}, the current device is {torch.cuda.current_device()}")
     _check(load().asynclm_draft_verify(ctypes.byref(rows), flat[0], batch, drafts, flat[1], flat[2], flat[3], flat[4], flat[5], wa, _stream_ptr(stream)),
            "asynclm_draft_verify")
 

@@ -21,10 +21,16 @@ static int (*fn_kv8_attn)(const asynclm_plan_t*, const void*, const void*, const
 static int (*fn_kv8_gather)(const asynclm_plan_t*, const int64_t*, const int32_t*, int64_t, const void*, const void*, void*, void*, void*);
 static int (*fn_plan_shape)(const asynclm_plan_t*, asynclm_shape*, int32_t*, int32_t*);
 static int (*fn_rope)(const asynclm_rope_table*, const int32_t*, int32_t, int32_t, const asynclm_rope_rows*, int32_t, void*);
+static int (*fn_bounds)(const asynclm_plan_t*, const void*, void*, int32_t, void*);
+static int (*fn_kv8_bounds)(const asynclm_plan_t*, const void*, const void*, void*, int32_t, void*);
+static int (*fn_select)(const asynclm_plan_t*, const void*, const void*, int32_t*, void*);
+static int (*fn_plan_sparse)(const asynclm_plan_t*, asynclm_sparse*);
+static int (*fn_verify)(const asynclm_draft_rows*, const int32_t*, int32_t, int32_t, const int32_t*, const float*, const float*, int32_t*, int32_t*, void*, void*);
+static size_t (*fn_verify_bytes)(int32_t, int32_t);
 static PyObject *current_device, *raw_stream;      /* callables: () -> device, (device) -> stream handle */
 static PyObject *s_data_ptr, *s_numel, *s_cuda_stream, *s_num_q_heads, *s_num_kv_heads, *s_head_dim, *s_page_size;
 /* what a tensor is asked for, and the dtypes of rows, of a quantised cache's tensors and of indices */
-static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous;
+static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous, *s_get_device;
 static PyObject *t_bf16, *t_e4m3, *t_e8m0, *t_u8, *t_i32, *t_i64, *t_f32;
 
 /* (these return -1 with an exception set on failure) */
@@ -389,6 +395,144 @@ static PyObject* py_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+/* kv_bounds(handle, kv_pool, kv8_scales or None, key_bounds, from_start, stream) */
+static PyObject* py_bounds(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "6 arguments expected");
+    void *plan, *pool, *scales = NULL, *bounds, *stream;
+    plan_sizes s;
+    if (handle_of(a[0], &plan)) return NULL;
+    TAKE(sizes_of(plan, &s));
+    const int kv8 = a[2] != Py_None;
+    TAKE(flat(a[1], kv8 ? t_e4m3 : t_bf16, kv8 ? t_u8 : NULL, s.cache_rows * s.shape.head_dim, &pool));
+    if (kv8) TAKE(flat(a[2], t_e8m0, t_u8, s.cache_rows, &scales));
+    TAKE(flat(a[3], t_bf16, NULL, (Py_ssize_t)s.shape.num_pages * s.shape.num_kv_heads * 2 * s.shape.head_dim, &bounds));
+    const int from_start = PyObject_IsTrue(a[4]);
+    if (from_start < 0 || stream_of(a[5], &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = kv8 ? fn_kv8_bounds(plan, pool, scales, bounds, from_start, stream) : fn_bounds(plan, pool, bounds, from_start, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* select(handle, q, key_bounds, pages_out or None, stream) */
+static PyObject* py_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "5 arguments expected");
+    void *plan, *q, *bounds, *out = NULL, *stream;
+    plan_sizes s;
+    asynclm_sparse sparse;
+    if (handle_of(a[0], &plan)) return NULL;
+    TAKE(sizes_of(plan, &s));
+    TAKE(fn_plan_sparse(plan, &sparse) == 0);
+    TAKE(flat(a[1], t_bf16, NULL, (Py_ssize_t)s.tokens * s.shape.num_q_heads * s.shape.head_dim, &q));
+    TAKE(flat(a[2], t_bf16, NULL, (Py_ssize_t)s.shape.num_pages * s.shape.num_kv_heads * 2 * s.shape.head_dim, &bounds));
+    if (a[3] != Py_None) TAKE(flat(a[3], t_i32, NULL, (Py_ssize_t)s.tokens * s.shape.num_kv_heads * sparse.budget_pages, &out));
+    if (stream_of(a[4], &stream)) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_select(plan, q, bounds, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* The device of a tensor, or -2 with an exception set on failure. */
+static long device_of(PyObject* t) {
+    PyObject* v = PyObject_CallMethodNoArgs(t, s_get_device);
+    if (!v) return -2;
+    const long d = PyLong_AsLong(v);
+    Py_DECREF(v);
+    return PyErr_Occurred() ? -2 : d;
+}
+
+/* Rows [n][vocab] of fp32 or bf16 that do not overlap.  1, 0 or -1 as above. */
+static int probabilities(PyObject* t, PyObject* type, Py_ssize_t* n, Py_ssize_t* vocab, Py_ssize_t* stride, void** out) {
+    const int right = is_cuda_of(t, type, NULL);
+    if (right <= 0) return right;
+    Py_ssize_t dim[2], step[2];
+    for (int which = 0; which < 2; ++which) {
+        PyObject* v = which ? PyObject_CallMethodNoArgs(t, s_stride) : PyObject_GetAttr(t, s_shape);
+        if (!v) return -1;
+        if (!PyTuple_Check(v) || PyTuple_GET_SIZE(v) != 2) {
+            Py_DECREF(v);
+            return 0;
+        }
+        for (int k = 0; k < 2; ++k) (which ? step : dim)[k] = PyLong_AsSsize_t(PyTuple_GET_ITEM(v, k));
+        Py_DECREF(v);
+        if (PyErr_Occurred()) return -1;
+    }
+    if ((dim[1] > 1 && step[1] != 1) || (dim[0] > 1 && step[0] < dim[1])) return 0;
+    *n = dim[0];
+    *vocab = dim[1];
+    *stride = dim[0] > 1 ? step[0] : dim[1];
+    return address(t, out) ? -1 : 1;
+}
+
+/* verify(draft_indptr, target, draft or None, draft_tokens, accept_u, sample_u, accepted, tokens_out, workspace, stream); all on the current device */
+static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    if (n != 10) return PyErr_Format(PyExc_TypeError, "10 arguments expected");
+    Py_ssize_t rows, vocab, stride, d_rows = 0, d_vocab = 0, d_stride = 0;
+    void *target, *draft = NULL, *p[6], *workspace, *stream;
+    PyObject* v = PyObject_GetAttr(a[1], s_dtype);
+    if (!v) return NULL;
+    PyObject* const type = v == t_f32 ? t_f32 : t_bf16;
+    Py_DECREF(v);
+    TAKE(probabilities(a[1], type, &rows, &vocab, &stride, &target));
+    v = PyObject_CallMethodNoArgs(a[0], s_numel);
+    if (!v) return NULL;
+    const Py_ssize_t batch = PyLong_AsSsize_t(v) - 1, drafts = rows - batch;
+    Py_DECREF(v);
+    if (PyErr_Occurred()) return NULL;
+    if (batch < 0 || drafts < 0 || batch > INT32_MAX || drafts > INT32_MAX || vocab <= 0 || vocab > INT32_MAX) Py_RETURN_NONE;
+    if (a[2] != Py_None) {
+        TAKE(probabilities(a[2], type, &d_rows, &d_vocab, &d_stride, &draft));
+        if (d_rows != drafts || d_vocab != vocab) Py_RETURN_NONE;
+        if (drafts == 0) draft = NULL;
+    }
+    TAKE(flat(a[0], t_i32, NULL, batch + 1, &p[0]));
+    TAKE(flat(a[3], t_i32, NULL, drafts, &p[1]));
+    TAKE(flat(a[4], t_f32, NULL, drafts, &p[2]));
+    TAKE(flat(a[5], t_f32, NULL, batch, &p[3]));
+    TAKE(flat(a[6], t_i32, NULL, batch, &p[4]));
+    TAKE(flat(a[7], t_i32, NULL, rows, &p[5]));
+    v = PyObject_CallMethodNoArgs(a[8], s_numel);
+    if (!v) return NULL;
+    const Py_ssize_t bytes = PyLong_AsSsize_t(v);
+    Py_DECREF(v);
+    if (PyErr_Occurred()) return NULL;
+    TAKE(flat(a[8], t_u8, NULL, bytes, &workspace));
+    if ((size_t)bytes < fn_verify_bytes((int32_t)batch, (int32_t)vocab)) Py_RETURN_NONE;
+    v = PyObject_CallNoArgs(current_device);
+    if (!v) return NULL;
+    const long device = PyLong_AsLong(v);
+    Py_DECREF(v);
+    if (PyErr_Occurred()) return NULL;
+    for (int k = 0; k < 9; ++k) {
+        if (a[k] == Py_None) continue;
+        const long d = device_of(a[k]);
+        if (d == -2) return NULL;
+        if (d != device) Py_RETURN_NONE;
+    }
+    if (stream_of(a[9], &stream)) return NULL;
+    const asynclm_draft_rows r = {target, draft, stride, d_stride, (int32_t)vocab, type == t_f32 ? ASYNCLM_DTYPE_F32 : ASYNCLM_DTYPE_BF16};
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn_verify(&r, p[0], (int32_t)batch, (int32_t)drafts, p[1], p[2], p[3], p[4], p[5], workspace, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+static PyObject* py_bind_pages(PyObject* self, PyObject* args) {
+    Py_ssize_t bounds, kv8_bounds, select, sparse, verify, verify_bytes;
+    if (!PyArg_ParseTuple(args, "nnnnnn", &bounds, &kv8_bounds, &select, &sparse, &verify, &verify_bytes)) return NULL;
+    fn_bounds = (void*)bounds;
+    fn_kv8_bounds = (void*)kv8_bounds;
+    fn_select = (void*)select;
+    fn_plan_sparse = (void*)sparse;
+    fn_verify = (void*)verify;
+    fn_verify_bytes = (void*)verify_bytes;
+    Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, "bind(plan, append, append_rope, attn, step, current_device, raw_stream)"},
                                 {"plan", (PyCFunction)(void*)py_plan, METH_FASTCALL, NULL},
                                 {"append", (PyCFunction)(void*)py_append, METH_FASTCALL, NULL},
@@ -400,6 +544,10 @@ static PyMethodDef methods[] = {{"bind", py_bind, METH_VARARGS, "bind(plan, appe
                                 {"kv8_attn", (PyCFunction)(void*)py_kv8_attn, METH_FASTCALL, NULL},
                                 {"kv8_gather", (PyCFunction)(void*)py_kv8_gather, METH_FASTCALL, NULL},
                                 {"rope", (PyCFunction)(void*)py_rope, METH_FASTCALL, NULL},
+                                {"bind_pages", py_bind_pages, METH_VARARGS, "bind_pages(bounds, kv8_bounds, select_pages, plan_get_sparse, draft_verify, workspace_bytes)"},
+                                {"bounds", (PyCFunction)(void*)py_bounds, METH_FASTCALL, NULL},
+                                {"select", (PyCFunction)(void*)py_select, METH_FASTCALL, NULL},
+                                {"verify", (PyCFunction)(void*)py_verify, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "call_ext", NULL, -1, methods};
 
@@ -416,6 +564,8 @@ PyMODINIT_FUNC PyInit_call_ext(void) {
     s_dtype = PyUnicode_InternFromString("dtype");
     s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    if (!s_get_device) return NULL;
     if (!s_shape || !s_stride || !s_dtype || !s_is_cuda || !s_is_contiguous) return NULL;
     if (!s_data_ptr || !s_numel || !s_cuda_stream || !s_num_q_heads || !s_num_kv_heads || !s_head_dim || !s_page_size) return NULL;
     return PyModule_Create(&module);
