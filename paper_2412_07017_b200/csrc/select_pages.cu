@@ -203,13 +203,20 @@ __device__ __forceinline__ double held_value(__nv_bfloat16 x) {      // (as held
 
 // The sum of one query in shared memory and a page's bounds in 64 bits, by a warp.
 __device__ __forceinline__ double exact_sum(const __nv_bfloat16* q, const __nv_bfloat16* __restrict__ bounds, int head_dim, int lane) {
+    const int n = head_dim / 32, at = n * lane;      // four channels to a lane, or two
+    __nv_bfloat162 l[2], u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l[i] = reinterpret_cast<const __nv_bfloat162*>(bounds + at)[n == 4 ? i : 0];
+        u[i] = reinterpret_cast<const __nv_bfloat162*>(bounds + head_dim + at)[n == 4 ? i : 0];
+    }
     double s = 0.0;
-#pragma unroll 1
-    for (int i = 2 * lane; i < head_dim; i += 64) {
-        const __nv_bfloat162 l = *reinterpret_cast<const __nv_bfloat162*>(bounds + i), u = *reinterpret_cast<const __nv_bfloat162*>(bounds + head_dim + i);
-        const double x = held_value(q[i]), y = held_value(q[i + 1]);
-        s = fma(x, held_value(x < 0.0 ? l.x : u.x), s);
-        s = fma(y, held_value(y < 0.0 ? l.y : u.y), s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (2 * i >= n) break;
+        const double x = held_value(q[at + 2 * i]), y = held_value(q[at + 2 * i + 1]);
+        s = fma(x, held_value(x < 0.0 ? l[i].x : u[i].x), s);
+        s = fma(y, held_value(y < 0.0 ? l[i].y : u[i].y), s);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
@@ -221,7 +228,8 @@ template <int THREADS>
 __global__ void __launch_bounds__(THREADS)
 select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ bounds, int32_t* __restrict__ pages_out) {
     constexpr int kWarps = THREADS / 32;
-    __shared__ unsigned s_some[THREADS];               // the keys of t's bin; the pages that are scored again
+    __shared__ unsigned s_some[THREADS];               // the keys of t's bin; the pages that are scored again,
+    __shared__ int s_ids[THREADS];                     // and where they are
     __shared__ unsigned long long s_exact[THREADS];
     __shared__ int s_hist[256];
     __shared__ unsigned s_lo[kWarps], s_hi[kWarps], s_threshold;
@@ -237,6 +245,15 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
     int32_t* list = p.select_pages + (size_t)blockIdx.x * budget;
     int32_t* out = pages_out == nullptr ? nullptr : pages_out + (size_t)blockIdx.x * budget;
     unsigned* keys = p.select_keys + row_keys + (size_t)h * np;
+    const int steps = (np + THREADS - 1) / THREADS, stretch0 = warp * steps * 32;
+    const bool resident = steps <= kThreadKeys;
+    unsigned mine[kThreadKeys];
+    int ids[kThreadKeys];
+#pragma unroll
+    for (int i = 0; i < kThreadKeys; ++i) {
+        const int j = stretch0 + 32 * i + lane;
+        ids[i] = resident && i < steps && j < np ? __ldg(table + j) : 0;
+    }
     for (int i = tid; i < 256; i += THREADS) s_hist[i] = 0;
     if (tid == 0) s_n = s_open = s_total = 0;
     pdl_trigger();
@@ -248,35 +265,32 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         }
         return;
     }
-    const int D = p.head_dim, G = p.group;
-    for (int i = tid; i < G * D / 8; i += THREADS)
-        reinterpret_cast<uint4*>(s_q)[i] = reinterpret_cast<const uint4*>(q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D)[i];
-    const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-100f;
     // ---- this thread's keys: pages stretch0 + 32 i + lane
-    const int steps = (np + THREADS - 1) / THREADS, stretch0 = warp * steps * 32;
-    const bool resident = steps <= kThreadKeys;
-    unsigned mine[kThreadKeys];
 #pragma unroll
     for (int i = 0; i < kThreadKeys; ++i) {
         const int j = stretch0 + 32 * i + lane;
         mine[i] = resident && i < steps && j < np ? __ldcg(keys + j) : 0;      // (0 is below any score's)
     }
-    // use(page, key) for each of them, all lanes together; use returns the key, or another to put in its place
+    const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-100f;
+    const int D = p.head_dim, G = p.group;
+    for (int i = tid; i < G * D / 8; i += THREADS)
+        reinterpret_cast<uint4*>(s_q)[i] = reinterpret_cast<const uint4*>(q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D)[i];
+    // use(page, key, id) for each of them, all lanes together; use returns the key, or another to put in its place
     auto each = [&](auto use) {
         if (resident) {
 #pragma unroll
             for (int i = 0; i < kThreadKeys; ++i)
-                if (i < steps) mine[i] = use(stretch0 + 32 * i + lane, mine[i]);
+                if (i < steps) mine[i] = use(stretch0 + 32 * i + lane, mine[i], ids[i]);
         } else {
             for (int i = 0; i < steps; ++i) {
                 const int j = stretch0 + 32 * i + lane;
-                const unsigned k = j < np ? __ldcg(keys + j) : 0, now = use(j, k);
+                const unsigned k = j < np ? __ldcg(keys + j) : 0, now = use(j, k, j < np ? __ldg(table + j) : 0);
                 if (now != k && j < np) __stcg(keys + j, now);
             }
         }
     };
     unsigned lo = ~0u, hi = 0;      // of the scores
-    each([&](int, unsigned k) {
+    each([&](int, unsigned k, int) {
         if (k != kAlways && k != 0) lo = min(lo, k), hi = max(hi, k);
         return k;
     });
@@ -296,7 +310,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         int shift = lo == hi ? 0 : max(0, 24 - __clz(lo ^ hi));
         while (true) {
             const unsigned base = lo >> shift;
-            each([&](int, unsigned k) {
+            each([&](int, unsigned k, int) {
                 if (k >= lo && k <= hi) atomicAdd(&s_hist[(k >> shift) - base], 1);
                 return k;
             });
@@ -333,7 +347,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
             hi = min(hi, last);
             if (shift == 0) break;
             if (in <= THREADS) {      // few: the need-th of them by rank
-                each([&](int, unsigned k) {
+                each([&](int, unsigned k, int) {
                     if (k >= lo && k <= hi) s_some[atomicAdd(&s_n, 1)] = k;
                     return k;
                 });
@@ -357,11 +371,11 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         lo = ordered(__fadd_rd(t, -2.f * error));
         hi = ordered(__fadd_ru(t, 2.f * error));
         int above = 0;
-        each([&](int j, unsigned k) {
+        each([&](int j, unsigned k, int id) {
             above += k > hi && k != kAlways;
             if (k >= lo && k <= hi) {
                 const int at = atomicAdd(&s_open, 1);
-                if (at < THREADS) s_some[at] = (unsigned)j;
+                if (at < THREADS) s_some[at] = (unsigned)j, s_ids[at] = id;
             }
             return k;
         });
@@ -371,20 +385,18 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         need = all - s_total;      // to be taken of these
         const int open = s_open;
         if (open > need) {
-            auto exact = [&](int j, int g) {
-                return ordered(exact_sum(s_q + g * D, bounds + (((size_t)__ldg(table + j) * p.num_kv_heads + h) * 2) * D, D, lane));
-            };
+            auto exact = [&](int id, int g) { return ordered(exact_sum(s_q + g * D, bounds + (((size_t)id * p.num_kv_heads + h) * 2) * D, D, lane)); };
             if (open <= THREADS) {
                 s_exact[tid] = 0;
                 __syncthreads();
 #pragma unroll 1
                 for (int i = warp; i < open * G; i += kWarps) {      // a page and head to a warp: the code is met once, and cold
-                    const unsigned long long x = exact((int)s_some[i / G], i % G);
+                    const unsigned long long x = exact(s_ids[i / G], i % G);
                     if (lane == 0) atomicMax(&s_exact[i / G], x);
                 }
                 __syncthreads();
                 // an open page is in if fewer than `need` go in front of it (of equal scores the lower page)
-                each([&](int j, unsigned k) {
+                each([&](int j, unsigned k, int id) {
                     if (k < lo || k > hi) return k;
                     unsigned long long x = 0;
                     for (int i = 0; i < open; ++i)
@@ -397,12 +409,12 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
             } else {
                 // many scores that are (nearly) equal: the least of those in, bit by bit
                 unsigned long long* all_exact = p.select_exact + row_keys + (size_t)h * np;
-                each([&](int j, unsigned k) {
+                each([&](int j, unsigned k, int id) {
                     unsigned which = __ballot_sync(0xffffffffu, k >= lo && k <= hi);
                     for (; which; which &= which - 1) {
-                        const int at = __shfl_sync(0xffffffffu, j, __ffs(which) - 1);
+                        const int at = __shfl_sync(0xffffffffu, j, __ffs(which) - 1), page = __shfl_sync(0xffffffffu, id, __ffs(which) - 1);
                         unsigned long long x = 0;
-                        for (int g = 0; g < G; ++g) x = max(x, exact(at, g));
+                        for (int g = 0; g < G; ++g) x = max(x, exact(page, g));
                         if (lane == 0) __stcg(all_exact + at, x);
                     }
                     return k;
@@ -412,7 +424,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
                     if (tid == 0) s_total = 0;
                     __syncthreads();
                     int n = 0;
-                    each([&](int j, unsigned k) {
+                    each([&](int j, unsigned k, int id) {
                         if (k >= lo && k <= hi) n += __ldcg(all_exact + j) >= least;
                         return k;
                     });
@@ -425,7 +437,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
                 for (int bit = 63; bit >= 0; --bit)
                     if (count(least | 1ull << bit) >= need) least |= 1ull << bit;
                 need -= count(least + 1);      // (no score is the largest integer)
-                each([&](int j, unsigned k) {
+                each([&](int j, unsigned k, int id) {
                     if (k < lo || k > hi) return k;
                     const unsigned long long x = __ldcg(all_exact + j);
                     return x > least ? kTaken : x == least ? hi : 0u;
@@ -436,7 +448,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
     }
     // ---- the list: pages with keys above `hi`, and the first `need` of those from `lo` to `hi`
     int above = 0, among = 0;      // of the warp's stretch
-    each([&](int, unsigned k) {
+    each([&](int, unsigned k, int) {
         above += __popc(__ballot_sync(0xffffffffu, k > hi));
         among += __popc(__ballot_sync(0xffffffffu, k >= lo && k <= hi));
         return k;
@@ -446,12 +458,12 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
     above = among = 0;      // in front of the stretch
     for (int w = 0; w < warp; ++w) above += s_count[w][0], among += s_count[w][1];
     const unsigned below = (1u << lane) - 1;
-    each([&](int j, unsigned k) {
+    each([&](int j, unsigned k, int id) {
         const unsigned over = __ballot_sync(0xffffffffu, k > hi), in = __ballot_sync(0xffffffffu, k >= lo && k <= hi);
         const int among_here = among + __popc(in & below);
         if (k > hi || (k >= lo && k <= hi && among_here < need)) {
             const int at = above + __popc(over & below) + min(among_here, need);
-            list[at] = __ldg(table + j);
+            list[at] = id;
             if (out != nullptr) out[at] = j;
         }
         above += __popc(over);
