@@ -676,7 +676,8 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // sizes.  Not at head_dim 64 with a unit or more for every CTA, where it is worth 2 % on average over 20 batches, 0.91 to 1.2 of the time by turns: 40
     // sequences of 2-6 K keys, 8 kv heads, 58-60 | 53-55, 20 of 4-30 K 104-109 | 96-101, 64 of 1-3 K 42-43 | 41-43, 32 of 0.5-8 K 47, 56 | 57,
     // 54, 100 of 1-10 K, 2 kv heads, 44-51 | 45-56, short ones and 128 of 16 kv heads equal.
-    const bool even = model.kv8 && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
+    // Selected pages of either cache, too: their units are of one length or nearly (16 sequences with 128 pages of 16 bits, 128 units on 148 CTAs, 30.7 | 26.2).
+    const bool even = (model.kv8 || queue_only) && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
     if (even) {
         std::vector<int64_t> joins;
         for (int k = 0; k < used; ++k) joins.push_back(ctas[(size_t)k].load);

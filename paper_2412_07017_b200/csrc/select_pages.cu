@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "asynclm.h"
+#include "attn_launch.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "plan_internal.h"
@@ -65,12 +66,23 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Of a warp: two tiles of bounds in shared memory, one on its way while the other is in use, [page][least, largest][channel].  The 16-byte vectors of
+// odd pages change places with those four further, so that the eight lanes that a bank serves at once (two pages, four vectors) read different ones.
+template <int D>
+struct ScoreSlots {
+    static constexpr int kPageBytes = 4 * D, kBytes = kTilePages * kPageBytes;
+    static constexpr size_t kSmem = (size_t)kScoreWarps * 2 * kBytes;
+    static __device__ __forceinline__ int offset(int page, int vec) { return page * kPageBytes + (vec ^ (page & 1) * 4) * 16; }
+};
+
 // Thread (g, t) = (lane / 4, lane % 4) of an MMA holds channels 32 j + 8 t .. + 7 of pages g and g + 8 (A) and of query g (B): a 16-byte vector's
 // first two words are the k columns 2t, 2t + 1 and 2t + 8, 2t + 9 of one instruction, its last two those of the next.
 template <int D, int G>
-__global__ void __launch_bounds__(kScoreThreads, 4)
+__global__ void __launch_bounds__(kScoreThreads)
 select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __restrict__ bounds) {
     constexpr int J = D / 32, kColumns = 8, kGroups = kSelectQueries / kColumns;
+    using Slots = ScoreSlots<D>;
+    extern __shared__ __align__(16) uint8_t s_slots[];
     __shared__ uint4 s_q[kGroups][J][2][32];      // max(q, 0) and min(q, 0) as the threads take them
     __shared__ unsigned s_error[kSelectQueries];
     pdl_trigger();
@@ -82,26 +94,24 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     const int end = min(c.page0 + p.select_chunk_pages, (pos0 + c.rows - 1) / kPage + 1);
     const int queries = c.rows * G;
     auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
-    int j0 = c.page0 + warp * kTilePages, ids = id_of(j0);
+    constexpr int kStep = kScoreWarps * kTilePages;
+    int j0 = c.page0 + warp * kTilePages, ids = id_of(j0), ids_next = id_of(j0 + kStep);
     if (tid < kSelectQueries) s_error[tid] = 0;
-    uint4 lo[J][2], hi[J][2];      // of pages g and g + 8
-    auto load = [&]() {
+    uint8_t* slots = s_slots + (size_t)warp * 2 * Slots::kBytes;
+    auto request = [&](int slot, int my_id) {
+        constexpr int kVecs = Slots::kPageBytes / 16;      // of a page: all lanes, or half of them
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t page = __shfl_sync(0xffffffffu, ids, g + 8 * half);
-            const uint4* src = reinterpret_cast<const uint4*>(bounds + ((max(page, (int64_t)0) * p.num_kv_heads + h) * 2) * D * 2) + t;
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                lo[j][half] = hi[j][half] = make_uint4(0, 0, 0, 0);
-                if (page >= 0) {
-                    lo[j][half] = src[4 * j];
-                    hi[j][half] = src[4 * j + D / 8];
-                }
-            }
+        for (int i = 0; i < kTilePages * kVecs / 32; ++i) {
+            const int page = (i * 32 + lane) / kVecs, vec = (i * 32 + lane) % kVecs;
+            const int64_t id = __shfl_sync(0xffffffffu, my_id, page);
+            const uint8_t* src = bounds + ((max(id, (int64_t)0) * p.num_kv_heads + h) * 2) * D * 2 + vec * 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slots + slot * Slots::kBytes + Slots::offset(page, vec))),
+                         "l"(src), "r"(id >= 0 ? 16 : 0) : "memory");
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
     pdl_wait();      // queries and bounds are the kernels' in front
-    load();
+    if (j0 < end) request(0, ids);
     for (int i = tid; i < kGroups * J * 32; i += kScoreThreads) {
         const int l = i % 32, j = i / 32 % J, k = i / 32 / J * kColumns + l / 4;
         uint4 w = make_uint4(0, 0, 0, 0);
@@ -115,8 +125,16 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     float error[kGroups][2];
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) error[k][0] = error[k][1] = 0.f;
-    for (; j0 < end; j0 += kScoreWarps * kTilePages) {
-        ids = id_of(j0 + kScoreWarps * kTilePages);
+    for (int slot = 0; j0 < end; j0 += kStep, slot ^= 1) {
+        if (j0 + kStep < end) {
+            request(slot ^ 1, ids_next);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        ids_next = id_of(j0 + 2 * kStep);
+        __syncwarp();      // all lanes' copies are there
+        const uint8_t* tile = slots + slot * Slots::kBytes;
         const bool more = queries > kColumns;
         float s_all[kGroups][4], a_all[kGroups][4];      // scores, sums of magnitudes
 #pragma unroll
@@ -128,7 +146,9 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
             uint32_t l[2][4], u[2][4], m[2][4];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const uint32_t x[4] = {lo[j][half].x, lo[j][half].y, lo[j][half].z, lo[j][half].w}, y[4] = {hi[j][half].x, hi[j][half].y, hi[j][half].z, hi[j][half].w};
+                const uint4 lo = *reinterpret_cast<const uint4*>(tile + Slots::offset(g + 8 * half, 4 * j + t));
+                const uint4 hi = *reinterpret_cast<const uint4*>(tile + Slots::offset(g + 8 * half, D / 8 + 4 * j + t));
+                const uint32_t x[4] = {lo.x, lo.y, lo.z, lo.w}, y[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     l[half][e] = held(x[e]);
@@ -180,7 +200,7 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
                 }
             }
         }
-        if (j0 + kScoreWarps * kTilePages < end) load();
+        __syncwarp();      // (the slot is free)
     }
     // ---- how far the scores may be off: a row's largest (positive floats compare as integers)
 #pragma unroll
@@ -474,7 +494,9 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
 
 template <int D, int G>
 cudaError_t launch_scores(const DevPlan& p, const void* q, const void* bounds, cudaStream_t s) {
-    return launch_when(!p.full_launch, select_score_kernel<D, G>, dim3((unsigned)(p.num_select_chunks * p.num_kv_heads)), dim3(kScoreThreads), 0, s, p,
+    constexpr size_t smem = ScoreSlots<D>::kSmem;
+    if (cudaError_t e = allow_smem<select_score_kernel<D, G>>(smem)) return e;
+    return launch_when(!p.full_launch, select_score_kernel<D, G>, dim3((unsigned)(p.num_select_chunks * p.num_kv_heads)), dim3(kScoreThreads), smem, s, p,
                       (const uint8_t*)q, (const uint8_t*)bounds);
 }
 
