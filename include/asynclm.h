@@ -206,6 +206,8 @@ int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
  * so does the batch where little would be saved (ASYNCLM_PLAN_SHARE_ALL shares that, too).
  *   Workspaces: make the plan without a device workspace first (asynclm_plan_info then says what is needed) or retry on WORKSPACE_TOO_SMALL;
  * asynclm_plan_workspace_size does not cover these plans.
+ *   Rows that share a prefix have partial results whatever the cuts, so the plan is not cut down to fit asynclm_attn_mixed_static's array: that call refuses
+ * the larger ones.
  * Errors: those of asynclm_plan; INVALID_ARG (groups out of order or outside the batch, a prefix that is not whole pages or longer than a
  * sequence's context), PAGE_TABLE (sequences of a group differ in the pages of their prefix).
  */

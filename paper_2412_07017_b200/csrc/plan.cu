@@ -104,6 +104,7 @@ static size_t partial_bytes(int64_t rows, int group, int head_dim) {
 // shortest sixth has 0.05 to 0.6 of a share there.  Near a share, cutting wins: 19 of 3 K keys 45.4 | 50.)
 constexpr int kTailChunksPerCta = 2;
 constexpr int kMinChunkTiles = 4;
+constexpr int kMinSharedTiles = 2;      // of a span unit with a shared prefix
 constexpr int kShortUnitShareNum = 2, kShortUnitShareDen = 3;
 constexpr int kSaturatingCtas = 74;      // stream 6.2 TB/s of pages, 148 6.6, 37 4.4
 // That alone leaves the last wave nearly empty where the units are of about one length and not a multiple of the CTAs, so
@@ -500,9 +501,11 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     }
 
     // ---- span units under a load limit
-    std::vector<int> order(ids_tensor);
+    // (those with a shared prefix apart: they are cut wherever a CTA is full)
+    std::vector<int> order, shared_order;
     std::vector<int64_t> tiles(units.size()), tns(units.size());
-    for (int id : order) {
+    for (int id : ids_tensor) {
+        (units[(size_t)id].flat ? shared_order : order).push_back(id);
         tiles[(size_t)id] = tiles_of(units[id].n_keys, tc.gran);
         tns[(size_t)id] = units[id].u.ntok * group > 128 ? dual_tile_ns : tc.tile_ns;
     }
@@ -522,7 +525,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // Packs the span units under `cap`; returns false if they do not fit or leave too little room for
     // the queue.  With emit == false only the verdict is computed (the bisection's probes).
     int64_t span_work = 0;      // all span items without the per-CTA start
-    for (int id : order) span_work += tc.item_ns + tiles[(size_t)id] * tns[(size_t)id];
+    for (int id : ids_tensor) span_work += tc.item_ns + tiles[(size_t)id] * tns[(size_t)id];
     const int64_t floor_ns = kStartNs + kv_bytes * 1000 / kDramBytesPerUs;
     const int64_t bound = std::max<int64_t>(std::max<int64_t>(1, (warp_ns + span_work) / n_ctas), floor_ns);      // of the load limit
     auto fill = [&](int64_t limit, bool emit) {
@@ -532,11 +535,11 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
             ? (warp_tiles * kWarpCost.tile_ns * kStreamShare64 / 64 + (limit - kStartNs) - 1) / (limit - kStartNs) : n_ctas;
         // (a lone CTA does both)
         const int64_t span_ctas = ids_warp.empty() || n_ctas == 1 ? n_ctas : n_ctas - stream_ctas;
-        if (!order.empty() && span_ctas < 1) return false;
+        if (!ids_tensor.empty() && span_ctas < 1) return false;
         // what a span CTA may be given: the span work spread over those CTAs with some slack for the
         // packing, at most the load limit less the safety margin.  Spreading the spans thin costs little (a
         // span CTA that is done early joins the queue), filling span CTAs to the brim risks a late finish.
-        const int64_t thin = order.empty() ? 0 : span_work / span_ctas * 5 / 4 + tc.phase_ns + tc.item_ns + dual_tile_ns;
+        const int64_t thin = ids_tensor.empty() ? 0 : span_work / span_ctas * 5 / 4 + tc.phase_ns + tc.item_ns + dual_tile_ns;
         // (Past twice the lower bound the spread is given up: items of more than half of `thin` take a CTA each,
         // and there may be more of them than CTAs.)
         const int64_t full = limit * 64 / span_margin64(head_dim);
@@ -556,6 +559,33 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
             std::move_backward(ctas.begin() + to, ctas.begin() + at, ctas.begin() + at + 1);
             ctas[(size_t)to] = c;
         };
+        // Shared prefixes first: their rows are partial ones and joined whatever the cuts, so each unit goes on where the last one ended, and CTAs
+        // are filled to the brim.  (us, pieces of one length for a unit | so: 30 sequences with 6 spans of 4-100 tokens 84 | 79, 30 with 3 of 300-600
+        // 193 | 173, 10 over the 8-bit cache with 3 of 200-500 310 | 202, 96 with one token each at 8/2 heads of 64 21.0 | 19.5, 64 with one 46 | 46.)
+        for (int id : shared_order) {
+            const int64_t t = tiles[(size_t)id], ns = tns[(size_t)id];
+            int32_t c = 0;
+            for (int64_t k0 = 0; k0 < t; ++c) {
+                auto room = [&]() { return (cap - ctas[(size_t)used - 1].load - tc.item_ns) / ns; };
+                if (used == 0 || room() < std::min(t - k0, (int64_t)kMinSharedTiles)) {
+                    if (used < n_ctas) {
+                        ctas[(size_t)used] = Cta{tc.phase_ns, (int32_t)used};
+                        ++used;
+                    }
+                    if (!emit && used > span_ctas) return false;
+                }
+                const bool last = used == n_ctas && room() < kMinSharedTiles;      // (no CTA is left)
+                if (last && !emit) return false;
+                int64_t take = last ? t - k0 : std::min(t - k0, std::max<int64_t>(1, room()));
+                if (t - k0 - take < kMinSharedTiles) take = t - k0;
+                if (emit)
+                    pieces_out.push_back(Piece{Item{id, (int32_t)(k0 * tc.gran), (int32_t)std::min<int64_t>(units[id].n_keys, (k0 + take) * tc.gran), c},
+                                               ctas[(size_t)used - 1].id});
+                ctas[(size_t)used - 1].load += tc.item_ns + take * ns;
+                k0 += take;
+            }
+        }
+        std::sort(ctas.begin(), ctas.begin() + used, [](const Cta& x, const Cta& y) { return x.load != y.load ? x.load > y.load : x.id < y.id; });
         for (const Batch& batch : batches) {
             const int64_t t = batch.tiles, ns = batch.ns;
             const int64_t fresh_room = std::max<int64_t>(1, (cap - tc.phase_ns - tc.item_ns) / ns);
@@ -1168,11 +1198,9 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
             (void)share(best < 0 ? 0 : best);
         }
     }
-    // (rows that share a prefix have partial rows whatever the cuts: where those alone are too many, no other cuts are tried)
-    int64_t least_rows = 0;
-    for (const Run& r : runs) least_rows += r.tokens > 0 ? 2 * (int64_t)r.rows * Hkv : 0;
-    rc = deal(fastest, tensor_wanted, least_rows > static_rows ? INT64_MAX : static_rows);
-    if (rc == ASYNCLM_OK && !fits_static() && least_rows <= static_rows) {
+    // (rows that share a prefix have partial rows whatever the cuts: such a plan is not cut down for that array)
+    rc = deal(fastest, tensor_wanted, runs.empty() ? static_rows : INT64_MAX);
+    if (rc == ASYNCLM_OK && !fits_static() && runs.empty()) {
         if (fixed_chunk == 0) {
             int64_t span_rows = 0, span_units = 0, warp_rows = 0;
             for (const UnitBuild& ub : units) {
