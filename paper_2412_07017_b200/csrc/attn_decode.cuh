@@ -730,13 +730,14 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
         int unappended_from = INT_MAX;
         if (i0 < i1) {
             cur = unpack(head + kHeadWorkCuda);
-            pages_cur = head[kHeadPagesCuda + lane];
+            if (p.select_budget == 0) pages_cur = head[kHeadPagesCuda + lane];
             if constexpr (APPEND) unappended_from = cur.kv_limit0 - 1 - (cur.q_row0 - cur.q_seq0);
         }
         // The plan is there when this kernel starts (behind an upload by kernel the first launch starts when that has
         // completed: PlanUse), so all of the above overlaps the tail of the kernel in front; the pool, Q and the queue
         // are touched only from here on.
         pdl_wait();
+        if (p.select_budget != 0 && cur.kv_end > 0) pages_cur = load_pages(cur, 0);      // selected pages: their ids are the kernel's in front
         if (cur.kv_end == 0) cur = take();      // a CTA that came from span tiles starts on the queue
         while (cur.kv_end > 0 && ok) {
             const int ntiles = (cur.kv_end - cur.kv0 + kTileTok - 1) / kTileTok;
@@ -920,7 +921,7 @@ __device__ __forceinline__ void decode_body(const DevPlan& p, const CUtensorMap*
     if constexpr (PREFETCH) {
         const int32_t* head = p.cta_heads + (size_t)blockIdx.x * kHeadWords;
         const Work* w = reinterpret_cast<const Work*>(head + kHeadWorkCuda);
-        const int pages = head[2] < head[3] ? (w->kv_end - w->kv0 + kPage - 1) / kPage : 0;
+        const int pages = head[2] < head[3] && p.select_budget == 0 ? (w->kv_end - w->kv0 + kPage - 1) / kPage : 0;
         if (pages >= kPrefetchMinPages) prefetch_first_pages<D, KV8>(p, pool, head + kHeadPagesCuda, pages, w->kv_head, warp, kWarps, lane);
     }
     pdl_wait();

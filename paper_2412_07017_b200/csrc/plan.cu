@@ -440,12 +440,12 @@ int64_t queue_ns(const std::vector<Item>& queue, const std::vector<int64_t>& joi
 // and merged in chunk order, so the output does not depend on which CTA ran what.
 //   The load limit is the smallest one under which the span units fit and the room left on all CTAs
 // covers the modelled time of the queue; it is found by bisection.
-//   queue_only: no CTA starts on a chunk of its own (its header would hold page ids, which selected pages have none of yet).
+//   selected: the units are those of selected pages.
 //   Returns false, with only the units (their division and n_chunks) filled in, if the cuts leave more than
 // max_partial_rows partial rows.
 bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp,
                   std::vector<UnitBuild>& units, int group, int head_dim, const Model& model, int64_t kv_bytes, int n_ctas, const CutPolicy& policy,
-                  int64_t max_partial_rows, bool queue_only, int64_t* limit_ns, std::vector<Item>& items,
+                  int64_t max_partial_rows, bool selected, int64_t* limit_ns, std::vector<Item>& items,
                   std::vector<int32_t>& cta_indptr_warp, std::vector<int32_t>& cta_indptr_tensor,
                   std::vector<int32_t>& item_cta, int32_t* queue_first, int32_t* queue_count) {
     struct Piece { Item it; int32_t cta; };
@@ -707,7 +707,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // sequences of 2-6 K keys, 8 kv heads, 58-60 | 53-55, 20 of 4-30 K 104-109 | 96-101, 64 of 1-3 K 42-43 | 41-43, 32 of 0.5-8 K 47, 56 | 57,
     // 54, 100 of 1-10 K, 2 kv heads, 44-51 | 45-56, short ones and 128 of 16 kv heads equal.
     // Selected pages of either cache, too: their units are of one length or nearly (16 sequences with 128 pages of 16 bits, 128 units on 148 CTAs, 30.7 | 26.2).
-    const bool even = (model.kv8 || queue_only) && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
+    const bool even = (model.kv8 || selected) && (head_dim != 64 || (int64_t)warp_order.size() < n_ctas);
     if (even) {
         std::vector<int64_t> joins;
         for (int k = 0; k < used; ++k) joins.push_back(ctas[(size_t)k].load);
@@ -813,7 +813,7 @@ bool deal_dynamic(std::vector<int>& ids_tensor, const std::vector<int>& ids_warp
     // queue), then the span items grouped by CTA
     cta_indptr_warp.assign((size_t)n_ctas + 1, 0);
     cta_indptr_tensor.assign((size_t)n_ctas + 1, 0);
-    const int n_start = queue_only ? 0 : (int)std::min<size_t>(chunks.size(), (size_t)(n_ctas - used));
+    const int n_start = (int)std::min<size_t>(chunks.size(), (size_t)(n_ctas - used));
     items.reserve(chunks.size() + pieces_out.size());
     item_cta.reserve(chunks.size() + pieces_out.size());
     for (size_t i = 0; i < chunks.size(); ++i) {
@@ -1334,7 +1334,7 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
             const Work& w = h_works[first];
             std::memcpy(h + (path == 0 ? kHeadWorkTensor : kHeadWorkCuda), &w, sizeof(Work));
             const int npg = (w.kv_end - w.kv0 + kPage - 1) / kPage;
-            for (int k = 0; k < 32 && k < npg; ++k)
+            for (int k = 0; k < 32 && k < npg && !sparse; ++k)      // (selected pages are not known yet)
                 h[(path == 0 ? kHeadPagesTensor : kHeadPagesCuda) + k] = batch->page_indices[w.page0 + k];
         }
     }

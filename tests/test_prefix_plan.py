@@ -98,7 +98,7 @@ def test_sparse_plan(heads, kv8):
     keys = np.minimum(pos // PAGE, 63) * PAGE + pos % PAGE + 1
     seen = [[np.zeros(n, int) for _ in range(shape.num_kv_heads)] for n in keys]
     for it in plan.items():
-        assert it["ntok"] == 1 and it["cta"] == -1 and it["path"] == 0      # handed out at run time, when the lists are there
+        assert it["ntok"] == 1 and it["path"] == 0
         seen[args[0][it["seq"]] + it["tok0"]][it["kv_head"]][it["kv0"]:it["kv1"]] += 1
     assert all((h == 1).all() for r in seen for h in r)
     for bad in ((4, 2, 3), (4, -1, 1), (4, 0, 0), (0, 0, 1), (2 ** 31 - 1, 2 ** 31 - 1, 2)):
