@@ -111,15 +111,23 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     pdl_wait();      // queries and bounds are the kernels' in front
-    if (j0 < end) request(0, ids);
-    for (int i = tid; i < kGroups * J * 32; i += kScoreThreads) {
-        const int l = i % 32, j = i / 32 % J, k = i / 32 / J * kColumns + l / 4;
-        uint4 w = make_uint4(0, 0, 0, 0);
+    // (all that is read first is on its way before any of it is waited for: a CTA's start takes longer than a tile)
+    constexpr int kQueryVecs = kGroups * J * 32 / kScoreThreads;
+    uint4 w[kQueryVecs];
+#pragma unroll
+    for (int n = 0; n < kQueryVecs; ++n) {
+        const int i = tid + n * kScoreThreads, l = i % 32, j = i / 32 % J, k = i / 32 / J * kColumns + l / 4;
+        w[n] = make_uint4(0, 0, 0, 0);
         if (k < queries)
-            w = *reinterpret_cast<const uint4*>(q + (((size_t)(c.row0 + k / G) * p.num_q_heads + (size_t)h * G + k % G) * D + 32 * j + 8 * (l % 4)) * 2);
-        w = make_uint4(held(w.x), held(w.y), held(w.z), held(w.w));
-        s_q[i / 32 / J][j][0][l] = make_uint4(max2(w.x, 0), max2(w.y, 0), max2(w.z, 0), max2(w.w, 0));
-        s_q[i / 32 / J][j][1][l] = make_uint4(min2(w.x, 0), min2(w.y, 0), min2(w.z, 0), min2(w.w, 0));
+            w[n] = *reinterpret_cast<const uint4*>(q + (((size_t)(c.row0 + k / G) * p.num_q_heads + (size_t)h * G + k % G) * D + 32 * j + 8 * (l % 4)) * 2);
+    }
+    if (j0 < end) request(0, ids);
+#pragma unroll
+    for (int n = 0; n < kQueryVecs; ++n) {
+        const int i = tid + n * kScoreThreads;
+        const uint4 x = make_uint4(held(w[n].x), held(w[n].y), held(w[n].z), held(w[n].w));
+        s_q[i / 32 / J][i / 32 % J][0][i % 32] = make_uint4(max2(x.x, 0), max2(x.y, 0), max2(x.z, 0), max2(x.w, 0));
+        s_q[i / 32 / J][i / 32 % J][1][i % 32] = make_uint4(min2(x.x, 0), min2(x.y, 0), min2(x.z, 0), min2(x.w, 0));
     }
     __syncthreads();
     float error[kGroups][2];
@@ -141,8 +149,8 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
         for (int k = 0; k < kGroups; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s_all[k][e] = a_all[k][e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
+#pragma unroll 1
+        for (int j = 0; j < J; ++j) {      // (not unrolled: a launch's code is cold, and a CTA has one to four tiles a warp)
             uint32_t l[2][4], u[2][4], m[2][4];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
