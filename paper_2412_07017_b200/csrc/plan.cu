@@ -854,8 +854,10 @@ struct Run {
     int32_t first, tokens, row0, rows, seqs;
 };
 
-// Selected pages: a chunk of scores is a multiple of these pages (16 for each warp of a CTA), and so many CTAs run on an SM.
-constexpr int kSelectChunkUnit = 64, kSelectCtasPerSm = 4;
+// Selected pages: a chunk of scores is a multiple of these pages (16 for each warp of a CTA), about so many for an SM.  (us of bounds, selection and attention,
+// chunks of 64 | 128 | 192 | 256 | 320 pages: 4 sequences of 16-60 K tokens 39.7 | 37.8 | 37.6 | 38.7 | 39.8, 48 of 3-12 K with 1-4 new tokens 120 | 114 |
+// 113 | 112 | 113, 150 of 0.3-9 K at 8/2 heads of 64 43.5 | 43.8 | 43.6 | 45.9 | 47.3; the rule takes 128, 192 and 128.)
+constexpr int kSelectChunkUnit = 64, kSelectChunksPerSm = 8;
 
 // Rows of a kv head (G * q_len) up to which a sequence always shares its prefix.  Longer spans' items are bound by the products, of which sharing
 // saves none, and their partial rows are many, but their prefixes are cut by keys and evened out where they share it: for batches with such spans the planner
@@ -1028,9 +1030,8 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
                     scored += pages;
                 }
             }
-        // chunks of one length, about two for each of the CTAs that run at once
-        const int64_t ctas = (int64_t)kSelectCtasPerSm * n_sms * 2;
-        chunk_pages = (int32_t)std::min<int64_t>(std::max<int64_t>((scored * Hkv + ctas * kSelectChunkUnit - 1) / (ctas * kSelectChunkUnit), 1) * kSelectChunkUnit, 1 << 24);
+        const int64_t chunks = (int64_t)kSelectChunksPerSm * n_sms;
+        chunk_pages = (int32_t)std::min<int64_t>(std::max<int64_t>((scored * Hkv + chunks * kSelectChunkUnit - 1) / (chunks * kSelectChunkUnit), 1) * kSelectChunkUnit, 1 << 24);
         for (const Group& g : groups)
             for (int64_t j = 0; j < g.pages; j += chunk_pages)
                 select_chunks.push_back(SelectChunk{g.row0, g.rows, (int32_t)j, batch->kv_len_before[g.seq] + (g.row0 - q_indptr[g.seq]), page_indptr[g.seq], {0, 0, 0}});

@@ -224,9 +224,13 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     if (tid < queries) atomicMax(p.select_error + (size_t)(c.row0 + tid / G) * p.num_kv_heads + h, s_error[tid]);
 }
 
-__device__ __forceinline__ double held_value(__nv_bfloat16 x) {      // (as held() has it)
-    const float f = __bfloat162float(x);
-    return (double)(f != f ? -0x1p56f : fminf(fmaxf(f, -0x1p56f), 0x1p56f));
+// A bf16 number as held() has it, exactly (fp32 instructions would flush subnormal ones): the exponent field goes into an fp64 number's, whose bias is
+// 896 more.
+__device__ __forceinline__ double held_value(__nv_bfloat16 x) {
+    const uint32_t bits = __bfloat16_as_ushort(x);
+    if ((bits & 0x7fffu) > 0x7f80u) return -0x1p56;
+    const int32_t word = ((int32_t)(bits << 16) >> 3) & (int32_t)0x8fffe000;
+    return fmin(fmax(__hiloint2double(word, 0) * 0x1p896, -0x1p56), 0x1p56);
 }
 
 // The sum of one query in shared memory and a page's bounds in 64 bits, by a warp.
@@ -299,7 +303,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         const int j = stretch0 + 32 * i + lane;
         mine[i] = resident && i < steps && j < np ? __ldcg(keys + j) : 0;      // (0 is below any score's)
     }
-    const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-100f;
+    const float error = __uint_as_float(__ldcg(p.select_error + blockIdx.x)) * 0x1p-14f + 0x1p-60f;      // (products with subnormal numbers may be lost)
     const int D = p.head_dim, G = p.group;
     for (int i = tid; i < G * D / 8; i += THREADS)
         reinterpret_cast<uint4*>(s_q)[i] = reinterpret_cast<const uint4*>(q + ((size_t)row * p.num_q_heads + (size_t)h * G) * D)[i];

@@ -141,6 +141,39 @@ def test_ties_and_odd_scores():
     assert all(sorted(set(h)) == h and 0 <= h[0] and h[-1] == n[r] - 1 for r, row in enumerate(got) for h in row)
 
 
+def test_tiny_and_huge_values():
+    """Bounds and queries at the ends of their range: scores whose 32 bits say nothing are decided in 64; beyond 2^56 all count as 2^56."""
+    c = Cache((8, 2, 128), [4000, 9000], [1, 2])
+    plan = B.asynclm_plan_sparse(*c.args, 30, 1, 2)
+    pages = torch.zeros((3, 2, 30), dtype=torch.int32, device="cuda")
+    plain, q = c.bounds().nan_to_num(0.0), c.q.clone()
+    for scale_b, scale_q in ((2.0 ** -126, 1.0), (2.0 ** -126, 2.0 ** 50), (2.0 ** 50, 2.0 ** 50), (2.0 ** -70, 2.0 ** -60), (1.0, 0.0)):
+        bounds = (plain * scale_b).bfloat16()
+        c.q.copy_(q.float() * scale_q)
+        B.asynclm_select_pages(plan, c.q, bounds, pages)
+        assert pages.cpu().tolist() == chosen_pages(c, bounds, 30, 1, 2), (scale_b, scale_q)
+    c.q.copy_(q)
+    bounds = plain.bfloat16()
+    bounds[c.ids[c.indptr[1] + 300], :, 0], bounds[c.ids[c.indptr[1] + 300], :, 1] = -3e38, 3e38
+    bounds[c.ids[c.indptr[1] + 301]] = bounds[c.ids[c.indptr[1] + 300]]
+    B.asynclm_select_pages(plan, c.q, bounds, pages)
+    assert pages.cpu().tolist() == chosen_pages(c, bounds.double().clamp(-2.0 ** 56, 2.0 ** 56), 30, 1, 2)
+
+
+def test_many_equal_scores():
+    """Far more pages at the threshold than a CTA ranks at once, in 32 bits and in 64, also where a row's keys are not held in registers."""
+    c = Cache((4, 1, 64), [80000, 30000], [1, 1])
+    plan = B.asynclm_plan_sparse(*c.args, 900, 3, 4)
+    pages = torch.zeros((2, 1, 900), dtype=torch.int32, device="cuda")
+    bounds = torch.zeros((c.num_pages, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for kinds in (1, 2, 5):
+        kind = torch.randint(0, kinds, (c.num_pages,), generator=g, device="cuda")
+        bounds[:] = (1.0 + kind.float() * 2.0 ** -7).bfloat16()[:, None, None, None]      # neighbours in bf16
+        B.asynclm_select_pages(plan, c.q, bounds, pages)
+        assert pages.cpu().tolist() == chosen_pages(c, bounds, 900, 3, 4), kinds
+
+
 def test_long_sequence():
     """More pages than the selection holds in shared memory, more keys than one list."""
     c = Cache((4, 1, 64), [90000, 66000], [2, 1])
