@@ -8,8 +8,8 @@
 // values alone.  So it is made in two steps: scores from the tensor cores with a bound of their error, e = 2^-14 sum_c |q_c| max(|lo_c|, |hi_c|), the
 // largest of the row; then, as the budget's last score t in 32 bits lies within e of the one in full, pages above t + 2e are in, pages below
 // t - 2e are out, and the few in between (one to five, where scores are not equal) are scored again in 64 bits, where a product of bf16 values is exact.
-//   (e: a score is 2 D / 16 instructions one after the other, each of which adds 16 exact products to the sum; with truncation to 2^-23 of the largest
-// for each of the 17 terms that is 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128.)
+//   (e: either product is D / 16 instructions one after the other, each of which adds 16 exact products to the sum; with truncation to 2^-23 of the largest
+// for each of the 17 terms that is, over both, 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128, and 2^-24 where they are added.)
 //   In 64 bits for all pages the score kernel took 106 us for 48 sequences of 3-12 K tokens with 1-4 new ones each (451 K sums over 4 heads of 128):
 // for every product a bit operation, an fma and a move, 112 instructions a sum.
 //
@@ -96,6 +96,19 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
     constexpr int kStep = kScoreWarps * kTilePages;
     int j0 = c.page0 + warp * kTilePages, ids = id_of(j0), ids_next = id_of(j0 + kStep);
+    // where this thread's scores go: of queries 2 t and, for one head to a row, 2 t + 1 of each eight
+    constexpr int kMine = G == 1 ? 2 : 1;
+    unsigned* keys[kGroups][kMine];
+    int np[kGroups][kMine];      // pages that the row sees; 0: no such row, or another thread has it
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) {
+            const int query = k * kColumns + 2 * t + e, r = query / G;
+            const bool on = query % G == 0 && r < c.rows;
+            np[k][e] = on ? (pos0 + r) / kPage + 1 : 0;
+            keys[k][e] = on ? p.select_keys + __ldg(p.select_base + c.row0 + r) * p.num_kv_heads + (size_t)h * np[k][e] : nullptr;
+        }
     if (tid < kSelectQueries) s_error[tid] = 0;
     uint8_t* slots = s_slots + (size_t)warp * 2 * Slots::kBytes;
     auto request = [&](int slot, int my_id) {
@@ -144,11 +157,11 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
         __syncwarp();      // all lanes' copies are there
         const uint8_t* tile = slots + slot * Slots::kBytes;
         const bool more = queries > kColumns;
-        float s_all[kGroups][4], a_all[kGroups][4];      // scores, sums of magnitudes
+        float s_all[kGroups][4], d_all[kGroups][4], a_all[kGroups][4];      // scores in two parts, sums of magnitudes
 #pragma unroll
         for (int k = 0; k < kGroups; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s_all[k][e] = a_all[k][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s_all[k][e] = d_all[k][e] = a_all[k][e] = 0.f;
 #pragma unroll 1
         for (int j = 0; j < J; ++j) {      // (not unrolled: a launch's code is cold, and a CTA has one to four tiles a warp)
             uint32_t l[2][4], u[2][4], m[2][4];
@@ -168,11 +181,11 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
             for (int k = 0; k < kGroups; ++k) {
                 if (k > 0 && !more) break;
                 const uint4 up = s_q[k][j][0][lane], down = s_q[k][j][1][lane];
-                float(&s)[4] = s_all[k], (&a)[4] = a_all[k];
+                float(&s)[4] = s_all[k], (&d)[4] = d_all[k], (&a)[4] = a_all[k];
                 mma16(s, u[0][0], u[1][0], u[0][1], u[1][1], up.x, up.y);
                 mma16(s, u[0][2], u[1][2], u[0][3], u[1][3], up.z, up.w);
-                mma16(s, l[0][0], l[1][0], l[0][1], l[1][1], down.x, down.y);
-                mma16(s, l[0][2], l[1][2], l[0][3], l[1][3], down.z, down.w);
+                mma16(d, l[0][0], l[1][0], l[0][1], l[1][1], down.x, down.y);
+                mma16(d, l[0][2], l[1][2], l[0][3], l[1][3], down.z, down.w);
                 mma16(a, m[0][0], m[1][0], m[0][1], m[1][1], (up.x | down.x) & kAbs, (up.y | down.y) & kAbs);
                 mma16(a, m[0][2], m[1][2], m[0][3], m[1][3], (up.z | down.z) & kAbs, (up.w | down.w) & kAbs);
             }
@@ -182,6 +195,8 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
             if (k > 0 && !more) break;
             float(&s)[4] = s_all[k];
             const float(&a)[4] = a_all[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += d_all[k][e];
             // this thread: pages g (0, 1) and g + 8 (2, 3), queries 2 t and 2 t + 1 of the eight
             error[k][0] = fmaxf(error[k][0], fmaxf(a[0], a[2]));
             error[k][1] = fmaxf(error[k][1], fmaxf(a[1], a[3]));
@@ -196,17 +211,12 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
                 }
             }
 #pragma unroll
-            for (int e = 0; e < (G == 1 ? 2 : 1); ++e) {
-                const int query = k * kColumns + 2 * t + e, r = query / G;
-                if (query % G != 0 || r >= c.rows) continue;
-                const int row = c.row0 + r, np = (pos0 + r) / kPage + 1;
-                unsigned* keys = p.select_keys + p.select_base[row] * p.num_kv_heads + (size_t)h * np;
+            for (int e = 0; e < kMine; ++e)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const int j = j0 + g + 8 * half;
-                    if (j < min(end, np)) keys[j] = j < p.select_first || j >= np - p.select_last ? kAlways : ordered(s[2 * half + e]);
+                    if (j < min(end, np[k][e])) keys[k][e][j] = j < p.select_first || j >= np[k][e] - p.select_last ? kAlways : ordered(s[2 * half + e]);
                 }
-            }
         }
         __syncwarp();      // (the slot is free)
     }
