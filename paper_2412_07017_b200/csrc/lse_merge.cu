@@ -103,7 +103,8 @@ lse_merge_kernel(DevPlan p, __nv_bfloat16* __restrict__ out, float* __restrict__
     merge_row<D>(p, u.n_chunks, [&](int c) { return prow0 + (size_t)c * u.ntok; }, (size_t)u.q_row0 + t, u.kv_head, g, out, lse);
 }
 
-// Rows of sequences with a shared prefix: the chunks of the unit with the sequence's own keys, then those of the unit with the shared ones.
+// Rows of sequences with a shared prefix: the chunks of the unit with the sequence's own keys, then those of the unit with the shared ones.  One record a block,
+// read ahead of the wait.  (2048 rows of five chunks, 5.3 MB: 3 us behind the attention, which leaves no registers for blocks beside its CTAs.)
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads)
 lse_join_kernel(DevPlan p, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {

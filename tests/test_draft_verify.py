@@ -89,6 +89,18 @@ def test_strides(vocab, stride, offset, dtype):
     Case([3, 1, 0, 5], vocab, dtype, True, 3, stride, offset=offset).check()
 
 
+def test_rows_beyond_32_bits():
+    """Rows that lie more than 2^31 values behind the first."""
+    c = Case([7, 8, 4], 5000, torch.bfloat16, seed=8)
+    for name in ("target", "draft"):
+        t = getattr(c, name)
+        base = torch.empty(t.shape[0] * (2 ** 27 + 3), dtype=t.dtype, device="cuda").view(t.shape[0], -1)[:, :5000]
+        base.copy_(t)
+        setattr(c, name, base)
+    assert 21 * (2 ** 27 + 3) > 2 ** 31
+    c.check()
+
+
 def test_random_numbers_at_the_ends():
     c = Case([2, 2, 2], 5000, seed=4)
     for x in (0.0, 1.0 - 2.0 ** -24):

@@ -227,6 +227,30 @@ def test_graph_of_layers(kv8):
             check((c.out, c.lse), c.exact(as_mask(c, lists)))
 
 
+def test_offsets_beyond_32_bits():
+    """Pages whose keys lie beyond 2^31 values and whose bounds lie beyond 2^31 bytes."""
+    small = Cache((8, 1, 128), [3000, 700], [1, 2], seed=11)
+    num_pages = 4_300_000
+    far = (np.arange(small.num_pages) * 13 % small.num_pages).astype(np.int64)
+    far[far % 2 == 0] += num_pages - small.num_pages      # half of them at the end, the others at the start
+    pool = torch.empty((num_pages, 2, 1, PAGE, 128), dtype=torch.bfloat16, device="cuda")
+    pool[torch.as_tensor(far).cuda()] = small.pool
+    bounds = torch.empty((num_pages, 1, 2, 128), dtype=torch.bfloat16, device="cuda")
+    assert bounds.numel() * 2 > 2 ** 31 and pool.numel() > 2 ** 31
+    args = (small.shape, num_pages, small.q_indptr, small.ctx, small.indptr, far[small.ids].astype(np.int32))
+    plan = B.asynclm_plan_sparse(*args, 20, 1, 2)
+    B.asynclm_kv_bounds(plan, pool, bounds, True)
+    want = small.bounds()
+    used = torch.as_tensor(np.unique(small.ids).astype(np.int64)).cuda()
+    assert torch.equal(bounds[torch.as_tensor(far).cuda()[used]].double(), want[used])
+    pages = torch.zeros((3, 1, 20), dtype=torch.int32, device="cuda")
+    B.asynclm_select_pages(plan, small.q, bounds, pages)
+    lists = chosen_pages(small, want.nan_to_num(0.0), 20, 1, 2)
+    assert pages.cpu().tolist() == lists
+    out, lse = small.attend(plan, call=lambda p, q, _, o, z: B.asynclm_attn_mixed(p, q, pool, o, z))
+    check((out, lse), small.exact(as_mask(small, lists)))
+
+
 def test_refusals():
     c = Cache((8, 4, 64), [100], [1])
     plan, ordinary = B.asynclm_plan_sparse(*c.args, 4, 1, 1), B.asynclm_plan(*c.args)
