@@ -67,12 +67,14 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Of a warp: two tiles of bounds in shared memory, one on its way while the other is in use, [page][least, largest][channel].  The 16-byte vectors of
-// odd pages change places with those four further, so that the eight lanes that a bank serves at once (two pages, four vectors) read different ones.
+// Of a warp: a tile of bounds in shared memory, [page][least, largest][channel], or two, one on its way while the other is in use, where that leaves room for
+// as many CTAs as the registers do: at head_dim 128 five CTAs with a tile a warp do better than three with two (us of bounds, selection and
+// attention 112.4 | 114.5 for 48 sequences, 36.8 | 37.7 for 4, at head_dim 64 43.2 | 42.5 for 150).  The 16-byte vectors of odd pages change places with
+// those four further, so that the eight lanes that a bank serves at once (two pages, four vectors) read different ones.
 template <int D>
 struct ScoreSlots {
-    static constexpr int kPageBytes = 4 * D, kBytes = kTilePages * kPageBytes;
-    static constexpr size_t kSmem = (size_t)kScoreWarps * 2 * kBytes;
+    static constexpr int kPageBytes = 4 * D, kBytes = kTilePages * kPageBytes, kSlots = D == 128 ? 1 : 2;
+    static constexpr size_t kSmem = (size_t)kScoreWarps * kSlots * kBytes;
     static __device__ __forceinline__ int offset(int page, int vec) { return page * kPageBytes + (vec ^ (page & 1) * 4) * 16; }
 };
 
@@ -111,7 +113,7 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
             keys[k][e] = on ? p.select_keys + __ldg(p.select_base + c.row0 + r) * p.num_kv_heads + (size_t)h * np[k][e] : nullptr;
         }
     if (tid < kSelectQueries) s_error[tid] = 0;
-    uint8_t* slots = s_slots + (size_t)warp * 2 * Slots::kBytes;
+    uint8_t* slots = s_slots + (size_t)warp * Slots::kSlots * Slots::kBytes;
     auto request = [&](int slot, int my_id) {
         constexpr int kVecs = Slots::kPageBytes / 16;      // of a page: all lanes, or half of them
 #pragma unroll
@@ -147,9 +149,11 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     float error[kGroups][2];
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) error[k][0] = error[k][1] = 0.f;
-    for (int slot = 0; j0 < end; j0 += kStep, slot ^= 1) {
-        if (j0 + kStep < end) {
-            request(slot ^ 1, ids_next);
+    for (int slot = 0; j0 < end; j0 += kStep) {
+        const bool last = j0 + kStep >= end;
+        const int next = Slots::kSlots == 2 ? slot ^ 1 : slot, ids_then = ids_next;
+        if (Slots::kSlots == 2 && !last) {
+            request(next, ids_then);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -220,6 +224,8 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
                 }
         }
         __syncwarp();      // (the slot is free)
+        if (Slots::kSlots == 1 && !last) request(next, ids_then);
+        slot = next;
     }
     // ---- how far the scores may be off: a row's largest (positive floats compare as integers)
 #pragma unroll
