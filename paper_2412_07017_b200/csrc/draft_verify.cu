@@ -8,7 +8,7 @@
 // held in 64 bits, where neither depends on the order of the additions but within 2^-45.  A value becomes an fp64 one by its bits, without the
 // exponents' difference in bias: all weights and sums are times 2^-896, which changes no comparison, and zeros and subnormal numbers are right as they
 // are.  (With conversions, of which an SM does 16 a cycle, 300 bf16 rows of 100 003 took 45.7 us and 64 pairs of fp32 rows of 128 256 26.4; now, in a graph
-// with inputs in cache, 19.3 and 16.1, out of cache 23.0 and 19.9, 2.6 and 3.1 TB/s; two sequences of four drafts from 32 001 tokens 7.5.)
+// with inputs in cache, 19.1 and 16.6, out of cache 20.1 and 18.8, 3.0 and 3.3 TB/s; two sequences of four drafts from 32 001 tokens 7.5.)
 //
 // One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself); a warp has pieces of 2 KB brought into shared memory, the
 // next one while it sums the last, and leaves each piece's sum in the workspace; the CTA that completes the row finds the piece by the sums, and brings
@@ -372,10 +372,12 @@ extern "C" int asynclm_draft_verify(const asynclm_draft_rows* rows, const int32_
     a.vocab = rows->vocab;
     const int piece = size == 4 ? kPiece<float> : kPiece<__nv_bfloat16>;
     a.pieces = (int)(((int64_t)rows->vocab + 16 / (int)size - 1 + piece - 1) / piece);      // wherever a row starts
-    // as many CTAs as run at once (by their shared memory), each with a piece or more for its warps
+    // Two fifths of the CTAs that fit (by their shared memory), each with a piece or more for its warps: every CTA has the chain in front of its stream, and the
+    // next kernel's find room beside them.  (us with inputs out of cache, all that fit | three fifths | two fifths | three tenths: 64 pairs of fp32 rows of 128 256
+    // 20.0 | 22.8 | 18.9 | 20.0, 300 bf16 rows of 100 003 22.8 | 23.8 | 20.2 | 20.7, 300 pairs of fp32 rows of 50 001 29.1 | 26.0 | 28.4 | 41.5.)
     const size_t smem = (size_t)kVerifyWarps * kSlots * (rows->draft ? kSlotBytesQ : kSlotBytes);
-    const int resident = 148 * (int)((size_t)(227 << 10) / (smem + 1536));
-    const int slices = std::max(1, std::min(resident / batch, (a.pieces + kVerifyWarps - 1) / kVerifyWarps));
+    const int fit = 148 * (int)((size_t)(227 << 10) / (smem + 1536));
+    const int slices = std::max(1, std::min(fit * 2 / 5 / batch, (a.pieces + kVerifyWarps - 1) / kVerifyWarps));
     auto kernel = size == 4 ? draft_verify_kernel<float> : draft_verify_kernel<__nv_bfloat16>;
     return cuda_status(launch_pdl(kernel, dim3(slices, batch), dim3(kVerifyThreads), smem, (cudaStream_t)stream, a));
 }
