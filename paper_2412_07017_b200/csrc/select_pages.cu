@@ -11,7 +11,7 @@
 //   (e: either product is D / 16 instructions one after the other, each of which adds 16 exact products to the sum; with truncation to 2^-23 of the largest
 // for each of the 17 terms that is, over both, 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128, and 2^-24 where they are added.)
 //   In 64 bits for all pages the score kernel took 106 us for 48 sequences of 3-12 K tokens with 1-4 new ones each (451 K sums over 4 heads of 128):
-// for every product a bit operation, an fma and a move, 112 instructions a sum; now it takes 24 us of 92 MB of bounds, and the choice 14.  (4 sequences of
+// for every product a bit operation, an fma and a move, 112 instructions a sum; now it takes 22 us of 92 MB of bounds, and the choice 14.  (4 sequences of
 // 16-60 K tokens: 13 us of 39 MB, and 7.)
 //
 // select_score_kernel: a warp takes 16 pages, the M of its MMAs, a CTA a stretch of a sequence's pages for one kv head and all of the sequence's rows
