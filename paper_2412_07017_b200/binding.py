@@ -334,6 +334,8 @@ def _planner(shape, num_pages, q_indptr, kv_len_before, page_indptr, page_indice
     cs, co = _cshape(shape, num_pages, sm_scale), _copts(**opts)
     cb, keep = _cbatch(q_indptr, kv_len_before, page_indptr, page_indices)
     front = (ctypes.byref(cs), ctypes.byref(co), ctypes.byref(cb))
+    if groups is not None and sparse is not None:
+        raise ValueError("groups and sparse: a plan shares prefixes or selects pages")
     if groups is not None:
         rows = [tuple(int(x) for x in g) for g in groups]
         if any(len(g) != 3 for g in rows):

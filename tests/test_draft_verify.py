@@ -75,7 +75,7 @@ class Case:
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("with_draft", [True, False])
 @pytest.mark.parametrize("drafts,vocab", [([1], 1), ([0], 5), ([4, 0, 2], 511), ([1, 2, 3], 512), ([5] * 3, 513), ([3, 0, 8, 1], 32001), ([40, 0, 33], 700), ([2] * 7, 128256),
-                                          ([1] * 700, 1030), ([0] * 5, 4096)])
+                                          ([1] * 700, 1030), ([0] * 5, 4096), ([1, 0, 2], 600001)])
 def test_exact(drafts, vocab, with_draft, dtype):
     for seed in range(3):
         c = Case(drafts, vocab, dtype, with_draft, seed, apart=(0.05, 0.7, 2.0)[seed])

@@ -88,6 +88,8 @@ def test_groups_and_pages_of_the_binding():
     for groups in ([(0, 3)], [(0, 1, 2, 3)]):
         with pytest.raises(ValueError, match="groups"):
             B.plan_host(SHAPE, PAGES, *BATCH, groups=groups)
+    with pytest.raises(ValueError, match="groups and sparse"):
+        B.plan_host(SHAPE, PAGES, *BATCH, groups=[], sparse=(3, 1, 1))
     lib, out, ws = B.load(), ctypes.c_void_p(), np.zeros(1 << 14, np.int64)
     cs, co = B._cshape(SHAPE, PAGES), B._copts(num_sms=148)
     cb, _keep = B._cbatch(*BATCH)
