@@ -619,8 +619,10 @@ __device__ __forceinline__ void leave_queue(const DevPlan& p) {
     atomicExch(p.counters + 1, 0);
 }
 
-// For a CTA that comes from span tiles, instead of the barrier in front of the warp body: whether the queue has anything left; where it has not, the CTA has left
-// it.  (The warp body takes 3 to 4 us to find that out.  64 sequences behind 4096 shared keys 49.4 -> 46.4 us.)
+// For a CTA that comes from span tiles of a batch that shares a prefix, instead of the barrier in front of the warp body: whether the queue has anything
+// left; where it has not, the CTA has left it.  (The warp body takes 3 to 4 us to find that out, and there most of the CTAs come from span tiles that end
+// with the queue: 64 sequences behind 4096 shared keys 49.4 -> 46.4 us.  In other batches the question costs what it saves: 62.0 | 62.3, 50.6 | 49.3, 8-bit cache
+// 75.0 | 76.0.)
 __device__ __forceinline__ bool queue_has_items(const DevPlan& p) {
     int taken = 0;
     if (threadIdx.x == 0) {
@@ -628,7 +630,7 @@ __device__ __forceinline__ bool queue_has_items(const DevPlan& p) {
         asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(taken) : "l"(p.counters) : "memory");
     }
     if (__syncthreads_or(threadIdx.x == 0 && taken < p.queue_count)) return true;
-    if (threadIdx.x == 0 && p.queue_count > 0) leave_queue(p);
+    if (threadIdx.x == 0) leave_queue(p);
     return false;
 }
 

@@ -67,9 +67,10 @@ attn_fused_kernel(DevPlan p, const __grid_constant__ CUtensorMap kv_map, const _
     }
     tc::tc_body<D, G, false>(p, &span_map, q, pool, out, lse, smem);
     if (threadIdx.x == 0) trace_mark(1);
+    if (head[2] == head[3] && p.queue_count == 0) return;      // nothing left for the warp body
     // (the barrier: tensor memory released, shared memory free for the second phase)
-    if (head[2] == head[3]) {
-        if (!dec::queue_has_items(p)) return;      // nothing left for the warp body
+    if (head[2] == head[3] && p.num_join_blocks > 0) {
+        if (!dec::queue_has_items(p)) return;
     } else {
         __syncthreads();
     }

@@ -65,8 +65,9 @@ __device__ __forceinline__ void fused_kv8(const DevPlan& p, const CUtensorMap* k
         }
         tc::tc_body<D, G, false, true, ROLE>(p, k_map, q, nullptr, out, lse, smem, pool, scales);
         if (threadIdx.x == 0) trace_mark(1);
+        if (head[2] == head[3] && p.queue_count == 0) return;      // nothing left for the warp body
         // (as in attn_fused_kernel)
-        if (head[2] == head[3]) {
+        if (head[2] == head[3] && p.num_join_blocks > 0) {
             if (!dec::queue_has_items(p)) return;
         } else {
             __syncthreads();
