@@ -104,11 +104,12 @@ __device__ __forceinline__ void clean_piece(const Weights<T>& w, T* slot, int pi
 __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
 
-// max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  NaN counts as zero, and so does a negative q.
+// max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  Where p or q is NaN, of either sign, there is no weight; a negative q counts as zero.
 __device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
 template <bool WITH_Q>
 __device__ __forceinline__ double weight(uint32_t p, uint32_t q) {
     if (!WITH_Q) return __uint_as_float(p) > 0.f ? scaled(p) : 0.0;
+    if (q > 0xff800000u) return 0.0;      // (a NaN with its sign set; the other sign fails the comparison)
     const uint32_t from = (uint32_t)max((int)q, 0);
     return __uint_as_float(p) > __uint_as_float(from) ? scaled(p) - scaled(from) : 0.0;
 }
