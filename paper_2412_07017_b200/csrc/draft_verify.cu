@@ -104,6 +104,9 @@ __device__ __forceinline__ void clean_piece(const Weights<T>& w, T* slot, int pi
 __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
 
+// The number for the test of acceptance: a negative one counts as zero, NaN of either sign stays.
+__device__ __forceinline__ double probability(uint32_t bits) { return (int)bits < 0 && bits <= 0xff800000u ? 0.0 : (double)__uint_as_float(bits); }
+
 // max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  Where p or q is NaN, of either sign, there is no weight; a negative q counts as zero.
 __device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
 template <bool WITH_Q>
@@ -274,8 +277,8 @@ draft_verify_kernel(VerifyArgs a) {
             x = __ldg(a.tokens + i0 + k);
             bad = true;      // (a token outside the vocabulary has no probability)
             if (x >= 0 && x < a.vocab) {
-                const double pv = (double)(float)target[(int64_t)k * a.target_stride + x];
-                const double qv = draft == nullptr ? 1.0 : (double)(float)draft[(int64_t)k * a.draft_stride + x];
+                const double pv = probability(bits_of(target[(int64_t)k * a.target_stride + x]));
+                const double qv = draft == nullptr ? 1.0 : probability(bits_of(draft[(int64_t)k * a.draft_stride + x]));
                 bad = !((double)__ldg(a.accept_u + i0 + k) * qv < pv);
             }
         }

@@ -71,3 +71,32 @@ def test_nan_in_the_draft_weighs_nothing(vocab, stride, offset, dtype, bits):
         set_numbers(c, k)
         check(c)
         assert c.accepted.sum() == 0 and (c.out[0::2] % 3 != 1).all()
+
+
+# p, q, u of a draft and whether it is accepted: u * q < p, negative probabilities being none
+ACCEPTED = [(0.0, -0.25, 0.5, False), (-0.125, -0.5, 0.5, False), (-0.125, 0.25, 0.0, False), (0.0, 0.25, 0.0, False), (0.25, -0.5, 0.9, True), (0.25, -0.0, 0.9, True),
+            (-0.0, -0.5, 0.25, False), (0.25, float("nan"), 0.0, False), (float("nan"), 0.25, 0.0, False), (0.25, -float("inf"), 0.5, True), (-float("inf"), 0.25, 0.5, False)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab,stride,offset", PLACES)
+def test_negative_numbers_accept_nothing(vocab, stride, offset, dtype):
+    n = len(ACCEPTED)
+    c = Case([1] * n, vocab, dtype, True, 2, stride, offset=offset)
+    for b, (p, q, u, _) in enumerate(ACCEPTED):
+        c.target[2 * b, c.tokens[b].long()], c.draft[b, c.tokens[b].long()], c.u[b] = p, q, u
+    check(c)
+    assert c.accepted.tolist() == [int(x[3]) for x in ACCEPTED]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab,stride,offset", PLACES)
+def test_negative_numbers_weigh_nothing(vocab, stride, offset, dtype):
+    """Negative numbers among p and q: no weight, and nothing that a weight is lessened by."""
+    c = Case([1] * 9, vocab, dtype, True, 4, stride, offset=offset)
+    c.target[:, ::3] *= -1
+    c.draft[:, ::5] *= -1
+    c.draft[:, 3:20:4] = -0.0
+    for k in range(3):
+        set_numbers(c, k)
+        check(c)
