@@ -104,17 +104,31 @@ __device__ __forceinline__ void clean_piece(const Weights<T>& w, T* slot, int pi
 __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
 
+// (The compiler's comparisons and conversions of fp32 numbers flush subnormal ones, and a sum that has what a comparison does not see would send the search
+// to a place without a weight.  So all of it goes by the bits, or compares without flushing.)
+//
+// A positive number times 2^-896.
+__device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
+__device__ __forceinline__ bool positive(uint32_t bits) { return bits - 1 < 0x7f800000u; }      // and no NaN
+__device__ __forceinline__ bool greater(uint32_t a, uint32_t b) {
+    int r;
+    asm("{\n\t.reg .pred t;\n\tsetp.gt.f32 t, %1, %2;\n\tselp.s32 %0, 1, 0, t;\n\t}" : "=r"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+    return r != 0;
+}
 // The number for the test of acceptance: a negative one counts as zero, NaN of either sign stays.
-__device__ __forceinline__ double probability(uint32_t bits) { return (int)bits < 0 && bits <= 0xff800000u ? 0.0 : (double)__uint_as_float(bits); }
+__device__ __forceinline__ double probability(uint32_t bits) {
+    if ((int)bits < 0 && bits <= 0xff800000u) return 0.0;
+    return bits & 0x7f800000u ? (double)__uint_as_float(bits) : scaled(bits) * 0x1p896;
+}
 
 // max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  Where p or q is NaN, of either sign, there is no weight; a negative q counts as zero.
-__device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
 template <bool WITH_Q>
 __device__ __forceinline__ double weight(uint32_t p, uint32_t q) {
-    if (!WITH_Q) return __uint_as_float(p) > 0.f ? scaled(p) : 0.0;
+    if (!positive(p)) return 0.0;
+    if (!WITH_Q) return scaled(p);
     if (q > 0xff800000u) return 0.0;      // (a NaN with its sign set; the other sign fails the comparison)
     const uint32_t from = (uint32_t)max((int)q, 0);
-    return __uint_as_float(p) > __uint_as_float(from) ? scaled(p) - scaled(from) : 0.0;
+    return p > from ? scaled(p) - scaled(from) : 0.0;
 }
 // The weight of value j of a piece in its slot.
 template <typename T>
@@ -165,7 +179,7 @@ __device__ __forceinline__ double sum_by_vectors(const T* slot, int lane, bool& 
             for (int e = 0; e < N / 4; ++e) {
                 const uint32_t a = sizeof(T) == 4 ? x[i] : e ? x[i] & 0xffff0000u : x[i] << 16, b = sizeof(T) == 4 ? y[i] : e ? y[i] & 0xffff0000u : y[i] << 16;
                 if constexpr (!WITH_Q) sum[i & 1] += scaled(a);
-                else if (__uint_as_float(a) > __uint_as_float(b)) sum[i & 1] += scaled(a) - scaled(b);
+                else if (greater(a, b)) sum[i & 1] += scaled(a) - scaled(b);
             }
         }
     }
@@ -206,14 +220,14 @@ __device__ __forceinline__ void sum_pieces(const Weights<T>& w, T* slots, int sl
 
 // The least token whose inclusive sum of weights exceeds u * (sum of all); -1 if no weight is positive.  By one warp; sum_of(i): a piece's sum.
 template <typename T, typename SumOf>
-__device__ __forceinline__ int search(const Weights<T>& w, T* slot, SumOf sum_of, int pieces, float u, int lane) {
+__device__ __forceinline__ int search(const Weights<T>& w, T* slot, SumOf sum_of, int pieces, double u, int lane) {
     // a stretch of pieces to a lane, then the pieces of the stretch
     const int per = (pieces + 31) / 32, c0 = min(lane * per, pieces), c1 = min(c0 + per, pieces);
     double mine = 0.0;
     for (int c = c0; c < c1; ++c) mine += sum_of(c);
     const double upto = warp_scan(mine, lane), total = __shfl_sync(0xffffffffu, upto, 31);
     if (!(total > 0.0)) return -1;
-    const double threshold = (double)u * total;
+    const double threshold = u * total;
     // (Rounding may leave nothing beyond the threshold, and a u of one or more does: then the last with a weight.)
     const unsigned beyond = __ballot_sync(0xffffffffu, mine > 0.0 && upto > threshold), some = __ballot_sync(0xffffffffu, mine > 0.0);
     const int at = beyond ? __ffs(beyond) - 1 : 31 - __clz(some), at0 = at * per, at1 = min(at0 + per, pieces);
@@ -279,7 +293,7 @@ draft_verify_kernel(VerifyArgs a) {
             if (x >= 0 && x < a.vocab) {
                 const double pv = probability(bits_of(target[(int64_t)k * a.target_stride + x]));
                 const double qv = draft == nullptr ? 1.0 : probability(bits_of(draft[(int64_t)k * a.draft_stride + x]));
-                bad = !((double)__ldg(a.accept_u + i0 + k) * qv < pv);
+                bad = !(probability(bits_of(__ldg(a.accept_u + i0 + k))) * qv < pv);
             }
         }
         const unsigned ballot = __ballot_sync(0xffffffffu, bad);
@@ -318,7 +332,7 @@ draft_verify_kernel(VerifyArgs a) {
             __syncthreads();
         }
         if (warp == 0) {
-            token = search(w, slots, [&](int i) { return shared ? s_sums[i] : __ldcg(sums + i); }, a.pieces, __ldg(a.sample_u + b), lane);
+            token = search(w, slots, [&](int i) { return shared ? s_sums[i] : __ldcg(sums + i); }, a.pieces, probability(bits_of(__ldg(a.sample_u + b))), lane);
             if (lane == 0) s_again = token < 0 && rejected && attempt == 0;
         }
         __syncthreads();

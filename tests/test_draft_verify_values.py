@@ -100,3 +100,44 @@ def test_negative_numbers_weigh_nothing(vocab, stride, offset, dtype):
     for k in range(3):
         set_numbers(c, k)
         check(c)
+
+
+def subnormal(shape, dtype, seed):
+    """Random subnormal numbers, a quarter of them zero."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    most = 2 ** 23 if dtype == torch.float32 else 2 ** 7
+    x = torch.randint(1, most, shape, generator=g, device="cuda") * (torch.rand(shape, generator=g, device="cuda") > 0.25)
+    return x.to(torch.int32).view(torch.float32) if dtype == torch.float32 else x.to(torch.int16).view(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab,stride,offset", PLACES)
+def test_subnormal_weights(vocab, stride, offset, dtype):
+    """Rows that begin with subnormal numbers, or have no others; with a draft and behind the last one."""
+    c = Case([0, 1] * 6, vocab, dtype, True, 6, stride, offset=offset)
+    c.u.fill_(0.999)
+    front = vocab // 2
+    c.target[:, :front] = subnormal((c.total + c.n, front), dtype, 1)
+    c.target[6:] = subnormal((c.total + c.n - 6, vocab), dtype, 2)      # the later sequences have no others
+    c.draft[:, :front] = subnormal((c.total, front), dtype, 3)
+    c.draft[4:] = subnormal((c.total - 4, vocab), dtype, 4)
+    c.draft[2] = c.target[7]
+    c.draft[2, 5] = c.target[7, 5] = 0
+    x = c.tokens.long()
+    c.target[torch.arange(1, 18, 3, device="cuda"), x] = 0      # rejected
+    for v in (0.0, 2.0 ** -149, 2.0 ** -24, 0.25, 0.6171875, 1.0 - 2.0 ** -24):
+        c.v.fill_(v)
+        check(c)
+    assert c.accepted.sum() == 0 and (c.out[torch.arange(0, 18, 3, device="cuda")] >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_subnormal_numbers_in_the_test_of_acceptance(dtype):
+    small, tiny = (2.0 ** -140, 2.0 ** -149) if dtype == torch.float32 else (2.0 ** -130, 2.0 ** -133)
+    rows = [(small, small, 0.5, 1), (small, small, 1.0 - 2.0 ** -24, 1), (small, small * 2, 0.5, 0), (tiny, 0.0, 0.5, 1), (0.0, tiny, 0.0, 0), (tiny, tiny, 0.25, 1),
+            (small, 1.0, 2.0 ** -149, 1), (tiny, 1.0, 2.0 ** -133, 0), (2.0 ** -126, small, 0.5, 1), (small, 2.0 ** -126, 0.5, 0)]
+    c = Case([1] * len(rows), 600, dtype, True, 7)
+    for b, (p, q, u, _) in enumerate(rows):
+        c.target[2 * b, c.tokens[b].long()], c.draft[b, c.tokens[b].long()], c.u[b] = p, q, u
+    check(c)
+    assert c.accepted.tolist() == [x[3] for x in rows]
