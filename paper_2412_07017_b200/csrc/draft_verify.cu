@@ -105,16 +105,10 @@ __device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x)
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 x) { return (uint32_t)__bfloat16_as_ushort(x) << 16; }
 
 // (The compiler's comparisons and conversions of fp32 numbers flush subnormal ones, and a sum that has what a comparison does not see would send the search
-// to a place without a weight.  So all of it goes by the bits, or compares without flushing.)
+// to a place without a weight.  So all of it goes by the bits.)
 //
 // A positive number times 2^-896.
 __device__ __forceinline__ double scaled(uint32_t bits) { return __hiloint2double((int)(bits >> 3), (int)(bits << 29)); }
-__device__ __forceinline__ bool positive(uint32_t bits) { return bits - 1 < 0x7f800000u; }      // and no NaN
-__device__ __forceinline__ bool greater(uint32_t a, uint32_t b) {
-    int r;
-    asm("{\n\t.reg .pred t;\n\tsetp.gt.f32 t, %1, %2;\n\tselp.s32 %0, 1, 0, t;\n\t}" : "=r"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
-    return r != 0;
-}
 // The number for the test of acceptance: a negative one counts as zero, NaN of either sign stays.
 __device__ __forceinline__ double probability(uint32_t bits) {
     if ((int)bits < 0 && bits <= 0xff800000u) return 0.0;
@@ -124,11 +118,10 @@ __device__ __forceinline__ double probability(uint32_t bits) {
 // max(p - q, 0) times 2^-896, of fp32 numbers given by their bits.  Where p or q is NaN, of either sign, there is no weight; a negative q counts as zero.
 template <bool WITH_Q>
 __device__ __forceinline__ double weight(uint32_t p, uint32_t q) {
-    if (!positive(p)) return 0.0;
-    if (!WITH_Q) return scaled(p);
-    if (q > 0xff800000u) return 0.0;      // (a NaN with its sign set; the other sign fails the comparison)
-    const uint32_t from = (uint32_t)max((int)q, 0);
-    return p > from ? scaled(p) - scaled(from) : 0.0;
+    if constexpr (!WITH_Q) return p - 1 < 0x7f800000u ? scaled(p) : 0.0;
+    const uint32_t from = q - 0x80000000u <= 0x7f800000u ? 0u : q;      // (what is left with a sign is NaN, and greater than any p)
+    const double left = scaled(p) - scaled(from);
+    return p > from && p <= 0x7f800000u ? left : 0.0;
 }
 // The weight of value j of a piece in its slot.
 template <typename T>
@@ -152,15 +145,31 @@ __device__ __forceinline__ double warp_scan(double x, int lane) {
     return x;
 }
 
-// The sum of a piece in its slot, lane by lane: value by value, whatever the numbers and q's place.
+// The sum of a piece in its slot, lane by lane: value by value, whatever the numbers and q's place.  (Hardly ever met: kept short.)
 template <typename T, bool WITH_Q>
-__device__ __forceinline__ double sum_by_values(const T* slot, int apart, int lane) {
+__device__ __forceinline__ double sum_of_any(const T* slot, int apart, int lane) {
     double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 1
     for (int j = lane; j < kPiece<T>; j += 32) sum += weight<WITH_Q>(bits_of(slot[j]), WITH_Q ? bits_of(slot[kPiece<T> + apart + j]) : 0u);
     return sum;
 }
-// The same by vectors, where q's lie as p's do; `odd` is set where a number is no probability, and the sum is none then.
+// The same of probabilities; `odd` is set where a number is none, and the sum is none then.  (Bits compare as the numbers do where no sign is set and p is no NaN.  A
+// NaN among p that is greater than q adds 2^104 or more, the step of the numbers in front of infinity.)
+constexpr double kOddSum = 0x1p-792;      // 2^104 times 2^-896
+template <typename T>
+__device__ __forceinline__ double sum_by_values(const T* slot, int apart, int lane, bool& odd) {
+    double sum = 0.0;
+    uint32_t signs = 0;
+#pragma unroll 4
+    for (int j = lane; j < kPiece<T>; j += 32) {
+        const uint32_t a = bits_of(slot[j]), b = bits_of(slot[kPiece<T> + apart + j]);
+        signs |= a | b;
+        if (a > b) sum += scaled(a) - scaled(b);
+    }
+    odd = signs >> 31 || sum >= kOddSum;
+    return sum;
+}
+// The same by vectors, where q's lie as p's do, or without q.
 template <typename T, bool WITH_Q>
 __device__ __forceinline__ double sum_by_vectors(const T* slot, int lane, bool& odd) {
     constexpr int N = 16 / sizeof(T);
@@ -174,27 +183,28 @@ __device__ __forceinline__ double sum_by_vectors(const T* slot, int lane, bool& 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (!WITH_Q) most = sizeof(T) == 4 ? max(most, x[i]) : __vmaxu2(most, x[i]);
-            signs |= y[i];
+            else signs |= x[i] | y[i];
 #pragma unroll
             for (int e = 0; e < N / 4; ++e) {
                 const uint32_t a = sizeof(T) == 4 ? x[i] : e ? x[i] & 0xffff0000u : x[i] << 16, b = sizeof(T) == 4 ? y[i] : e ? y[i] & 0xffff0000u : y[i] << 16;
                 if constexpr (!WITH_Q) sum[i & 1] += scaled(a);
-                else if (greater(a, b)) sum[i & 1] += scaled(a) - scaled(b);
+                else if (a > b) sum[i & 1] += scaled(a) - scaled(b);
             }
         }
     }
-    if constexpr (sizeof(T) == 4) odd = most > 0x7f800000u || signs >> 31;
-    else odd = most >> 16 > 0x7f80u || (most & 0xffffu) > 0x7f80u || (signs & 0x80008000u);
-    return sum[0] + sum[1];
+    const double all = sum[0] + sum[1];
+    if constexpr (WITH_Q) odd = (signs & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)) != 0 || all >= kOddSum;
+    else if constexpr (sizeof(T) == 4) odd = most > 0x7f800000u;
+    else odd = most >> 16 > 0x7f80u || (most & 0xffffu) > 0x7f80u;
+    return all;
 }
 template <typename T, bool WITH_Q>
 __device__ __forceinline__ double sum_of_piece(const T* slot, int apart, int lane) {
-    if (!WITH_Q || apart == 0) {
-        bool odd;
-        const double sum = sum_by_vectors<T, WITH_Q>(slot, lane, odd);
-        if (!__any_sync(0xffffffffu, odd)) return sum;
-    }
-    return sum_by_values<T, WITH_Q>(slot, apart, lane);
+    bool odd;
+    double sum;
+    if (!WITH_Q || apart == 0) sum = sum_by_vectors<T, WITH_Q>(slot, lane, odd);
+    else sum = sum_by_values(slot, apart, lane, odd);
+    return __any_sync(0xffffffffu, odd) ? sum_of_any<T, WITH_Q>(slot, apart, lane) : sum;
 }
 
 // The sums of pieces first, first + step, ... below `end` by this warp, in its two slots.
