@@ -17,16 +17,17 @@
 // the 16-byte vectors that memory has them in, and shared memory is read value by value.  (Out of registers, by vectors, with the checks that the ends of
 // a row need, the loop outgrew the instruction cache or the registers: 300 bf16 rows of 100 003 took 33 to 126 us.)
 #include <algorithm>
+#include <atomic>
 
 #include "asynclm.h"
 #include "common.cuh"
+#include "draft_grid.h"
 #include "kernels.h"
 
 namespace asynclm {
 
 namespace {
 
-constexpr int kVerifyThreads = 64, kVerifyWarps = kVerifyThreads / 32;
 constexpr int kPieceBytes = 2048;
 template <typename T>
 constexpr int kPiece = kPieceBytes / (int)sizeof(T);
@@ -358,6 +359,22 @@ draft_verify_kernel(VerifyArgs a) {
     if (lane == 0) a.accepted[b] = accepted;
 }
 
+// CTAs of a kernel that the current device holds at once; asked once for each device and kernel.
+cudaError_t ctas_that_fit(void (*kernel)(VerifyArgs), size_t smem, bool wide, bool pairs, int* fit) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices][4];
+    int device = 0, sms = 0, per_sm = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    std::atomic<int>* at = device < kDevices ? &known[device][2 * wide + pairs] : nullptr;
+    if (at && (*fit = at->load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kVerifyThreads, smem);
+    *fit = sms * per_sm;
+    if (e == cudaSuccess && at) at->store(*fit, std::memory_order_relaxed);
+    return e;
+}
+
 }  // namespace
 
 }  // namespace asynclm
@@ -400,12 +417,10 @@ extern "C" int asynclm_draft_verify(const asynclm_draft_rows* rows, const int32_
     a.vocab = rows->vocab;
     const int piece = size == 4 ? kPiece<float> : kPiece<__nv_bfloat16>;
     a.pieces = (int)(((int64_t)rows->vocab + 16 / (int)size - 1 + piece - 1) / piece);      // wherever a row starts
-    // Two fifths of the CTAs that fit (by their shared memory), each with a piece or more for its warps: every CTA has the chain in front of its stream, and the
-    // next kernel's find room beside them.  (us with inputs out of cache, all that fit | three fifths | two fifths | three tenths: 64 pairs of fp32 rows of 128 256
-    // 20.0 | 22.8 | 18.9 | 20.0, 300 bf16 rows of 100 003 22.8 | 23.8 | 20.2 | 20.7, 300 pairs of fp32 rows of 50 001 29.1 | 26.0 | 28.4 | 41.5.)
     const size_t smem = (size_t)kVerifyWarps * kSlots * (rows->draft ? kSlotBytesQ : kSlotBytes);
-    const int fit = 148 * (int)((size_t)(227 << 10) / (smem + 1536));
-    const int slices = std::max(1, std::min(fit * 2 / 5 / batch, (a.pieces + kVerifyWarps - 1) / kVerifyWarps));
     auto kernel = size == 4 ? draft_verify_kernel<float> : draft_verify_kernel<__nv_bfloat16>;
+    int fit = 0;
+    if (int rc = cuda_status(ctas_that_fit(kernel, smem, size == 4, rows->draft != nullptr, &fit))) return rc;
+    const int slices = draft_slices(batch, a.pieces, fit, rows->draft != nullptr);
     return cuda_status(launch_pdl(kernel, dim3(slices, batch), dim3(kVerifyThreads), smem, (cudaStream_t)stream, a));
 }
