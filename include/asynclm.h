@@ -203,7 +203,8 @@ int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
  * full, and the plan serves the same calls (append, attention over either cache, the static form, the read-back) with the same results to rounding.
  *   Groups rise in first_seq and do not overlap; sequences may be in none.  Every sequence with new tokens has kv_len_before >= prefix_tokens.
  *   What is not worth sharing is planned as if it were not shared: a batch where little would be saved (ASYNCLM_PLAN_SHARE_ALL shares that, too), and spans
- * of more than 1024 rows (G * q_len), or the batch with them, where the model has it take longer.
+ * of more than 1024 rows (G * q_len), or the batch with them, where the model has it take longer.  Rows are shared in stretches of sequences next to each other, and a
+ * long span that does not share ends one: sequences with few new tokens do best next to each other.  (With kv_chunk_tokens set nothing is modelled, and long spans do not share.)
  *   Workspaces: make the plan without a device workspace first (asynclm_plan_info then says what is needed) or retry on WORKSPACE_TOO_SMALL;
  * asynclm_plan_workspace_size does not cover these plans.
  *   Rows that share a prefix have partial results whatever the cuts, so the plan is not cut down to fit asynclm_attn_mixed_static's array: that call refuses

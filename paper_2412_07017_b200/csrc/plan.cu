@@ -866,6 +866,12 @@ constexpr int kSelectChunkUnit = 64, kSelectChunksPerSm = 8;
 // head_dim 64 134 | 124 | 112 | 93 | 93; 30 with 3 of 300-600 193 | 267 | 266 | 265 | 193; 6 of 250-500 alone 151 | 151 | 152 | 152 | 184; 4 prompts of
 // 500-1500 358-389 | 358 | 358 | 358 | 358, and 496 if all share.)
 constexpr int64_t kMostSharedRows = 1024;
+// Where short sequences alone share nothing (single tokens between long spans, which end their runs, or long spans alone), all share if the model has that take less
+// by a sixteenth: it makes too much of the time of long spans, and more of it where they share nothing.  (us, unshared | all share, and the model's ratio, 32/8 heads of
+// 128: 10 single tokens and 10 spans of 300 in turn behind 16 000 keys 802 | 779, 0.93, over the 8-bit cache 1197 | 1233, 0.91; 20 and 20 of 257 behind 8000 908 |
+// 766, 0.91; 2 and 2 of 300 behind 30 000 498 | 339, 0.51; 6 of 300 behind 4096 151 | 189, 0.97; 3 and 3 of 600 behind 3008, 8 bits, 180 | 205, 0.98;
+// 4 and 4 of 300 behind 2000, 8 bits, 132 | 122, 0.77, at head_dim 64 66 | 69, 0.95.)
+constexpr int kSharedMargin = 16;
 // Sharing costs partial rows and the join behind the attention; it has to save as many bytes of K and V as cross the bus in this time.
 constexpr int64_t kLeastSavedNs = 2500;
 
@@ -1181,20 +1187,25 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     while (partial_bytes(static_rows, G, shape->head_dim) > ASYNCLM_STATIC_SCRATCH_BYTES) --static_rows;
     auto fits_static = [&]() { return !too_many && partial_rows <= static_rows; };
     const CutPolicy fastest;
-    if (!runs.empty() && !share_all && fixed_chunk == 0) {
+    if (extra.n_groups > 0 && !share_all && fixed_chunk == 0) {
         int64_t longest = 0;      // rows of a sequence in a group
         for (int g = 0; g < extra.n_groups; ++g)
             for (int b = extra.groups[g].first_seq; b < extra.groups[g].first_seq + extra.groups[g].n_seqs; ++b)
                 longest = std::max<int64_t>(longest, (int64_t)(q_indptr[b + 1] - q_indptr[b]) * G);
-        if (longest > kMostSharedRows) {
+        // (also where short sequences alone share nothing, as between long spans, which end their runs)
+        if (longest > kMostSharedRows && (share(INT64_MAX), !runs.empty())) {
             // partial rows are written and read, past what the model has in its load limit
             int64_t best = -1, best_ns = 0;
+            bool unshared = false;
             for (const int64_t most : {kMostSharedRows, INT64_MAX, (int64_t)0}) {
                 (void)share(most);
+                if (runs.empty() && unshared) continue;
+                unshared = unshared || runs.empty();
                 rc = deal(fastest, tensor_wanted, INT64_MAX);
                 if (rc != ASYNCLM_OK) continue;
                 const int64_t ns = limit_ns + partial_rows * G * (shape->head_dim + 1) * 8 * 1000 / kDramBytesPerUs;
-                if (best < 0 || ns < best_ns) best = most, best_ns = ns;
+                const int64_t margin = unshared && !runs.empty() ? best_ns / kSharedMargin : 0;
+                if (best < 0 || ns < best_ns - margin) best = most, best_ns = ns;
             }
             (void)share(best < 0 ? 0 : best);
         }
