@@ -52,8 +52,9 @@ typedef enum asynclm_status {
     ASYNCLM_ERR_CUDA = -5,                /* a CUDA runtime call or a launch failed            */
     ASYNCLM_ERR_ARCH = -6,                /* current device is not compute capability 10.x     */
     ASYNCLM_ERR_DEVICE_STATUS = -7,       /* a kernel reported a bounded wait that ran out     */
-    ASYNCLM_ERR_STATIC_SCRATCH_TOO_SMALL = -8  /* asynclm_attn_mixed_static: the plan's partial
+    ASYNCLM_ERR_STATIC_SCRATCH_TOO_SMALL = -8, /* asynclm_attn_mixed_static: the plan's partial
                                              results exceed ASYNCLM_STATIC_SCRATCH_BYTES         */
+    ASYNCLM_ERR_MEMORY = -9               /* a planner found no host memory for its own lists    */
 } asynclm_status;
 
 /* Supported: head_dim in {64, 128}; page_size = 16; num_q_heads / num_kv_heads in {1, 2, 4, 8}. */
@@ -188,7 +189,7 @@ int asynclm_plan_workspace_size(const asynclm_shape* shape, const asynclm_plan_o
  *   out_plan              receives a pointer into host_ws.
  *
  * The batch arrays may be freed as soon as the call returns.  Errors: INVALID_ARG (NULL, negative
- * or non-monotone indptr), UNSUPPORTED_SHAPE, PAGE_TABLE, WORKSPACE_TOO_SMALL, ARCH, CUDA.
+ * or non-monotone indptr), UNSUPPORTED_SHAPE, PAGE_TABLE, WORKSPACE_TOO_SMALL, MEMORY, ARCH, CUDA.
  */
 int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
                  const asynclm_batch* batch, void* host_ws, size_t host_bytes,

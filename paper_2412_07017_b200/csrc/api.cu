@@ -39,6 +39,7 @@ extern "C" const char* asynclm_strerror(int status) {
         case ASYNCLM_ERR_DEVICE_STATUS: return "a kernel reported a bounded wait that ran out";
         case ASYNCLM_ERR_STATIC_SCRATCH_TOO_SMALL:
             return "the plan's split-KV partial results do not fit the library's fixed scratch array";
+        case ASYNCLM_ERR_MEMORY: return "no host memory for the planner's lists";
         default: return "unknown status";
     }
 }

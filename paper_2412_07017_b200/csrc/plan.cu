@@ -10,6 +10,7 @@
 #include <cfloat>
 #include <climits>
 #include <cstring>
+#include <exception>
 #include <vector>
 
 #include "asynclm.h"
@@ -1480,13 +1481,23 @@ int make_plan(const asynclm_shape* shape, const asynclm_plan_options* opts, cons
     return ASYNCLM_OK;
 }
 
+// The planner's lists grow with the batch; no exception passes a C entry.
+template <typename... Args>
+int plan_or_error(const Args&... args) {
+    try {
+        return make_plan(args...);
+    } catch (const std::exception&) {      // (bad_alloc, or length_error: nothing else is thrown)
+        return ASYNCLM_ERR_MEMORY;
+    }
+}
+
 }  // namespace
 
 extern "C" int asynclm_plan(const asynclm_shape* shape, const asynclm_plan_options* opts,
                             const asynclm_batch* batch, void* host_ws, size_t host_bytes,
                             void* dev_ws, size_t dev_bytes, void* stream,
                             asynclm_plan_t** out_plan) {
-    return make_plan(shape, opts, batch, PlanExtra{}, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
+    return plan_or_error(shape, opts, batch, PlanExtra{}, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
 }
 
 extern "C" int asynclm_plan_prefix(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch,
@@ -1496,7 +1507,7 @@ extern "C" int asynclm_plan_prefix(const asynclm_shape* shape, const asynclm_pla
     PlanExtra extra;
     extra.groups = groups;
     extra.n_groups = n_groups;
-    return make_plan(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
+    return plan_or_error(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
 }
 
 extern "C" int asynclm_plan_sparse(const asynclm_shape* shape, const asynclm_plan_options* opts, const asynclm_batch* batch, const asynclm_sparse* sparse,
@@ -1506,7 +1517,7 @@ extern "C" int asynclm_plan_sparse(const asynclm_shape* shape, const asynclm_pla
         return ASYNCLM_ERR_INVALID_ARG;
     PlanExtra extra;
     extra.sparse = sparse;
-    return make_plan(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
+    return plan_or_error(shape, opts, batch, extra, host_ws, host_bytes, dev_ws, dev_bytes, stream, out_plan);
 }
 
 extern "C" int asynclm_plan_get_info(const asynclm_plan_t* plan, asynclm_plan_info* info) {
