@@ -223,7 +223,8 @@ int asynclm_plan_prefix(const asynclm_shape* shape, const asynclm_plan_options* 
 
 /*
  * asynclm_plan for attention over selected pages: every (new token, kv head) attends to at most budget_pages of the pages that hold the keys it
- * sees, the first first_pages and the last last_pages (its own key's among them) and, for the rest, those that asynclm_select_pages chooses.  A step is
+ * sees, the first first_pages and the last last_pages (its own key's among them) and, for the rest, those that asynclm_select_pages chooses.  (A plan shares prefixes or selects pages,
+ * not both.)  A step is
  *     append, asynclm_kv_bounds, asynclm_select_pages, asynclm_attn_mixed (or the quantised cache's calls)
  * for every layer; the attention reads the lists that the selection left in the plan's device workspace, and is refused (INVALID_ARG) before the first
  * one.  Meant for decoding sequences and short spans (every token's lists and scores have room in the device workspace) over long contexts; out
@@ -555,7 +556,8 @@ int asynclm_kv8_gather(const asynclm_plan_t* plan, const int64_t* out_indptr, co
  *     key_bounds   device, bf16 [num_pages][num_kv_heads][2 (least, largest)][head_dim], 16-byte aligned
  * exact, as they are values of the cache (of a quantised one, as asynclm_kv8_gather reads them); a channel with a NaN gets -infinity and +infinity.
  * Taken of the plan's sequences that have new tokens: of the pages with a new token (from_start == 0: behind every append, on the same stream), or of all
- * pages up to ctx_b + q_len_b (from_start != 0: for a cache whose bounds nothing has kept).  Any kind of plan.  Other pages' bounds are left alone.
+ * pages up to ctx_b + q_len_b (from_start != 0: for a cache whose bounds nothing has kept; a page that several sequences have is read for each).  Any kind of plan.  Other
+ * pages' bounds are left alone.
  * One kernel.  Errors: INVALID_ARG, CUDA.
  */
 int asynclm_kv_bounds(const asynclm_plan_t* plan, const void* kv_pool, void* key_bounds, int32_t from_start, void* stream);
@@ -581,8 +583,8 @@ int asynclm_select_pages(const asynclm_plan_t* plan, const void* q, const void* 
  *   Draft i is accepted if accept_u[i] * q(x) < p(x) and all drafts of its sequence in front of it are (draft == NULL: q(x) = 1, a proposal made with
  * certainty).  The token behind the accepted ones has the weights w_t = max(p_t - q_t, 0) of the first rejected draft's rows, or w = p of the row behind
  * the last draft: it is the least t with sum_{t' <= t} w > sample_u[b] * sum w, evaluated in 64 bits.  Where rounding has left no weight, w = p; where
- * that has none either, the token is -1.  Weights that are NaN count as zero, negative probabilities as none; a draft outside the vocabulary is
- * rejected.  Random numbers lie in [0, 1).
+ * that has none either, the token is -1.  Where p or q is NaN there is no weight and nothing is accepted; negative probabilities count as none, in the weights as in the
+ * test of acceptance; a draft outside the vocabulary is rejected.  Random numbers lie in [0, 1).
  *
  *   rows          host.  target [drafts + batch][vocab] and draft [drafts][vocab] or NULL: device, bf16 or fp32 (dtype), rows any stride >= vocab apart
  *   draft_indptr  device, int32 [batch + 1], from 0, not falling, up to `drafts`
@@ -591,7 +593,7 @@ int asynclm_select_pages(const asynclm_plan_t* plan, const void* q, const void* 
  *   tokens_out    device, int32 [drafts + batch]: from draft_indptr[b] + b on the accepted drafts, the next token, then -1 in the sequence's other places
  *   workspace     device, 16-byte aligned, asynclm_draft_verify_workspace_bytes(batch, vocab) bytes, owned by the caller and all zero before the first call;
  *                 every call leaves it fit for the next, of any batch and vocab that it is large enough for; calls that share it must not overlap on the GPU
- * One kernel; one row of p and at most one of q are read a sequence; batch <= 65535.  Errors: INVALID_ARG, CUDA.
+ * One kernel; one row of p and at most one of q are read a sequence, and that of p again where rounding has left no weight; batch <= 65535.  Errors: INVALID_ARG, CUDA.
  */
 typedef struct asynclm_draft_rows {
     const void *target, *draft;

@@ -8,13 +8,13 @@
 // held in 64 bits, where neither depends on the order of the additions but within 2^-45.  A value becomes an fp64 one by its bits, without the
 // exponents' difference in bias: all weights and sums are times 2^-896, which changes no comparison, and zeros and subnormal numbers are right as they
 // are.  (With conversions, of which an SM does 16 a cycle, 300 bf16 rows of 100 003 took 45.7 us and 64 pairs of fp32 rows of 128 256 26.4; now, in a graph
-// with inputs in cache, 19.1 and 16.6, out of cache 20.1 and 18.8, 3.0 and 3.3 TB/s; two sequences of four drafts from 32 001 tokens 7.5.)
+// with inputs in cache, 18.9 and 16.6, out of cache 20.3 and 19.3, 3.0 and 3.1 TB/s; two sequences of four drafts from 32 001 tokens 7.4.)
 //
 // One launch: a CTA takes a slice of one sequence's row (which row, every warp finds out for itself); a warp has pieces of 2 KB brought into shared memory, the
 // next one while it sums the last, and leaves each piece's sum in the workspace; the CTA that completes the row finds the piece by the sums, and brings
-// that one again.  Every value is read once, so the bytes of one row of p and one of q a sequence are what bounds a large batch, and a chain of
+// that one again.  (Where nothing is left of max(p - q, 0), that CTA sums all of p's row by itself.)  Every value is read once, so the bytes of one row of p and one of q a sequence are what bounds a large batch, and a chain of
 // round trips (bounds of the sequence, tokens, their probabilities, values; count, sums, one piece) a small one.  Rows start anywhere: what is copied are
-// the 16-byte vectors that memory has them in, and shared memory is read value by value.  (Out of registers, by vectors, with the checks that the ends of
+// the 16-byte vectors that memory has them in, and shared memory is read by vectors, or value by value where q's do not lie as p's.  How many CTAs a row has: draft_grid.h.  (Out of registers, by vectors, with the checks that the ends of
 // a row need, the loop outgrew the instruction cache or the registers: 300 bf16 rows of 100 003 took 33 to 126 us.)
 #include <algorithm>
 #include <atomic>

@@ -3,7 +3,8 @@
 // A warp takes one (page, kv head): 16 slots of head_dim values, read as 16-byte vectors (a row is 16 or 8 lanes of bf16, 8 or 4 of 8-bit
 // codes), folded per lane, then over the lanes that hold the same channels.  Bound by the bytes of K: one pass, nothing is kept between
 // calls, so a page that is appended to is read again as a whole (16 rows of one page a kv head for a decoding sequence).  All of 164 K tokens, 8 kv heads of
-// 128: 62.6 us, 6.07 TB/s, 0.94 of a copy's rate; 48 sequences' pages of one to four new tokens 1.9 us.
+// 128: 62.6 us, 6.07 TB/s, 0.94 of a copy's rate; 48 sequences' pages of one to four new tokens 1.9 us.  Of the 8-bit cache 75 us (32.8 at the copy's rate) and 2.7: there a
+// pair of codes takes a decoding, two products and a packing that the 16-bit form has not; what of it bounds has not been separated.
 #include <algorithm>
 
 #include "asynclm.h"

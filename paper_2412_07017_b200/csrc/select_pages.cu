@@ -9,7 +9,8 @@
 // largest of the row; then, as the budget's last score t in 32 bits lies within e of the one in full, pages above t + 2e are in, pages below
 // t - 2e are out, and the few in between (one to five, where scores are not equal) are scored again in 64 bits, where a product of bf16 values is exact.
 //   (e: either product is D / 16 instructions one after the other, each of which adds 16 exact products to the sum; with truncation to 2^-23 of the largest
-// for each of the 17 terms that is, over both, 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128, and 2^-24 where they are added.)
+// for each of the 17 terms that is, over both, 16 * 17 * 2^-23 < 2^-14.9 of the sum of magnitudes for D = 128, and 2^-24 where they are added.  That the instruction does
+// no worse is an assumption; the tests hold choices by products that cancel, with scores apart by 2^-6 to 2^-36 of a product, against 64 bits.)
 //   In 64 bits for all pages the score kernel took 106 us for 48 sequences of 3-12 K tokens with 1-4 new ones each (451 K sums over 4 heads of 128):
 // for every product a bit operation, an fma and a move, 112 instructions a sum; now it takes 22 us of 92 MB of bounds, and the choice 14.  (4 sequences of
 // 16-60 K tokens: 13 us of 39 MB, and 7.)
