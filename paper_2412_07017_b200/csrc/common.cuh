@@ -117,7 +117,8 @@ __device__ __forceinline__ bool page_ok(int64_t page, int64_t num_pages, int32_t
 #else
 __device__ __forceinline__ bool page_ok(int64_t, int64_t, int32_t*, int) { return true; }
 #endif
-constexpr int kStatusBadPageAppend = 41, kStatusBadPageSpan = 42, kStatusBadPageWarp = 43, kStatusBadPageStep = 44, kStatusBadPageBounds = 46;
+constexpr int kStatusBadPageAppend = 41, kStatusBadPageSpan = 42, kStatusBadPageWarp = 43, kStatusBadPageStep = 44, kStatusBadPageBounds = 46,
+              kStatusBadPageSelect = 47;
 
 // Element offset of the first value of (page, K|V, kv head, slot) in the pool.
 __device__ __forceinline__ size_t pool_row_offset(int64_t page, int which, int kv_head, int slot,

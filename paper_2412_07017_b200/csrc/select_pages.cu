@@ -56,6 +56,9 @@ __device__ __forceinline__ unsigned ordered(float x) {
     const unsigned u = __float_as_uint(x + 0.f);
     return u >> 31 ? ~u : u | 0x80000000u;
 }
+// The page whose bounds are read for `id`, which the checked build holds against the pool's size.
+__device__ __forceinline__ int bounds_page(const DevPlan& p, int id) { return page_ok(id, p.num_pages, p.status, kStatusBadPageSelect) ? id : 0; }
+
 __device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ unsigned long long ordered(double x) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
@@ -97,7 +100,7 @@ select_score_kernel(DevPlan p, const uint8_t* __restrict__ q, const uint8_t* __r
     const int pos0 = c.pos0;
     const int end = min(c.page0 + p.select_chunk_pages, (pos0 + c.rows - 1) / kPage + 1);
     const int queries = c.rows * G;
-    auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? __ldg(table + j0 + (lane & 15)) : -1; };
+    auto id_of = [&](int j0) { return j0 + (lane & 15) < end ? bounds_page(p, __ldg(table + j0 + (lane & 15))) : -1; };
     constexpr int kStep = kScoreWarps * kTilePages;
     int j0 = c.page0 + warp * kTilePages, ids = id_of(j0), ids_next = id_of(j0 + kStep);
     // where this thread's scores go: of queries 2 t and, for one head to a row, 2 t + 1 of each eight
@@ -435,7 +438,7 @@ select_choose_kernel(DevPlan p, const __nv_bfloat16* __restrict__ q, const __nv_
         need = all - s_total;      // to be taken of these
         const int open = s_open;
         if (open > need) {
-            auto exact = [&](int id, int g) { return ordered(exact_sum(s_q + g * D, bounds + (((size_t)id * p.num_kv_heads + h) * 2) * D, D, lane)); };
+            auto exact = [&](int id, int g) { return ordered(exact_sum(s_q + g * D, bounds + (((size_t)bounds_page(p, id) * p.num_kv_heads + h) * 2) * D, D, lane)); };
             if (open <= THREADS) {
                 s_exact[tid] = 0;
                 __syncthreads();
