@@ -136,3 +136,32 @@ print("ok")
 def test_first_call_in_a_capture(dtype, draft):
     p = subprocess.run([sys.executable, "-c", CHILD.format(dtype=dtype, draft=draft)], capture_output=True, text=True, timeout=200, cwd=__file__.rsplit("/tests/", 1)[0])
     assert p.stdout.split() == ["ok"], p.stderr[-600:]
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("heads,n,ctx", [((32, 8, 128), 64, 1500), ((8, 2, 64), 200, 300), ((8, 8, 64), 100, 40)])
+def test_calls_one_behind_the_other(heads, n, ctx, kv8):
+    """Attention, append, bounds and selection again and again under one plan, with nothing between them: every call sees what the ones in front of it wrote."""
+    c = Cache(heads, ctx + np.arange(n) % 16, [1] * n, kv8=kv8, seed=3)
+    plan = B.asynclm_plan_sparse(*c.args, 24, 1, 2, kv8=kv8)
+    bounds = torch.zeros((c.num_pages, c.hkv, 2, c.d), dtype=torch.bfloat16, device="cuda")
+    update_bounds(c, plan, bounds, True)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows = [(torch.randn((c.total, c.hkv, c.d), generator=g, device="cuda") * 2.0 ** (i % 5 - 2)).bfloat16() for i in range(12)]      # (a row's scale differs from time to time)
+    pages = torch.zeros((c.total, c.hkv, 24), dtype=torch.int32, device="cuda")
+    B.asynclm_select_pages(plan, c.q, bounds, pages)
+    out, lse = c.attend(plan)
+    torch.cuda.synchronize()
+    for i in range(0, 12, 3):
+        for k in rows[i:i + 3]:
+            c.attend(plan, out, lse)
+            if kv8:
+                B.asynclm_kv8_append(plan, k, k, c.pool, c.scales)
+            else:
+                B.asynclm_kv_append(plan, k, k, c.pool)
+            update_bounds(c, plan, bounds, False)
+            B.asynclm_select_pages(plan, c.q, bounds, pages)
+        torch.cuda.synchronize()
+        want, used = c.bounds(), c.used.any(-1)
+        assert torch.equal(bounds[used].double(), want[used])
+    assert pages.cpu().tolist() == [[h + [-1] * (24 - len(h)) for h in row] for row in chosen_pages(c, c.bounds().nan_to_num(0.0), 24, 1, 2)]
